@@ -64,7 +64,7 @@ const char* arrol_status_string(int status); /* static string, never NULL */
  * arrol_prune_rebatch_host, the policy loss, the training step of a bf16 MLP head) must be ordered on the device with respect to one
  * another, e.g. by issuing them on one stream.  Calls that work in the caller's buffers alone may be in flight on several
  * streams at once, each with a workspace and outputs of its own: arrol_token_logprob and its variants,
- * arrol_lm_head_backward, scoring and training of a linear head, training of an fp32 head, arrol_select, the vote, the
+ * arrol_lm_head_backward, attention, scoring and training of a linear head, training of an fp32 head, arrol_select, the vote, the
  * trace confidence, and the calibrator's calls (those on one state in order).  They share the GPU then; results do not depend on it. */
 int arrol_create(arrol_ctx** out, int device);
 int arrol_destroy(arrol_ctx* ctx);
@@ -305,6 +305,99 @@ int arrol_lm_head_backward(arrol_ctx* ctx, const void* hidden, const void* W_voc
                            const float* grad_logp, const float* lse, int64_t T_max, const int64_t* d_T, int32_t d,
                            int32_t V, float inv_temperature, float* dH, float* dW, void* workspace,
                            size_t workspace_bytes, void* stream);
+
+/* ---- Attention of the packed survivors over their prompts and their own tokens -----------------------------------
+ * The policy's forward and backward over the re-batched survivors (Section 4.3 (ii); Algorithm 1 "log-probs on R'", "Backprop") is
+ * row by row except for attention, which follows cu_seqlens; and the rollouts of a group share one prompt, whose keys and values are
+ * given once and are read by all of them.
+ * Packed token r = cu_seqlens[s] + t of survivor s attends to all rows cu_prompts[p] .. cu_prompts[p + 1] - 1 of prompt_k / prompt_v,
+ * p = survivor_idx[s] / G (s / G when survivor_idx is NULL), then to rows cu_seqlens[s] .. r of k / v (itself included).  Query head h
+ * uses key head g = h / (Hq / Hkv):
+ *     z_j = scale q[r, h] . k_j[g];   o[r, h] = sum_j exp(z_j - lse[r, h]) v_j[g];   lse[r, h] = log sum_j exp(z_j).
+ * arrol_attention writes o and lse.  arrol_attention_backward, given them and d_o = d loss / d o, writes (overwrites)
+ *     dq[r, h] = scale sum_j ds_j k_j[g],   dk_j[g] = scale sum ds q,   dv_j[g] = sum p d_o,
+ *     p = exp(z - lse), ds = p (d_o . v - d_o . o),  the sums of dk and dv over all rows and heads that attend to key j; dprompt_k and
+ *     dprompt_v hold the sums over all survivors of the prompt (0 where it has none).
+ * Every tensor is bf16 (lse float), [rows, heads, D] with D contiguous, heads D apart and rows `stride` elements apart, so a slice of a
+ * fused projection can be given; bases 16-byte aligned, strides multiples of 8 and at least heads * D.
+ * q, o, d_o, dq [T_max, Hq, D]; k, v, dk, dv [T_max, Hkv, D]; lse [T_max, Hq] dense; prompt_k, prompt_v, dprompt_k, dprompt_v [prompt_rows,
+ * Hkv, D]; cu_seqlens [S_max + 1], cu_prompts [P + 1] int64, both starting at 0, not decreasing; survivor_idx [S_max] int32, not
+ * decreasing; d_num [2] int64 = {S, T} on the device, clamped to S_max and T_max: the outputs of arrol_compact.  Sequences and prompts may
+ * be empty.  Without prompts give NULL for prompt_k, prompt_v, cu_prompts and 0 for prompt_rows, P.
+ * Rows >= T of the outputs, and rows of dprompt_k / dprompt_v outside the prompts, are not written; inputs there may hold anything, and an
+ * infinity or NaN in one row reaches only what attends to that row.  Of rows that do attend to one, o and the gradients are not finite.
+ * Supported: D a multiple of 8, 8 <= D <= 128; Hq a multiple of Hkv, Hq / Hkv <= 64; T_max, prompt_rows < 2^31 - 512.
+ * Products of bf16 with fp32 sums; probabilities and ds are rounded to bf16 before the second contractions; sums, maxima and lse are
+ * fp32; every sum has a fixed order, so equal calls give equal bits.
+ * Row numbers out of order or outside (cu_seqlens, cu_prompts, survivor_idx) are not followed; ARROL_DEV_BAD_INDEX is recorded and the
+ * outputs are undefined.
+ * workspace: arrol_attention_workspace(...) bytes, 256-byte aligned; `backward` != 0 for arrol_attention_backward (a larger one that serves
+ * both).  Contents need not be initialised or kept.  The calls use nothing of the context's buffers: they may be in flight on several
+ * streams, each with a workspace and outputs of its own, and may be captured. */
+typedef struct arrol_attention_args {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    const int64_t* cu_seqlens;
+    const int64_t* d_num;
+    const void *prompt_k, *prompt_v;
+    int64_t prompt_k_stride, prompt_v_stride;
+    const int64_t* cu_prompts;
+    const int32_t* survivor_idx;
+    int64_t T_max, prompt_rows;
+    int32_t S_max, P, G, Hq, Hkv, D;
+    float scale;
+    int32_t reserved;
+    void* o; /* written by arrol_attention, read by arrol_attention_backward */
+    int64_t o_stride;
+    float* lse; /* likewise */
+    /* arrol_attention_backward only */
+    const void* d_o;
+    int64_t d_o_stride;
+    void *dq, *dk, *dv;
+    int64_t dq_stride, dk_stride, dv_stride;
+    void *dprompt_k, *dprompt_v;
+    int64_t dprompt_k_stride, dprompt_v_stride;
+    void* workspace;
+    size_t workspace_bytes;
+} arrol_attention_args;
+size_t arrol_attention_workspace(arrol_ctx* ctx, int32_t S_max, int64_t T_max, int64_t prompt_rows, int32_t Hq, int32_t Hkv, int32_t D,
+                                 int32_t backward);
+int arrol_attention(arrol_ctx* ctx, const arrol_attention_args* args, void* stream);
+int arrol_attention_backward(arrol_ctx* ctx, const arrol_attention_args* args, void* stream);
+
+/* ---- Attention of one generated token per rollout (Algorithm 1, backend: generation up to and past the detection length) -------------
+ * The groups' prompts are shared as above, every rollout has a cache of its own, and rollouts that arrol_select pruned drop out:
+ * rollout i < N with keep[i] != 0 (all when keep is NULL) attends with q[i] to rows cu_prompts[p] .. cu_prompts[p + 1] - 1 of prompt_k /
+ * prompt_v, p = i / G, and to rows src_tok_off[i] .. src_tok_off[i] + lengths[i] - 1 of the caches k / v [cache_rows, Hkv, D] (the current
+ * token's own row among them, if the caller has written it).  o [N, Hq, D] and lse [N, Hq] (or NULL) as above; a rollout without any key
+ * gets o = 0, lse = -inf; rows of rollouts that are not kept are not written, nor are their offsets and lengths followed.
+ * A prompt's keys and values are read once for all of its live rollouts (up to 128 rows of query heads per key head; beyond, again).
+ * N = P G where there are prompts (rollouts of group p are p G .. p G + G - 1); without prompts (NULL, P = 0, prompt_rows = 0) N and G >= 1
+ * are free.
+ * Types, layouts, alignment, D, Hq, Hkv, infinities and NaN as above; cache_rows, prompt_rows < 2^31 - 512; G <= 1024.
+ * A rollout whose rows are not inside [0, cache_rows) (or a prompt's inside [0, prompt_rows)) is treated as if it had none there, and
+ * ARROL_DEV_BAD_INDEX is recorded.  workspace: arrol_attention_decode_workspace(...) bytes, 256-byte aligned, contents as above. */
+typedef struct arrol_decode_args {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    const int64_t* src_tok_off;
+    const int32_t* lengths;
+    const uint8_t* keep;
+    const void *prompt_k, *prompt_v;
+    int64_t prompt_k_stride, prompt_v_stride;
+    const int64_t* cu_prompts;
+    int64_t cache_rows, prompt_rows;
+    int32_t N, P, G, Hq, Hkv, D;
+    float scale;
+    int32_t reserved;
+    void* o;
+    int64_t o_stride;
+    float* lse;
+    void* workspace;
+    size_t workspace_bytes;
+} arrol_decode_args;
+size_t arrol_attention_decode_workspace(arrol_ctx* ctx, int32_t N, int32_t P, int32_t Hq, int32_t Hkv, int32_t D);
+int arrol_attention_decode(arrol_ctx* ctx, const arrol_decode_args* args, void* stream);
 
 /* ---- Trace confidence (Section 3 "Trace Confidence") ---------------------------------------------------------
  * arrol_token_logprob_conf: arrol_token_logprob with one more output from the same launch, the token confidence

@@ -28,6 +28,8 @@ EXPORTS = [
     "arrol_head_grad_workspace", "arrol_head_grad", "arrol_token_logprob_conf", "arrol_trace_confidence",
     "arrol_prune_step", "arrol_token_logprob_splits", "arrol_token_logprob_form", "arrol_test_hook", "arrol_set_source_rows",
     "arrol_token_logprob_gathered", "arrol_token_logprob_gathered_workspace",
+    "arrol_attention_workspace", "arrol_attention", "arrol_attention_backward", "arrol_attention_decode_workspace",
+    "arrol_attention_decode",
 ]
 
 

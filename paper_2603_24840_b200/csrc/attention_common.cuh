@@ -1,0 +1,70 @@
+// Shared parts of the attention kernels: the packed tokens' key ranges, checks of the arguments, the workspace.
+#pragma once
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include "tc_common.cuh"
+
+// Keys of one packed token: prompt rows [pre_lo, pre_hi), own rows [own_lo, token]; its sequence ends at own_hi.
+struct TokenBounds {
+    int pre_lo, pre_hi, own_lo, own_hi;
+};
+
+// The pieces of a packed call's workspace.
+struct AttnWorkspace {
+    uint32_t* counters;           // 64 words, zeroed by the bounds kernel
+    TokenBounds* bounds;
+    int2* prompt_range;
+    float* delta;
+    size_t bytes;
+};
+
+namespace {
+
+constexpr int ATTN_MAX_D = 128;
+constexpr int ATTN_MAX_RATIO = 64;                        // query heads per key head
+constexpr int64_t ATTN_MAX_ROWS = ((int64_t)1 << 31) - 512;   // row numbers plus a tile fit 32 bits
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// What the kernels of the packed calls share; built by the host, passed by value.
+struct AttnShape {
+    const int64_t* d_num;
+    const TokenBounds* bounds;    // [T_max]
+    const int2* prompt_range;     // [prompt_rows]: packed tokens [x, y) that attend to the prompt row; backward only
+    int T_max, prompt_rows;
+    int Hq, Hkv, D, ratio;        // ratio = Hq / Hkv
+    float scale, scale_log2;      // scale_log2 = scale log2(e)
+};
+
+inline size_t attn_round(size_t n) { return (n + 255) & ~(size_t)255; }
+
+inline AttnWorkspace attn_workspace(void* base, int64_t T_max, int64_t prompt_rows, int Hq, bool backward) {
+    AttnWorkspace w = {};
+    uint8_t* p = static_cast<uint8_t*>(base);
+    size_t at = 0;
+    w.counters = reinterpret_cast<uint32_t*>(p + at);
+    at += 256;
+    w.bounds = reinterpret_cast<TokenBounds*>(p + at);
+    at += attn_round((size_t)T_max * sizeof(TokenBounds));
+    if (backward) {
+        w.prompt_range = reinterpret_cast<int2*>(p + at);
+        at += attn_round((size_t)prompt_rows * sizeof(int2));
+        w.delta = reinterpret_cast<float*>(p + at);
+        at += attn_round((size_t)T_max * Hq * sizeof(float));
+    }
+    w.bytes = at;
+    return w;
+}
+
+inline bool attn_heads_ok(int Hq, int Hkv, int D) {
+    return Hkv >= 1 && Hq >= Hkv && Hq <= 65536 && Hq % Hkv == 0 && Hq / Hkv <= ATTN_MAX_RATIO && D >= 8 && D <= ATTN_MAX_D && D % 8 == 0;
+}
+inline bool attn_rows_ok(const void* p, int64_t stride, int heads, int D) {
+    return p && arrol_aligned(p, 16) && stride % 8 == 0 && stride >= (int64_t)heads * D && stride < ((int64_t)1 << 38);
+}
+
+}  // namespace
+
+// attention.cu: the packed tokens' bounds (and, where delta is wanted, delta[t, h] = d_o . o); zeroes the counters.
+int arrol_internal_attention_bounds(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWorkspace& w, bool backward, cudaStream_t s);
+int arrol_internal_check_attention(const arrol_attention_args* a);
