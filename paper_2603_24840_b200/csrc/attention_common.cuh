@@ -63,6 +63,49 @@ inline bool attn_rows_ok(const void* p, int64_t stride, int heads, int D) {
     return p && arrol_aligned(p, 16) && stride % 8 == 0 && stride >= (int64_t)heads * D && stride < ((int64_t)1 << 38);
 }
 
+// [rows, heads, D] bf16, rows `stride` elements apart, as boxes of `tokens` rows x `group` heads x 64 dimensions: a box lands as tokens * group rows
+// of 128 bytes, 128-byte swizzle; dimensions past D and rows outside are zeros.
+int make_map_heads(arrol_ctx* ctx, CUtensorMap* map, const void* base, int64_t rows, int heads, int D, int64_t stride, int group, int tokens) {
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)group, (cuuint32_t)tokens};
+    const cuuint32_t elem_strides[3] = {1, 1, 1};
+    CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(
+        map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, elem_strides,
+        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? ARROL_OK : ARROL_ERR_CUDA;
+}
+
+__device__ __forceinline__ int clamp_row(int64_t x, int lo, int hi) { return (int)(x < lo ? lo : x > hi ? hi : x); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// A row of 128 bytes (64 bf16) of a tile in shared memory: infinities and NaN become zero; true if there were any.  Called for consecutive
+// rows by consecutive lanes, which start at different 16-byte words so that they do not meet in a bank.  `before_write` runs
+// once, before the first change.
+template <typename F>
+__device__ __forceinline__ bool drop_not_finite(uint8_t* row, int lane, F before_write) {
+    bool bad = false;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        uint4* at = reinterpret_cast<uint4*>(row + (((c + lane) & 7) << 4));
+        uint4 w = *at;
+        const uint32_t e = 0x7F807F80u;
+        const uint32_t x = __vcmpeq2(w.x & e, e), y = __vcmpeq2(w.y & e, e), z = __vcmpeq2(w.z & e, e), u = __vcmpeq2(w.w & e, e);
+        if (x | y | z | u) {
+            if (!bad) before_write();
+            bad = true;
+            w.x &= ~x; w.y &= ~y; w.z &= ~z; w.w &= ~u;
+            *at = w;
+        }
+    }
+    return bad;
+}
+
 }  // namespace
 
 // attention.cu: the packed tokens' bounds (and, where delta is wanted, delta[t, h] = d_o . o); zeroes the counters.
