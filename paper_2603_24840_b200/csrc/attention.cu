@@ -76,13 +76,13 @@ attention_bounds_kernel(const int64_t* __restrict__ cu_seqlens, const int64_t* _
     if (bad) atomicOr(status, ARROL_DEV_BAD_INDEX);
 }
 
-// delta[t, h] = sum_d d_o[t, h, d] o[t, h, d]: a warp per row.
+// What the backward needs of a query row: lse log2(e) and delta = sum_d d_o[t, h, d] o[t, h, d].  A warp per row.
 __global__ void __launch_bounds__(BOUNDS_THREADS)
-attention_delta_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_stride, const __nv_bfloat16* __restrict__ d_o, int64_t d_o_stride,
-                       const int64_t* __restrict__ d_num, int T_max, int Hq, int D, float* __restrict__ delta) {
+attention_stats_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_stride, const __nv_bfloat16* __restrict__ d_o, int64_t d_o_stride,
+                       const float* __restrict__ lse, const int64_t* __restrict__ d_num, int T_max, int Hq, int D, float2* __restrict__ stats) {
     pdl_launch_dependents();
     pdl_wait();
-    o = pdl_acquire(o); d_o = pdl_acquire(d_o); d_num = pdl_acquire(d_num);
+    o = pdl_acquire(o); d_o = pdl_acquire(d_o); lse = pdl_acquire(lse); d_num = pdl_acquire(d_num);
     const int T = clamp_row(d_num[1], 0, T_max);
     const int lane = threadIdx.x & 31;
     const int64_t rows = (int64_t)T * Hq, warps = (int64_t)gridDim.x * (BOUNDS_THREADS / 32);
@@ -99,7 +99,7 @@ attention_delta_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_stride, co
         }
 #pragma unroll
         for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-        if (lane == 0) delta[i] = sum;
+        if (lane == 0) stats[i] = make_float2(lse[i] * LOG2E, sum);
     }
 }
 
@@ -617,9 +617,9 @@ int arrol_internal_attention_bounds(arrol_ctx* ctx, const arrol_attention_args* 
     if (backward && a->T_max > 0) {
         int64_t rows = (a->T_max * a->Hq + 7) / 8;
         if (rows > 16 * ctx->sm_count) rows = 16 * ctx->sm_count;
-        ARROL_CUDA_OK(arrol_launch_pdl(attention_delta_kernel, dim3((unsigned)rows), dim3(BOUNDS_THREADS), 0, s,
+        ARROL_CUDA_OK(arrol_launch_pdl(attention_stats_kernel, dim3((unsigned)rows), dim3(BOUNDS_THREADS), 0, s,
                                        static_cast<const __nv_bfloat16*>(a->o), a->o_stride, static_cast<const __nv_bfloat16*>(a->d_o),
-                                       a->d_o_stride, a->d_num, (int)a->T_max, a->Hq, a->D, w.delta));
+                                       a->d_o_stride, static_cast<const float*>(a->lse), a->d_num, (int)a->T_max, a->Hq, a->D, w.stats));
         ctx->launches += 1;
     }
     return ARROL_OK;

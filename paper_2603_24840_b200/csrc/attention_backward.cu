@@ -1,91 +1,542 @@
 // arrol_attention_backward: gradients of the packed survivors' attention.
+//
+// P and dS are recomputed from q, k, the logarithms of the sums and delta = d_o . o, twice: once for the keys' gradients and once for the
+// queries', 7 products of 2 D flops a pair where 5 would do with sums of dq in memory.  Those sums would be atomics, whose order would change the
+// result; this way each tile of gradients has one block that adds in a fixed order in tensor memory.
+//
+// One kernel, two uses.  128 rows stay (two operands a1, a2), 64 rows a block stream past (b1, b2):
+//     x = a1 b1^T,  y = a2 b2^T  (128 x 64),  p = exp(scale x - lse),  ds = p (y - delta),
+//   keys' gradients (KEYS):  rows are keys, a1 = k, a2 = v; columns are query rows (tokens x heads of the group), b1 = q, b2 = d_o;
+//       dv += p b2,  dk += ds b1;  lse and delta belong to columns;
+//   queries' gradients:      rows are query rows, a1 = q, a2 = d_o; columns are keys, b1 = k, b2 = v;
+//       dq += ds b1;  lse and delta belong to rows.
+// x and y are double-buffered in tensor memory (2 x 128 columns beside the accumulators' 2 x D), p and ds replace them as bf16 and are read from
+// there by the second products; two groups of four warps take the blocks in turn.
 #include "attention_common.cuh"
 
 namespace {
 
-constexpr int AB_THREADS = 256;
+constexpr int BWD_THREADS = 320;
+constexpr int BWD_BLOCK = 64;                     // columns: query rows or keys a block
+constexpr int BWD_SLOTS = 2;
+constexpr uint32_t ROWS_HALF_BYTES = 128 * 128;   // 128 rows x 64 dimensions
+constexpr uint32_t COLS_HALF_BYTES = 64 * 128;
 
-__device__ __forceinline__ float4 load_bf4(const __nv_bfloat16* p, bool on) {
-    float4 f = {0.f, 0.f, 0.f, 0.f};
-    if (on) {
-        const uint2 x = *reinterpret_cast<const uint2*>(p);
-        const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x.x)), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x.y));
-        f = {a.x, a.y, b.x, b.y};
+struct BwdParams {
+    AttnShape sh;
+    const float2* stats;                          // [T_max, Hq]: lse log2(e), delta
+    const int64_t* cu_prompts;
+    int P;
+    __nv_bfloat16 *out1, *out2;                   // dv and dk; dq in out2
+    int64_t out1_stride, out2_stride;
+    __nv_bfloat16 *shared1, *shared2;             // dprompt_v, dprompt_k
+    int64_t shared1_stride, shared2_stride;
+    uint32_t* counter;
+    uint32_t* status;
+};
+
+struct BwdItem {
+    int valid, g, shared, row0, rows;             // rows row0 .. of keys (prompt rows where shared) or tokens
+    int pre0, n_pre, own0, n;                     // blocks, as in the forward kernel; KEYS: tokens own0 + TOKQ b ..
+    int pre_in_lo, pre_in_hi, in_lo, in_hi;       // columns (keys or tokens) that every row has
+};
+
+template <int DP>
+struct BwdConf {
+    static constexpr int HALVES = DP / 64;
+    static constexpr uint32_t ROWS_BYTES = HALVES * ROWS_HALF_BYTES, COLS_BYTES = HALVES * COLS_HALF_BYTES;
+    static constexpr int STAGES = DP == 128 ? 4 : 8;
+    static constexpr size_t SMEM = 1024 + 2 * (size_t)ROWS_BYTES + STAGES * 2 * (size_t)COLS_BYTES;
+};
+
+struct BwdShared {
+    uint64_t full[8], empty[8], a_full, a_empty, xy_full[2], ps_full[2], acc_full, acc_empty, item_full[BWD_SLOTS], item_empty[BWD_SLOTS], scanned[2], drain;
+    alignas(16) float lse[8][BWD_BLOCK];          // read four at a time
+    alignas(16) float delta[8][BWD_BLOCK];
+    uint32_t bad[8][2];                           // per stage: rows of an edge block that are not finite
+    BwdItem items[BWD_SLOTS];
+    uint32_t tmem, abort;
+};
+
+// Block b's first column and whether some row does not have all of it.
+template <bool KEYS>
+__device__ __forceinline__ int bwd_start(const BwdItem& it, int b, int TOKQ) {
+    if (KEYS) return it.own0 + b * TOKQ;
+    return b < it.n_pre ? it.pre0 + b * BWD_BLOCK : it.own0 + (b - it.n_pre) * BWD_BLOCK;
+}
+template <bool KEYS>
+__device__ __forceinline__ bool bwd_masked(const BwdItem& it, int b, int TOKQ) {
+    const int c0 = bwd_start<KEYS>(it, b, TOKQ);
+    const bool pre = !KEYS && b < it.n_pre;
+    return c0 < (pre ? it.pre_in_lo : it.in_lo) || c0 + (KEYS ? TOKQ : BWD_BLOCK) > (pre ? it.pre_in_hi : it.in_hi);
+}
+
+template <int DP, bool KEYS>
+__global__ void __launch_bounds__(BWD_THREADS, 1)
+attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_a2,
+                          const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2,
+                          const __grid_constant__ CUtensorMap map_p1, const __grid_constant__ CUtensorMap map_p2, const BwdParams p) {
+    // the prompts' keys and values (p1, p2) are rows of KEYS items, columns otherwise
+    using C = BwdConf<DP>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ BwdShared sm;
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* const rows_a = smem;
+    uint8_t* const ring = smem + 2 * C::ROWS_BYTES;
+    volatile uint32_t* abort_flag = &sm.abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int ratio = p.sh.ratio, TOK = 128 / ratio, TOKQ = BWD_BLOCK / ratio;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); }
+        mbar_init(&sm.a_full, 1);
+        mbar_init(&sm.a_empty, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(&sm.xy_full[i], 1); mbar_init(&sm.ps_full[i], 4); mbar_init(&sm.scanned[i], 4); }
+        mbar_init(&sm.acc_full, 1);
+        mbar_init(&sm.acc_empty, 8);
+        for (int i = 0; i < BWD_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], 9); }
+        mbar_init(&sm.drain, 1);
+        sm.abort = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a1) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a2) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b1) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b2) : "memory");
     }
-    return f;
-}
-__device__ __forceinline__ void store_bf4(__nv_bfloat16* p, bool on, float4 f, float by) {
-    if (!on) return;
-    __nv_bfloat162 r[2] = {__floats2bfloat162_rn(f.x * by, f.y * by), __floats2bfloat162_rn(f.z * by, f.w * by)};
-    *reinterpret_cast<uint2*>(p) = *reinterpret_cast<uint2*>(r);
-}
-__device__ __forceinline__ float dot4_warp(float4 a, float4 b) {
-    float z = a.x * b.x + a.y * b.y + (a.z * b.z + a.w * b.w);
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) z += __shfl_xor_sync(0xffffffffu, z, x);
-    return z;
-}
-__device__ __forceinline__ void axpy4(float4& y, float a, float4 x) { y.x += a * x.x; y.y += a * x.y; y.z += a * x.z; y.w += a * x.w; }
-
-// First form: a warp per (token, query head) for dq.
-__global__ void __launch_bounds__(AB_THREADS) attention_dq_rows_kernel(AttnShape sh, arrol_attention_args a, const float* delta) {
+    if (KEYS && TOKQ * ratio < BWD_BLOCK) {       // rows behind the last whole token are never loaded: zeros, for the second products
+        for (uint32_t i = threadIdx.x * 16; i < C::STAGES * 2 * C::COLS_BYTES; i += BWD_THREADS * 16) *reinterpret_cast<uint4*>(ring + i) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+    }
+    if (warp == 1) {
+        tcgen05_alloc(&sm.tmem, 512);
+        tcgen05_relinquish();
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = sm.tmem;                // accumulators 1 and 2 at columns 0 and 128; x, y of buffer i at 256 + 128 i and + 64
     pdl_launch_dependents();
     pdl_wait();
-    using bf = const __nv_bfloat16*;
-    const int64_t n = sh.d_num[1];
-    const int T = (int)(n < 0 ? 0 : n > sh.T_max ? sh.T_max : n), lane = threadIdx.x & 31, c = lane * 4;
-    const bool on = c < sh.D;
-    const int64_t rows = (int64_t)T * sh.Hq, warps = (int64_t)gridDim.x * (AB_THREADS / 32);
-    for (int64_t i = blockIdx.x * (int64_t)(AB_THREADS / 32) + (threadIdx.x >> 5); i < rows; i += warps) {
-        const int t = (int)(i / sh.Hq), h = (int)(i - (int64_t)t * sh.Hq);
-        const int64_t gc = (int64_t)(h / sh.ratio) * sh.D + c, hc = (int64_t)h * sh.D + c;
-        const TokenBounds b = sh.bounds[t];
-        const float4 q = load_bf4((bf)a.q + t * a.q_stride + hc, on), go = load_bf4((bf)a.d_o + t * a.d_o_stride + hc, on);
-        const float lse = a.lse[i], del = delta[i];
-        float4 acc = {0.f, 0.f, 0.f, 0.f};
-        auto visit = [&](bf kr, bf vr) {
-            const float4 k = load_bf4(kr, on);
-            const float z = dot4_warp(q, k) * sh.scale, dp = dot4_warp(go, load_bf4(vr, on));
-            axpy4(acc, expf(z - lse) * (dp - del), k);
-        };
-        for (int j = b.pre_lo; j < b.pre_hi; ++j) visit((bf)a.prompt_k + j * a.prompt_k_stride + gc, (bf)a.prompt_v + j * a.prompt_v_stride + gc);
-        for (int j = b.own_lo; j <= t; ++j) visit((bf)a.k + j * a.k_stride + gc, (bf)a.v + j * a.v_stride + gc);
-        store_bf4((__nv_bfloat16*)a.dq + t * a.dq_stride + hc, on, acc, sh.scale);
-    }
-}
+    const int T = clamp_row(*pdl_acquire(p.sh.d_num + 1), 0, p.sh.T_max);
+    const int live_prompt = KEYS && p.P > 0 ? clamp_row(pdl_acquire(p.cu_prompts)[p.P], 0, p.sh.prompt_rows) : 0;
+    const TokenBounds* bounds = pdl_acquire(p.sh.bounds);
+    const int2* prompt_range = pdl_acquire(p.sh.prompt_range);
+    const int prompt_tiles = (live_prompt + 127) / 128;
+    const int tiles = KEYS ? prompt_tiles + (T + 127) / 128 : (T + TOK - 1) / TOK;
+    const int64_t items = (int64_t)tiles * p.sh.Hkv;
 
-// First form: a warp per (key row, key head) for dk and dv; prompt rows after the packed ones.
-__global__ void __launch_bounds__(AB_THREADS) attention_dkv_rows_kernel(AttnShape sh, arrol_attention_args a, const float* delta) {
-    pdl_launch_dependents();
-    pdl_wait();
-    using bf = const __nv_bfloat16*;
-    const int64_t n = sh.d_num[1];
-    const int T = (int)(n < 0 ? 0 : n > sh.T_max ? sh.T_max : n), lane = threadIdx.x & 31, c = lane * 4;
-    const int64_t pn = a.P > 0 ? a.cu_prompts[a.P] : 0;
-    const int live = (int)(pn < 0 ? 0 : pn > sh.prompt_rows ? sh.prompt_rows : pn);
-    const bool on = c < sh.D;
-    const int64_t items = ((int64_t)T + live) * sh.Hkv, warps = (int64_t)gridDim.x * (AB_THREADS / 32);
-    for (int64_t i = blockIdx.x * (int64_t)(AB_THREADS / 32) + (threadIdx.x >> 5); i < items; i += warps) {
-        int64_t j = i / sh.Hkv;
-        const int g = (int)(i - j * sh.Hkv);
-        const int64_t gc = (int64_t)g * sh.D + c;
-        const bool shared = j >= T;
-        if (shared) j -= T;
-        const int lo = shared ? sh.prompt_range[j].x : (int)j, hi = shared ? sh.prompt_range[j].y : sh.bounds[j].own_hi;
-        const float4 k = load_bf4(shared ? (bf)a.prompt_k + j * a.prompt_k_stride + gc : (bf)a.k + j * a.k_stride + gc, on);
-        const float4 v = load_bf4(shared ? (bf)a.prompt_v + j * a.prompt_v_stride + gc : (bf)a.v + j * a.v_stride + gc, on);
-        float4 dk = {0.f, 0.f, 0.f, 0.f}, dv = {0.f, 0.f, 0.f, 0.f};
-        for (int t = lo; t < hi; ++t)
-            for (int h = g * sh.ratio; h < (g + 1) * sh.ratio; ++h) {
-                const int64_t hc = (int64_t)h * sh.D + c, r = (int64_t)t * sh.Hq + h;
-                const float4 q = load_bf4((bf)a.q + t * a.q_stride + hc, on), go = load_bf4((bf)a.d_o + t * a.d_o_stride + hc, on);
-                const float p = expf(dot4_warp(q, k) * sh.scale - a.lse[r]), ds = p * (dot4_warp(go, v) - delta[r]);
-                axpy4(dv, p, go);
-                axpy4(dk, ds, q);
+    if (warp == 0) {
+        // ---- producer
+        const float2* stats = pdl_acquire(p.stats);
+        uint32_t pos = 0, a_loads = 0;
+        bool ok = true;
+        for (uint32_t n = 0; ok; ++n) {
+            const uint32_t slot = n % BWD_SLOTS, use = n / BWD_SLOTS;
+            if (!mbar_wait_warp(&sm.item_empty[slot], (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+            uint32_t idx = 0;
+            if (lane == 0) idx = atomicAdd(p.counter, 1u);
+            idx = __shfl_sync(0xffffffffu, idx, 0);
+            BwdItem it = {};
+            it.valid = (int64_t)idx < items;
+            if (it.valid) {
+                const int tile = (int)(idx / (uint32_t)p.sh.Hkv);
+                it.g = (int)(idx % (uint32_t)p.sh.Hkv);
+                if (KEYS) {
+                    // the prompts' tiles first: every survivor's tokens pass by them; then the own ones from the first token on
+                    it.shared = tile < prompt_tiles;
+                    it.row0 = (it.shared ? tile : tile - prompt_tiles) * 128;
+                    it.rows = min(128, (it.shared ? live_prompt : T) - it.row0);
+                    int lo = INT_MAX, hi = 0, in_lo = 0, in_hi = INT_MAX;
+                    for (int r = lane; r < it.rows; r += 32) {
+                        const int j = it.row0 + r;
+                        const int2 x = it.shared ? prompt_range[j] : make_int2(j, bounds[j].own_hi);
+                        if (x.x < x.y) { lo = min(lo, x.x); hi = max(hi, x.y); }
+                        in_lo = max(in_lo, x.x);
+                        in_hi = min(in_hi, x.y);
+                    }
+                    lo = __reduce_min_sync(0xffffffffu, lo);
+                    hi = __reduce_max_sync(0xffffffffu, hi);
+                    it.in_lo = __reduce_max_sync(0xffffffffu, in_lo);
+                    it.in_hi = __reduce_min_sync(0xffffffffu, in_hi);
+                    it.own0 = lo;
+                    it.n = lo < hi ? (hi - lo + TOKQ - 1) / TOKQ : 0;
+                } else {
+                    it.row0 = (tiles - 1 - tile) * TOK;      // last tokens first: theirs are the longest ranges
+                    it.rows = min(TOK, T - it.row0);
+                    const int last = it.row0 + it.rows - 1;
+                    const TokenBounds a = bounds[it.row0], z = bounds[last];
+                    it.pre0 = a.pre_lo;
+                    it.n_pre = z.pre_hi > a.pre_lo ? (z.pre_hi - a.pre_lo + BWD_BLOCK - 1) / BWD_BLOCK : 0;
+                    it.pre_in_lo = z.pre_lo;
+                    it.pre_in_hi = a.pre_hi;
+                    it.own0 = a.own_lo;
+                    it.n = it.n_pre + (last + 1 - a.own_lo + BWD_BLOCK - 1) / BWD_BLOCK;
+                    it.in_lo = z.own_lo;
+                    it.in_hi = it.row0 + 1;
+                }
             }
-        store_bf4(shared ? (__nv_bfloat16*)a.dprompt_k + j * a.dprompt_k_stride + gc : (__nv_bfloat16*)a.dk + j * a.dk_stride + gc, on, dk, sh.scale);
-        store_bf4(shared ? (__nv_bfloat16*)a.dprompt_v + j * a.dprompt_v_stride + gc : (__nv_bfloat16*)a.dv + j * a.dv_stride + gc, on, dv, 1.f);
+            if (lane == 0) sm.items[slot] = it;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.item_full[slot]);
+            __syncwarp();
+            if (!it.valid) break;
+            if (it.n == 0) continue;              // a prompt without survivors: nothing is loaded
+            if (!mbar_wait_warp(&sm.a_empty, (a_loads & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+            if (elect_one()) {
+                mbar_expect_tx(&sm.a_full, 2u * C::HALVES * (KEYS ? 128u : (uint32_t)(TOK * ratio)) * 128u);
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    const CUtensorMap* m = KEYS && it.shared ? (o ? &map_p2 : &map_p1) : (o ? &map_a2 : &map_a1);
+#pragma unroll
+                    for (int h = 0; h < C::HALVES; ++h)
+                        tma_load_3d(rows_a + o * C::ROWS_BYTES + h * ROWS_HALF_BYTES, m, h * 64, KEYS ? it.g : it.g * ratio, it.row0, &sm.a_full);
+                }
+            }
+            __syncwarp();
+            ++a_loads;
+            // a column's statistics are asked for one block ahead; columns without a query row: p = exp(-inf)
+            float2 next[2];
+            auto ask = [&](int b) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int c = u * 32 + lane, tok = c / ratio, t = bwd_start<KEYS>(it, b, TOKQ) + tok;
+                    next[u] = make_float2(INFINITY, 0.f);
+                    if (b < it.n && tok < TOKQ && t < T) next[u] = stats[(int64_t)t * p.sh.Hq + it.g * ratio + (c - tok * ratio)];
+                }
+            };
+            if (KEYS) ask(0);
+            for (int b = 0; b < it.n; ++b, ++pos) {
+                const uint32_t st = pos % C::STAGES;
+                if (!mbar_wait_warp(&sm.empty[st], ((pos / C::STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                if (lane < 2) sm.bad[st][lane] = 0u;
+                if (KEYS) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) { sm.lse[st][u * 32 + lane] = next[u].x; sm.delta[st][u * 32 + lane] = next[u].y; }
+                }
+                __syncwarp();
+                if (elect_one()) {
+                    const bool pre = !KEYS && b < it.n_pre;
+                    const int row = bwd_start<KEYS>(it, b, TOKQ);
+                    mbar_expect_tx(&sm.full[st], 2u * C::HALVES * (KEYS ? (uint32_t)(TOKQ * ratio) : (uint32_t)BWD_BLOCK) * 128u);
+#pragma unroll
+                    for (int o = 0; o < 2; ++o) {
+                        const CUtensorMap* m = pre ? (o ? &map_p2 : &map_p1) : (o ? &map_b2 : &map_b1);
+#pragma unroll
+                        for (int h = 0; h < C::HALVES; ++h)
+                            tma_load_3d(ring + (st * 2 + o) * C::COLS_BYTES + h * COLS_HALF_BYTES, m, h * 64, KEYS ? it.g * ratio : it.g, row, &sm.full[st]);
+                    }
+                }
+                __syncwarp();
+                if (KEYS) ask(b + 1);
+            }
+        }
+        if (!ok) {                                // let the copies in flight land before the block's shared memory goes away
+            for (uint32_t i = 1; i <= C::STAGES && i <= pos; ++i)
+                for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
+                    if (mbar_try_wait(&sm.full[(pos - i) % C::STAGES], ((pos - i) / C::STAGES) & 1u)) break;
+            if (a_loads > 0)
+                for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
+                    if (mbar_try_wait(&sm.a_full, (a_loads - 1u) & 1u)) break;
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---- MMA issuer: x and y of a block, then the second products of the block before it
+        constexpr uint32_t idesc_xy = make_idesc(128, BWD_BLOCK), idesc_acc = make_idesc(128, DP, false, true);
+        const uint32_t a_base = smem_u32(rows_a), ring_base = smem_u32(ring);
+        uint32_t c = 0, with_blocks = 0;          // blocks, items with blocks so far
+        bool ok = true;
+        for (uint32_t n = 0; ok; ++n) {
+            const uint32_t slot = n % BWD_SLOTS;
+            if (!mbar_wait_warp(&sm.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
+            if (!sm.items[slot].valid) break;
+            const int blocks = sm.items[slot].n;
+            if (blocks > 0) {
+                if (!mbar_wait_warp(&sm.a_full, with_blocks & 1u, abort_flag)) { ok = false; break; }
+                for (int b = 0; b <= blocks; ++b) {
+                    if (b < blocks) {
+                        const uint32_t cur = c + b, st = cur % C::STAGES, xy = tmem + 256 + (cur & 1u) * 128;
+                        if (!mbar_wait_warp(&sm.full[st], (cur / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                        tcgen05_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int o = 0; o < 2; ++o)
+#pragma unroll
+                                for (int h = 0; h < C::HALVES; ++h) {
+                                    const uint64_t a_desc = make_smem_desc(a_base + o * C::ROWS_BYTES + h * ROWS_HALF_BYTES);
+                                    const uint64_t b_desc = make_smem_desc(ring_base + (st * 2 + o) * C::COLS_BYTES + h * COLS_HALF_BYTES);
+#pragma unroll
+                                    for (int k = 0; k < 64 / UMMA_K; ++k)
+                                        tcgen05_mma_bf16(xy + o * 64, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_xy, (h | k) != 0 ? 1u : 0u);
+                                }
+                            tcgen05_commit(&sm.xy_full[cur & 1u]);
+                            if (b == blocks - 1) tcgen05_commit(&sm.a_empty);
+                        }
+                        __syncwarp();
+                    }
+                    if (b > 0) {
+                        const uint32_t cur = c + b - 1, st = cur % C::STAGES, xy = tmem + 256 + (cur & 1u) * 128;
+                        if (b == 1 && !mbar_wait_warp(&sm.acc_empty, (with_blocks & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                        if (!mbar_wait_warp(&sm.ps_full[cur & 1u], (cur >> 1) & 1u, abort_flag)) { ok = false; break; }
+                        tcgen05_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int o = KEYS ? 0 : 1; o < 2; ++o) {
+                                // accumulator 1: p b2; accumulator 2: ds b1
+                                const uint64_t b_desc = make_smem_desc_mn(ring_base + (st * 2 + 1 - o) * C::COLS_BYTES, BWD_BLOCK);
+#pragma unroll
+                                for (int k = 0; k < BWD_BLOCK / UMMA_K; ++k)
+                                    tcgen05_mma_bf16_tmem_a(tmem + o * 128, xy + o * 64 + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_acc, b == 1 && k == 0 ? 0u : 1u);
+                            }
+                            tcgen05_commit(&sm.empty[st]);
+                            if (b == blocks) tcgen05_commit(&sm.acc_full);
+                        }
+                        __syncwarp();
+                    }
+                }
+                c += blocks;
+                ++with_blocks;
+            }
+            if (ok && elect_one()) mbar_arrive(&sm.item_empty[slot]);
+            __syncwarp();
+        }
+        if (!ok) {
+            if (elect_one()) tcgen05_commit(&sm.drain);
+            __syncwarp();
+            for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
+                if (mbar_try_wait(&sm.drain, 0u)) break;
+        }
+        __syncwarp();
+    } else {
+        // ---- groups w = 0, 1: blocks in turn; thread = row
+        const int w = (warp - 2) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const float scale2 = p.sh.scale_log2;
+        const uint64_t scale_x2 = pack_f32x2(scale2, scale2);
+        const float2* stats = pdl_acquire(p.stats);
+        uint32_t c = 0, with_blocks = 0, scans = 0;
+        bool ok = true;
+        for (uint32_t n = 0; ok; ++n) {
+            const uint32_t slot = n % BWD_SLOTS;
+            if (!mbar_wait_warp(&sm.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
+            const BwdItem& it = sm.items[slot];
+            if (!it.valid) break;
+            const int blocks = it.n, tok = KEYS ? row : row / ratio, head = it.g * ratio + (KEYS ? 0 : row - tok * ratio);
+            const int j = it.row0 + tok;              // key row or token of this thread
+            const bool live = tok < it.rows;
+            int lo = 0, hi = 0, pre_lo = 0, pre_hi = 0;
+            float2 mine = make_float2(0.f, 0.f);
+            if (live) {
+                if (KEYS) {
+                    const int2 x = it.shared ? prompt_range[j] : make_int2(j, bounds[j].own_hi);
+                    lo = x.x; hi = x.y;
+                } else {
+                    const TokenBounds x = bounds[j];
+                    pre_lo = x.pre_lo; pre_hi = x.pre_hi; lo = x.own_lo; hi = j + 1;
+                    mine = stats[(int64_t)j * p.sh.Hq + head];
+                }
+            }
+            for (int b = 0; b < blocks; ++b) {
+                const uint32_t cur = c + b;
+                if ((cur & 1u) != (uint32_t)w) continue;
+                const uint32_t st = cur % C::STAGES, xy = tmem + lanes + 256 + w * 128;
+                const bool masked = bwd_masked<KEYS>(it, b, TOKQ);
+                int first = 0, len = BWD_BLOCK;       // this row's columns
+                if (masked) {
+                    const int c0 = bwd_start<KEYS>(it, b, TOKQ);
+                    if (KEYS) {
+                        first = min(max(lo - c0, 0), TOKQ) * ratio;
+                        len = min(max(hi - c0, 0), TOKQ) * ratio - first;
+                    } else {
+                        const bool pre = b < it.n_pre;
+                        first = (pre ? pre_lo : lo) - c0;
+                        len = (pre ? pre_hi - pre_lo : hi - lo);
+                        if (first < 0) { len += first; first = 0; }
+                    }
+                    if (!live || len < 0) len = 0;
+                }
+                if (!mbar_wait_warp(&sm.full[st], (cur / C::STAGES) & 1u, abort_flag) ||
+                    !mbar_wait_warp(&sm.xy_full[w], (cur >> 1) & 1u, abort_flag)) { ok = false; break; }
+                tcgen05_fence_after();
+                uint32_t x[2][32], y[2][32];
+                __syncwarp();
+#pragma unroll
+                for (int u = 0; u < 2; ++u) { tcgen05_ld_32x32_issue(xy + u * 32, x[u]); tcgen05_ld_32x32_issue(xy + 64 + u * 32, y[u]); }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) { tcgen05_ld_wait(x[u]); tcgen05_ld_wait(y[u]); }
+                uint32_t bad[2] = {0u, 0u};
+                if (masked) {
+                    // as in the forward kernel: what a masked 0 would meet in the second products must be finite; a row that does have such a column
+                    // gets NaN instead
+                    bool wrote = false;
+                    const int r = row & 63, o = row >> 6;
+                    uint8_t* at = ring + st * 2 * C::COLS_BYTES + r * 128;
+                    auto note = [&] {
+                        atomicOr(&sm.bad[st][r >> 5], 1u << lane);
+                        __threadfence_block();
+                    };
+                    if (KEYS) {
+#pragma unroll
+                        for (int h = 0; h < C::HALVES; ++h) wrote |= drop_not_finite(at + o * C::COLS_BYTES + h * COLS_HALF_BYTES, lane, note);
+                    } else if (o < C::HALVES) {
+                        wrote = drop_not_finite(at + o * COLS_HALF_BYTES, lane, note);
+                    }
+                    if (wrote) fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm.scanned[w]);
+                    __syncwarp();
+                    if (!mbar_wait_warp(&sm.scanned[w], scans++ & 1u, abort_flag)) { ok = false; break; }
+                    bad[0] = *reinterpret_cast<volatile uint32_t*>(&sm.bad[st][0]);
+                    bad[1] = *reinterpret_cast<volatile uint32_t*>(&sm.bad[st][1]);
+                }
+                uint32_t pk[32], dk[32];
+                const uint64_t neg_lse = pack_f32x2(-mine.x, -mine.x), neg_delta = pack_f32x2(-mine.y, -mine.y);
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) {
+                    float4 l4, d4;
+                    if (KEYS) {
+                        l4 = *reinterpret_cast<const float4*>(&sm.lse[st][2 * i]);
+                        d4 = *reinterpret_cast<const float4*>(&sm.delta[st][2 * i]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int col = 2 * (i + k), u = col >> 5, v = col & 31;
+                        const uint64_t nl = KEYS ? (k ? pack_f32x2(-l4.z, -l4.w) : pack_f32x2(-l4.x, -l4.y)) : neg_lse;
+                        const uint64_t nd = KEYS ? (k ? pack_f32x2(-d4.z, -d4.w) : pack_f32x2(-d4.x, -d4.y)) : neg_delta;
+                        float p0, p1, s0, s1;
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[u][v]), __uint_as_float(x[u][v + 1])), scale_x2, nl), p0, p1);
+                        p0 = ex2_approx(p0);
+                        p1 = ex2_approx(p1);
+                        unpack_f32x2(mul_f32x2(pack_f32x2(p0, p1), add_f32x2(pack_f32x2(__uint_as_float(y[u][v]), __uint_as_float(y[u][v + 1])), nd)), s0, s1);
+                        if (masked) {
+                            const bool on0 = (uint32_t)(col - first) < (uint32_t)len, on1 = (uint32_t)(col + 1 - first) < (uint32_t)len;
+                            p0 = on0 ? p0 : 0.f; s0 = on0 ? s0 : 0.f;
+                            p1 = on1 ? p1 : 0.f; s1 = on1 ? s1 : 0.f;
+                            if (bad[u] >> v & 3u) {
+                                if (on0 && (bad[u] >> v & 1u)) p0 = s0 = NAN;
+                                if (on1 && (bad[u] >> v & 2u)) p1 = s1 = NAN;
+                            }
+                        }
+                        if (KEYS) pk[i + k] = pack_bf16(p0, p1);
+                        dk[i + k] = pack_bf16(s0, s1);
+                    }
+                }
+                __syncwarp();
+                if (KEYS) tcgen05_st_32x32(xy, pk);
+                tcgen05_st_32x32(xy + 64, dk);
+                tcgen05_st_wait();
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.ps_full[w]);
+                __syncwarp();
+            }
+            if (!ok) break;
+            c += blocks;
+            // KEYS: group 0 writes dv, group 1 dk; else each half of dq
+            if (blocks > 0) {
+                if (!mbar_wait_warp(&sm.acc_full, with_blocks & 1u, abort_flag)) { ok = false; break; }
+                tcgen05_fence_after();
+                ++with_blocks;
+            }
+            __nv_bfloat16* out;
+            if (KEYS) {
+                out = w == 0 ? (it.shared ? p.shared1 + j * p.shared1_stride : p.out1 + j * p.out1_stride)
+                             : (it.shared ? p.shared2 + j * p.shared2_stride : p.out2 + j * p.out2_stride);
+                out += (int64_t)it.g * p.sh.D;
+            } else {
+                out = p.out2 + j * p.out2_stride + (int64_t)head * p.sh.D;
+            }
+            const float by = KEYS && w == 0 ? 1.f : p.sh.scale;
+            constexpr int PIECES = DP / 32;
+#pragma unroll 1
+            for (int piece = KEYS ? 0 : w * (PIECES / 2); piece < (KEYS ? PIECES : (w + 1) * (PIECES / 2)); ++piece) {
+                uint32_t v[32];
+                __syncwarp();
+                if (blocks > 0) {
+                    tcgen05_ld_32x32_issue(tmem + lanes + (KEYS && w == 0 ? 0 : 128) + piece * 32, v);
+                    tcgen05_ld_wait(v);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = 0u;
+                }
+                if (live) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8)
+                        if (piece * 32 + i < p.sh.D) {
+                            uint4 o4;
+                            o4.x = pack_bf16(__uint_as_float(v[i]) * by, __uint_as_float(v[i + 1]) * by);
+                            o4.y = pack_bf16(__uint_as_float(v[i + 2]) * by, __uint_as_float(v[i + 3]) * by);
+                            o4.z = pack_bf16(__uint_as_float(v[i + 4]) * by, __uint_as_float(v[i + 5]) * by);
+                            o4.w = pack_bf16(__uint_as_float(v[i + 6]) * by, __uint_as_float(v[i + 7]) * by);
+                            *reinterpret_cast<uint4*>(out + piece * 32 + i) = o4;
+                        }
+                }
+            }
+            __syncwarp();
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (blocks > 0) mbar_arrive(&sm.acc_empty);
+                mbar_arrive(&sm.item_empty[slot]);
+            }
+            __syncwarp();
+        }
     }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, ARROL_DEV_WAIT_EXPIRED);
+    if (warp == 1) {
+        tcgen05_fence_after();
+        tcgen05_dealloc(tmem, 512);
+    }
+}
+
+template <int DP>
+int launch_backward(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWorkspace& w, cudaStream_t s) {
+    using C = BwdConf<DP>;
+    bool& set = ctx->attention_backward_smem_set[DP == 128];
+    if (!set) {
+        ARROL_CUDA_OK(cudaFuncSetAttribute(attention_backward_kernel<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+        ARROL_CUDA_OK(cudaFuncSetAttribute(attention_backward_kernel<DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+        set = true;
+    }
+    const int ratio = a->Hq / a->Hkv;
+    BwdParams p = {};
+    p.sh = {a->d_num, w.bounds, w.prompt_range, (int)a->T_max, (int)a->prompt_rows, a->Hq, a->Hkv, a->D, ratio, a->scale, a->scale * LOG2E};
+    p.stats = w.stats;
+    p.cu_prompts = a->cu_prompts;
+    p.P = a->P;
+    p.status = ctx->d_status;
+    CUtensorMap q_cols, do_cols, q_rows, do_rows, k_cols, v_cols, k_rows, v_rows, pk_cols, pv_cols, pk_rows, pv_rows;
+    struct { CUtensorMap* map; const void* base; int64_t rows, stride; int heads, group, tokens; } maps[] = {
+        {&q_rows, a->q, a->T_max, a->q_stride, a->Hq, ratio, 128 / ratio},       {&do_rows, a->d_o, a->T_max, a->d_o_stride, a->Hq, ratio, 128 / ratio},
+        {&q_cols, a->q, a->T_max, a->q_stride, a->Hq, ratio, BWD_BLOCK / ratio}, {&do_cols, a->d_o, a->T_max, a->d_o_stride, a->Hq, ratio, BWD_BLOCK / ratio},
+        {&k_rows, a->k, a->T_max, a->k_stride, a->Hkv, 1, 128},                  {&v_rows, a->v, a->T_max, a->v_stride, a->Hkv, 1, 128},
+        {&k_cols, a->k, a->T_max, a->k_stride, a->Hkv, 1, BWD_BLOCK},            {&v_cols, a->v, a->T_max, a->v_stride, a->Hkv, 1, BWD_BLOCK},
+        {&pk_rows, a->prompt_k, a->prompt_rows, a->prompt_k_stride, a->Hkv, 1, 128}, {&pv_rows, a->prompt_v, a->prompt_rows, a->prompt_v_stride, a->Hkv, 1, 128},
+        {&pk_cols, a->prompt_k, a->prompt_rows, a->prompt_k_stride, a->Hkv, 1, BWD_BLOCK}, {&pv_cols, a->prompt_v, a->prompt_rows, a->prompt_v_stride, a->Hkv, 1, BWD_BLOCK}};
+    for (auto& m : maps) {
+        if (m.rows == 0) continue;
+        if (make_map_heads(ctx, m.map, m.base, m.rows, m.heads, a->D, m.stride, m.group, m.tokens) != ARROL_OK) return ARROL_ERR_CUDA;
+    }
+    if (a->prompt_rows == 0) { pk_rows = k_rows; pv_rows = v_rows; pk_cols = k_cols; pv_cols = v_cols; }     // never read then
+    if (a->T_max == 0) { q_cols = do_cols = k_rows = v_rows = pk_rows; }
+    p.out1 = static_cast<__nv_bfloat16*>(a->dv); p.out1_stride = a->dv_stride;
+    p.out2 = static_cast<__nv_bfloat16*>(a->dk); p.out2_stride = a->dk_stride;
+    p.shared1 = static_cast<__nv_bfloat16*>(a->dprompt_v); p.shared1_stride = a->dprompt_v_stride;
+    p.shared2 = static_cast<__nv_bfloat16*>(a->dprompt_k); p.shared2_stride = a->dprompt_k_stride;
+    p.counter = w.counters + 1;
+    int64_t items = ((a->T_max + 127) / 128 + (a->prompt_rows + 127) / 128) * a->Hkv;
+    ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, true>, dim3((unsigned)(items < ctx->sm_count ? items : ctx->sm_count)), dim3(BWD_THREADS), C::SMEM, s,
+                                   k_rows, v_rows, q_cols, do_cols, pk_rows, pv_rows, p));
+    ctx->launches += 1;
+    if (a->T_max == 0) return ARROL_OK;
+    p.out1 = nullptr;
+    p.out2 = static_cast<__nv_bfloat16*>(a->dq); p.out2_stride = a->dq_stride;
+    p.counter = w.counters + 2;
+    items = (a->T_max + 128 / ratio - 1) / (128 / ratio) * a->Hkv;
+    ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, false>, dim3((unsigned)(items < ctx->sm_count ? items : ctx->sm_count)), dim3(BWD_THREADS), C::SMEM, s,
+                                   q_rows, do_rows, k_cols, v_cols, pk_cols, pv_cols, p));
+    ctx->launches += 1;
+    return ARROL_OK;
 }
 
 }  // namespace
@@ -107,9 +558,5 @@ extern "C" int arrol_attention_backward(arrol_ctx* ctx, const arrol_attention_ar
     cudaStream_t s = (cudaStream_t)stream;
     const int rb = arrol_internal_attention_bounds(ctx, a, w, true, s);
     if (rb != ARROL_OK) return rb;
-    const AttnShape sh = {a->d_num, w.bounds, w.prompt_range, (int)a->T_max, (int)a->prompt_rows, a->Hq, a->Hkv, a->D, a->Hq / a->Hkv, a->scale, a->scale * LOG2E};
-    ARROL_CUDA_OK(arrol_launch_pdl(attention_dkv_rows_kernel, dim3((unsigned)(8 * ctx->sm_count)), dim3(AB_THREADS), 0, s, sh, *a, static_cast<const float*>(w.delta)));
-    ARROL_CUDA_OK(arrol_launch_pdl(attention_dq_rows_kernel, dim3((unsigned)(8 * ctx->sm_count)), dim3(AB_THREADS), 0, s, sh, *a, static_cast<const float*>(w.delta)));
-    ctx->launches += 2;
-    return ARROL_OK;
+    return a->D <= 64 ? launch_backward<64>(ctx, a, w, s) : launch_backward<128>(ctx, a, w, s);
 }

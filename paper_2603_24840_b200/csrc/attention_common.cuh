@@ -1,12 +1,13 @@
 // Shared parts of the attention kernels: the packed tokens' key ranges, checks of the arguments, the workspace.
 #pragma once
 #include <cuda_bf16.h>
+#include <limits.h>
 #include <math.h>
 
 #include "tc_common.cuh"
 
 // Keys of one packed token: prompt rows [pre_lo, pre_hi), own rows [own_lo, token]; its sequence ends at own_hi.
-struct TokenBounds {
+struct alignas(16) TokenBounds {
     int pre_lo, pre_hi, own_lo, own_hi;
 };
 
@@ -15,7 +16,7 @@ struct AttnWorkspace {
     uint32_t* counters;           // 64 words, zeroed by the bounds kernel
     TokenBounds* bounds;
     int2* prompt_range;
-    float* delta;
+    float2* stats;                // per packed token and query head: lse log2(e), d_o . o
     size_t bytes;
 };
 
@@ -49,8 +50,8 @@ inline AttnWorkspace attn_workspace(void* base, int64_t T_max, int64_t prompt_ro
     if (backward) {
         w.prompt_range = reinterpret_cast<int2*>(p + at);
         at += attn_round((size_t)prompt_rows * sizeof(int2));
-        w.delta = reinterpret_cast<float*>(p + at);
-        at += attn_round((size_t)T_max * Hq * sizeof(float));
+        w.stats = reinterpret_cast<float2*>(p + at);
+        at += attn_round((size_t)T_max * Hq * sizeof(float2));
     }
     w.bytes = at;
     return w;
@@ -108,6 +109,6 @@ __device__ __forceinline__ bool drop_not_finite(uint8_t* row, int lane, F before
 
 }  // namespace
 
-// attention.cu: the packed tokens' bounds (and, where delta is wanted, delta[t, h] = d_o . o); zeroes the counters.
+// attention.cu: the packed tokens' bounds (for the backward the prompt rows' ranges and the statistics too); zeroes the counters.
 int arrol_internal_attention_bounds(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWorkspace& w, bool backward, cudaStream_t s);
 int arrol_internal_check_attention(const arrol_attention_args* a);
