@@ -109,31 +109,30 @@ attention_stats_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_stride, co
 // Keys come in blocks of 128: those of the tiles' prompts (consecutive prompts are consecutive rows), then the own ones; a block
 // that lies inside every row's range is not masked at all.
 constexpr int FWD_BLOCK = 128;
-constexpr int FWD_THREADS = 320;             // producer, MMA issuer, two softmax groups of four warps
+constexpr int FWD_THREADS = 384;             // producer, MMA issuer, scanner, a spare warp; two softmax groups of four warps
 constexpr int FWD_SLOTS = 2;                 // work items announced ahead
 constexpr uint32_t HALF_BYTES = 128 * 128;   // 128 rows x 64 dimensions
 constexpr float RESCALE_AT = 8.0f;           // the running maximum follows once it is 2^8 behind
 
 struct FwdTile {
     int tokens;                              // live tokens of the tile
-    int pre_lo, pre_hi, own_lo, own_hi;      // keys that any row needs
-    int pre_in_lo, pre_in_hi, own_in_lo, own_in_hi;   // keys that every row needs
+    int pad[3];
+    int4 need;                               // blocks with keys that any row has: prompt blocks [x, y), own blocks [z, w)
+    int4 whole;                              // blocks whose keys every row has, likewise
 };
-struct FwdItem {
+struct alignas(16) FwdItem {
     int t0, g, valid;
     int pre0, n_pre, own0, n;                // block b < n_pre: prompt rows pre0 + 128 b .., then own rows own0 + 128 (b - n_pre) ..
+    int pad;
     FwdTile tile[2];
 };
-__device__ __forceinline__ int fwd_block_start(const FwdItem& it, int b) { return b < it.n_pre ? it.pre0 + b * FWD_BLOCK : it.own0 + (b - it.n_pre) * FWD_BLOCK; }
-__device__ __forceinline__ bool fwd_needs(const FwdItem& it, int i, int b) {
-    const FwdTile& t = it.tile[i];
-    const int k0 = fwd_block_start(it, b), lo = b < it.n_pre ? t.pre_lo : t.own_lo, hi = b < it.n_pre ? t.pre_hi : t.own_hi;
-    return k0 < hi && k0 + FWD_BLOCK > lo;
+__device__ __forceinline__ bool in_ranges(const int4& r, int b) { return (b >= r.x && b < r.y) || (b >= r.z && b < r.w); }
+// Blocks of 128 keys from `base` on, the first of them number `b0`, that meet [lo, hi); and that lie inside.
+__device__ __forceinline__ int2 blocks_meeting(int lo, int hi, int base, int b0) {
+    return hi > lo ? make_int2(b0 + (lo - base) / FWD_BLOCK, b0 + (hi - base + FWD_BLOCK - 1) / FWD_BLOCK) : make_int2(0, 0);
 }
-__device__ __forceinline__ bool fwd_masked(const FwdItem& it, int i, int b) {
-    const FwdTile& t = it.tile[i];
-    const int k0 = fwd_block_start(it, b), lo = b < it.n_pre ? t.pre_in_lo : t.own_in_lo, hi = b < it.n_pre ? t.pre_in_hi : t.own_in_hi;
-    return k0 < lo || k0 + FWD_BLOCK > hi;
+__device__ __forceinline__ int2 blocks_inside(int lo, int hi, int base, int b0) {
+    return hi > lo && hi > base ? make_int2(b0 + (max(lo - base, 0) + FWD_BLOCK - 1) / FWD_BLOCK, b0 + (hi - base) / FWD_BLOCK) : make_int2(0, 0);
 }
 
 template <int DP>
@@ -142,6 +141,10 @@ struct FwdConf {
     static constexpr uint32_t TILE_BYTES = HALVES * HALF_BYTES;
     static constexpr int STAGES = DP == 128 ? 4 : 8;
     static constexpr size_t SMEM = 1024 + (2 + STAGES) * (size_t)TILE_BYTES;
+    // Tensor memory: S of the two tiles at 0 and 128, O behind them.  With 64 dimensions there is room for P beside S, and the next block's S is
+    // computed while this one's exponentials are; with 128 P takes the place of S, whose next block has to wait for P V.
+    static constexpr bool AHEAD = DP == 64;
+    static constexpr uint32_t O_AT = 256, P_AT = AHEAD ? 384 : 0, P_STEP = AHEAD ? 64 : 128;
 };
 
 struct FwdParams {
@@ -155,8 +158,8 @@ struct FwdParams {
 };
 
 struct FwdShared {
-    uint64_t full[8], empty[8], q_full, q_empty, s_full[2], p_full[2], pv_done[2], item_full[FWD_SLOTS], item_empty[FWD_SLOTS], scanned[2], drain;
-    uint32_t bad_keys[8][4];                 // per stage with values: keys of an edge block that are not finite
+    uint64_t full[8], empty[8], scanned[8], q_full[2], q_empty[2], s_full[2], s_free[2], p_most[2], p_full[2], pv_done[2], item_full[FWD_SLOTS], item_empty[FWD_SLOTS], drain;
+    alignas(16) uint32_t bad_keys[8][4];     // per stage with values: keys of an edge block that are not finite
     FwdItem items[FWD_SLOTS];
     uint32_t tmem, abort;
 };
@@ -172,13 +175,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     uint8_t* const q_tiles = smem;
     uint8_t* const ring = smem + 2 * C::TILE_BYTES;
     volatile uint32_t* abort_flag = &sm.abort;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); }
-        mbar_init(&sm.q_full, 1);
-        mbar_init(&sm.q_empty, 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&sm.s_full[i], 1); mbar_init(&sm.p_full[i], 4); mbar_init(&sm.pv_done[i], 1); mbar_init(&sm.scanned[i], 4); }
-        for (int i = 0; i < FWD_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], 9); }
+        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], i & 1 ? 2 : 1); mbar_init(&sm.scanned[i], 1); }     // odd stages hold values, which the scanner hands back too
+        for (int i = 0; i < 2; ++i) { mbar_init(&sm.q_full[i], 1); mbar_init(&sm.q_empty[i], 1); mbar_init(&sm.s_full[i], 1); mbar_init(&sm.s_free[i], 4); mbar_init(&sm.p_most[i], 4); mbar_init(&sm.p_full[i], 4); mbar_init(&sm.pv_done[i], 1);}
+        for (int i = 0; i < FWD_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], 10); }
         mbar_init(&sm.drain, 1);
         sm.abort = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -193,7 +194,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
-    const uint32_t tmem = sm.tmem;           // S of the two tiles (P in its place), then O
+    const uint32_t tmem = uniform(sm.tmem);  // S of the two tiles (P in its place), then O
     pdl_launch_dependents();
     pdl_wait();
     const int T = clamp_row(*pdl_acquire(p.sh.d_num + 1), 0, p.sh.T_max);
@@ -204,7 +205,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     if (warp == 0) {
         // ---- producer: fetches work items, announces them, loads queries, keys and values
         const TokenBounds* bounds = pdl_acquire(p.sh.bounds);
-        uint32_t pos = 0, q_loads = 0;       // ring positions filled so far, items whose queries were asked for
+        uint32_t pos = 0, q_loads[2] = {0, 0};   // ring positions filled, tiles of queries asked for so far
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % FWD_SLOTS, use = n / FWD_SLOTS;
@@ -217,35 +218,39 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (valid) {
                 // last tokens first: theirs are the longest ranges of a long sequence
                 const int t0 = (pairs - 1 - (int)(idx / (uint32_t)p.sh.Hkv)) * 2 * TOK;
-                FwdTile tl = {0, 0, 0, 0, 0, 0, 0, 0, 0};
+                TokenBounds a = {0, 0, 0, 0}, z = a;     // of the tile's first and last live token; lane = tile
+                int tokens = 0, last = 0;
+                const int first = t0 + lane * TOK;
+                if (lane < 2 && first < T) {
+                    tokens = min(TOK, T - first);
+                    last = first + tokens - 1;
+                    a = bounds[first];
+                    z = bounds[last];
+                }
+                // what the two tiles need together; the second may have no tokens, a tile no prompt rows
+                const bool has_pre = tokens > 0 && z.pre_hi > a.pre_lo;
+                const int pl = __reduce_min_sync(0xffffffffu, has_pre ? a.pre_lo : INT_MAX), ph = __reduce_max_sync(0xffffffffu, has_pre ? z.pre_hi : 0);
+                const int ol = __reduce_min_sync(0xffffffffu, tokens > 0 ? a.own_lo : INT_MAX), oh = __reduce_max_sync(0xffffffffu, tokens > 0 ? last + 1 : 0);
+                const int n_pre = ph > pl ? (ph - pl + FWD_BLOCK - 1) / FWD_BLOCK : 0;
+                const int n_own = (oh - ol + FWD_BLOCK - 1) / FWD_BLOCK;
                 if (lane < 2) {
-                    const int first = t0 + lane * TOK;
-                    tl.tokens = min(TOK, T - first);
-                    if (tl.tokens > 0) {
-                        const int last = first + tl.tokens - 1;
-                        const TokenBounds a = bounds[first], z = bounds[last];
-                        tl = {tl.tokens, a.pre_lo, z.pre_hi, a.own_lo, last + 1, z.pre_lo, a.pre_hi, z.own_lo, first + 1};
-                        if (tl.pre_hi <= tl.pre_lo) tl.pre_hi = tl.pre_lo = 0;
-                    } else {
-                        tl.tokens = 0;
+                    FwdTile tl = {};
+                    tl.tokens = tokens;
+                    if (tokens > 0) {
+                        const int2 np = has_pre ? blocks_meeting(a.pre_lo, z.pre_hi, pl, 0) : make_int2(0, 0), no = blocks_meeting(a.own_lo, last + 1, ol, n_pre);
+                        const int2 wp = blocks_inside(z.pre_lo, a.pre_hi, pl, 0), wo = blocks_inside(z.own_lo, first + 1, ol, n_pre);
+                        tl.need = make_int4(np.x, np.y, no.x, no.y);
+                        tl.whole = make_int4(wp.x, min(wp.y, n_pre), wo.x, wo.y);
                     }
                     it.tile[lane] = tl;
                 }
-                __syncwarp();
                 if (lane == 0) {
-                    const FwdTile &a = it.tile[0], &z = it.tile[1];
-                    int pl = a.pre_lo, ph = a.pre_hi;
-                    if (z.pre_hi > z.pre_lo) {
-                        pl = ph > pl ? min(pl, z.pre_lo) : z.pre_lo;
-                        ph = max(ph, z.pre_hi);
-                    }
-                    const int ol = a.own_lo, oh = z.tokens > 0 ? z.own_hi : a.own_hi;
                     it.t0 = t0;
                     it.g = (int)(idx % (uint32_t)p.sh.Hkv);
                     it.pre0 = pl;
-                    it.n_pre = (ph - pl + FWD_BLOCK - 1) / FWD_BLOCK;
+                    it.n_pre = n_pre;
                     it.own0 = ol;
-                    it.n = it.n_pre + (oh - ol + FWD_BLOCK - 1) / FWD_BLOCK;
+                    it.n = n_pre + n_own;
                 }
             }
             if (lane == 0) it.valid = valid;
@@ -253,27 +258,27 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (lane == 0) mbar_arrive(&sm.item_full[slot]);
             __syncwarp();
             if (!valid) break;
-            const int g = it.g, t0 = it.t0, blocks = it.n;
-            if (!mbar_wait_warp(&sm.q_empty, (n & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-            if (elect_one()) {
-                mbar_expect_tx(&sm.q_full, 2u * C::HALVES * (uint32_t)(TOK * ratio) * 128u);
+            const int g = it.g, t0 = it.t0, blocks = it.n, n_pre = it.n_pre, pre0 = it.pre0, own0 = it.own0;
+            auto load_q = [&](int i) {
+                if (!mbar_wait_warp(&sm.q_empty[i], (n & 1u) ^ 1u, abort_flag)) return false;
+                if (elect_one()) {
+                    mbar_expect_tx(&sm.q_full[i], C::HALVES * (uint32_t)(TOK * ratio) * 128u);
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int h = 0; h < C::HALVES; ++h)
-                        tma_load_3d(q_tiles + i * C::TILE_BYTES + h * HALF_BYTES, &map_q, h * 64, g * ratio, t0 + i * TOK, &sm.q_full);
-            }
-            __syncwarp();
-            ++q_loads;
+                    for (int h = 0; h < C::HALVES; ++h) tma_load_3d(q_tiles + i * C::TILE_BYTES + h * HALF_BYTES, &map_q, h * 64, g * ratio, t0 + i * TOK, &sm.q_full[i]);
+                }
+                __syncwarp();
+                ++q_loads[i];
+                return true;
+            };
             for (int b = 0; b < blocks && ok; ++b) {
-                const bool pre = b < it.n_pre;
-                const int row = fwd_block_start(it, b);
+                const bool pre = b < n_pre;
+                const int row = pre ? pre0 + b * FWD_BLOCK : own0 + (b - n_pre) * FWD_BLOCK;
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv, ++pos) {
                     const uint32_t st = pos % C::STAGES;
+                    // queries behind the first keys and values: those stages are free earlier than the last item's queries
+                    if (b == 0 && kv == 1 && !(load_q(0) && load_q(1))) { ok = false; break; }
                     if (!mbar_wait_warp(&sm.empty[st], ((pos / C::STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-                    if (lane < 4) sm.bad_keys[st][lane] = 0u;
-                    __syncwarp();
                     if (elect_one()) {
                         mbar_expect_tx(&sm.full[st], C::TILE_BYTES);
                         const CUtensorMap* m = kv == 0 ? (pre ? &map_pk : &map_k) : (pre ? &map_pv : &map_v);
@@ -288,87 +293,112 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             for (uint32_t i = 1; i <= C::STAGES && i <= pos; ++i)
                 for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
                     if (mbar_try_wait(&sm.full[(pos - i) % C::STAGES], ((pos - i) / C::STAGES) & 1u)) break;
-            if (q_loads > 0)
-                for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
-                    if (mbar_try_wait(&sm.q_full, (q_loads - 1u) & 1u)) break;
+            for (int i = 0; i < 2; ++i)
+                for (uint32_t spin = 0; q_loads[i] > 0 && spin < SPIN_LIMIT; ++spin)
+                    if (mbar_try_wait(&sm.q_full[i], (q_loads[i] - 1u) & 1u)) break;
         }
         __syncwarp();
     } else if (warp == 1) {
-        // ---- MMA issuer.  Per tile and block: S = Q K^T, and once the softmax group has put P in its place, O += P V, directly followed by
-        // the next block's S; while one tile's softmax runs, the tensor cores work for the other one.
+        // ---- MMA issuer.  Per tile and block: S = Q K^T, and once the softmax group has written P (three quarters are enough to begin), O += P V.
+        // One warp for both tiles, in turn: that keeps their softmax groups half a block apart, so that one's exponentials run while the tensor cores
+        // work for the other.  (A warp per tile let them fall in step, both waiting for the same unit: 8,192 tokens of 32 heads of 128 517 -> 700 us.)
         constexpr uint32_t idesc_s = make_idesc(128, FWD_BLOCK), idesc_o = make_idesc(128, DP, false, true);
         const uint32_t q_base = smem_u32(q_tiles), ring_base = smem_u32(ring);
-        uint32_t pos0 = 0, parity_p[2] = {0, 0};
-        bool ok = true;
+        uint32_t pos0 = 0, parity_p[2] = {0, 0}, parity_s[2] = {0, 0};
+        bool ok = true, s_used[2] = {false, false};  // S was written before
+        auto wait_stage = [&](uint32_t pos) { return mbar_wait_warp(&sm.full[pos % C::STAGES], (pos / C::STAGES) & 1u, abort_flag); };
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % FWD_SLOTS;
             if (!mbar_wait_warp(&sm.item_full[slot], (n / FWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
             const FwdItem& it = sm.items[slot];
             if (!it.valid) break;
-            if (!mbar_wait_warp(&sm.q_full, n & 1u, abort_flag)) { ok = false; break; }
-            tcgen05_fence_after();
-            int pending[2] = {-1, -1};       // block whose P V is still to be issued
+            const int blocks = uniform(it.n);
+            const int4 need0 = uniform(it.tile[0].need), need1 = uniform(it.tile[1].need);
             bool first[2] = {true, true};
-            // a stage is free after the last tile that needs it: tile 1 where it does, as its MMAs are issued behind tile 0's
-            auto issue_pv = [&](int i) {
-                const uint32_t pos = pos0 + 2 * pending[i] + 1, st = pos % C::STAGES;
-                if (!mbar_wait_warp(&sm.p_full[i], parity_p[i], abort_flag)) return false;
-                parity_p[i] ^= 1u;
-                if (!mbar_wait_warp(&sm.full[st], (pos / C::STAGES) & 1u, abort_flag)) return false;
+            uint32_t pv_pos[2] = {0, 0};             // ring position of the values whose P V is still to be issued; 0: none
+            bool pv_frees[2] = {false, false};       // and whether no other tile uses them after that
+            auto issue_s = [&](int i, uint32_t pos, bool frees, bool last) {
+                if (C::AHEAD && s_used[i]) {
+                    if (!mbar_wait_warp(&sm.s_free[i], parity_s[i], abort_flag)) return false;
+                    parity_s[i] ^= 1u;
+                }
+                s_used[i] = true;
+                const uint32_t st = pos % C::STAGES;
                 tcgen05_fence_after();
                 if (elect_one()) {
-                    const uint64_t b_desc = make_smem_desc_mn(ring_base + st * C::TILE_BYTES, 128);
 #pragma unroll
-                    for (int k = 0; k < FWD_BLOCK / UMMA_K; ++k)
-                        tcgen05_mma_bf16_tmem_a(tmem + 256 + i * 128, tmem + i * 128 + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o,
-                                                first[i] && k == 0 ? 0u : 1u);
-                    if (i == 1 || !fwd_needs(it, 1, pending[i])) tcgen05_commit(&sm.empty[st]);
+                    for (int h = 0; h < C::HALVES; ++h) {
+                        const uint64_t a_desc = make_smem_desc(q_base + i * C::TILE_BYTES + h * HALF_BYTES), b_desc = make_smem_desc(ring_base + st * C::TILE_BYTES + h * HALF_BYTES);
+#pragma unroll
+                        for (int k = 0; k < 64 / UMMA_K; ++k)
+                            tcgen05_mma_bf16(tmem + i * 128, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_s, (h | k) != 0 ? 1u : 0u);
+                    }
+                    tcgen05_commit(&sm.s_full[i]);
+                    if (frees) tcgen05_commit(&sm.empty[st]);
+                    if (last) tcgen05_commit(&sm.q_empty[i]);
+                }
+                __syncwarp();
+                return true;
+            };
+            auto issue_pv = [&](int i) {
+                const uint32_t st = pv_pos[i] % C::STAGES, o_at = tmem + C::O_AT + i * DP, p_at = tmem + C::P_AT + i * C::P_STEP;
+                if (!wait_stage(pv_pos[i]) || !mbar_wait_warp(&sm.p_most[i], parity_p[i], abort_flag)) return false;
+                tcgen05_fence_after();
+                const uint64_t b_desc = make_smem_desc_mn(ring_base + st * C::TILE_BYTES, 128);
+                const bool elected = elect_one();
+                if (elected) {
+#pragma unroll
+                    for (int k = 0; k < 6; ++k)
+                        tcgen05_mma_bf16_tmem_a(o_at, p_at + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o, first[i] && k == 0 ? 0u : 1u);
+                }
+                __syncwarp();
+                if (!mbar_wait_warp(&sm.p_full[i], parity_p[i], abort_flag)) return false;
+                tcgen05_fence_after();
+                if (elected) {
+#pragma unroll
+                    for (int k = 6; k < 8; ++k)
+                        tcgen05_mma_bf16_tmem_a(o_at, p_at + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o, 1u);
+                    if (pv_frees[i]) tcgen05_commit(&sm.empty[st]);
                     tcgen05_commit(&sm.pv_done[i]);
                 }
                 __syncwarp();
+                parity_p[i] ^= 1u;
                 first[i] = false;
-                pending[i] = -1;
+                pv_pos[i] = 0;
                 return true;
             };
-            for (int b = 0; b < it.n && ok; ++b) {
-                const uint32_t pos = pos0 + 2 * b, st = pos % C::STAGES;
-                if (!fwd_needs(it, 0, b) && !fwd_needs(it, 1, b)) {      // only where row numbers are out of order
-                    const uint32_t sv = (pos + 1) % C::STAGES;
-                    if (!mbar_wait_warp(&sm.full[st], (pos / C::STAGES) & 1u, abort_flag) ||
-                        !mbar_wait_warp(&sm.full[sv], ((pos + 1) / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
-                    if (elect_one()) { mbar_arrive(&sm.empty[st]); mbar_arrive(&sm.empty[sv]); }
-                    __syncwarp();
-                    continue;
-                }
+            bool q_here[2] = {false, false};
+            for (int b = 0; b < blocks && ok; ++b) {
+                const uint32_t pos = pos0 + 2 * b;
+                const bool use[2] = {in_ranges(need0, b), in_ranges(need1, b)};
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    if (!ok) break;
-                    if (pending[i] >= 0 && !issue_pv(i)) { ok = false; break; }
-                    if (!fwd_needs(it, i, b)) continue;
-                    if (!mbar_wait_warp(&sm.full[st], (pos / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
-                    tcgen05_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int h = 0; h < C::HALVES; ++h) {
-                            const uint64_t a_desc = make_smem_desc(q_base + i * C::TILE_BYTES + h * HALF_BYTES);
-                            const uint64_t b_desc = make_smem_desc(ring_base + st * C::TILE_BYTES + h * HALF_BYTES);
-#pragma unroll
-                            for (int k = 0; k < 64 / UMMA_K; ++k)
-                                tcgen05_mma_bf16(tmem + i * 128, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_s, (h | k) != 0 ? 1u : 0u);
-                        }
-                        tcgen05_commit(&sm.s_full[i]);
-                        if (i == 1 || !fwd_needs(it, 1, b)) tcgen05_commit(&sm.empty[st]);
+                    // a tile's pending P V goes first even where it does not need this block: stages are freed in order, tile 1 last
+                    if ((!C::AHEAD || !use[i]) && ok && pv_pos[i] && !issue_pv(i)) ok = false;
+                    if (use[i] && ok) {
+                        if (!q_here[i] && !mbar_wait_warp(&sm.q_full[i], n & 1u, abort_flag)) { ok = false; break; }
+                        q_here[i] = true;
+                        if (!wait_stage(pos) || !issue_s(i, pos, i == 1 || !use[1], b + 1 == (i ? need1.w : need0.w))) { ok = false; break; }
+                        if (C::AHEAD && pv_pos[i] && !issue_pv(i)) { ok = false; break; }
+                        pv_pos[i] = pos + 1;
+                        pv_frees[i] = i == 1 || !use[1];
                     }
+                }
+                if (!use[0] && !use[1] && ok) {      // only where row numbers are out of order
+                    if (!wait_stage(pos) || !wait_stage(pos + 1)) { ok = false; break; }
+                    if (elect_one()) { mbar_arrive(&sm.empty[pos % C::STAGES]); mbar_arrive(&sm.empty[(pos + 1) % C::STAGES]); }
                     __syncwarp();
-                    pending[i] = b;
                 }
             }
-            if (ok && elect_one()) tcgen05_commit(&sm.q_empty);      // the item's last use of its queries
-            __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (ok && pending[i] >= 0 && !issue_pv(i)) ok = false;
-            pos0 += 2 * it.n;
+            for (int i = 0; i < 2; ++i) {
+                if (ok && pv_pos[i] && !issue_pv(i)) ok = false;
+                if (ok && !q_here[i]) {              // a tile without tokens
+                    if (!mbar_wait_warp(&sm.q_full[i], n & 1u, abort_flag)) ok = false;
+                    else if (elect_one()) mbar_arrive(&sm.q_empty[i]);
+                }
+            }
+            pos0 += 2 * blocks;
             if (ok && elect_one()) mbar_arrive(&sm.item_empty[slot]);
             __syncwarp();
         }
@@ -379,16 +409,61 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 if (mbar_try_wait(&sm.drain, 0u)) break;
         }
         __syncwarp();
-    } else {
+    } else if (warp == 2) {
+        // ---- scanner.  Where a block lies at the edge of some row's range, 0 times an infinity or a NaN would carry values of keys that the row does not
+        // attend to into its sum: such values become zeros here, and the softmax groups give NaN to rows that do attend to them.
+        uint32_t pos0 = 0;
+        bool ok = true;
+        for (uint32_t n = 0; ok; ++n) {
+            const uint32_t slot = n % FWD_SLOTS;
+            if (!mbar_wait_warp(&sm.item_full[slot], (n / FWD_SLOTS) & 1u, abort_flag)) break;
+            const FwdItem& it = sm.items[slot];
+            if (!it.valid) break;
+            const int blocks = it.n;
+            const int4 need0 = it.tile[0].need, need1 = it.tile[1].need, whole0 = it.tile[0].whole, whole1 = it.tile[1].whole;
+            for (int b = 0; b < blocks; ++b) {
+                const uint32_t pos = pos0 + 2 * b + 1, st = pos % C::STAGES;
+                if (!mbar_wait_warp(&sm.full[st], (pos / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                if ((in_ranges(need0, b) && !in_ranges(whole0, b)) || (in_ranges(need1, b) && !in_ranges(whole1, b))) {
+#pragma unroll 1
+                    for (int w = 0; w < 4; ++w) {
+                        bool bad = false;
+#pragma unroll
+                        for (int h = 0; h < C::HALVES; ++h) {
+                            uint8_t* at = ring + st * C::TILE_BYTES + h * HALF_BYTES + (w * 32 + lane) * 128;
+                            if (row_not_finite(at, lane)) {
+                                bad = true;
+                                drop_not_finite(at);
+                                fence_proxy_async_smem();
+                            }
+                        }
+                        const uint32_t all = __ballot_sync(0xffffffffu, bad);
+                        if (lane == 0) sm.bad_keys[st][w] = all;
+                    }
+                } else if (lane < 4) {
+                    sm.bad_keys[st][lane] = 0u;
+                }
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&sm.scanned[st]);
+                    mbar_arrive(&sm.empty[st]);
+                }
+                __syncwarp();
+            }
+            pos0 += 2 * blocks;
+            if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
+            __syncwarp();
+        }
+    } else if (warp >= 4) {
         // ---- softmax group i: thread = query row.  Probabilities are taken against a maximum that may be up to 2^8 behind the running one, which
         // changes nothing (sum and products carry the same factor) and spares nearly all passes over O.
-        const int i = (warp - 2) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const int i = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        const uint32_t s_at = tmem + lanes + i * 128, o_at = tmem + lanes + 256 + i * 128;
+        const uint32_t s_at = tmem + lanes + i * 128, o_at = tmem + lanes + C::O_AT + i * DP, p_at = tmem + lanes + C::P_AT + i * C::P_STEP;
         const float scale = p.sh.scale_log2;
         const TokenBounds* bounds = pdl_acquire(p.sh.bounds);
         const int tok = row / ratio, head = row - tok * ratio;
-        uint32_t pos0 = 0, s_count = 0, scans = 0;   // blocks of this tile so far: parity of s_full, pv_done
+        uint32_t pos0 = 0, s_count = 0;      // blocks of this tile so far: parity of s_full, pv_done
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % FWD_SLOTS;
@@ -401,15 +476,18 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (live) bd = bounds[t];
             float m = -INFINITY, l = 0.f;
             bool have_o = false;
-            for (int b = 0; b < it.n && ok; ++b) {
-                if (!fwd_needs(it, i, b)) continue;
-                const bool masked = fwd_masked(it, i, b);
-                const bool edge = masked || (fwd_needs(it, 1 - i, b) && fwd_masked(it, 1 - i, b));
-                const int k0 = fwd_block_start(it, b);
+            const int4 need = it.tile[i].need, whole = it.tile[i].whole;
+            const int n_pre = it.n_pre;
+            for (int b = need.y > need.x ? need.x : need.z; b < need.w; b = b + 1 == need.y ? need.z : b + 1) {
+                const bool pre = b < n_pre;
+                const bool masked = !in_ranges(whole, b);
                 int lo = 0, len = FWD_BLOCK;
                 if (masked) {
-                    lo = (b < it.n_pre ? bd.pre_lo : bd.own_lo) - k0;
-                    len = !live ? 0 : (b < it.n_pre ? bd.pre_hi : t + 1) - k0 - lo;
+                    const int k0 = pre ? it.pre0 + b * FWD_BLOCK : it.own0 + (b - n_pre) * FWD_BLOCK;
+                    lo = (pre ? bd.pre_lo : bd.own_lo) - k0;
+                    len = !live ? 0 : (pre ? bd.pre_hi : t + 1) - k0 - lo;
+                    if (lo < 0) { len += lo; lo = 0; }
+                    len = min(max(len, 0), FWD_BLOCK - lo);
                 }
                 if (!mbar_wait_warp(&sm.s_full[i], s_count & 1u, abort_flag)) { ok = false; break; }
                 tcgen05_fence_after();
@@ -417,14 +495,30 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 __syncwarp();
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tcgen05_ld_32x32_issue(s_at + c * 32, s[c]);
+                uint32_t on[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};     // this row's keys of the block
+                if (masked) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int a = min(max(lo - c * 32, 0), 32), z = min(max(lo + len - c * 32, 0), 32);
+                        on[c] = z > a ? (0xffffffffu >> (32 - z + a)) << a : 0u;
+                    }
+                }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tcgen05_ld_wait(s[c]);
+                if (C::AHEAD) {                  // S is in registers: the next block's may take its place
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm.s_free[i]);
+                    __syncwarp();
+                }
                 if (masked) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
+                        if (!__all_sync(0xffffffffu, on[c] == 0xffffffffu)) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (len <= 0 || (uint32_t)(c * 32 + j - lo) >= (uint32_t)len) s[c][j] = 0xFF800000u;
+                            for (int j = 0; j < 32; ++j)
+                                if (!(on[c] >> j & 1u)) s[c][j] = 0xFF800000u;
+                        }
                 }
                 float mx[4];
 #pragma unroll
@@ -440,78 +534,85 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     m = top;
                     l *= up;
                 }
+                const bool rescale = have_o && __any_sync(0xffffffffu, up != 1.f);
+                if (have_o && (C::AHEAD || rescale)) {       // P V of the block before is done: P may be written over, O changed
+                    if (!mbar_wait_warp(&sm.pv_done[i], (s_count - 1u) & 1u, abort_flag)) { ok = false; break; }
+                    tcgen05_fence_after();
+                }
+                if (rescale) {
+#pragma unroll 1
+                    for (int c = 0; c < DP / 16; ++c) {
+                        float v[16];
+                        __syncwarp();
+                        tcgen05_ld_32(o_at + c * 16, v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) v[j] *= up;
+                        tcgen05_st_32x16(o_at + c * 16, v);
+                    }
+                }
                 const float sub = m == -INFINITY ? 0.f : -m;
                 const uint64_t scale2 = pack_f32x2(scale, scale), sub2 = pack_f32x2(sub, sub);
                 uint64_t sum[2] = {0, 0};
+                auto quarter_of_p = [&](int c) {
+                    uint32_t pk[16];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t pk[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const int cc = c * 2 + j / 16, jj = (j % 16) * 2;
+                    for (int j = 0; j < 16; ++j) {
                         float x, y;
-                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[cc][jj]), __uint_as_float(s[cc][jj + 1])), scale2, sub2), x, y);
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[c][2 * j]), __uint_as_float(s[c][2 * j + 1])), scale2, sub2), x, y);
                         x = ex2_approx(x);
                         y = ex2_approx(y);
                         sum[j & 1] = add_f32x2(sum[j & 1], pack_f32x2(x, y));
                         pk[j] = pack_bf16(x, y);
                     }
                     __syncwarp();
-                    tcgen05_st_32x32(s_at + c * 32, pk);
+                    tcgen05_st_32x16(p_at + c * 16, pk);
+                };
+                auto publish = [&](uint64_t* bar) {
+                    __syncwarp();
+                    tcgen05_st_wait();
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar);
+                    __syncwarp();
+                };
+                auto values_scanned = [&] {      // before P V may begin
+                    const uint32_t pos = pos0 + 2 * b + 1, st = pos % C::STAGES;
+                    if (!mbar_wait_warp(&sm.scanned[st], (pos / C::STAGES) & 1u, abort_flag)) return false;
+                    const uint4 bad = *reinterpret_cast<const uint4*>(sm.bad_keys[st]);
+                    if ((bad.x & on[0]) | (bad.y & on[1]) | (bad.z & on[2]) | (bad.w & on[3])) l = NAN;
+                    return true;
+                };
+                if (!masked) {
+                    quarter_of_p(0);
+                    quarter_of_p(1);
+                    quarter_of_p(2);
+                    if (!values_scanned()) { ok = false; break; }
+                    publish(&sm.p_most[i]);
+                    quarter_of_p(3);
+                    publish(&sm.p_full[i]);
+                } else {
+                    if (!values_scanned()) { ok = false; break; }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (__all_sync(0xffffffffu, on[c] == 0u)) {      // no key of any row of the warp
+                            const uint32_t none[16] = {};
+                            __syncwarp();
+                            tcgen05_st_32x16(p_at + c * 16, none);
+                        } else {
+                            quarter_of_p(c);
+                        }
+                        if (c >= 2) publish(c == 2 ? &sm.p_most[i] : &sm.p_full[i]);
+                    }
                 }
                 float x, y;
                 unpack_f32x2(add_f32x2(sum[0], sum[1]), x, y);
                 l += x + y;
-                if (have_o && __any_sync(0xffffffffu, up != 1.f)) {
-                    if (!mbar_wait_warp(&sm.pv_done[i], (s_count - 1u) & 1u, abort_flag)) { ok = false; break; }
-                    tcgen05_fence_after();
-#pragma unroll 1
-                    for (int c = 0; c < DP / 32; ++c) {
-                        uint32_t v[32];
-                        __syncwarp();
-                        tcgen05_ld_32x32_issue(o_at + c * 32, v);
-                        tcgen05_ld_wait(v);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * up);
-                        tcgen05_st_32x32(o_at + c * 32, v);
-                    }
-                }
-                if (edge) {
-                    // 0 times an infinity or a NaN would carry values of keys that a row does not attend to into its sum: they become zeros here,
-                    // and rows that do attend to them NaN
-                    const uint32_t pos = pos0 + 2 * b + 1, st = pos % C::STAGES;
-                    if (!mbar_wait_warp(&sm.full[st], (pos / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
-                    bool wrote = false;
-#pragma unroll
-                    for (int h = 0; h < C::HALVES; ++h)
-                        wrote |= drop_not_finite(ring + st * C::TILE_BYTES + h * HALF_BYTES + row * 128, lane, [&] {
-                            atomicOr(&sm.bad_keys[st][quarter], 1u << lane);
-                            __threadfence_block();
-                        });
-                    if (wrote) fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sm.scanned[i]);
-                    __syncwarp();
-                    if (!mbar_wait_warp(&sm.scanned[i], scans++ & 1u, abort_flag)) { ok = false; break; }
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&sm.bad_keys[st][w]);
-                        if (bad)
-                            for (int j = 0; j < 32; ++j)
-                                if ((bad >> j & 1u) && len > 0 && (uint32_t)(w * 32 + j - lo) < (uint32_t)len) l = NAN;
-                    }
-                }
-                __syncwarp();
-                tcgen05_st_wait();
-                tcgen05_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sm.p_full[i]);
-                __syncwarp();
                 ++s_count;
                 have_o = true;
             }
             pos0 += 2 * it.n;
-            if (ok && have_o) {
+            if (!ok) break;
+            if (have_o) {
                 if (!mbar_wait_warp(&sm.pv_done[i], (s_count - 1u) & 1u, abort_flag)) { ok = false; break; }
                 tcgen05_fence_after();
                 const int h = it.g * ratio + head;

@@ -366,20 +366,20 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 if (masked) {
                     // as in the forward kernel: what a masked 0 would meet in the second products must be finite; a row that does have such a column
                     // gets NaN instead
-                    bool wrote = false;
                     const int r = row & 63, o = row >> 6;
                     uint8_t* at = ring + st * 2 * C::COLS_BYTES + r * 128;
-                    auto note = [&] {
+                    auto scan = [&](uint8_t* piece) {
+                        if (!row_not_finite(piece, lane)) return;
                         atomicOr(&sm.bad[st][r >> 5], 1u << lane);
-                        __threadfence_block();
+                        drop_not_finite(piece);
+                        fence_proxy_async_smem();
                     };
                     if (KEYS) {
 #pragma unroll
-                        for (int h = 0; h < C::HALVES; ++h) wrote |= drop_not_finite(at + o * C::COLS_BYTES + h * COLS_HALF_BYTES, lane, note);
+                        for (int h = 0; h < C::HALVES; ++h) scan(at + o * C::COLS_BYTES + h * COLS_HALF_BYTES);
                     } else if (o < C::HALVES) {
-                        wrote = drop_not_finite(at + o * COLS_HALF_BYTES, lane, note);
+                        scan(at + o * COLS_HALF_BYTES);
                     }
-                    if (wrote) fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sm.scanned[w]);
                     __syncwarp();

@@ -85,26 +85,32 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 
-// A row of 128 bytes (64 bf16) of a tile in shared memory: infinities and NaN become zero; true if there were any.  Called for consecutive
-// rows by consecutive lanes, which start at different 16-byte words so that they do not meet in a bank.  `before_write` runs
-// once, before the first change.
-template <typename F>
-__device__ __forceinline__ bool drop_not_finite(uint8_t* row, int lane, F before_write) {
-    bool bad = false;
+// A row of 128 bytes (64 bf16) of a tile in shared memory: whether any value is an infinity or NaN (times 0 they leave NaN in the sum, everything
+// else leaves 0).  Called for consecutive rows by consecutive lanes, which start at different 16-byte words so that they do not meet in a bank.
+__device__ __forceinline__ bool row_not_finite(const uint8_t* row, int lane) {
+    const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+    __nv_bfloat162 sum[4] = {zero, zero, zero, zero};
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-        uint4* at = reinterpret_cast<uint4*>(row + (((c + lane) & 7) << 4));
-        uint4 w = *at;
-        const uint32_t e = 0x7F807F80u;
-        const uint32_t x = __vcmpeq2(w.x & e, e), y = __vcmpeq2(w.y & e, e), z = __vcmpeq2(w.z & e, e), u = __vcmpeq2(w.w & e, e);
-        if (x | y | z | u) {
-            if (!bad) before_write();
-            bad = true;
-            w.x &= ~x; w.y &= ~y; w.z &= ~z; w.w &= ~u;
-            *at = w;
-        }
+        const uint4 w = *reinterpret_cast<const uint4*>(row + (((c + lane) & 7) << 4));
+        sum[0] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w.x), zero, sum[0]);
+        sum[1] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w.y), zero, sum[1]);
+        sum[2] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w.z), zero, sum[2]);
+        sum[3] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w.w), zero, sum[3]);
     }
-    return bad;
+    const __nv_bfloat162 all = __hadd2(__hadd2(sum[0], sum[1]), __hadd2(sum[2], sum[3]));
+    return __hisnan(__low2bfloat16(all)) || __hisnan(__high2bfloat16(all));
+}
+// Puts zeros in their place.
+__device__ __forceinline__ void drop_not_finite(uint8_t* row) {
+    uint32_t* w = reinterpret_cast<uint32_t*>(row);
+    for (int c = 0; c < 32; ++c) {
+        const uint32_t x = w[c];
+        uint32_t y = x;
+        if ((x & 0x7F80u) == 0x7F80u) y &= 0xFFFF0000u;
+        if ((x & 0x7F800000u) == 0x7F800000u) y &= 0x0000FFFFu;
+        if (y != x) w[c] = y;
+    }
 }
 
 }  // namespace
