@@ -371,10 +371,11 @@ int arrol_attention_backward(arrol_ctx* ctx, const arrol_attention_args* args, v
  * prompt_v, p = i / G, and to rows src_tok_off[i] .. src_tok_off[i] + lengths[i] - 1 of the caches k / v [cache_rows, Hkv, D] (the current
  * token's own row among them, if the caller has written it).  o [N, Hq, D] and lse [N, Hq] (or NULL) as above; a rollout without any key
  * gets o = 0, lse = -inf; rows of rollouts that are not kept are not written, nor are their offsets and lengths followed.
- * A prompt's keys and values are read once for all of its live rollouts (up to 128 rows of query heads per key head; beyond, again).
+ * A prompt's keys and values are read once for all of its live rollouts (up to 64 query rows, rollouts x Hq / Hkv, per key head; beyond, again
+ * for each 64).
  * N = P G where there are prompts (rollouts of group p are p G .. p G + G - 1); without prompts (NULL, P = 0, prompt_rows = 0) N and G >= 1
  * are free.
- * Types, layouts, alignment, D, Hq, Hkv, infinities and NaN as above; cache_rows, prompt_rows < 2^31 - 512; G <= 1024.
+ * Types, layouts, alignment, D, Hq, Hkv, infinities and NaN as above; cache_rows, prompt_rows < 2^31 - 512; G <= 1024, N <= 2^24.
  * A rollout whose rows are not inside [0, cache_rows) (or a prompt's inside [0, prompt_rows)) is treated as if it had none there, and
  * ARROL_DEV_BAD_INDEX is recorded.  workspace: arrol_attention_decode_workspace(...) bytes, 256-byte aligned, contents as above. */
 typedef struct arrol_decode_args {

@@ -29,6 +29,7 @@ struct arrol_ctx {
     bool backward_smem_set;    // likewise for the lm_head backward
     bool attention_smem_set[2];   // likewise for attention, D <= 64 and above
     bool attention_backward_smem_set[2];
+    bool attention_decode_smem_set[2];
     bool prune_smem_set;       // likewise for the fused prune step
     int score_max_clusters[3][9]; // scoring kernel, tiles of 128 x 64, 64 x 64 and 128 x 128 rollouts x hidden units: clusters of so many
                                // blocks that are resident at once; 0 = not asked yet

@@ -56,6 +56,7 @@ extern "C" int arrol_create(arrol_ctx** out, int device) {
     ctx->backward_smem_set = false;
     ctx->attention_smem_set[0] = ctx->attention_smem_set[1] = false;
     ctx->attention_backward_smem_set[0] = ctx->attention_backward_smem_set[1] = false;
+    ctx->attention_decode_smem_set[0] = ctx->attention_decode_smem_set[1] = false;
     ctx->prune_smem_set = false;
     for (int& n : ctx->backward_max_pairs) n = 0;
     for (auto& rows : ctx->score_max_clusters)
