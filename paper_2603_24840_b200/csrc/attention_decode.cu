@@ -11,33 +11,35 @@
 namespace {
 
 constexpr int DEC_ROWS = 64;                       // query rows a unit
-constexpr int DEC_WARPS = 4;                       // consumers; one more warp loads
-constexpr int DEC_THREADS = 32 * (DEC_WARPS + 1);
+constexpr int DEC_WARPS = 4;                       // consumers; one more warp loads keys and values, one looks up what comes next
+constexpr int DEC_THREADS = 32 * (DEC_WARPS + 2);
 constexpr int DEC_STAGES = 4;
-constexpr int DEC_SLOTS = 2;
+constexpr int DEC_SLOTS = 4;                       // pairs looked up ahead
 constexpr int DEC_STAGE_BYTES = 16384;             // keys and values of 32 tokens of 128 dimensions, of 64 tokens of 64
-constexpr int DEC_MIN_CHUNK = 128;                 // tokens
-constexpr int DEC_OWN_PER_SM = 32, DEC_SHARED_PER_SM = 8;   // (unit, head) pairs that the chunks' lengths aim at; partial sums of prompt units are many
+// Tokens of a chunk: as many as make DEC_FEW_PER_SM (unit, head) pairs an SM, between 128 and 512; more where that would make more than
+// DEC_OWN_PER_SM pairs (DEC_SHARED_PER_SM of prompts, whose partial sums are many).
+constexpr int DEC_MIN_CHUNK = 128, DEC_GOOD_CHUNK = 512;
+constexpr int DEC_FEW_PER_SM = 4, DEC_OWN_PER_SM = 32, DEC_SHARED_PER_SM = 8;
 constexpr int PLAN_THREADS = 1024;
+constexpr float RESCALE_AT = 8.0f;                 // the running maximum follows once it is 2^8 behind
 
 struct alignas(16) DecodeUnit {
     int tok0, ntok;        // rows of the cache, or of the prompts
-    int rows, src;         // query rows; the rollout, or the first live rollout's number among the live ones
+    int rows, src;         // query rows; number of the first of its rollouts among the live ones
     int slot, shared;      // record of each of its rollouts: own chunk `slot`, or chunk `slot` of the prompt behind the own ones
     int pad[2];
 };
-// A rollout's records: own chunks, then the prompt's.
-struct alignas(16) RolloutRecords {
-    int base, own, count, pad;
+// A live rollout and its records: own chunks, then the prompt's.
+struct alignas(16) LiveRollout {
+    int rollout, base, own, count;
 };
 
 struct DecodeWorkspace {
     int* head;             // [0] work counter, [1] units
     DecodeUnit* units;
-    RolloutRecords* records;
-    int* live;             // live rollouts in order
-    int* scan;             // [N][2], of the plan: own units before, live before
-    int2* scan_prompt;     // [P]: units before
+    LiveRollout* live;     // in order
+    int* live_before;      // [N]: live rollouts before each
+    int* prompt_chunks;    // [P]
     float* o;              // [records][Hq][D]
     float2* ml;            // [records][Hq]: maximum (of scores log2 e), sum
     int64_t max_units, max_records;
@@ -58,10 +60,9 @@ DecodeWorkspace decode_workspace(void* base, int sm_count, int N, int P, int Hq,
     auto take = [&](size_t n) { uint8_t* q = p + at; at += attn_round(n); return q; };
     w.head = reinterpret_cast<int*>(take(256));
     w.units = reinterpret_cast<DecodeUnit*>(take((size_t)w.max_units * sizeof(DecodeUnit)));
-    w.records = reinterpret_cast<RolloutRecords*>(take((size_t)N * sizeof(RolloutRecords)));
-    w.live = reinterpret_cast<int*>(take((size_t)N * sizeof(int)));
-    w.scan = reinterpret_cast<int*>(take((size_t)N * 2 * sizeof(int)));
-    w.scan_prompt = reinterpret_cast<int2*>(take((size_t)P * sizeof(int2)));
+    w.live = reinterpret_cast<LiveRollout*>(take((size_t)N * sizeof(LiveRollout)));
+    w.live_before = reinterpret_cast<int*>(take((size_t)N * sizeof(int)));
+    w.prompt_chunks = reinterpret_cast<int*>(take((size_t)P * sizeof(int)));
     w.ml = reinterpret_cast<float2*>(take((size_t)w.max_records * Hq * sizeof(float2)));
     w.o = reinterpret_cast<float*>(take((size_t)w.max_records * Hq * D * sizeof(float)));
     w.bytes = at;
@@ -72,7 +73,7 @@ struct DecodeParams {
     arrol_decode_args a;
     DecodeWorkspace w;
     int ratio, group;
-    int own_target, shared_target;      // units
+    int few_units, own_target, shared_target;
     float scale_log2;
     uint32_t* status;
 };
@@ -124,8 +125,10 @@ __device__ __forceinline__ long long block_sum(long long v, long long* warp_sums
     __syncthreads();
     return v;
 }
-__device__ __forceinline__ int chunk_tokens(long long tokens, int target) {
-    const long long c = (tokens + target - 1) / target;
+__device__ __forceinline__ int chunk_tokens(long long tokens, int few, int target) {
+    long long c = (tokens + few - 1) / few;
+    if (c > DEC_GOOD_CHUNK) c = DEC_GOOD_CHUNK;
+    c = max(c, (tokens + target - 1) / target);
     return c <= DEC_MIN_CHUNK ? DEC_MIN_CHUNK : c >= 1 << 30 ? 1 << 30 : (int)((c + 63) / 64 * 64);
 }
 
@@ -145,30 +148,36 @@ __global__ void __launch_bounds__(PLAN_THREADS) decode_plan_kernel(const DecodeP
         const int i = i0 + tid, n = i < a.N ? own_tokens(a, i, bad) : -1;
         int2 total;
         const int2 before = block_scan(make_int2(n >= 0, 0), total, warp_sums);
-        if (n >= 0) {
-            own_total += n;
-            p.w.live[live_before + before.x] = i;
-        }
-        if (i < a.N) p.w.scan[2 * i + 1] = live_before + before.x;
+        if (n >= 0) own_total += n;
+        if (i < a.N) p.w.live_before[i] = live_before + before.x;
         live_before += total.x;
     }
-    const int own_chunk = chunk_tokens(block_sum(own_total, sums), p.own_target);     // its barriers publish the numbers above
+    const int own_chunk = chunk_tokens(block_sum(own_total, sums), p.few_units, p.own_target);     // its barriers publish the numbers above
     // prompt tokens, once per group of live rollouts that a unit takes
-    auto live_of = [&](int q) { return (q + 1 < a.P ? p.w.scan[2 * (q + 1) * a.G + 1] : live_before) - p.w.scan[2 * q * a.G + 1]; };
+    auto live_of = [&](int q) { return (q + 1 < a.P ? p.w.live_before[(q + 1) * a.G] : live_before) - p.w.live_before[q * a.G]; };
     long long shared_total = 0;
     for (int q = tid; q < a.P; q += PLAN_THREADS) {
         const int live = live_of(q);
         if (live > 0) shared_total += (long long)prompt_tokens(a, q, bad) * ((live + p.group - 1) / p.group);
     }
-    const int shared_chunk = chunk_tokens(block_sum(shared_total, sums), p.shared_target);
-    // prompt units
+    const int shared_chunk = chunk_tokens(block_sum(shared_total, sums), p.few_units, p.shared_target);
+    // prompt units: a thread writes those of its prompt
     int units = 0;
     for (int q0 = 0; q0 < a.P; q0 += PLAN_THREADS) {
-        const int q = q0 + tid, live = q < a.P ? live_of(q) : 0;
-        const int chunks = live > 0 ? (prompt_tokens(a, q, bad) + shared_chunk - 1) / shared_chunk : 0;
+        const int q = q0 + tid, live = q < a.P ? live_of(q) : 0, n = live > 0 ? prompt_tokens(a, q, bad) : 0;
+        const int chunks = (n + shared_chunk - 1) / shared_chunk, groups = (live + p.group - 1) / p.group;
         int2 total;
-        const int2 before = block_scan(make_int2(chunks * ((live + p.group - 1) / p.group), 0), total, warp_sums);
-        if (q < a.P) p.w.scan_prompt[q] = make_int2(units + before.x, chunks);
+        const int2 before = block_scan(make_int2(chunks * groups, 0), total, warp_sums);
+        if (q < a.P) p.w.prompt_chunks[q] = chunks;
+        if (n > 0) {
+            const int first = p.w.live_before[q * a.G], x = (int)a.cu_prompts[q];
+            int64_t at = units + before.x;
+            for (int c = 0; c < chunks; ++c)
+                for (int g = 0; g < groups && at < p.w.max_units; ++g, ++at) {        // a chunk's groups side by side: they read the same rows
+                    const DecodeUnit d = {x + c * shared_chunk, min(shared_chunk, n - c * shared_chunk), min(p.group, live - g * p.group) * p.ratio, first + g * p.group, c, 1, {0, 0}};
+                    p.w.units[at] = d;
+                }
+        }
         units += total.x;
     }
     __syncthreads();
@@ -177,39 +186,23 @@ __global__ void __launch_bounds__(PLAN_THREADS) decode_plan_kernel(const DecodeP
     for (int i0 = 0; i0 < a.N; i0 += PLAN_THREADS) {
         const int i = i0 + tid, n = i < a.N ? own_tokens(a, i, bad) : -1;
         const int own = n > 0 ? (n + own_chunk - 1) / own_chunk : 0;
-        const int count = n < 0 ? 0 : own + (a.P > 0 ? p.w.scan_prompt[i / a.G].y : 0);
+        const int count = n < 0 ? 0 : own + (a.P > 0 ? p.w.prompt_chunks[i / a.G] : 0);
         int2 total;
         const int2 before = block_scan(make_int2(own, count), total, warp_sums);
-        if (i < a.N) {
-            RolloutRecords r = {records + before.y, own, count, 0};
-            if (r.base + (int64_t)count > p.w.max_records) { r = {0, 0, 0, 0}; bad = true; }     // only past 2^30 tokens a unit
-            p.w.records[i] = r;
-            p.w.scan[2 * i] = units + before.x;
+        if (n >= 0) {
+            const int number = p.w.live_before[i];
+            LiveRollout r = {i, records + before.y, own, count};
+            if (r.base + (int64_t)count > p.w.max_records) { r = {i, 0, 0, 0}; bad = true; }     // only past 2^30 tokens a unit
+            p.w.live[number] = r;
+            int64_t at = units + before.x;
+            const int off = n > 0 ? (int)a.src_tok_off[i] : 0;
+            for (int c = 0; c < r.own && at < p.w.max_units; ++c, ++at) {
+                const DecodeUnit d = {off + c * own_chunk, min(own_chunk, n - c * own_chunk), p.ratio, number, c, 0, {0, 0}};
+                p.w.units[at] = d;
+            }
         }
         units += total.x;
         records += total.y;
-    }
-    __syncthreads();
-    // the units themselves: a warp per prompt, then per rollout
-    const int lane = tid & 31, warp = tid >> 5;
-    for (int q = warp; q < a.P; q += PLAN_THREADS / 32) {
-        const int2 at = p.w.scan_prompt[q];
-        if (at.y == 0) continue;
-        const int live = live_of(q), first = p.w.scan[2 * q * a.G + 1], groups = (live + p.group - 1) / p.group;
-        const int64_t x = a.cu_prompts[q];
-        const int n = (int)(a.cu_prompts[q + 1] - x);
-        for (int u = lane; u < groups * at.y && at.x + u < p.w.max_units; u += 32) {
-            const int c = u / groups, g = u - c * groups;          // a chunk's groups side by side: they read the same rows
-            DecodeUnit d = {(int)x + c * shared_chunk, min(shared_chunk, n - c * shared_chunk), min(p.group, live - g * p.group) * p.ratio, first + g * p.group, c, 1, {0, 0}};
-            p.w.units[at.x + u] = d;
-        }
-    }
-    for (int i = warp; i < a.N; i += PLAN_THREADS / 32) {
-        const int own = p.w.records[i].own, at = p.w.scan[2 * i];
-        for (int c = lane; c < own && at + c < p.w.max_units; c += 32) {
-            DecodeUnit d = {(int)a.src_tok_off[i] + c * own_chunk, min(own_chunk, a.lengths[i] - c * own_chunk), p.ratio, i, c, 0, {0, 0}};
-            p.w.units[at + c] = d;
-        }
     }
     if (tid == 0) {
         p.w.head[0] = 0;
@@ -245,8 +238,8 @@ struct DecConf {
 };
 
 struct DecodeItem {
-    DecodeUnit unit;
-    int g, valid;
+    int tok0, ntok, rows, shared, g, valid;
+    int2 of[DEC_ROWS];                             // per rollout of the unit: its number, the record
 };
 struct DecodeShared {
     uint64_t full[DEC_STAGES], empty[DEC_STAGES], item_full[DEC_SLOTS], item_empty[DEC_SLOTS], part_full, part_free;
@@ -269,7 +262,7 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     const arrol_decode_args& a = p.a;
     if (threadIdx.x == 0) {
         for (int i = 0; i < DEC_STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], DEC_WARPS); }
-        for (int i = 0; i < DEC_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], DEC_WARPS); }
+        for (int i = 0; i < DEC_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], DEC_WARPS + 1); }
         mbar_init(&sm.part_full, DEC_WARPS);
         mbar_init(&sm.part_free, DEC_WARPS);
         sm.abort = 0u;
@@ -283,31 +276,62 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     const int* head = pdl_acquire(p.w.head);
     const int64_t items = (int64_t)head[1] * a.Hkv;
 
-    if (warp == DEC_WARPS) {
+    if (warp == DEC_WARPS + 1) {
+        // ---- looks up what comes next: while a pair's rollouts are fetched, the next one's unit is, and a number for the one after it
         const DecodeUnit* units = pdl_acquire(p.w.units);
+        const LiveRollout* live = pdl_acquire(p.w.live);
+        auto number = [&] {
+            uint32_t idx = 0;
+            if (lane == 0) idx = atomicAdd(reinterpret_cast<unsigned int*>(p.w.head), 1u);
+            return idx;
+        };
+        uint32_t idx = __shfl_sync(0xffffffffu, number(), 0);
+        bool valid = (int64_t)idx < items;
+        DecodeUnit u = {};
+        if (valid) u = units[idx / (uint32_t)a.Hkv];           // the heads of a unit side by side: they read the same rows
+        uint32_t after = number();
+        for (uint32_t n = 0;; ++n) {
+            const uint32_t next = __shfl_sync(0xffffffffu, after, 0);
+            const bool next_valid = valid && (int64_t)next < items;
+            DecodeUnit next_u = {};
+            if (next_valid) {
+                next_u = units[next / (uint32_t)a.Hkv];
+                after = number();
+            }
+            const int rollouts = u.rows / p.ratio;
+            LiveRollout r[DEC_ROWS / 32];
+#pragma unroll
+            for (int k = 0; k < DEC_ROWS / 32; ++k)
+                if (valid && k * 32 + lane < rollouts) r[k] = live[u.src + k * 32 + lane];
+            const uint32_t slot = n % DEC_SLOTS;
+            if (!mbar_wait_warp(&sm.item_empty[slot], ((n / DEC_SLOTS) & 1u) ^ 1u, abort_flag)) break;
+            DecodeItem& it = sm.items[slot];
+#pragma unroll
+            for (int k = 0; k < DEC_ROWS / 32; ++k)
+                if (valid && k * 32 + lane < rollouts) it.of[k * 32 + lane] = make_int2(r[k].rollout, r[k].base + (u.shared ? r[k].own : 0) + u.slot);
+            if (lane == 0) {
+                it.tok0 = u.tok0; it.ntok = u.ntok; it.rows = u.rows; it.shared = u.shared;
+                it.g = (int)(idx % (uint32_t)a.Hkv);
+                it.valid = valid;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.item_full[slot]);
+            __syncwarp();
+            if (!valid) break;
+            idx = next; valid = next_valid; u = next_u;
+        }
+    } else if (warp == DEC_WARPS) {
         uint32_t pos = 0;
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % DEC_SLOTS;
-            if (!mbar_wait_warp(&sm.item_empty[slot], ((n / DEC_SLOTS) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-            uint32_t idx = 0;
-            if (lane == 0) idx = atomicAdd(reinterpret_cast<unsigned int*>(p.w.head), 1u);
-            idx = __shfl_sync(0xffffffffu, idx, 0);
-            const bool valid = (int64_t)idx < items;
-            DecodeUnit u = {};
-            const int g = (int)(idx % (uint32_t)a.Hkv);
-            if (valid) u = units[idx / (uint32_t)a.Hkv];       // the heads of a unit side by side: they read the same rows
-            if (lane == 0) {
-                sm.items[slot].unit = u;
-                sm.items[slot].g = g;
-                sm.items[slot].valid = valid;
-                mbar_arrive(&sm.item_full[slot]);
-            }
-            __syncwarp();
-            if (!valid) break;
-            const CUtensorMap* mk = u.shared ? &map_pk : &map_k;
-            const CUtensorMap* mv = u.shared ? &map_pv : &map_v;
-            for (int t = 0; t < u.ntok; t += C::TOKENS, ++pos) {
+            if (!mbar_wait_warp(&sm.item_full[slot], (n / DEC_SLOTS) & 1u, abort_flag)) { ok = false; break; }
+            const DecodeItem& it = sm.items[slot];
+            if (!it.valid) break;
+            const int ntok = uniform(it.ntok), tok0 = uniform(it.tok0), g = uniform(it.g);
+            const CUtensorMap* mk = it.shared ? &map_pk : &map_k;
+            const CUtensorMap* mv = it.shared ? &map_pv : &map_v;
+            for (int t = 0; t < ntok; t += C::TOKENS, ++pos) {
                 const uint32_t st = pos % DEC_STAGES;
                 if (!mbar_wait_warp(&sm.empty[st], ((pos / DEC_STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
                 if (elect_one()) {
@@ -315,12 +339,14 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     uint8_t* at = ring + st * DEC_STAGE_BYTES;
 #pragma unroll
                     for (int h = 0; h < C::HALVES; ++h) {
-                        tma_load_3d(at + h * C::HALF_BYTES, mk, h * 64, g, u.tok0 + t, &sm.full[st]);
-                        tma_load_3d(at + C::KEYS_BYTES + h * C::HALF_BYTES, mv, h * 64, g, u.tok0 + t, &sm.full[st]);
+                        tma_load_3d(at + h * C::HALF_BYTES, mk, h * 64, g, tok0 + t, &sm.full[st]);
+                        tma_load_3d(at + C::KEYS_BYTES + h * C::HALF_BYTES, mv, h * 64, g, tok0 + t, &sm.full[st]);
                     }
                 }
                 __syncwarp();
             }
+            if (ok && lane == 0) mbar_arrive(&sm.item_empty[slot]);
+            __syncwarp();
         }
         if (!ok) {                           // let the copies in flight land before the block's shared memory goes away
             for (uint32_t i = 1; i <= DEC_STAGES && i <= pos; ++i)
@@ -330,33 +356,38 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         __syncwarp();
     } else {
         // ---- consumers.  A unit's rows are 1, 2 or 4 tiles of 16; the warps that are left share its tokens.
-        const int* live = pdl_acquire(p.w.live);
-        const RolloutRecords* records = pdl_acquire(p.w.records);
-        uint32_t pos0 = 0;
-        for (uint32_t n = 0;; ++n) {
+        // The next pair's queries are on their way while this one's sums are added up.
+        const uint32_t ratio_inv = (65536u + p.ratio - 1) / p.ratio;          // row / ratio = row * ratio_inv >> 16 for rows below 64
+        uint32_t pos0 = 0, merged = 0;
+        uint32_t q[DP / 16][4];              // query rows (lane / 4) and (lane / 4) + 8 of the tile as fragments
+        auto begin = [&](uint32_t n) {
             const uint32_t slot = n % DEC_SLOTS;
-            if (!mbar_wait_warp(&sm.item_full[slot], (n / DEC_SLOTS) & 1u, abort_flag)) break;
+            if (!mbar_wait_warp(&sm.item_full[slot], (n / DEC_SLOTS) & 1u, abort_flag)) return false;
             const DecodeItem& it = sm.items[slot];
-            if (!it.valid) break;
-            const DecodeUnit u = it.unit;
-            const int g = it.g, ratio = p.ratio;
-            const int row_tiles = u.rows <= 16 ? 1 : u.rows <= 32 ? 2 : 4, parts = DEC_WARPS / row_tiles;
-            const int tile = warp % row_tiles, share = warp / row_tiles;
-            const int tiles = (u.ntok + C::TOKENS - 1) / C::TOKENS;
-            // query rows (lane / 4) and (lane / 4) + 8 of the tile as fragments
-            uint32_t q[DP / 16][4];
+            if (!it.valid) return false;
+            const int row_tiles = it.rows <= 16 ? 1 : it.rows <= 32 ? 2 : 4;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                const int row = tile * 16 + (lane >> 2) + r * 8, l = row / ratio;
-                const bool there = row < u.rows;
-                const int i = !there ? 0 : u.shared ? live[u.src + l] : u.src;
-                const __nv_bfloat16* at = static_cast<const __nv_bfloat16*>(a.q) + i * a.q_stride + (int64_t)(g * ratio + row - l * ratio) * a.D + (lane & 3) * 2;
+                const int row = (warp & (row_tiles - 1)) * 16 + (lane >> 2) + r * 8, l = (int)(row * ratio_inv >> 16);
+                const bool there = row < it.rows;
+                const int i = there ? it.of[l].x : 0;
+                const __nv_bfloat16* at = static_cast<const __nv_bfloat16*>(a.q) + i * a.q_stride + (int64_t)(it.g * p.ratio + row - l * p.ratio) * a.D + (lane & 3) * 2;
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
                         q[k][c * 2 + r] = there && k * 16 + c * 8 < a.D ? *reinterpret_cast<const uint32_t*>(at + k * 16 + c * 8) : 0u;
             }
+            return true;
+        };
+        bool more = begin(0);
+        for (uint32_t n = 0; more; ++n) {
+            const uint32_t slot = n % DEC_SLOTS;
+            const DecodeItem& it = sm.items[slot];
+            const int rows = it.rows, ntok = it.ntok, head0 = it.g * p.ratio;
+            const int row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, parts = DEC_WARPS / row_tiles;
+            const int tile = warp & (row_tiles - 1), share = warp / row_tiles;
+            const int tiles = (ntok + C::TOKENS - 1) / C::TOKENS;
             float o[DP / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
             for (int d = 0; d < DP / 8; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f;
@@ -366,21 +397,28 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 if (!mbar_wait_warp(&sm.full[st], (pos / DEC_STAGES) & 1u, abort_flag)) { ok = false; break; }
                 uint8_t* const stage = ring + st * DEC_STAGE_BYTES;
                 const uint32_t keys = smem_u32(stage), values = keys + C::KEYS_BYTES;
-                const int there = u.ntok - t * C::TOKENS;      // tokens of the unit from here on
+                const int there = ntok - t * C::TOKENS;      // tokens of the unit from here on
                 float s[C::TOKENS / 8][4];
+                // dimensions outermost: a warp issues in order, and one score's products would each wait for the one before
+                constexpr int AT_ONCE = 4;
 #pragma unroll
-                for (int j = 0; j < C::TOKENS / 8; ++j) {
-                    s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-                    const int row = j * 8 + (lane & 7);
+                for (int j = 0; j < C::TOKENS / 8; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
 #pragma unroll
-                    for (int k = 0; k < DP / 32; ++k) {
+                for (int k = 0; k < DP / 32; ++k)
+#pragma unroll
+                    for (int j0 = 0; j0 < C::TOKENS / 8; j0 += AT_ONCE) {
+                        uint32_t b[AT_ONCE][4];
                         const int c = k * 4 + (lane >> 3);
-                        uint32_t b[4];
-                        ldmatrix_x4(keys + (c >> 3) * C::HALF_BYTES + row * 128 + (((c & 7) ^ (row & 7)) << 4), b);
-                        mma_16x8x16(s[j], q[2 * k], b[0], b[1]);
-                        mma_16x8x16(s[j], q[2 * k + 1], b[2], b[3]);
+#pragma unroll
+                        for (int j = 0; j < AT_ONCE; ++j) {
+                            const int row = (j0 + j) * 8 + (lane & 7);
+                            ldmatrix_x4(keys + (c >> 3) * C::HALF_BYTES + row * 128 + (((c & 7) ^ (row & 7)) << 4), b[j]);
+                        }
+#pragma unroll
+                        for (int j = 0; j < AT_ONCE; ++j) mma_16x8x16(s[j0 + j], q[2 * k], b[j][0], b[j][1]);
+#pragma unroll
+                        for (int j = 0; j < AT_ONCE; ++j) mma_16x8x16(s[j0 + j], q[2 * k + 1], b[j][2], b[j][3]);
                     }
-                }
                 if (there < C::TOKENS) {
                     // tokens behind the unit: no weight, and nothing that 0 times it would not make 0
 #pragma unroll
@@ -394,20 +432,27 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     fence_proxy_async_smem();
                     __syncwarp();
                 }
-                float up[2];
+                // The reference is let fall up to 2^8 behind the maximum, which changes nothing (sums and products carry the same factor): only where
+                // some row is further behind do its four lanes settle on a new one.
+                float mx[2];
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    float mx = -INFINITY;
+                    mx[r] = fmaxf(s[0][2 * r], s[0][2 * r + 1]);
 #pragma unroll
-                    for (int j = 0; j < C::TOKENS / 8; ++j) mx = fmaxf(mx, fmaxf(s[j][2 * r], s[j][2 * r + 1]));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2)) * p.scale_log2;
-                    const float top = fmaxf(m[r], mx);
-                    up[r] = top == -INFINITY ? 1.f : ex2_approx(m[r] - top);
-                    m[r] = top;
-                    l[r] *= up[r];
+                    for (int j = 1; j < C::TOKENS / 8; ++j) mx[r] = fmaxf(mx[r], fmaxf(s[j][2 * r], s[j][2 * r + 1]));
+                    mx[r] *= p.scale_log2;
                 }
-                if (__any_sync(0xffffffffu, up[0] != 1.f || up[1] != 1.f)) {
+                if (__any_sync(0xffffffffu, mx[0] > m[0] + RESCALE_AT || mx[1] > m[1] + RESCALE_AT)) {
+                    float up[2];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
+                        mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
+                        const float top = fmaxf(m[r], mx[r]);
+                        up[r] = top == -INFINITY ? 1.f : ex2_approx(m[r] - top);
+                        m[r] = top;
+                        l[r] *= up[r];
+                    }
 #pragma unroll
                     for (int d = 0; d < DP / 8; ++d) { o[d][0] *= up[0]; o[d][1] *= up[0]; o[d][2] *= up[1]; o[d][3] *= up[1]; }
                 }
@@ -425,12 +470,18 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                                            pack_bf16(s[2 * k + 1][2], s[2 * k + 1][3])};
                     const int row = k * 16 + (lane & 15);
 #pragma unroll
-                    for (int d = 0; d < DP / 16; ++d) {
-                        const int c = d * 2 + (lane >> 4);
-                        uint32_t b[4];
-                        ldmatrix_x4_trans(values + (c >> 3) * C::HALF_BYTES + row * 128 + (((c & 7) ^ (row & 7)) << 4), b);
-                        mma_16x8x16(o[2 * d], w, b[0], b[1]);
-                        mma_16x8x16(o[2 * d + 1], w, b[2], b[3]);
+                    for (int d0 = 0; d0 < DP / 16; d0 += AT_ONCE) {
+                        uint32_t b[AT_ONCE][4];
+#pragma unroll
+                        for (int d = 0; d < AT_ONCE; ++d) {
+                            const int c = (d0 + d) * 2 + (lane >> 4);
+                            ldmatrix_x4_trans(values + (c >> 3) * C::HALF_BYTES + row * 128 + (((c & 7) ^ (row & 7)) << 4), b[d]);
+                        }
+#pragma unroll
+                        for (int d = 0; d < AT_ONCE; ++d) {
+                            mma_16x8x16(o[2 * (d0 + d)], w, b[d][0], b[d][1]);
+                            mma_16x8x16(o[2 * (d0 + d) + 1], w, b[d][2], b[d][3]);
+                        }
                     }
                 }
                 __syncwarp();
@@ -445,48 +496,77 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
                 l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
             }
-            if (!mbar_wait_warp(&sm.part_free, (n & 1u) ^ 1u, abort_flag)) break;
-            float* const mine = part + warp * 16 * C::PITCH;
+            int2 of[2];                      // head and record of this lane's two rows, before the slot is left
 #pragma unroll
-            for (int d = 0; d < DP / 8; ++d) {
-                *reinterpret_cast<float2*>(mine + (lane >> 2) * C::PITCH + d * 8 + (lane & 3) * 2) = make_float2(o[d][0], o[d][1]);
-                *reinterpret_cast<float2*>(mine + ((lane >> 2) + 8) * C::PITCH + d * 8 + (lane & 3) * 2) = make_float2(o[d][2], o[d][3]);
+            for (int r = 0; r < 2; ++r) {
+                const int row = tile * 16 + (lane >> 2) + r * 8, lr = (int)(row * ratio_inv >> 16);
+                of[r] = make_int2(head0 + row - lr * p.ratio, row < rows ? it.of[lr].y : -1);
             }
-            if ((lane & 3) == 0) {
-                sm.ml[warp][lane >> 2] = make_float2(m[0], l[0]);
-                sm.ml[warp][(lane >> 2) + 8] = make_float2(m[1], l[1]);
-            }
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&sm.part_full);
-                mbar_arrive(&sm.item_empty[slot]);
-            }
-            __syncwarp();
-            if (!mbar_wait_warp(&sm.part_full, n & 1u, abort_flag)) break;
-            const int pieces = a.D / 4;
-            for (int x = warp * 32 + lane; x < u.rows * pieces; x += 32 * DEC_WARPS) {
-                const int row = x / pieces, d = (x - row * pieces) * 4, t = row >> 4, r = row & 15;
-                float top = -INFINITY;
-                for (int s = 0; s < parts; ++s) top = fmaxf(top, sm.ml[s * row_tiles + t][r].x);
-                float4 sum = {0.f, 0.f, 0.f, 0.f};
-                float total = 0.f;
-                for (int s = 0; s < parts; ++s) {
-                    const float2 ml = sm.ml[s * row_tiles + t][r];
-                    const float by = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : ex2_approx(ml.x - top);       // a NaN without a maximum stays one
-                    const float4 v = *reinterpret_cast<const float4*>(part + ((s * row_tiles + t) * 16 + r) * C::PITCH + d);
-                    sum.x += by * v.x; sum.y += by * v.y; sum.z += by * v.z; sum.w += by * v.w;
-                    total += by * ml.y;
+            if (parts > 1) {
+                if (!mbar_wait_warp(&sm.part_free, (merged & 1u) ^ 1u, abort_flag)) break;
+                float* const mine = part + warp * 16 * C::PITCH;
+#pragma unroll
+                for (int d = 0; d < DP / 8; ++d) {
+                    *reinterpret_cast<float2*>(mine + (lane >> 2) * C::PITCH + d * 8 + (lane & 3) * 2) = make_float2(o[d][0], o[d][1]);
+                    *reinterpret_cast<float2*>(mine + ((lane >> 2) + 8) * C::PITCH + d * 8 + (lane & 3) * 2) = make_float2(o[d][2], o[d][3]);
                 }
-                const int lr = row / ratio, h = g * ratio + row - lr * ratio;
-                const RolloutRecords rec = records[u.shared ? live[u.src + lr] : u.src];
-                const int64_t at = (int64_t)(rec.base + (u.shared ? rec.own : 0) + u.slot) * a.Hq + h;
-                if (at >= p.w.max_records * a.Hq) continue;
-                *reinterpret_cast<float4*>(p.w.o + at * a.D + d) = sum;
-                if (d == 0) p.w.ml[at] = make_float2(top, total);
+                if ((lane & 3) == 0) {
+                    sm.ml[warp][lane >> 2] = make_float2(m[0], l[0]);
+                    sm.ml[warp][(lane >> 2) + 8] = make_float2(m[1], l[1]);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.part_full);
+                __syncwarp();
+                more = begin(n + 1);
+                if (!mbar_wait_warp(&sm.part_full, merged++ & 1u, abort_flag)) break;
+                for (int x = warp * 32 + lane; x < rows * (DP / 4); x += 32 * DEC_WARPS) {
+                    const int row = x / (DP / 4), d = x % (DP / 4) * 4, t = row >> 4, r = row & 15;
+                    if (d >= a.D) continue;
+                    float2 ml[DEC_WARPS];
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int s = 0; s < DEC_WARPS; ++s) {
+                        ml[s] = s < parts ? sm.ml[s * row_tiles + t][r] : make_float2(-INFINITY, 0.f);
+                        top = fmaxf(top, ml[s].x);
+                    }
+                    float4 sum = {0.f, 0.f, 0.f, 0.f};
+                    float total = 0.f;
+#pragma unroll
+                    for (int s = 0; s < DEC_WARPS; ++s)
+                        if (s < parts) {
+                            const float by = ml[s].x == -INFINITY ? (ml[s].y == 0.f ? 0.f : 1.f) : ex2_approx(ml[s].x - top);     // a NaN without a maximum stays one
+                            const float4 v = *reinterpret_cast<const float4*>(part + ((s * row_tiles + t) * 16 + r) * C::PITCH + d);
+                            sum.x += by * v.x; sum.y += by * v.y; sum.z += by * v.z; sum.w += by * v.w;
+                            total += by * ml[s].y;
+                        }
+                    const int lr = (int)(row * ratio_inv >> 16);
+                    const int64_t at = (int64_t)it.of[lr].y * a.Hq + head0 + row - lr * p.ratio;
+                    if (at >= p.w.max_records * a.Hq) continue;
+                    *reinterpret_cast<float4*>(p.w.o + at * a.D + d) = sum;
+                    if (d == 0) p.w.ml[at] = make_float2(top, total);
+                }
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&sm.part_free);
+                    mbar_arrive(&sm.item_empty[slot]);
+                }
+                __syncwarp();
+            } else {                         // every warp has its rows to itself
+                if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
+                __syncwarp();
+                more = begin(n + 1);
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int64_t at = (int64_t)of[r].y * a.Hq + of[r].x;
+                    if (of[r].y < 0 || at >= p.w.max_records * a.Hq) continue;
+                    float* out = p.w.o + at * a.D + (lane & 3) * 2;
+#pragma unroll
+                    for (int d = 0; d < DP / 8; ++d)
+                        if (d * 8 < a.D) *reinterpret_cast<float2*>(out + d * 8) = make_float2(o[d][2 * r], o[d][2 * r + 1]);
+                    if ((lane & 3) == 0) p.w.ml[at] = make_float2(m[r], l[r]);
+                }
+                __syncwarp();
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.part_free);
-            __syncwarp();
         }
     }
     __syncthreads();
@@ -503,24 +583,38 @@ __global__ void __launch_bounds__(256) decode_merge_kernel(const DecodeParams p)
     if (row >= (int64_t)a.N * a.Hq) return;
     const int i = (int)(row / a.Hq), h = (int)(row - (int64_t)i * a.Hq);
     if (a.keep && !a.keep[i]) return;
-    const RolloutRecords rec = *pdl_acquire(p.w.records + i);
+    const LiveRollout rec = pdl_acquire(p.w.live)[pdl_acquire(p.w.live_before)[i]];
     const float2* ml = pdl_acquire(p.w.ml) + (int64_t)rec.base * a.Hq + h;
     const float* o = pdl_acquire(p.w.o) + ((int64_t)rec.base * a.Hq + h) * a.D;
-    float top = -INFINITY;
-    for (int r = lane; r < rec.count; r += 32) top = fmaxf(top, ml[(int64_t)r * a.Hq].x);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    // eight records a round trip, each with its maximum; the sums follow the running one
+    constexpr int AT_ONCE = 8;
+    float top = -INFINITY, total = 0.f;
     float4 sum = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
     const int d = lane * 4;
-#pragma unroll 4
-    for (int r = 0; r < rec.count; ++r) {
-        const float2 x = ml[(int64_t)r * a.Hq];
-        const float by = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : ex2_approx(x.x - top);
-        total += by * x.y;
-        if (d < a.D) {
-            const float4 v = *reinterpret_cast<const float4*>(o + (int64_t)r * a.Hq * a.D + d);
-            sum.x += by * v.x; sum.y += by * v.y; sum.z += by * v.z; sum.w += by * v.w;
+    for (int r0 = 0; r0 < rec.count; r0 += AT_ONCE) {
+        float2 x[AT_ONCE];
+        float4 v[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            x[k] = make_float2(-INFINITY, 0.f);
+            v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r0 + k < rec.count) {
+                x[k] = ml[(int64_t)(r0 + k) * a.Hq];
+                if (d < a.D) v[k] = *reinterpret_cast<const float4*>(o + (int64_t)(r0 + k) * a.Hq * a.D + d);
+            }
+        }
+        float next = top;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) next = fmaxf(next, x[k].x);
+        const float up = next == -INFINITY ? 1.f : ex2_approx(top - next);
+        total *= up;
+        sum.x *= up; sum.y *= up; sum.z *= up; sum.w *= up;
+        top = next;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const float by = x[k].x == -INFINITY ? (x[k].y == 0.f ? 0.f : 1.f) : ex2_approx(x[k].x - top);
+            total += by * x[k].y;
+            sum.x += by * v[k].x; sum.y += by * v[k].y; sum.z += by * v[k].z; sum.w += by * v[k].w;
         }
     }
     const bool none = total == 0.f;
@@ -586,6 +680,7 @@ extern "C" int arrol_attention_decode(arrol_ctx* ctx, const arrol_decode_args* a
     if (a->workspace_bytes < p.w.bytes) return ARROL_ERR_WORKSPACE;
     p.ratio = a->Hq / a->Hkv;
     p.group = dec_group(p.ratio);
+    p.few_units = ctx->sm_count * DEC_FEW_PER_SM / a->Hkv + 1;
     p.own_target = ctx->sm_count * DEC_OWN_PER_SM / a->Hkv + 1;
     p.shared_target = ctx->sm_count * DEC_SHARED_PER_SM / a->Hkv + 1;
     p.scale_log2 = a->scale * LOG2E;
