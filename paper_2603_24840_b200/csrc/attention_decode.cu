@@ -14,12 +14,15 @@ constexpr int DEC_ROWS = 64;                       // query rows a unit
 constexpr int DEC_WARPS = 4;                       // consumers; one more warp loads keys and values, one looks up what comes next
 constexpr int DEC_THREADS = 32 * (DEC_WARPS + 2);
 constexpr int DEC_STAGES = 4;
+// A warp waits for every fourth stage at most: were the ring shorter, it could wait for a fill that is two ahead of the last one, whose parity is the
+// same as that of the one before, and would not wait at all.
+static_assert(DEC_STAGES >= DEC_WARPS, "parity waits");
 constexpr int DEC_SLOTS = 4;                       // pairs looked up ahead
 constexpr int DEC_STAGE_BYTES = 16384;             // keys and values of 32 tokens of 128 dimensions, of 64 tokens of 64
 // Tokens of a chunk: as many as make DEC_FEW_PER_SM (unit, head) pairs an SM, between 128 and 512; more where that would make more than
 // DEC_OWN_PER_SM pairs (DEC_SHARED_PER_SM of prompts, whose partial sums are many).
 constexpr int DEC_MIN_CHUNK = 128, DEC_GOOD_CHUNK = 512;
-constexpr int DEC_FEW_PER_SM = 4, DEC_OWN_PER_SM = 32, DEC_SHARED_PER_SM = 8;
+constexpr int DEC_FEW_PER_SM = 2, DEC_OWN_PER_SM = 32, DEC_SHARED_PER_SM = 8;
 constexpr int PLAN_THREADS = 1024;
 constexpr float RESCALE_AT = 8.0f;                 // the running maximum follows once it is 2^8 behind
 
