@@ -729,7 +729,7 @@ int arrol_internal_attention_bounds(arrol_ctx* ctx, const arrol_attention_args* 
 extern "C" size_t arrol_attention_workspace(arrol_ctx* ctx, int32_t S_max, int64_t T_max, int64_t prompt_rows, int32_t Hq, int32_t Hkv,
                                             int32_t D, int32_t backward) {
     if (!ctx || S_max < 0 || T_max < 0 || prompt_rows < 0 || T_max >= ATTN_MAX_ROWS || prompt_rows >= ATTN_MAX_ROWS || !attn_heads_ok(Hq, Hkv, D)) return 0;
-    return attn_workspace(nullptr, T_max, prompt_rows, Hq, backward != 0).bytes;
+    return attn_workspace(nullptr, ctx->sm_count, T_max, prompt_rows, Hq, Hkv, D, backward != 0).bytes;
 }
 
 extern "C" int arrol_attention(arrol_ctx* ctx, const arrol_attention_args* a, void* stream) {
@@ -737,7 +737,7 @@ extern "C" int arrol_attention(arrol_ctx* ctx, const arrol_attention_args* a, vo
     const int rc = arrol_internal_check_attention(a);
     if (rc != ARROL_OK) return rc;
     if (a->T_max == 0) return ARROL_OK;
-    const AttnWorkspace w = attn_workspace(a->workspace, a->T_max, a->prompt_rows, a->Hq, false);
+    const AttnWorkspace w = attn_workspace(a->workspace, ctx->sm_count, a->T_max, a->prompt_rows, a->Hq, a->Hkv, a->D, false);
     if (a->workspace_bytes < w.bytes) return ARROL_ERR_WORKSPACE;
     ArrolDeviceGuard guard(ctx->device);
     if (!guard.ok) return ARROL_ERR_CUDA;

@@ -16,7 +16,7 @@
 
 namespace {
 
-constexpr int BWD_THREADS = 320;
+constexpr int BWD_THREADS = 384;                  // producer, MMA issuer, scanner, a spare warp; two groups of four warps
 constexpr int BWD_BLOCK = 64;                     // columns: query rows or keys a block
 constexpr int BWD_SLOTS = 2;
 constexpr uint32_t ROWS_HALF_BYTES = 128 * 128;   // 128 rows x 64 dimensions
@@ -31,12 +31,15 @@ struct BwdParams {
     int64_t out1_stride, out2_stride;
     __nv_bfloat16 *shared1, *shared2;             // dprompt_v, dprompt_k
     int64_t shared1_stride, shared2_stride;
+    int splits;                                   // parts of the tokens that pass by a prompt's tile, each an item; with more than one their sums go to
+    float *part1, *part2;                         // [splits][prompt tiles][Hkv][128][DP]
     uint32_t* counter;
     uint32_t* status;
 };
 
 struct BwdItem {
     int valid, g, shared, row0, rows;             // rows row0 .. of keys (prompt rows where shared) or tokens
+    int split;
     int pre0, n_pre, own0, n;                     // blocks, as in the forward kernel; KEYS: tokens own0 + TOKQ b ..
     int pre_in_lo, pre_in_hi, in_lo, in_hi;       // columns (keys or tokens) that every row has
 };
@@ -50,10 +53,10 @@ struct BwdConf {
 };
 
 struct BwdShared {
-    uint64_t full[8], empty[8], a_full, a_empty, xy_full[2], ps_full[2], acc_full, acc_empty, item_full[BWD_SLOTS], item_empty[BWD_SLOTS], scanned[2], drain;
-    alignas(16) float lse[8][BWD_BLOCK];          // read four at a time
+    uint64_t full[8], empty[8], a_full, a_empty, xy_full[2], ps_full[2], acc_full, acc_empty, item_full[BWD_SLOTS], item_empty[BWD_SLOTS], scanned[8], drain;
+    alignas(16) float lse[8][BWD_BLOCK];          // negative, as delta; read four at a time
     alignas(16) float delta[8][BWD_BLOCK];
-    uint32_t bad[8][2];                           // per stage: rows of an edge block that are not finite
+    uint32_t bad[8][2], bad_stats[8][2];          // per stage: rows of an edge block that are not finite, or whose statistics are not
     BwdItem items[BWD_SLOTS];
     uint32_t tmem, abort;
 };
@@ -84,16 +87,16 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
     uint8_t* const rows_a = smem;
     uint8_t* const ring = smem + 2 * C::ROWS_BYTES;
     volatile uint32_t* abort_flag = &sm.abort;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int ratio = p.sh.ratio, TOK = 128 / ratio, TOKQ = BWD_BLOCK / ratio;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); }
+        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 2); mbar_init(&sm.scanned[i], 1); }
         mbar_init(&sm.a_full, 1);
         mbar_init(&sm.a_empty, 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&sm.xy_full[i], 1); mbar_init(&sm.ps_full[i], 4); mbar_init(&sm.scanned[i], 4); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sm.xy_full[i], 1); mbar_init(&sm.ps_full[i], 4); }
         mbar_init(&sm.acc_full, 1);
         mbar_init(&sm.acc_empty, 8);
-        for (int i = 0; i < BWD_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], 9); }
+        for (int i = 0; i < BWD_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], 10); }
         mbar_init(&sm.drain, 1);
         sm.abort = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -113,7 +116,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
-    const uint32_t tmem = sm.tmem;                // accumulators 1 and 2 at columns 0 and 128; x, y of buffer i at 256 + 128 i and + 64
+    const uint32_t tmem = uniform(sm.tmem);                // accumulators 1 and 2 at columns 0 and 128; x, y of buffer i at 256 + 128 i and + 64
     pdl_launch_dependents();
     pdl_wait();
     const int T = clamp_row(*pdl_acquire(p.sh.d_num + 1), 0, p.sh.T_max);
@@ -121,7 +124,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
     const TokenBounds* bounds = pdl_acquire(p.sh.bounds);
     const int2* prompt_range = pdl_acquire(p.sh.prompt_range);
     const int prompt_tiles = (live_prompt + 127) / 128;
-    const int tiles = KEYS ? prompt_tiles + (T + 127) / 128 : (T + TOK - 1) / TOK;
+    const int tiles = KEYS ? prompt_tiles * p.splits + (T + 127) / 128 : (T + TOK - 1) / TOK;
     const int64_t items = (int64_t)tiles * p.sh.Hkv;
 
     if (warp == 0) {
@@ -142,8 +145,9 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 it.g = (int)(idx % (uint32_t)p.sh.Hkv);
                 if (KEYS) {
                     // the prompts' tiles first: every survivor's tokens pass by them; then the own ones from the first token on
-                    it.shared = tile < prompt_tiles;
-                    it.row0 = (it.shared ? tile : tile - prompt_tiles) * 128;
+                    it.shared = tile < prompt_tiles * p.splits;
+                    it.split = it.shared ? tile % p.splits : 0;
+                    it.row0 = (it.shared ? tile / p.splits : tile - prompt_tiles * p.splits) * 128;
                     it.rows = min(128, (it.shared ? live_prompt : T) - it.row0);
                     int lo = INT_MAX, hi = 0, in_lo = 0, in_hi = INT_MAX;
                     for (int r = lane; r < it.rows; r += 32) {
@@ -159,6 +163,11 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                     it.in_hi = __reduce_min_sync(0xffffffffu, in_hi);
                     it.own0 = lo;
                     it.n = lo < hi ? (hi - lo + TOKQ - 1) / TOKQ : 0;
+                    if (it.shared && p.splits > 1) {
+                        const int each = (it.n + p.splits - 1) / p.splits, from = min(it.split * each, it.n);
+                        it.own0 += from * TOKQ;
+                        it.n = min(each, it.n - from);
+                    }
                 } else {
                     it.row0 = (tiles - 1 - tile) * TOK;      // last tokens first: theirs are the longest ranges
                     it.rows = min(TOK, T - it.row0);
@@ -200,17 +209,27 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 for (int u = 0; u < 2; ++u) {
                     const int c = u * 32 + lane, tok = c / ratio, t = bwd_start<KEYS>(it, b, TOKQ) + tok;
                     next[u] = make_float2(INFINITY, 0.f);
-                    if (b < it.n && tok < TOKQ && t < T) next[u] = stats[(int64_t)t * p.sh.Hq + it.g * ratio + (c - tok * ratio)];
+                    if (b < it.n && tok < TOKQ && t < T) {
+                        next[u] = stats[(int64_t)t * p.sh.Hq + it.g * ratio + (c - tok * ratio)];
+                        if (next[u].x == INFINITY) next[u].x = NAN;
+                    }
                 }
             };
             if (KEYS) ask(0);
             for (int b = 0; b < it.n; ++b, ++pos) {
                 const uint32_t st = pos % C::STAGES;
                 if (!mbar_wait_warp(&sm.empty[st], ((pos / C::STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-                if (lane < 2) sm.bad[st][lane] = 0u;
                 if (KEYS) {
+                    const bool masked = bwd_masked<KEYS>(it, b, TOKQ);
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) { sm.lse[st][u * 32 + lane] = next[u].x; sm.delta[st][u * 32 + lane] = next[u].y; }
+                    for (int u = 0; u < 2; ++u) {
+                        // where some row does not have the column, statistics that are not finite go the way of such values
+                        const bool bad = masked && next[u].x != INFINITY && !(fabsf(next[u].x) < INFINITY && fabsf(next[u].y) < INFINITY);
+                        sm.lse[st][u * 32 + lane] = bad ? 0.f : -next[u].x;
+                        sm.delta[st][u * 32 + lane] = bad ? 0.f : -next[u].y;
+                        const uint32_t all = __ballot_sync(0xffffffffu, bad);
+                        if (lane == 0) sm.bad_stats[st][u] = all;
+                    }
                 }
                 __syncwarp();
                 if (elect_one()) {
@@ -248,7 +267,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
             const uint32_t slot = n % BWD_SLOTS;
             if (!mbar_wait_warp(&sm.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
             if (!sm.items[slot].valid) break;
-            const int blocks = sm.items[slot].n;
+            const int blocks = uniform(sm.items[slot].n);
             if (blocks > 0) {
                 if (!mbar_wait_warp(&sm.a_full, with_blocks & 1u, abort_flag)) { ok = false; break; }
                 for (int b = 0; b <= blocks; ++b) {
@@ -305,14 +324,55 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 if (mbar_try_wait(&sm.drain, 0u)) break;
         }
         __syncwarp();
-    } else {
+    } else if (warp == 2) {
+        // ---- scanner: in a block that some row does not have all of, what a masked 0 would meet in the second products must be finite
+        uint32_t c = 0;
+        bool ok = true;
+        for (uint32_t n = 0; ok; ++n) {
+            const uint32_t slot = n % BWD_SLOTS;
+            if (!mbar_wait_warp(&sm.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) break;
+            const BwdItem& it = sm.items[slot];
+            if (!it.valid) break;
+            const int blocks = it.n;
+            for (int b = 0; b < blocks; ++b) {
+                const uint32_t cur = c + b, st = cur % C::STAGES;
+                if (!mbar_wait_warp(&sm.full[st], (cur / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                if (bwd_masked<KEYS>(it, b, TOKQ)) {
+#pragma unroll 1
+                    for (int r = 0; r < 2; ++r) {
+                        bool bad = false;
+#pragma unroll
+                        for (int piece = 0; piece < (KEYS ? 2 : 1) * C::HALVES; ++piece) {
+                            uint8_t* at = ring + st * 2 * C::COLS_BYTES + piece * COLS_HALF_BYTES + (r * 32 + lane) * 128;
+                            if (row_not_finite(at, lane)) {
+                                bad = true;
+                                drop_not_finite(at);
+                                fence_proxy_async_smem();
+                            }
+                        }
+                        const uint32_t all = __ballot_sync(0xffffffffu, bad);
+                        if (lane == 0) sm.bad[st][r] = all;
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&sm.scanned[st]);
+                    mbar_arrive(&sm.empty[st]);
+                }
+                __syncwarp();
+            }
+            c += blocks;
+            if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
+            __syncwarp();
+        }
+    } else if (warp >= 4) {
         // ---- groups w = 0, 1: blocks in turn; thread = row
-        const int w = (warp - 2) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const int w = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const float scale2 = p.sh.scale_log2;
         const uint64_t scale_x2 = pack_f32x2(scale2, scale2);
         const float2* stats = pdl_acquire(p.stats);
-        uint32_t c = 0, with_blocks = 0, scans = 0;
+        uint32_t c = 0, with_blocks = 0;
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % BWD_SLOTS;
@@ -323,7 +383,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
             const int j = it.row0 + tok;              // key row or token of this thread
             const bool live = tok < it.rows;
             int lo = 0, hi = 0, pre_lo = 0, pre_hi = 0;
-            float2 mine = make_float2(0.f, 0.f);
+            float2 mine = make_float2(0.f, 0.f);      // the row's statistics
             if (live) {
                 if (KEYS) {
                     const int2 x = it.shared ? prompt_range[j] : make_int2(j, bounds[j].own_hi);
@@ -334,6 +394,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                     mine = stats[(int64_t)j * p.sh.Hq + head];
                 }
             }
+            const uint64_t neg_lse = pack_f32x2(-mine.x, -mine.x), neg_delta = pack_f32x2(-mine.y, -mine.y);
             for (int b = 0; b < blocks; ++b) {
                 const uint32_t cur = c + b;
                 if ((cur & 1u) != (uint32_t)w) continue;
@@ -353,75 +414,70 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                     }
                     if (!live || len < 0) len = 0;
                 }
-                if (!mbar_wait_warp(&sm.full[st], (cur / C::STAGES) & 1u, abort_flag) ||
+                if (!mbar_wait_warp(&sm.full[st], (cur / C::STAGES) & 1u, abort_flag) ||      // the columns' statistics
                     !mbar_wait_warp(&sm.xy_full[w], (cur >> 1) & 1u, abort_flag)) { ok = false; break; }
                 tcgen05_fence_after();
-                uint32_t x[2][32], y[2][32];
-                __syncwarp();
-#pragma unroll
-                for (int u = 0; u < 2; ++u) { tcgen05_ld_32x32_issue(xy + u * 32, x[u]); tcgen05_ld_32x32_issue(xy + 64 + u * 32, y[u]); }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) { tcgen05_ld_wait(x[u]); tcgen05_ld_wait(y[u]); }
-                uint32_t bad[2] = {0u, 0u};
+                uint32_t on[2] = {0xffffffffu, 0xffffffffu}, bad[2] = {0u, 0u};
+                bool select = false, none_of_it = false;
                 if (masked) {
-                    // as in the forward kernel: what a masked 0 would meet in the second products must be finite; a row that does have such a column
-                    // gets NaN instead
-                    const int r = row & 63, o = row >> 6;
-                    uint8_t* at = ring + st * 2 * C::COLS_BYTES + r * 128;
-                    auto scan = [&](uint8_t* piece) {
-                        if (!row_not_finite(piece, lane)) return;
-                        atomicOr(&sm.bad[st][r >> 5], 1u << lane);
-                        drop_not_finite(piece);
-                        fence_proxy_async_smem();
-                    };
-                    if (KEYS) {
+                    if (!mbar_wait_warp(&sm.scanned[st], (cur / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
 #pragma unroll
-                        for (int h = 0; h < C::HALVES; ++h) scan(at + o * C::COLS_BYTES + h * COLS_HALF_BYTES);
-                    } else if (o < C::HALVES) {
-                        scan(at + o * COLS_HALF_BYTES);
+                    for (int u = 0; u < 2; ++u) {
+                        const int a = min(max(first - u * 32, 0), 32), z = min(max(first + len - u * 32, 0), 32);
+                        on[u] = z > a ? (0xffffffffu >> (32 - z + a)) << a : 0u;
+                        bad[u] = (sm.bad[st][u] | (KEYS ? sm.bad_stats[st][u] : 0u)) & on[u];
                     }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sm.scanned[w]);
-                    __syncwarp();
-                    if (!mbar_wait_warp(&sm.scanned[w], scans++ & 1u, abort_flag)) { ok = false; break; }
-                    bad[0] = *reinterpret_cast<volatile uint32_t*>(&sm.bad[st][0]);
-                    bad[1] = *reinterpret_cast<volatile uint32_t*>(&sm.bad[st][1]);
+                    none_of_it = __all_sync(0xffffffffu, len == 0);
+                    select = !__all_sync(0xffffffffu, len == (KEYS ? TOKQ * ratio : BWD_BLOCK) && (bad[0] | bad[1]) == 0u);
                 }
-                uint32_t pk[32], dk[32];
-                const uint64_t neg_lse = pack_f32x2(-mine.x, -mine.x), neg_delta = pack_f32x2(-mine.y, -mine.y);
+                // half of the columns at a time: both operands of all 64 would not leave room for the results.  p and ds take the first halves of x's and
+                // y's columns, which have been read by then.
 #pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    float4 l4, d4;
-                    if (KEYS) {
-                        l4 = *reinterpret_cast<const float4*>(&sm.lse[st][2 * i]);
-                        d4 = *reinterpret_cast<const float4*>(&sm.delta[st][2 * i]);
-                    }
+                for (int u = 0; u < 2; ++u) {
+                    uint32_t pk[16], dk[16];
+                    if (none_of_it) {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int col = 2 * (i + k), u = col >> 5, v = col & 31;
-                        const uint64_t nl = KEYS ? (k ? pack_f32x2(-l4.z, -l4.w) : pack_f32x2(-l4.x, -l4.y)) : neg_lse;
-                        const uint64_t nd = KEYS ? (k ? pack_f32x2(-d4.z, -d4.w) : pack_f32x2(-d4.x, -d4.y)) : neg_delta;
-                        float p0, p1, s0, s1;
-                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[u][v]), __uint_as_float(x[u][v + 1])), scale_x2, nl), p0, p1);
-                        p0 = ex2_approx(p0);
-                        p1 = ex2_approx(p1);
-                        unpack_f32x2(mul_f32x2(pack_f32x2(p0, p1), add_f32x2(pack_f32x2(__uint_as_float(y[u][v]), __uint_as_float(y[u][v + 1])), nd)), s0, s1);
-                        if (masked) {
-                            const bool on0 = (uint32_t)(col - first) < (uint32_t)len, on1 = (uint32_t)(col + 1 - first) < (uint32_t)len;
-                            p0 = on0 ? p0 : 0.f; s0 = on0 ? s0 : 0.f;
-                            p1 = on1 ? p1 : 0.f; s1 = on1 ? s1 : 0.f;
-                            if (bad[u] >> v & 3u) {
-                                if (on0 && (bad[u] >> v & 1u)) p0 = s0 = NAN;
-                                if (on1 && (bad[u] >> v & 2u)) p1 = s1 = NAN;
+                        for (int i = 0; i < 16; ++i) pk[i] = dk[i] = 0u;
+                    } else {
+                        uint32_t x[32], y[32];
+                        __syncwarp();
+                        tcgen05_ld_32x32_issue(xy + u * 32, x);
+                        tcgen05_ld_32x32_issue(xy + 64 + u * 32, y);
+                        tcgen05_ld_wait(x);
+                        tcgen05_ld_wait(y);
+                        if (select) {
+#pragma unroll
+                            for (int v = 0; v < 32; ++v) {
+                                if (!(on[u] >> v & 1u)) { x[v] = 0xFF800000u; y[v] = 0u; }      // p = 0, ds = 0
+                                if (bad[u] >> v & 1u) x[v] = 0x7FC00000u;                       // a row that has a column which was not finite
                             }
                         }
-                        if (KEYS) pk[i + k] = pack_bf16(p0, p1);
-                        dk[i + k] = pack_bf16(s0, s1);
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            float4 l4, d4;
+                            if (KEYS) {
+                                l4 = *reinterpret_cast<const float4*>(&sm.lse[st][u * 32 + 2 * i]);
+                                d4 = *reinterpret_cast<const float4*>(&sm.delta[st][u * 32 + 2 * i]);
+                            }
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const int v = 2 * (i + k);
+                                const uint64_t nl = KEYS ? (k ? pack_f32x2(l4.z, l4.w) : pack_f32x2(l4.x, l4.y)) : neg_lse;
+                                const uint64_t nd = KEYS ? (k ? pack_f32x2(d4.z, d4.w) : pack_f32x2(d4.x, d4.y)) : neg_delta;
+                                float p0, p1, s0, s1;
+                                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[v]), __uint_as_float(x[v + 1])), scale_x2, nl), p0, p1);
+                                p0 = ex2_approx(p0);
+                                p1 = ex2_approx(p1);
+                                unpack_f32x2(mul_f32x2(pack_f32x2(p0, p1), add_f32x2(pack_f32x2(__uint_as_float(y[v]), __uint_as_float(y[v + 1])), nd)), s0, s1);
+                                if (KEYS) pk[i + k] = pack_bf16(p0, p1);
+                                dk[i + k] = pack_bf16(s0, s1);
+                            }
+                        }
                     }
+                    __syncwarp();
+                    if (KEYS) tcgen05_st_32x16(xy + u * 16, pk);
+                    tcgen05_st_32x16(xy + 64 + u * 16, dk);
                 }
-                __syncwarp();
-                if (KEYS) tcgen05_st_32x32(xy, pk);
-                tcgen05_st_32x32(xy + 64, dk);
                 tcgen05_st_wait();
                 tcgen05_fence_before();
                 __syncwarp();
@@ -445,6 +501,8 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 out = p.out2 + j * p.out2_stride + (int64_t)head * p.sh.D;
             }
             const float by = KEYS && w == 0 ? 1.f : p.sh.scale;
+            const bool to_parts = KEYS && it.shared && p.splits > 1;
+            float* const sums = !to_parts ? nullptr : (w == 0 ? p.part1 : p.part2) + ((((int64_t)it.split * ((p.sh.prompt_rows + 127) / 128) + it.row0 / 128) * p.sh.Hkv + it.g) * 128 + row) * DP;
             constexpr int PIECES = DP / 32;
 #pragma unroll 1
             for (int piece = KEYS ? 0 : w * (PIECES / 2); piece < (KEYS ? PIECES : (w + 1) * (PIECES / 2)); ++piece) {
@@ -457,7 +515,13 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = 0u;
                 }
-                if (live) {
+                if (to_parts) {
+                    if (live) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            *reinterpret_cast<float4*>(sums + piece * 32 + i) = make_float4(__uint_as_float(v[i]) * by, __uint_as_float(v[i + 1]) * by, __uint_as_float(v[i + 2]) * by, __uint_as_float(v[i + 3]) * by);
+                    }
+                } else if (live) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 8)
                         if (piece * 32 + i < p.sh.D) {
@@ -486,6 +550,31 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
     if (warp == 1) {
         tcgen05_fence_after();
         tcgen05_dealloc(tmem, 512);
+    }
+}
+
+// The parts of a prompt tile's sums, in order.
+template <int DP>
+__global__ void __launch_bounds__(256) attention_add_parts_kernel(const BwdParams p) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int live = p.P > 0 ? clamp_row(pdl_acquire(p.cu_prompts)[p.P], 0, p.sh.prompt_rows) : 0;
+    const int tiles = (p.sh.prompt_rows + 127) / 128;
+    const int64_t pieces = (int64_t)live * p.sh.Hkv * (DP / 8), step = (int64_t)tiles * p.sh.Hkv * 128 * DP;
+    for (int64_t x = blockIdx.x * (int64_t)256 + threadIdx.x; x < 2 * pieces; x += (int64_t)gridDim.x * 256) {
+        const bool second = x >= pieces;
+        const int64_t y = second ? x - pieces : x;
+        const int d = (int)(y % (DP / 8)) * 8, g = (int)(y / (DP / 8) % p.sh.Hkv), j = (int)(y / (DP / 8) / p.sh.Hkv);
+        if (d >= p.sh.D) continue;
+        const float* at = pdl_acquire(second ? p.part2 : p.part1) + (((int64_t)(j / 128) * p.sh.Hkv + g) * 128 + j % 128) * DP + d;
+        float4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+        for (int s = 0; s < p.splits; ++s, at += step) {
+            const float4 u = *reinterpret_cast<const float4*>(at), v = *reinterpret_cast<const float4*>(at + 4);
+            a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
+            b.x += v.x; b.y += v.y; b.z += v.z; b.w += v.w;
+        }
+        __nv_bfloat16* out = (second ? p.shared2 + j * p.shared2_stride : p.shared1 + j * p.shared1_stride) + (int64_t)g * p.sh.D + d;
+        *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
     }
 }
 
@@ -524,10 +613,18 @@ int launch_backward(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWor
     p.shared1 = static_cast<__nv_bfloat16*>(a->dprompt_v); p.shared1_stride = a->dprompt_v_stride;
     p.shared2 = static_cast<__nv_bfloat16*>(a->dprompt_k); p.shared2_stride = a->dprompt_k_stride;
     p.counter = w.counters + 1;
-    int64_t items = ((a->T_max + 127) / 128 + (a->prompt_rows + 127) / 128) * a->Hkv;
+    p.splits = attn_prompt_splits(ctx->sm_count, a->T_max, a->prompt_rows, a->P, a->Hq, a->Hkv);
+    p.part1 = w.parts;
+    p.part2 = w.parts + (int64_t)p.splits * ((a->prompt_rows + 127) / 128) * a->Hkv * 128 * DP;
+    int64_t items = ((a->T_max + 127) / 128 + (a->prompt_rows + 127) / 128 * p.splits) * a->Hkv;
     ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, true>, dim3((unsigned)(items < ctx->sm_count ? items : ctx->sm_count)), dim3(BWD_THREADS), C::SMEM, s,
                                    k_rows, v_rows, q_cols, do_cols, pk_rows, pv_rows, p));
     ctx->launches += 1;
+    if (p.splits > 1) {
+        const int64_t pieces = 2 * a->prompt_rows * a->Hkv * (DP / 8), blocks = (pieces + 255) / 256;
+        ARROL_CUDA_OK(arrol_launch_pdl(attention_add_parts_kernel<DP>, dim3((unsigned)(blocks < 8 * ctx->sm_count ? blocks : 8 * ctx->sm_count)), dim3(256), 0, s, p));
+        ctx->launches += 1;
+    }
     if (a->T_max == 0) return ARROL_OK;
     p.out1 = nullptr;
     p.out2 = static_cast<__nv_bfloat16*>(a->dq); p.out2_stride = a->dq_stride;
@@ -551,7 +648,7 @@ extern "C" int arrol_attention_backward(arrol_ctx* ctx, const arrol_attention_ar
         return ARROL_ERR_INVALID_ARG;
     if (a->prompt_rows > 0 && (!attn_rows_ok(a->dprompt_k, a->dprompt_k_stride, a->Hkv, a->D) || !attn_rows_ok(a->dprompt_v, a->dprompt_v_stride, a->Hkv, a->D)))
         return ARROL_ERR_INVALID_ARG;
-    const AttnWorkspace w = attn_workspace(a->workspace, a->T_max, a->prompt_rows, a->Hq, true);
+    const AttnWorkspace w = attn_workspace(a->workspace, ctx->sm_count, a->T_max, a->prompt_rows, a->Hq, a->Hkv, a->D, true);
     if (a->workspace_bytes < w.bytes) return ARROL_ERR_WORKSPACE;
     ArrolDeviceGuard guard(ctx->device);
     if (!guard.ok) return ARROL_ERR_CUDA;

@@ -17,6 +17,7 @@ struct AttnWorkspace {
     TokenBounds* bounds;
     int2* prompt_range;
     float2* stats;                // per packed token and query head: lse log2(e), d_o . o
+    float* parts;                 // partial sums of the prompts' gradients
     size_t bytes;
 };
 
@@ -39,19 +40,29 @@ struct AttnShape {
 
 inline size_t attn_round(size_t n) { return (n + 255) & ~(size_t)255; }
 
-inline AttnWorkspace attn_workspace(void* base, int64_t T_max, int64_t prompt_rows, int Hq, bool backward) {
+// Items per tile of 128 prompt rows in the backward: every survivor's tokens pass by such a tile, which would make it the longest piece of work by far.
+// Parts of about 48 blocks of 64 query rows (30 to 40 us), but no more items than four an SM, whose partial sums take 128 KB each.
+inline int attn_prompt_splits(int sm_count, int64_t T_max, int64_t prompt_rows, int P, int Hq, int Hkv) {
+    if (prompt_rows == 0 || P < 1) return 1;
+    const int64_t blocks = T_max * (Hq / Hkv) / P / 64, tiles = (prompt_rows + 127) / 128 * Hkv;
+    int64_t n = (blocks + 47) / 48;
+    const int64_t most = (4 * (int64_t)sm_count + tiles - 1) / tiles;
+    if (n > most) n = most;
+    return (int)(n < 1 ? 1 : n > 16 ? 16 : n);
+}
+
+inline AttnWorkspace attn_workspace(void* base, int sm_count, int64_t T_max, int64_t prompt_rows, int Hq, int Hkv, int D, bool backward) {
     AttnWorkspace w = {};
     uint8_t* p = static_cast<uint8_t*>(base);
     size_t at = 0;
-    w.counters = reinterpret_cast<uint32_t*>(p + at);
-    at += 256;
-    w.bounds = reinterpret_cast<TokenBounds*>(p + at);
-    at += attn_round((size_t)T_max * sizeof(TokenBounds));
+    auto take = [&](size_t n) { uint8_t* q = p + at; at += attn_round(n); return q; };
+    w.counters = reinterpret_cast<uint32_t*>(take(256));
+    w.bounds = reinterpret_cast<TokenBounds*>(take((size_t)T_max * sizeof(TokenBounds)));
     if (backward) {
-        w.prompt_range = reinterpret_cast<int2*>(p + at);
-        at += attn_round((size_t)prompt_rows * sizeof(int2));
-        w.stats = reinterpret_cast<float2*>(p + at);
-        at += attn_round((size_t)T_max * Hq * sizeof(float2));
+        w.prompt_range = reinterpret_cast<int2*>(take((size_t)prompt_rows * sizeof(int2)));
+        w.stats = reinterpret_cast<float2*>(take((size_t)T_max * Hq * sizeof(float2)));
+        const int splits = attn_prompt_splits(sm_count, T_max, prompt_rows, 1, Hq, Hkv);      // one prompt has the most
+        if (splits > 1) w.parts = reinterpret_cast<float*>(take((size_t)splits * ((prompt_rows + 127) / 128) * Hkv * 128 * (D <= 64 ? 64 : 128) * 2 * sizeof(float)));
     }
     w.bytes = at;
     return w;
