@@ -109,7 +109,7 @@ attention_stats_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_stride, co
 // Keys come in blocks of 128: those of the tiles' prompts (consecutive prompts are consecutive rows), then the own ones; a block
 // that lies inside every row's range is not masked at all.
 constexpr int FWD_BLOCK = 128;
-constexpr int FWD_THREADS = 384;             // producer, MMA issuer, scanner, a spare warp; two softmax groups of four warps
+constexpr int FWD_THREADS = 384;             // producer, MMA issuer, scanner, second MMA issuer or a spare warp; two softmax groups of four warps
 constexpr int FWD_SLOTS = 2;                 // work items announced ahead
 constexpr uint32_t HALF_BYTES = 128 * 128;   // 128 rows x 64 dimensions
 constexpr float RESCALE_AT = 8.0f;           // the running maximum follows once it is 2^8 behind
@@ -158,7 +158,7 @@ struct FwdParams {
 };
 
 struct FwdShared {
-    uint64_t full[8], empty[8], scanned[8], q_full[2], q_empty[2], s_full[2], s_free[2], p_most[2], p_full[2], pv_done[2], item_full[FWD_SLOTS], item_empty[FWD_SLOTS], drain;
+    uint64_t full[8], empty[8], scanned[8], q_full[2], q_empty[2], s_full[2], s_free[2], p_most[2], p_full[2], pv_done[2], item_full[FWD_SLOTS], item_empty[FWD_SLOTS], drain[2];
     alignas(16) uint32_t bad_keys[8][4];     // per stage with values: keys of an edge block that are not finite
     FwdItem items[FWD_SLOTS];
     uint32_t tmem, abort;
@@ -177,10 +177,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     volatile uint32_t* abort_flag = &sm.abort;
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], i & 1 ? 2 : 1); mbar_init(&sm.scanned[i], 1); }     // odd stages hold values, which the scanner hands back too
+        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], (C::AHEAD ? 2 : 1) + (i & 1)); mbar_init(&sm.scanned[i], 1); }     // odd stages hold values, which the scanner hands back too
         for (int i = 0; i < 2; ++i) { mbar_init(&sm.q_full[i], 1); mbar_init(&sm.q_empty[i], 1); mbar_init(&sm.s_full[i], 1); mbar_init(&sm.s_free[i], 4); mbar_init(&sm.p_most[i], 4); mbar_init(&sm.p_full[i], 4); mbar_init(&sm.pv_done[i], 1);}
-        for (int i = 0; i < FWD_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], 10); }
-        mbar_init(&sm.drain, 1);
+        for (int i = 0; i < FWD_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], C::AHEAD ? 11 : 10); }
+        for (int i = 0; i < 2; ++i) mbar_init(&sm.drain[i], 1);
         sm.abort = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
@@ -298,14 +298,14 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (mbar_try_wait(&sm.q_full[i], (q_loads[i] - 1u) & 1u)) break;
         }
         __syncwarp();
-    } else if (warp == 1) {
+    } else if (!C::AHEAD && warp == 1) {
         // ---- MMA issuer.  Per tile and block: S = Q K^T, and once the softmax group has written P (three quarters are enough to begin), O += P V.
-        // One warp for both tiles, in turn: that keeps their softmax groups half a block apart, so that one's exponentials run while the tensor cores
+        // One warp for both tiles, in turn, where P V and the next S of a tile follow each other: that keeps their softmax groups half a block apart, so that one's exponentials run while the tensor cores
         // work for the other.  (A warp per tile let them fall in step, both waiting for the same unit: 8,192 tokens of 32 heads of 128 517 -> 700 us.)
         constexpr uint32_t idesc_s = make_idesc(128, FWD_BLOCK), idesc_o = make_idesc(128, DP, false, true);
         const uint32_t q_base = smem_u32(q_tiles), ring_base = smem_u32(ring);
-        uint32_t pos0 = 0, parity_p[2] = {0, 0}, parity_s[2] = {0, 0};
-        bool ok = true, s_used[2] = {false, false};  // S was written before
+        uint32_t pos0 = 0, parity_p[2] = {0, 0};
+        bool ok = true;
         auto wait_stage = [&](uint32_t pos) { return mbar_wait_warp(&sm.full[pos % C::STAGES], (pos / C::STAGES) & 1u, abort_flag); };
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % FWD_SLOTS;
@@ -318,11 +318,6 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             uint32_t pv_pos[2] = {0, 0};             // ring position of the values whose P V is still to be issued; 0: none
             bool pv_frees[2] = {false, false};       // and whether no other tile uses them after that
             auto issue_s = [&](int i, uint32_t pos, bool frees, bool last) {
-                if (C::AHEAD && s_used[i]) {
-                    if (!mbar_wait_warp(&sm.s_free[i], parity_s[i], abort_flag)) return false;
-                    parity_s[i] ^= 1u;
-                }
-                s_used[i] = true;
                 const uint32_t st = pos % C::STAGES;
                 tcgen05_fence_after();
                 if (elect_one()) {
@@ -338,7 +333,6 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (last) tcgen05_commit(&sm.q_empty[i]);
                 }
                 __syncwarp();
-                return true;
             };
             auto issue_pv = [&](int i) {
                 const uint32_t st = pv_pos[i] % C::STAGES, o_at = tmem + C::O_AT + i * DP, p_at = tmem + C::P_AT + i * C::P_STEP;
@@ -374,12 +368,12 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     // a tile's pending P V goes first even where it does not need this block: stages are freed in order, tile 1 last
-                    if ((!C::AHEAD || !use[i]) && ok && pv_pos[i] && !issue_pv(i)) ok = false;
+                    if (ok && pv_pos[i] && !issue_pv(i)) ok = false;
                     if (use[i] && ok) {
                         if (!q_here[i] && !mbar_wait_warp(&sm.q_full[i], n & 1u, abort_flag)) { ok = false; break; }
                         q_here[i] = true;
-                        if (!wait_stage(pos) || !issue_s(i, pos, i == 1 || !use[1], b + 1 == (i ? need1.w : need0.w))) { ok = false; break; }
-                        if (C::AHEAD && pv_pos[i] && !issue_pv(i)) { ok = false; break; }
+                        if (!(i == 1 && use[0]) && !wait_stage(pos)) { ok = false; break; }
+                        issue_s(i, pos, i == 1 || !use[1], b + 1 == (i ? need1.w : need0.w));
                         pv_pos[i] = pos + 1;
                         pv_frees[i] = i == 1 || !use[1];
                     }
@@ -403,10 +397,90 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             __syncwarp();
         }
         if (!ok) {
-            if (elect_one()) tcgen05_commit(&sm.drain);
+            if (elect_one()) tcgen05_commit(&sm.drain[0]);
             __syncwarp();
             for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
-                if (mbar_try_wait(&sm.drain, 0u)) break;
+                if (mbar_try_wait(&sm.drain[0], 0u)) break;
+        }
+        __syncwarp();
+    } else if (C::AHEAD && (warp == 1 || warp == 3)) {
+        // ---- MMA issuer of tile i where S runs ahead: neither tile's P V is in the way of the other's S then
+        constexpr uint32_t idesc_s = make_idesc(128, FWD_BLOCK), idesc_o = make_idesc(128, DP, false, true);
+        const int i = warp >> 1;
+        const uint32_t q_base = smem_u32(q_tiles) + i * C::TILE_BYTES, ring_base = smem_u32(ring);
+        const uint32_t s_at = tmem + i * 128, o_at = tmem + C::O_AT + i * DP, p_at = tmem + C::P_AT + i * C::P_STEP;
+        uint32_t pos0 = 0, parity_p = 0, parity_s = 0;
+        bool ok = true, s_used = false;              // S was written before
+        auto wait_stage = [&](uint32_t pos) { return mbar_wait_warp(&sm.full[pos % C::STAGES], (pos / C::STAGES) & 1u, abort_flag); };
+        for (uint32_t n = 0; ok; ++n) {
+            const uint32_t slot = n % FWD_SLOTS;
+            if (!mbar_wait_warp(&sm.item_full[slot], (n / FWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
+            const FwdItem& it = sm.items[slot];
+            if (!it.valid) break;
+            const int blocks = uniform(it.n);
+            const int4 need = uniform(it.tile[i].need);
+            bool pending = false, first = true;      // P V of the block before
+            if (!mbar_wait_warp(&sm.q_full[i], n & 1u, abort_flag)) { ok = false; break; }
+            for (int b = 0; b <= blocks; ++b) {
+                const uint32_t pos = pos0 + 2 * b, st = pos % C::STAGES;
+                const bool use = b < blocks && in_ranges(need, b);
+                if (b < blocks && !wait_stage(pos)) { ok = false; break; }
+                if (use) {
+                    if (s_used) {
+                        if (!mbar_wait_warp(&sm.s_free[i], parity_s, abort_flag)) { ok = false; break; }
+                        parity_s ^= 1u;
+                    }
+                    s_used = true;
+                    tcgen05_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int h = 0; h < C::HALVES; ++h) {
+                            const uint64_t a_desc = make_smem_desc(q_base + h * HALF_BYTES), b_desc = make_smem_desc(ring_base + st * C::TILE_BYTES + h * HALF_BYTES);
+#pragma unroll
+                            for (int k = 0; k < 64 / UMMA_K; ++k)
+                                tcgen05_mma_bf16(s_at, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_s, (h | k) != 0 ? 1u : 0u);
+                        }
+                        tcgen05_commit(&sm.s_full[i]);
+                        tcgen05_commit(&sm.empty[st]);
+                        if (b + 1 == need.w) tcgen05_commit(&sm.q_empty[i]);
+                    }
+                    __syncwarp();
+                }
+                if (pending) {
+                    const uint32_t sv = (pos - 1) % C::STAGES;
+                    if (!wait_stage(pos - 1) || !mbar_wait_warp(&sm.p_full[i], parity_p, abort_flag)) { ok = false; break; }
+                    parity_p ^= 1u;
+                    tcgen05_fence_after();
+                    if (elect_one()) {
+                        const uint64_t b_desc = make_smem_desc_mn(ring_base + sv * C::TILE_BYTES, 128);
+#pragma unroll
+                        for (int k = 0; k < FWD_BLOCK / UMMA_K; ++k)
+                            tcgen05_mma_bf16_tmem_a(o_at, p_at + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o, first && k == 0 ? 0u : 1u);
+                        tcgen05_commit(&sm.pv_done[i]);
+                        tcgen05_commit(&sm.empty[sv]);
+                    }
+                    __syncwarp();
+                    first = false;
+                }
+                pending = use;
+                if (b < blocks && !use) {            // handed back as it came, but not before: a stage's uses are counted in order
+                    if (!wait_stage(pos + 1)) { ok = false; break; }
+                    if (elect_one()) { mbar_arrive(&sm.empty[st]); mbar_arrive(&sm.empty[(pos + 1) % C::STAGES]); }
+                    __syncwarp();
+                }
+            }
+            pos0 += 2 * blocks;
+            if (ok && elect_one()) {
+                if (need.w == 0) mbar_arrive(&sm.q_empty[i]);       // a tile without tokens
+                mbar_arrive(&sm.item_empty[slot]);
+            }
+            __syncwarp();
+        }
+        if (!ok) {
+            if (elect_one()) tcgen05_commit(&sm.drain[i]);
+            __syncwarp();
+            for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
+                if (mbar_try_wait(&sm.drain[i], 0u)) break;
         }
         __syncwarp();
     } else if (warp == 2) {
@@ -587,7 +661,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     quarter_of_p(1);
                     quarter_of_p(2);
                     if (!values_scanned()) { ok = false; break; }
-                    publish(&sm.p_most[i]);
+                    if (!C::AHEAD) publish(&sm.p_most[i]);
                     quarter_of_p(3);
                     publish(&sm.p_full[i]);
                 } else {
@@ -601,7 +675,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         } else {
                             quarter_of_p(c);
                         }
-                        if (c >= 2) publish(c == 2 ? &sm.p_most[i] : &sm.p_full[i]);
+                        if (c == 3 || (c == 2 && !C::AHEAD)) publish(c == 2 ? &sm.p_most[i] : &sm.p_full[i]);
                     }
                 }
                 float x, y;
