@@ -158,9 +158,10 @@ struct FwdParams {
 };
 
 struct FwdShared {
-    uint64_t full[8], empty[8], scanned[8], q_full[2], q_empty[2], s_full[2], s_free[2], p_most[2], p_full[2], pv_done[2], item_full[FWD_SLOTS], item_empty[FWD_SLOTS], drain[2];
+    uint64_t full[8], empty[8], scanned[8], q_full[2], q_empty[2], s_full[2], s_free[2], p_most[2], p_full[2], pv_done[2], item_full[FWD_SLOTS], item_empty[FWD_SLOTS], item_scanned[FWD_SLOTS], drain[2];
     alignas(16) uint32_t bad_keys[8][4];     // per stage with values: keys of an edge block that are not finite
     FwdItem items[FWD_SLOTS];
+    uint32_t bad_whole[FWD_SLOTS];           // tiles that have values which are not finite in a block that they do not mask
     uint32_t tmem, abort;
 };
 
@@ -179,7 +180,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], (C::AHEAD ? 2 : 1) + (i & 1)); mbar_init(&sm.scanned[i], 1); }     // odd stages hold values, which the scanner hands back too
         for (int i = 0; i < 2; ++i) { mbar_init(&sm.q_full[i], 1); mbar_init(&sm.q_empty[i], 1); mbar_init(&sm.s_full[i], 1); mbar_init(&sm.s_free[i], 4); mbar_init(&sm.p_most[i], 4); mbar_init(&sm.p_full[i], 4); mbar_init(&sm.pv_done[i], 1);}
-        for (int i = 0; i < FWD_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], C::AHEAD ? 11 : 10); }
+        for (int i = 0; i < FWD_SLOTS; ++i) { mbar_init(&sm.item_scanned[i], 1); mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], C::AHEAD ? 11 : 10); }
         for (int i = 0; i < 2; ++i) mbar_init(&sm.drain[i], 1);
         sm.abort = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -495,6 +496,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (!it.valid) break;
             const int blocks = it.n;
             const int4 need0 = it.tile[0].need, need1 = it.tile[1].need, whole0 = it.tile[0].whole, whole1 = it.tile[1].whole;
+            uint32_t bad_whole = 0u;             // bit i: a block that all rows of tile i have was cleaned for the other one
             for (int b = 0; b < blocks; ++b) {
                 const uint32_t pos = pos0 + 2 * b + 1, st = pos % C::STAGES;
                 if (!mbar_wait_warp(&sm.full[st], (pos / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
@@ -513,9 +515,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         }
                         const uint32_t all = __ballot_sync(0xffffffffu, bad);
                         if (lane == 0) sm.bad_keys[st][w] = all;
+                        if (all) bad_whole |= (in_ranges(whole0, b) ? 1u : 0u) | (in_ranges(whole1, b) ? 2u : 0u);
                     }
-                } else if (lane < 4) {
-                    sm.bad_keys[st][lane] = 0u;
                 }
                 __syncwarp();
                 if (lane == 0) {
@@ -525,7 +526,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 __syncwarp();
             }
             pos0 += 2 * blocks;
-            if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
+            if (lane == 0) {
+                sm.bad_whole[slot] = bad_whole;
+                mbar_arrive(&sm.item_scanned[slot]);
+                mbar_arrive(&sm.item_empty[slot]);
+            }
             __syncwarp();
         }
     } else if (warp >= 4) {
@@ -552,9 +557,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             bool have_o = false;
             const int4 need = it.tile[i].need, whole = it.tile[i].whole;
             const int n_pre = it.n_pre;
-            for (int b = need.y > need.x ? need.x : need.z; b < need.w; b = b + 1 == need.y ? need.z : b + 1) {
+            int b = need.y > need.x ? need.x : need.z;
+            bool masked = !in_ranges(whole, b);
+            while (b < need.w) {
                 const bool pre = b < n_pre;
-                const bool masked = !in_ranges(whole, b);
                 int lo = 0, len = FWD_BLOCK;
                 if (masked) {
                     const int k0 = pre ? it.pre0 + b * FWD_BLOCK : it.own0 + (b - n_pre) * FWD_BLOCK;
@@ -597,9 +603,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 float mx[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    mx[c] = __uint_as_float(s[c][0]);
+                    mx[c] = fmaxf(__uint_as_float(s[c][0]), __uint_as_float(s[c][1]));
 #pragma unroll
-                    for (int j = 1; j < 32; ++j) mx[c] = fmaxf(mx[c], __uint_as_float(s[c][j]));
+                    for (int j = 2; j < 32; j += 2) mx[c] = max3(mx[c], __uint_as_float(s[c][j]), __uint_as_float(s[c][j + 1]));
                 }
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
                 float up = 1.f;
@@ -627,8 +633,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const float sub = m == -INFINITY ? 0.f : -m;
                 const uint64_t scale2 = pack_f32x2(scale, scale), sub2 = pack_f32x2(sub, sub);
                 uint64_t sum[2] = {0, 0};
+                uint32_t pk[4][16];
                 auto quarter_of_p = [&](int c) {
-                    uint32_t pk[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         float x, y;
@@ -636,10 +642,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         x = ex2_approx(x);
                         y = ex2_approx(y);
                         sum[j & 1] = add_f32x2(sum[j & 1], pack_f32x2(x, y));
-                        pk[j] = pack_bf16(x, y);
+                        pk[c][j] = pack_bf16(x, y);
                     }
-                    __syncwarp();
-                    tcgen05_st_32x16(p_at + c * 16, pk);
                 };
                 auto publish = [&](uint64_t* bar) {
                     __syncwarp();
@@ -649,35 +653,44 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (lane == 0) mbar_arrive(bar);
                     __syncwarp();
                 };
-                auto values_scanned = [&] {      // before P V may begin
+                if (masked) {
+                    // the values have been looked over before P V may begin
                     const uint32_t pos = pos0 + 2 * b + 1, st = pos % C::STAGES;
-                    if (!mbar_wait_warp(&sm.scanned[st], (pos / C::STAGES) & 1u, abort_flag)) return false;
+                    if (!mbar_wait_warp(&sm.scanned[st], (pos / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
                     const uint4 bad = *reinterpret_cast<const uint4*>(sm.bad_keys[st]);
                     if ((bad.x & on[0]) | (bad.y & on[1]) | (bad.z & on[2]) | (bad.w & on[3])) l = NAN;
-                    return true;
-                };
-                if (!masked) {
-                    quarter_of_p(0);
-                    quarter_of_p(1);
-                    quarter_of_p(2);
-                    if (!values_scanned()) { ok = false; break; }
-                    if (!C::AHEAD) publish(&sm.p_most[i]);
-                    quarter_of_p(3);
-                    publish(&sm.p_full[i]);
-                } else {
-                    if (!values_scanned()) { ok = false; break; }
+                    __syncwarp();
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         if (__all_sync(0xffffffffu, on[c] == 0u)) {      // no key of any row of the warp
-                            const uint32_t none[16] = {};
-                            __syncwarp();
-                            tcgen05_st_32x16(p_at + c * 16, none);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) pk[c][j] = 0u;
                         } else {
                             quarter_of_p(c);
                         }
-                        if (c == 3 || (c == 2 && !C::AHEAD)) publish(c == 2 ? &sm.p_most[i] : &sm.p_full[i]);
+                        __syncwarp();
+                        tcgen05_st_32x16(p_at + c * 16, pk[c]);
+                        if (c == 2 && !C::AHEAD) publish(&sm.p_most[i]);
+                    }
+                } else {
+                    // no barrier and no store between the exponentials that could keep their pipeline from filling
+                    quarter_of_p(0);
+                    quarter_of_p(1);
+                    quarter_of_p(2);
+                    if (C::AHEAD) quarter_of_p(3);
+                    __syncwarp();
+#pragma unroll
+                    for (int c = 0; c < (C::AHEAD ? 4 : 3); ++c) tcgen05_st_32x16(p_at + c * 16, pk[c]);
+                    if (!C::AHEAD) {
+                        publish(&sm.p_most[i]);
+                        quarter_of_p(3);
+                        __syncwarp();
+                        tcgen05_st_32x16(p_at + 48, pk[3]);
                     }
                 }
+                b = b + 1 == need.y ? need.z : b + 1;
+                masked = !in_ranges(whole, b);
+                publish(&sm.p_full[i]);
                 float x, y;
                 unpack_f32x2(add_f32x2(sum[0], sum[1]), x, y);
                 l += x + y;
@@ -689,6 +702,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (have_o) {
                 if (!mbar_wait_warp(&sm.pv_done[i], (s_count - 1u) & 1u, abort_flag)) { ok = false; break; }
                 tcgen05_fence_after();
+                if (!mbar_wait_warp(&sm.item_scanned[slot], (n / FWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
+                if (sm.bad_whole[slot] >> i & 1u) l = NAN;
                 const int h = it.g * ratio + head;
                 const float inv = 1.f / l;
                 __nv_bfloat16* out = p.o + (int64_t)t * p.o_stride + (int64_t)h * p.sh.D;
