@@ -303,105 +303,101 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         // ---- MMA issuer.  Per tile and block: S = Q K^T, and once the softmax group has written P (three quarters are enough to begin), O += P V.
         // One warp for both tiles, in turn, where P V and the next S of a tile follow each other: that keeps their softmax groups half a block apart, so that one's exponentials run while the tensor cores
         // work for the other.  (A warp per tile let them fall in step, both waiting for the same unit: 8,192 tokens of 32 heads of 128 517 -> 700 us.)
-        constexpr uint32_t idesc_s = make_idesc(128, FWD_BLOCK), idesc_o = make_idesc(128, DP, false, true);
-        const uint32_t q_base = smem_u32(q_tiles), ring_base = smem_u32(ring);
-        uint32_t pos0 = 0, parity_p[2] = {0, 0};
-        bool ok = true;
-        auto wait_stage = [&](uint32_t pos) { return mbar_wait_warp(&sm.full[pos % C::STAGES], (pos / C::STAGES) & 1u, abort_flag); };
-        for (uint32_t n = 0; ok; ++n) {
-            const uint32_t slot = n % FWD_SLOTS;
-            if (!mbar_wait_warp(&sm.item_full[slot], (n / FWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
-            const FwdItem& it = sm.items[slot];
-            if (!it.valid) break;
-            const int blocks = uniform(it.n);
-            const int4 need0 = uniform(it.tile[0].need), need1 = uniform(it.tile[1].need);
-            bool first[2] = {true, true};
-            uint32_t pv_pos[2] = {0, 0};             // ring position of the values whose P V is still to be issued; 0: none
-            bool pv_frees[2] = {false, false};       // and whether no other tile uses them after that
-            auto issue_s = [&](int i, uint32_t pos, bool frees, bool last) {
-                const uint32_t st = pos % C::STAGES;
-                tcgen05_fence_after();
-                if (elect_one()) {
+        // One thread: votes and converging barriers around every wait were half of its time (8,192 tokens as above 487 -> XXX us).
+        if (elect_one()) {
+            constexpr uint32_t idesc_s = make_idesc(128, FWD_BLOCK), idesc_o = make_idesc(128, DP, false, true);
+            const uint32_t q_base = smem_u32(q_tiles), ring_base = smem_u32(ring);
+            uint32_t pos0 = 0, parity_p[2] = {0, 0};
+            bool ok = true;
+            auto wait_stage = [&](uint32_t pos) { return mbar_wait(&sm.full[pos % C::STAGES], (pos / C::STAGES) & 1u, abort_flag); };
+            for (uint32_t n = 0; ok; ++n) {
+                const uint32_t slot = n % FWD_SLOTS;
+                if (!mbar_wait(&sm.item_full[slot], (n / FWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
+                const FwdItem& it = sm.items[slot];
+                if (!it.valid) break;
+                const int blocks = it.n;
+                const int4 need0 = it.tile[0].need, need1 = it.tile[1].need;
+                bool first[2] = {true, true};
+                uint32_t pv_pos[2] = {0, 0};             // ring position of the values whose P V is still to be issued; 0: none
+                bool pv_frees[2] = {false, false};       // and whether no other tile uses them after that
+                auto issue_s = [&](int i, uint32_t pos, bool frees, bool last) {
+                    const uint32_t st = pos % C::STAGES;
+                    tcgen05_fence_after();
+                    {
 #pragma unroll
-                    for (int h = 0; h < C::HALVES; ++h) {
-                        const uint64_t a_desc = make_smem_desc(q_base + i * C::TILE_BYTES + h * HALF_BYTES), b_desc = make_smem_desc(ring_base + st * C::TILE_BYTES + h * HALF_BYTES);
+                        for (int h = 0; h < C::HALVES; ++h) {
+                            const uint64_t a_desc = make_smem_desc(q_base + i * C::TILE_BYTES + h * HALF_BYTES), b_desc = make_smem_desc(ring_base + st * C::TILE_BYTES + h * HALF_BYTES);
 #pragma unroll
-                        for (int k = 0; k < 64 / UMMA_K; ++k)
-                            tcgen05_mma_bf16(tmem + i * 128, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_s, (h | k) != 0 ? 1u : 0u);
+                            for (int k = 0; k < 64 / UMMA_K; ++k)
+                                tcgen05_mma_bf16(tmem + i * 128, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_s, (h | k) != 0 ? 1u : 0u);
+                        }
+                        tcgen05_commit(&sm.s_full[i]);
+                        if (frees) tcgen05_commit(&sm.empty[st]);
+                        if (last) tcgen05_commit(&sm.q_empty[i]);
                     }
-                    tcgen05_commit(&sm.s_full[i]);
-                    if (frees) tcgen05_commit(&sm.empty[st]);
-                    if (last) tcgen05_commit(&sm.q_empty[i]);
-                }
-                __syncwarp();
-            };
-            auto issue_pv = [&](int i) {
-                const uint32_t st = pv_pos[i] % C::STAGES, o_at = tmem + C::O_AT + i * DP, p_at = tmem + C::P_AT + i * C::P_STEP;
-                if (!wait_stage(pv_pos[i]) || !mbar_wait_warp(&sm.p_most[i], parity_p[i], abort_flag)) return false;
-                tcgen05_fence_after();
-                const uint64_t b_desc = make_smem_desc_mn(ring_base + st * C::TILE_BYTES, 128);
-                const bool elected = elect_one();
-                if (elected) {
+                };
+                auto issue_pv = [&](int i) {
+                    const uint32_t st = pv_pos[i] % C::STAGES, o_at = tmem + C::O_AT + i * DP, p_at = tmem + C::P_AT + i * C::P_STEP;
+                    if (!wait_stage(pv_pos[i]) || !mbar_wait(&sm.p_most[i], parity_p[i], abort_flag)) return false;
+                    tcgen05_fence_after();
+                    const uint64_t b_desc = make_smem_desc_mn(ring_base + st * C::TILE_BYTES, 128);
+                                    {
 #pragma unroll
-                    for (int k = 0; k < 6; ++k)
-                        tcgen05_mma_bf16_tmem_a(o_at, p_at + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o, first[i] && k == 0 ? 0u : 1u);
-                }
-                __syncwarp();
-                if (!mbar_wait_warp(&sm.p_full[i], parity_p[i], abort_flag)) return false;
-                tcgen05_fence_after();
-                if (elected) {
+                        for (int k = 0; k < 6; ++k)
+                            tcgen05_mma_bf16_tmem_a(o_at, p_at + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o, first[i] && k == 0 ? 0u : 1u);
+                    }
+                    if (!mbar_wait(&sm.p_full[i], parity_p[i], abort_flag)) return false;
+                    tcgen05_fence_after();
+                    {
 #pragma unroll
-                    for (int k = 6; k < 8; ++k)
-                        tcgen05_mma_bf16_tmem_a(o_at, p_at + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o, 1u);
-                    if (pv_frees[i]) tcgen05_commit(&sm.empty[st]);
-                    tcgen05_commit(&sm.pv_done[i]);
+                        for (int k = 6; k < 8; ++k)
+                            tcgen05_mma_bf16_tmem_a(o_at, p_at + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o, 1u);
+                        if (pv_frees[i]) tcgen05_commit(&sm.empty[st]);
+                        tcgen05_commit(&sm.pv_done[i]);
+                    }
+                    parity_p[i] ^= 1u;
+                    first[i] = false;
+                    pv_pos[i] = 0;
+                    return true;
+                };
+                bool q_here[2] = {false, false};
+                for (int b = 0; b < blocks && ok; ++b) {
+                    const uint32_t pos = pos0 + 2 * b;
+                    const bool use[2] = {in_ranges(need0, b), in_ranges(need1, b)};
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        // a tile's pending P V goes first even where it does not need this block: stages are freed in order, tile 1 last
+                        if (ok && pv_pos[i] && !issue_pv(i)) ok = false;
+                        if (use[i] && ok) {
+                            if (!q_here[i] && !mbar_wait(&sm.q_full[i], n & 1u, abort_flag)) { ok = false; break; }
+                            q_here[i] = true;
+                            if (!(i == 1 && use[0]) && !wait_stage(pos)) { ok = false; break; }
+                            issue_s(i, pos, i == 1 || !use[1], b + 1 == (i ? need1.w : need0.w));
+                            pv_pos[i] = pos + 1;
+                            pv_frees[i] = i == 1 || !use[1];
+                        }
+                    }
+                    if (!use[0] && !use[1] && ok) {      // only where row numbers are out of order
+                        if (!wait_stage(pos) || !wait_stage(pos + 1)) { ok = false; break; }
+                        { mbar_arrive(&sm.empty[pos % C::STAGES]); mbar_arrive(&sm.empty[(pos + 1) % C::STAGES]); }
+                    }
                 }
-                __syncwarp();
-                parity_p[i] ^= 1u;
-                first[i] = false;
-                pv_pos[i] = 0;
-                return true;
-            };
-            bool q_here[2] = {false, false};
-            for (int b = 0; b < blocks && ok; ++b) {
-                const uint32_t pos = pos0 + 2 * b;
-                const bool use[2] = {in_ranges(need0, b), in_ranges(need1, b)};
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    // a tile's pending P V goes first even where it does not need this block: stages are freed in order, tile 1 last
                     if (ok && pv_pos[i] && !issue_pv(i)) ok = false;
-                    if (use[i] && ok) {
-                        if (!q_here[i] && !mbar_wait_warp(&sm.q_full[i], n & 1u, abort_flag)) { ok = false; break; }
-                        q_here[i] = true;
-                        if (!(i == 1 && use[0]) && !wait_stage(pos)) { ok = false; break; }
-                        issue_s(i, pos, i == 1 || !use[1], b + 1 == (i ? need1.w : need0.w));
-                        pv_pos[i] = pos + 1;
-                        pv_frees[i] = i == 1 || !use[1];
+                    if (ok && !q_here[i]) {              // a tile without tokens
+                        if (!mbar_wait(&sm.q_full[i], n & 1u, abort_flag)) ok = false;
+                        else mbar_arrive(&sm.q_empty[i]);
                     }
                 }
-                if (!use[0] && !use[1] && ok) {      // only where row numbers are out of order
-                    if (!wait_stage(pos) || !wait_stage(pos + 1)) { ok = false; break; }
-                    if (elect_one()) { mbar_arrive(&sm.empty[pos % C::STAGES]); mbar_arrive(&sm.empty[(pos + 1) % C::STAGES]); }
-                    __syncwarp();
-                }
+                pos0 += 2 * blocks;
+                if (ok) mbar_arrive(&sm.item_empty[slot]);
             }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (ok && pv_pos[i] && !issue_pv(i)) ok = false;
-                if (ok && !q_here[i]) {              // a tile without tokens
-                    if (!mbar_wait_warp(&sm.q_full[i], n & 1u, abort_flag)) ok = false;
-                    else if (elect_one()) mbar_arrive(&sm.q_empty[i]);
-                }
+            if (!ok) {
+                tcgen05_commit(&sm.drain[0]);
+                for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
+                    if (mbar_try_wait(&sm.drain[0], 0u)) break;
             }
-            pos0 += 2 * blocks;
-            if (ok && elect_one()) mbar_arrive(&sm.item_empty[slot]);
-            __syncwarp();
-        }
-        if (!ok) {
-            if (elect_one()) tcgen05_commit(&sm.drain[0]);
-            __syncwarp();
-            for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
-                if (mbar_try_wait(&sm.drain[0], 0u)) break;
         }
         __syncwarp();
     } else if (C::AHEAD && (warp == 1 || warp == 3)) {
