@@ -3,7 +3,6 @@ rollout (marshalling only)."""
 from __future__ import annotations
 
 import ctypes as C
-import math
 from typing import Optional
 
 import torch
@@ -50,27 +49,23 @@ def _lib():
     return lib
 
 
-def _rows(t: Optional[torch.Tensor], heads: int, D: int):
-    """(pointer, row stride) of a [rows, heads, D] tensor whose heads lie side by side."""
+# Small calls are bound by the host: shapes and strides are asked for once a tensor, structures filled in one constructor call.
+def _rows(t: Optional[torch.Tensor], rows: int, heads: int, D: int):
+    """(pointer, row stride) of a [rows or more, heads, D] tensor whose heads lie side by side."""
     if t is None:
         return None, 0
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not torch.bfloat16:
         raise TypeError("attention tensors are bfloat16")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D or t.numel() and (
-            (D > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != D)):
-        raise ValueError("attention tensors are [rows, heads, D] with the heads of a row side by side")
-    return t.data_ptr(), max(t.stride(0), heads * D) if t.shape[0] < 2 else t.stride(0)
-
-
-def _same_rows(name: str, t: torch.Tensor, rows: int):
-    if t.shape[0] < rows:
-        raise ValueError("%s has fewer rows than its counterpart" % name)
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != D or shape[0] < rows or (stride[1] != D and heads > 1 or stride[2] != 1 and D > 1) and t.numel():
+        raise ValueError("attention tensors are [rows, heads, D] with the heads of a row side by side, %d rows at least here" % rows)
+    return t.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], heads * D)
 
 
 def _lse(t: Optional[torch.Tensor], rows: int, heads: int):
     if t is None:
         return None
-    if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() < rows * heads:
+    if t.dtype is not torch.float32 or not t.is_contiguous() or t.numel() < rows * heads:
         raise ValueError("lse is a dense float32 tensor [rows, heads]")
     return t.data_ptr()
 
@@ -78,9 +73,23 @@ def _lse(t: Optional[torch.Tensor], rows: int, heads: int):
 def _ints(name: str, t: Optional[torch.Tensor], dtype, count: int = 0):
     if t is None:
         return None
-    if t.dtype != dtype or not t.is_contiguous() or t.numel() < count:
+    if t.dtype is not dtype or not t.is_contiguous() or t.numel() < count:
         raise ValueError("%s is a dense %s tensor of at least %d entries" % (name, dtype, count))
     return t.data_ptr()
+
+
+def _prompts(prompt_k, prompt_v, cu_prompts, Hkv: int, D: int):
+    """(rows, prompts, k, v, k stride, v stride, cu)"""
+    if prompt_k is None:
+        return 0, 0, None, None, 0, 0, None
+    rows = prompt_k.shape[0]
+    k, k_stride = _rows(prompt_k, rows, Hkv, D)
+    v, v_stride = _rows(prompt_v, rows, Hkv, D)
+    return rows, cu_prompts.numel() - 1, k, v, k_stride, v_stride, _ints("cu_prompts", cu_prompts, torch.int64, 1)
+
+
+def _bytes(workspace: Optional[torch.Tensor]) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
 
 def arrol_attention_workspace(ctx: B.Context, S_max: int, T_max: int, prompt_rows: int, Hq: int, Hkv: int, D: int,
@@ -89,33 +98,22 @@ def arrol_attention_workspace(ctx: B.Context, S_max: int, T_max: int, prompt_row
                                                 1 if backward else 0))
 
 
-def _packed(q, k, v, cu_seqlens, d_num, o, lse, workspace, scale, prompt_k, prompt_v, cu_prompts, survivor_idx, G) -> _Attention:
+def _packed(q, k, v, cu_seqlens, d_num, o, lse, workspace, scale, prompt_k, prompt_v, cu_prompts, survivor_idx, G, grads=(None, 0) * 6) -> _Attention:
     (T, Hq, D), Hkv = q.shape, k.shape[1]
-    a = _Attention()
-    a.q, a.q_stride = _rows(q, Hq, D)
-    a.k, a.k_stride = _rows(k, Hkv, D)
-    a.v, a.v_stride = _rows(v, Hkv, D)
-    a.o, a.o_stride = _rows(o, Hq, D)
-    for name, t in (("k", k), ("v", v), ("o", o)):
-        _same_rows(name, t, T)
-    a.lse = _lse(lse, T, Hq)
+    q_at, q_stride = _rows(q, T, Hq, D)
+    k_at, k_stride = _rows(k, T, Hkv, D)
+    v_at, v_stride = _rows(v, T, Hkv, D)
+    o_at, o_stride = _rows(o, T, Hq, D)
     S = cu_seqlens.numel() - 1
-    a.cu_seqlens = _ints("cu_seqlens", cu_seqlens, torch.int64, 1)
-    a.d_num = _ints("d_num", d_num, torch.int64, 2)
-    if prompt_k is not None:
-        a.prompt_k, a.prompt_k_stride = _rows(prompt_k, Hkv, D)
-        a.prompt_v, a.prompt_v_stride = _rows(prompt_v, Hkv, D)
-        _same_rows("prompt_v", prompt_v, prompt_k.shape[0])
-        a.cu_prompts = _ints("cu_prompts", cu_prompts, torch.int64, 1)
-        a.prompt_rows, a.P = prompt_k.shape[0], cu_prompts.numel() - 1
     if survivor_idx is not None:
         S = min(S, survivor_idx.numel())
-        a.survivor_idx = _ints("survivor_idx", survivor_idx, torch.int32)
-    a.T_max, a.S_max, a.G, a.Hq, a.Hkv, a.D = T, S, int(G), Hq, Hkv, D
-    a.scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
-    a.workspace = B._ptr(workspace)
-    a.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    return a
+    rows, P, pk, pv, pk_stride, pv_stride, cu_p = _prompts(prompt_k, prompt_v, cu_prompts, Hkv, D)
+    d_o, d_o_stride, dq, dq_stride, dk, dk_stride, dv, dv_stride, dpk, dpk_stride, dpv, dpv_stride = grads
+    return _Attention(q_at, k_at, v_at, q_stride, k_stride, v_stride, _ints("cu_seqlens", cu_seqlens, torch.int64, 1),
+                      _ints("d_num", d_num, torch.int64, 2), pk, pv, pk_stride, pv_stride, cu_p,
+                      _ints("survivor_idx", survivor_idx, torch.int32), T, rows, S, P, G, Hq, Hkv, D, D ** -0.5 if scale is None else scale, 0,
+                      o_at, o_stride, _lse(lse, T, Hq), d_o, d_o_stride, dq, dk, dv, dq_stride, dk_stride, dv_stride, dpk, dpv, dpk_stride,
+                      dpv_stride, B._ptr(workspace), _bytes(workspace))
 
 
 def arrol_attention(ctx: B.Context, q, k, v, cu_seqlens, d_num, o, lse, workspace, scale: Optional[float] = None, prompt_k=None,
@@ -130,18 +128,10 @@ def arrol_attention_backward(ctx: B.Context, q, k, v, cu_seqlens, d_num, o, lse,
                              scale: Optional[float] = None, prompt_k=None, prompt_v=None, dprompt_k=None, dprompt_v=None, cu_prompts=None,
                              survivor_idx=None, G: int = 1, stream=None):
     """Gradients (overwritten) of arrol_attention's o; o and lse are what that call wrote."""
-    a = _packed(q, k, v, cu_seqlens, d_num, o, lse, workspace, scale, prompt_k, prompt_v, cu_prompts, survivor_idx, G)
-    a.d_o, a.d_o_stride = _rows(d_o, a.Hq, a.D)
-    a.dq, a.dq_stride = _rows(dq, a.Hq, a.D)
-    a.dk, a.dk_stride = _rows(dk, a.Hkv, a.D)
-    a.dv, a.dv_stride = _rows(dv, a.Hkv, a.D)
-    for name, t in (("d_o", d_o), ("dq", dq), ("dk", dk), ("dv", dv)):
-        _same_rows(name, t, a.T_max)
-    if prompt_k is not None:
-        a.dprompt_k, a.dprompt_k_stride = _rows(dprompt_k, a.Hkv, a.D)
-        a.dprompt_v, a.dprompt_v_stride = _rows(dprompt_v, a.Hkv, a.D)
-        for name, t in (("dprompt_k", dprompt_k), ("dprompt_v", dprompt_v)):
-            _same_rows(name, t, a.prompt_rows)
+    (T, Hq, D), Hkv, rows = q.shape, k.shape[1], 0 if prompt_k is None else prompt_k.shape[0]
+    grads = _rows(d_o, T, Hq, D) + _rows(dq, T, Hq, D) + _rows(dk, T, Hkv, D) + _rows(dv, T, Hkv, D)
+    grads += (None, 0) * 2 if prompt_k is None else _rows(dprompt_k, rows, Hkv, D) + _rows(dprompt_v, rows, Hkv, D)
+    a = _packed(q, k, v, cu_seqlens, d_num, o, lse, workspace, scale, prompt_k, prompt_v, cu_prompts, survivor_idx, G, grads)
     B._check(_lib().arrol_attention_backward(ctx.handle, C.byref(a), B._stream(stream)), "arrol_attention_backward")
 
 
@@ -152,26 +142,14 @@ def arrol_attention_decode_workspace(ctx: B.Context, N: int, P: int, Hq: int, Hk
 def arrol_attention_decode(ctx: B.Context, q, k, v, src_tok_off, lengths, o, lse, workspace, keep=None, scale: Optional[float] = None,
                            prompt_k=None, prompt_v=None, cu_prompts=None, G: int = 1, stream=None):
     """One token per rollout: q, o [N, Hq, D], caches k, v [cache_rows, Hkv, D] bfloat16, lse float32 [N, Hq] or None."""
-    (N, Hq, D), Hkv = q.shape, k.shape[1]
-    a = _Decode()
-    a.q, a.q_stride = _rows(q, Hq, D)
-    a.k, a.k_stride = _rows(k, Hkv, D)
-    a.v, a.v_stride = _rows(v, Hkv, D)
-    a.o, a.o_stride = _rows(o, Hq, D)
-    _same_rows("o", o, N)
-    _same_rows("v", v, k.shape[0])
-    a.lse = _lse(lse, N, Hq)
-    a.src_tok_off = _ints("src_tok_off", src_tok_off, torch.int64, N)
-    a.lengths = _ints("lengths", lengths, torch.int32, N)
-    a.keep = _ints("keep", keep, torch.uint8, N)
-    if prompt_k is not None:
-        a.prompt_k, a.prompt_k_stride = _rows(prompt_k, Hkv, D)
-        a.prompt_v, a.prompt_v_stride = _rows(prompt_v, Hkv, D)
-        _same_rows("prompt_v", prompt_v, prompt_k.shape[0])
-        a.cu_prompts = _ints("cu_prompts", cu_prompts, torch.int64, 1)
-        a.prompt_rows, a.P = prompt_k.shape[0], cu_prompts.numel() - 1
-    a.cache_rows, a.N, a.G, a.Hq, a.Hkv, a.D = k.shape[0], N, int(G), Hq, Hkv, D
-    a.scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
-    a.workspace = B._ptr(workspace)
-    a.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    (N, Hq, D), Hkv, cache_rows = q.shape, k.shape[1], k.shape[0]
+    q_at, q_stride = _rows(q, N, Hq, D)
+    k_at, k_stride = _rows(k, cache_rows, Hkv, D)
+    v_at, v_stride = _rows(v, cache_rows, Hkv, D)
+    o_at, o_stride = _rows(o, N, Hq, D)
+    rows, P, pk, pv, pk_stride, pv_stride, cu_p = _prompts(prompt_k, prompt_v, cu_prompts, Hkv, D)
+    a = _Decode(q_at, k_at, v_at, q_stride, k_stride, v_stride, _ints("src_tok_off", src_tok_off, torch.int64, N),
+                _ints("lengths", lengths, torch.int32, N), _ints("keep", keep, torch.uint8, N), pk, pv, pk_stride, pv_stride, cu_p, cache_rows,
+                rows, N, P, G, Hq, Hkv, D, D ** -0.5 if scale is None else scale, 0, o_at, o_stride, _lse(lse, N, Hq), B._ptr(workspace),
+                _bytes(workspace))
     B._check(_lib().arrol_attention_decode(ctx.handle, C.byref(a), B._stream(stream)), "arrol_attention_decode")

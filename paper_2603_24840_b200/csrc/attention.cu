@@ -23,13 +23,22 @@ __device__ __forceinline__ int first_of_prompt(const int32_t* survivor_idx, int 
     }
     return lo;
 }
+// What the backward needs of a query row too: lse log2(e) and delta = sum_d d_o[t, h, d] o[t, h, d], a warp per row.
+struct RowStats {
+    const __nv_bfloat16 *o, *d_o;
+    int64_t o_stride, d_o_stride;
+    const float* lse;
+    float2* stats;           // NULL: not wanted
+    int Hq, D;
+};
+
 // One thread per packed token and per prompt row.  Everything that the other kernels follow is clamped to the buffers here, so numbers out
 // of order give wrong results and a status bit, never an access outside.
 __global__ void __launch_bounds__(BOUNDS_THREADS)
 attention_bounds_kernel(const int64_t* __restrict__ cu_seqlens, const int64_t* __restrict__ d_num, const int64_t* __restrict__ cu_prompts,
                         const int32_t* __restrict__ survivor_idx, int S_max, int T_max, int P, int G, int prompt_rows,
                         TokenBounds* __restrict__ bounds, int2* __restrict__ prompt_range, uint32_t* __restrict__ counters,
-                        uint32_t* __restrict__ status) {
+                        uint32_t* __restrict__ status, const RowStats rs) {
     pdl_launch_dependents();
     pdl_wait();
     cu_seqlens = pdl_acquire(cu_seqlens); d_num = pdl_acquire(d_num); cu_prompts = pdl_acquire(cu_prompts); survivor_idx = pdl_acquire(survivor_idx);
@@ -74,32 +83,27 @@ attention_bounds_kernel(const int64_t* __restrict__ cu_seqlens, const int64_t* _
         }
     }
     if (bad) atomicOr(status, ARROL_DEV_BAD_INDEX);
-}
-
-// What the backward needs of a query row: lse log2(e) and delta = sum_d d_o[t, h, d] o[t, h, d].  A warp per row.
-__global__ void __launch_bounds__(BOUNDS_THREADS)
-attention_stats_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_stride, const __nv_bfloat16* __restrict__ d_o, int64_t d_o_stride,
-                       const float* __restrict__ lse, const int64_t* __restrict__ d_num, int T_max, int Hq, int D, float2* __restrict__ stats) {
-    pdl_launch_dependents();
-    pdl_wait();
-    o = pdl_acquire(o); d_o = pdl_acquire(d_o); lse = pdl_acquire(lse); d_num = pdl_acquire(d_num);
-    const int T = clamp_row(d_num[1], 0, T_max);
-    const int lane = threadIdx.x & 31;
-    const int64_t rows = (int64_t)T * Hq, warps = (int64_t)gridDim.x * (BOUNDS_THREADS / 32);
-    for (int64_t i = blockIdx.x * (int64_t)(BOUNDS_THREADS / 32) + (threadIdx.x >> 5); i < rows; i += warps) {
-        const int64_t t = i / Hq;
-        const int h = (int)(i - t * Hq);
-        float sum = 0.f;
-        for (int c = lane * 4; c < D; c += 128) {
-            const uint2 x = *reinterpret_cast<const uint2*>(o + t * o_stride + (int64_t)h * D + c);
-            const uint2 y = *reinterpret_cast<const uint2*>(d_o + t * d_o_stride + (int64_t)h * D + c);
-            const float2 x0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x.x)), x1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x.y));
-            const float2 y0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y.x)), y1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y.y));
-            sum += x0.x * y0.x + x0.y * y0.y + (x1.x * y1.x + x1.y * y1.y);
-        }
+    if (rs.stats) {
+        const __nv_bfloat16 *o = pdl_acquire(rs.o), *d_o = pdl_acquire(rs.d_o);
+        const float* lse = pdl_acquire(rs.lse);
+        const int lane = threadIdx.x & 31;
+        const int64_t rows = (int64_t)T * rs.Hq, warps = (int64_t)gridDim.x * (BOUNDS_THREADS / 32);
+        for (int64_t i = blockIdx.x * (int64_t)(BOUNDS_THREADS / 32) + (threadIdx.x >> 5); i < rows; i += warps) {
+            const int64_t t = i / rs.Hq;
+            const int h = (int)(i - t * rs.Hq), c = lane * 4;
+            float sum = 0.f;
+            if (c < rs.D) {
+                const uint2 x = *reinterpret_cast<const uint2*>(o + t * rs.o_stride + (int64_t)h * rs.D + c);
+                const uint2 y = *reinterpret_cast<const uint2*>(d_o + t * rs.d_o_stride + (int64_t)h * rs.D + c);
+                const float2 x0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x.x)), x1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x.y));
+                const float2 y0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y.x)), y1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y.y));
+                sum = x0.x * y0.x + x0.y * y0.y + (x1.x * y1.x + x1.y * y1.y);
+            }
+            const float log_sum = lse[i];
 #pragma unroll
-        for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-        if (lane == 0) stats[i] = make_float2(lse[i] * LOG2E, sum);
+            for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+            if (lane == 0) rs.stats[i] = make_float2(log_sum * LOG2E, sum);
+        }
     }
 }
 
@@ -794,20 +798,17 @@ int arrol_internal_check_attention(const arrol_attention_args* a) {
 int arrol_internal_attention_bounds(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWorkspace& w, bool backward, cudaStream_t s) {
     int64_t items = a->T_max > a->prompt_rows ? a->T_max : a->prompt_rows;
     int64_t blocks = (items + BOUNDS_THREADS - 1) / BOUNDS_THREADS;
-    if (blocks > 4 * ctx->sm_count) blocks = 4 * ctx->sm_count;
+    RowStats rs = {};
+    if (backward && a->T_max > 0) {
+        rs = {static_cast<const __nv_bfloat16*>(a->o), static_cast<const __nv_bfloat16*>(a->d_o), a->o_stride, a->d_o_stride, a->lse, w.stats, a->Hq, a->D};
+        blocks = (a->T_max * a->Hq + BOUNDS_THREADS / 32 - 1) / (BOUNDS_THREADS / 32);
+    }
+    if (blocks > 8 * ctx->sm_count) blocks = 8 * ctx->sm_count;
     if (blocks < 1) blocks = 1;
     ARROL_CUDA_OK(arrol_launch_pdl(attention_bounds_kernel, dim3((unsigned)blocks), dim3(BOUNDS_THREADS), 0, s, a->cu_seqlens, a->d_num,
                                    a->cu_prompts, a->survivor_idx, a->S_max, (int)a->T_max, a->P, a->G, (int)a->prompt_rows, w.bounds,
-                                   backward ? w.prompt_range : nullptr, w.counters, ctx->d_status));
+                                   backward ? w.prompt_range : nullptr, w.counters, ctx->d_status, rs));
     ctx->launches += 1;
-    if (backward && a->T_max > 0) {
-        int64_t rows = (a->T_max * a->Hq + 7) / 8;
-        if (rows > 16 * ctx->sm_count) rows = 16 * ctx->sm_count;
-        ARROL_CUDA_OK(arrol_launch_pdl(attention_stats_kernel, dim3((unsigned)rows), dim3(BOUNDS_THREADS), 0, s,
-                                       static_cast<const __nv_bfloat16*>(a->o), a->o_stride, static_cast<const __nv_bfloat16*>(a->d_o),
-                                       a->d_o_stride, static_cast<const float*>(a->lse), a->d_num, (int)a->T_max, a->Hq, a->D, w.stats));
-        ctx->launches += 1;
-    }
     return ARROL_OK;
 }
 

@@ -117,8 +117,10 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
     __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = uniform(sm.tmem);                // accumulators 1 and 2 at columns 0 and 128; x, y of buffer i at 256 + 128 i and + 64
+    // The queries' launch needs nothing of the keys' launch before it, only what that one has waited for, so it starts as soon as that one's blocks are all
+    // there and takes the SMs that they leave; it waits for them before it ends, so that what follows it has both.
+    if (KEYS) pdl_wait();
     pdl_launch_dependents();
-    pdl_wait();
     const int T = clamp_row(*pdl_acquire(p.sh.d_num + 1), 0, p.sh.T_max);
     const int live_prompt = KEYS && p.P > 0 ? clamp_row(pdl_acquire(p.cu_prompts)[p.P], 0, p.sh.prompt_rows) : 0;
     const TokenBounds* bounds = pdl_acquire(p.sh.bounds);
@@ -551,6 +553,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
         tcgen05_fence_after();
         tcgen05_dealloc(tmem, 512);
     }
+    if (!KEYS) pdl_wait();
 }
 
 // The parts of a prompt tile's sums, in order.
@@ -620,12 +623,8 @@ int launch_backward(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWor
     ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, true>, dim3((unsigned)(items < ctx->sm_count ? items : ctx->sm_count)), dim3(BWD_THREADS), C::SMEM, s,
                                    k_rows, v_rows, q_cols, do_cols, pk_rows, pv_rows, p));
     ctx->launches += 1;
-    if (p.splits > 1) {
-        const int64_t pieces = 2 * a->prompt_rows * a->Hkv * (DP / 8), blocks = (pieces + 255) / 256;
-        ARROL_CUDA_OK(arrol_launch_pdl(attention_add_parts_kernel<DP>, dim3((unsigned)(blocks < 8 * ctx->sm_count ? blocks : 8 * ctx->sm_count)), dim3(256), 0, s, p));
-        ctx->launches += 1;
-    }
-    if (a->T_max == 0) return ARROL_OK;
+    if (a->T_max == 0) return ARROL_OK;      // one part then
+    BwdParams sums = p;
     p.out1 = nullptr;
     p.out2 = static_cast<__nv_bfloat16*>(a->dq); p.out2_stride = a->dq_stride;
     p.counter = w.counters + 2;
@@ -633,6 +632,11 @@ int launch_backward(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWor
     ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, false>, dim3((unsigned)(items < ctx->sm_count ? items : ctx->sm_count)), dim3(BWD_THREADS), C::SMEM, s,
                                    q_rows, do_rows, k_cols, v_cols, pk_cols, pv_cols, p));
     ctx->launches += 1;
+    if (p.splits > 1) {
+        const int64_t pieces = 2 * a->prompt_rows * a->Hkv * (DP / 8), blocks = (pieces + 255) / 256;
+        ARROL_CUDA_OK(arrol_launch_pdl(attention_add_parts_kernel<DP>, dim3((unsigned)(blocks < 8 * ctx->sm_count ? blocks : 8 * ctx->sm_count)), dim3(256), 0, s, sums));
+        ctx->launches += 1;
+    }
     return ARROL_OK;
 }
 

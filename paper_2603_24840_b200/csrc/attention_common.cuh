@@ -41,11 +41,14 @@ struct AttnShape {
 inline size_t attn_round(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Items per tile of 128 prompt rows in the backward: every survivor's tokens pass by such a tile, which would make it the longest piece of work by far.
-// Parts of about 48 blocks of 64 query rows (30 to 40 us), but no more items than four an SM, whose partial sums take 128 KB each.
+// Parts of about 48 blocks of 64 query rows (30 to 40 us); of 4 where the other tiles leave SMs free; and no more items than four an SM, whose
+// partial sums take 128 KB each.
 inline int attn_prompt_splits(int sm_count, int64_t T_max, int64_t prompt_rows, int P, int Hq, int Hkv) {
-    if (prompt_rows == 0 || P < 1) return 1;
-    const int64_t blocks = T_max * (Hq / Hkv) / P / 64, tiles = (prompt_rows + 127) / 128 * Hkv;
-    int64_t n = (blocks + 47) / 48;
+    if (prompt_rows == 0 || P < 1 || T_max == 0) return 1;
+    const int64_t blocks = T_max * (Hq / Hkv) / P / 64, tiles = (prompt_rows + 127) / 128 * Hkv, others = (T_max + 127) / 128 * Hkv;
+    int64_t n = (blocks + 47) / 48, fine = (sm_count - others) / tiles;
+    if (fine > blocks / 4) fine = blocks / 4;
+    if (n < fine) n = fine;
     const int64_t most = (4 * (int64_t)sm_count + tiles - 1) / tiles;
     if (n > most) n = most;
     return (int)(n < 1 ? 1 : n > 16 ? 16 : n);

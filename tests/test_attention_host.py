@@ -147,13 +147,19 @@ def test_decode_refuses(lib, over, code):
 
 def test_binding_refuses_other_layouts():
     q = torch.zeros(4, 8, 64, dtype=torch.bfloat16)
-    assert A._rows(q[:, :4], 4, 64) == (q.data_ptr(), 8 * 64)               # heads of a wider row
-    assert A._rows(q[:1, :4], 4, 64)[1] >= 4 * 64
+    assert A._rows(q[:, :4], 4, 4, 64) == (q.data_ptr(), 8 * 64)            # heads of a wider row
+    assert A._rows(q[:1, :4], 1, 4, 64)[1] >= 4 * 64
+    assert A._rows(q[:, :1], 4, 1, 64) == (q.data_ptr(), 8 * 64)
+    assert A._rows(None, 4, 8, 64) == (None, 0)
     for bad in (q.transpose(0, 1), q[:, ::2], q[..., ::2], q.view(4, -1)):
         with pytest.raises(ValueError):
-            A._rows(bad, bad.shape[1], bad.shape[-1])
+            A._rows(bad, bad.shape[0], bad.shape[1], bad.shape[-1])
+    with pytest.raises(ValueError):
+        A._rows(q, 5, 8, 64)                                                # fewer rows than its counterpart
+    with pytest.raises(ValueError):
+        A._rows(q, 4, 4, 64)
     with pytest.raises(TypeError):
-        A._rows(q.float(), 8, 64)
+        A._rows(q.float(), 4, 8, 64)
     with pytest.raises(ValueError):
         A._lse(torch.zeros(3, 8), 4, 8)
     with pytest.raises(ValueError):
