@@ -23,7 +23,7 @@ __device__ __forceinline__ int first_of_prompt(const int32_t* survivor_idx, int 
     }
     return lo;
 }
-// What the backward needs of a query row too: lse log2(e) and delta = sum_d d_o[t, h, d] o[t, h, d], a warp per row.
+// What the backward needs of a query row too: lse log2(e) and delta = sum_d d_o[t, h, d] o[t, h, d].
 struct RowStats {
     const __nv_bfloat16 *o, *d_o;
     int64_t o_stride, d_o_stride;
@@ -86,23 +86,40 @@ attention_bounds_kernel(const int64_t* __restrict__ cu_seqlens, const int64_t* _
     if (rs.stats) {
         const __nv_bfloat16 *o = pdl_acquire(rs.o), *d_o = pdl_acquire(rs.d_o);
         const float* lse = pdl_acquire(rs.lse);
-        const int lane = threadIdx.x & 31;
-        const int64_t rows = (int64_t)T * rs.Hq, warps = (int64_t)gridDim.x * (BOUNDS_THREADS / 32);
-        for (int64_t i = blockIdx.x * (int64_t)(BOUNDS_THREADS / 32) + (threadIdx.x >> 5); i < rows; i += warps) {
-            const int64_t t = i / rs.Hq;
-            const int h = (int)(i - t * rs.Hq), c = lane * 4;
-            float sum = 0.f;
-            if (c < rs.D) {
-                const uint2 x = *reinterpret_cast<const uint2*>(o + t * rs.o_stride + (int64_t)h * rs.D + c);
-                const uint2 y = *reinterpret_cast<const uint2*>(d_o + t * rs.d_o_stride + (int64_t)h * rs.D + c);
-                const float2 x0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x.x)), x1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x.y));
-                const float2 y0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y.x)), y1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y.y));
-                sum = x0.x * y0.x + x0.y * y0.y + (x1.x * y1.x + x1.y * y1.y);
-            }
-            const float log_sum = lse[i];
+        // 16 bytes a lane, 8 or 16 lanes a row, four rows of each group of lanes in flight
+        constexpr int AT_ONCE = 4;
+        const int width = rs.D <= 64 ? 8 : 16, c = (threadIdx.x & (width - 1)) * 8;
+        const int64_t rows = (int64_t)T * rs.Hq, groups = threads / width;
+        for (int64_t i0 = tid / width; i0 - (threadIdx.x & 31) / width < rows; i0 += AT_ONCE * groups) {
+            uint4 x[AT_ONCE], y[AT_ONCE];
+            float log_sum[AT_ONCE];
 #pragma unroll
-            for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-            if (lane == 0) rs.stats[i] = make_float2(log_sum * LOG2E, sum);
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int64_t i = i0 + k * groups, t = i / rs.Hq;
+                const int h = (int)(i - t * rs.Hq);
+                x[k] = y[k] = make_uint4(0u, 0u, 0u, 0u);
+                log_sum[k] = 0.f;
+                if (i < rows && c < rs.D) {
+                    x[k] = *reinterpret_cast<const uint4*>(o + t * rs.o_stride + (int64_t)h * rs.D + c);
+                    y[k] = *reinterpret_cast<const uint4*>(d_o + t * rs.d_o_stride + (int64_t)h * rs.D + c);
+                    if (c == 0) log_sum[k] = lse[i];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int64_t i = i0 + k * groups;
+                const uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w}, v[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
+                float sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u[w])), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v[w]));
+                    sum += a.x * b.x + a.y * b.y;
+                }
+#pragma unroll
+                for (int m = 8; m > 0; m >>= 1)
+                    if (m < width) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+                if (c == 0 && i < rows) rs.stats[i] = make_float2(log_sum[k] * LOG2E, sum);
+            }
         }
     }
 }
@@ -801,7 +818,8 @@ int arrol_internal_attention_bounds(arrol_ctx* ctx, const arrol_attention_args* 
     RowStats rs = {};
     if (backward && a->T_max > 0) {
         rs = {static_cast<const __nv_bfloat16*>(a->o), static_cast<const __nv_bfloat16*>(a->d_o), a->o_stride, a->d_o_stride, a->lse, w.stats, a->Hq, a->D};
-        blocks = (a->T_max * a->Hq + BOUNDS_THREADS / 32 - 1) / (BOUNDS_THREADS / 32);
+        const int64_t rows_a_block = BOUNDS_THREADS / (a->D <= 64 ? 8 : 16) * 2;
+        if (blocks < (a->T_max * a->Hq + rows_a_block - 1) / rows_a_block) blocks = (a->T_max * a->Hq + rows_a_block - 1) / rows_a_block;
     }
     if (blocks > 8 * ctx->sm_count) blocks = 8 * ctx->sm_count;
     if (blocks < 1) blocks = 1;
