@@ -49,11 +49,14 @@ struct BwdConf {
     static constexpr int HALVES = DP / 64;
     static constexpr uint32_t ROWS_BYTES = HALVES * ROWS_HALF_BYTES, COLS_BYTES = HALVES * COLS_HALF_BYTES;
     static constexpr int STAGES = DP == 128 ? 4 : 8;
+    // The rows that stay are put into tensor memory where there is room (not for keys' gradients of 128 dimensions): read from shared memory, 128 of them
+    // with every 64 columns, they make the first products wait for its bandwidth (96 KB at 128 a cycle against 512 cycles of products).
+    static constexpr uint32_t A_AT = DP == 128 ? 0 : 64, A_STEP = DP == 128 ? 64 : 128;
     static constexpr size_t SMEM = 1024 + 2 * (size_t)ROWS_BYTES + STAGES * 2 * (size_t)COLS_BYTES;
 };
 
 struct BwdShared {
-    uint64_t full[8], empty[8], a_full, a_empty, xy_full[2], ps_full[2], acc_full, acc_empty, item_full[BWD_SLOTS], item_empty[BWD_SLOTS], scanned[8], drain;
+    uint64_t full[8], empty[8], a_full, a_ready, a_empty, xy_full[2], ps_full[2], acc_full, acc_empty, item_full[BWD_SLOTS], item_empty[BWD_SLOTS], scanned[8], drain;
     alignas(16) float lse[8][BWD_BLOCK];          // negative, as delta; read four at a time
     alignas(16) float delta[8][BWD_BLOCK];
     uint32_t bad[8][2], bad_stats[8][2];          // per stage: rows of an edge block that are not finite, or whose statistics are not
@@ -81,6 +84,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                           const __grid_constant__ CUtensorMap map_p1, const __grid_constant__ CUtensorMap map_p2, const BwdParams p) {
     // the prompts' keys and values (p1, p2) are rows of KEYS items, columns otherwise
     using C = BwdConf<DP>;
+    constexpr bool A_TMEM = !(KEYS && DP == 128);
     extern __shared__ uint8_t smem_raw[];
     __shared__ BwdShared sm;
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -92,7 +96,8 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 2); mbar_init(&sm.scanned[i], 1); }
         mbar_init(&sm.a_full, 1);
-        mbar_init(&sm.a_empty, 1);
+        mbar_init(&sm.a_ready, 8);
+        mbar_init(&sm.a_empty, A_TMEM ? 8 : 1);
         for (int i = 0; i < 2; ++i) { mbar_init(&sm.xy_full[i], 1); mbar_init(&sm.ps_full[i], 4); }
         mbar_init(&sm.acc_full, 1);
         mbar_init(&sm.acc_empty, 8);
@@ -271,7 +276,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
             if (!sm.items[slot].valid) break;
             const int blocks = uniform(sm.items[slot].n);
             if (blocks > 0) {
-                if (!mbar_wait_warp(&sm.a_full, with_blocks & 1u, abort_flag)) { ok = false; break; }
+                if (!mbar_wait_warp(A_TMEM ? &sm.a_ready : &sm.a_full, with_blocks & 1u, abort_flag)) { ok = false; break; }
                 for (int b = 0; b <= blocks; ++b) {
                     if (b < blocks) {
                         const uint32_t cur = c + b, st = cur % C::STAGES, xy = tmem + 256 + (cur & 1u) * 128;
@@ -286,10 +291,13 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                                     const uint64_t b_desc = make_smem_desc(ring_base + (st * 2 + o) * C::COLS_BYTES + h * COLS_HALF_BYTES);
 #pragma unroll
                                     for (int k = 0; k < 64 / UMMA_K; ++k)
-                                        tcgen05_mma_bf16(xy + o * 64, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_xy, (h | k) != 0 ? 1u : 0u);
+                                        if (A_TMEM)
+                                            tcgen05_mma_bf16_tmem_a(xy + o * 64, tmem + C::A_AT + o * C::A_STEP + h * 32 + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_xy, (h | k) != 0 ? 1u : 0u);
+                                        else
+                                            tcgen05_mma_bf16(xy + o * 64, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_xy, (h | k) != 0 ? 1u : 0u);
                                 }
                             tcgen05_commit(&sm.xy_full[cur & 1u]);
-                            if (b == blocks - 1) tcgen05_commit(&sm.a_empty);
+                            if (!A_TMEM && b == blocks - 1) tcgen05_commit(&sm.a_empty);
                         }
                         __syncwarp();
                     }
@@ -376,6 +384,37 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
         const float2* stats = pdl_acquire(p.stats);
         uint32_t c = 0, with_blocks = 0;
         bool ok = true;
+        // Group w puts the rows of operand w into tensor memory, a row a thread.  All products of the item before are done by then.
+        uint32_t prepared = 0;
+        auto prepare = [&](uint32_t n) {
+            if (!A_TMEM) return true;
+            const uint32_t slot = n % BWD_SLOTS;
+            if (!mbar_wait_warp(&sm.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) return false;
+            if (!sm.items[slot].valid || sm.items[slot].n == 0) return true;
+            if (!mbar_wait_warp(&sm.a_full, prepared++ & 1u, abort_flag)) return false;
+#pragma unroll 1
+            for (int h = 0; h < C::HALVES; ++h) {
+                const uint8_t* at = rows_a + w * C::ROWS_BYTES + h * ROWS_HALF_BYTES + row * 128;
+                uint32_t v[32];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(at + ((j ^ (row & 7)) << 4));
+                    v[4 * j] = x.x; v[4 * j + 1] = x.y; v[4 * j + 2] = x.z; v[4 * j + 3] = x.w;
+                }
+                __syncwarp();
+                tcgen05_st_32x32(tmem + lanes + C::A_AT + w * C::A_STEP + h * 32, v);
+            }
+            tcgen05_st_wait();
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&sm.a_ready);
+                mbar_arrive(&sm.a_empty);
+            }
+            __syncwarp();
+            return true;
+        };
+        ok = prepare(0);
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % BWD_SLOTS;
             if (!mbar_wait_warp(&sm.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
@@ -494,6 +533,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 tcgen05_fence_after();
                 ++with_blocks;
             }
+            if (!prepare(n + 1)) { ok = false; break; }
             __nv_bfloat16* out;
             if (KEYS) {
                 out = w == 0 ? (it.shared ? p.shared1 + j * p.shared1_stride : p.out1 + j * p.out1_stride)
