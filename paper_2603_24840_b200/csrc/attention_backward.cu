@@ -137,6 +137,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
     if (warp == 0) {
         // ---- producer
         const float2* stats = pdl_acquire(p.stats);
+        const int col_tok[2] = {lane / ratio, (lane + 32) / ratio};       // tokens of columns lane and lane + 32 of a block (KEYS)
         uint32_t pos = 0, a_loads = 0;
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
@@ -209,20 +210,21 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
             }
             __syncwarp();
             ++a_loads;
-            // a column's statistics are asked for one block ahead; columns without a query row: p = exp(-inf)
-            float2 next[2];
-            auto ask = [&](int b) {
+            // the columns' statistics are asked for three blocks ahead; columns without a query row: p = exp(-inf)
+            constexpr int BLOCKS_AHEAD = 3;
+            float2 ahead[BLOCKS_AHEAD][2];
+            auto ask = [&](int b, float2 (&into)[2]) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int c = u * 32 + lane, tok = c / ratio, t = bwd_start<KEYS>(it, b, TOKQ) + tok;
-                    next[u] = make_float2(INFINITY, 0.f);
-                    if (b < it.n && tok < TOKQ && t < T) {
-                        next[u] = stats[(int64_t)t * p.sh.Hq + it.g * ratio + (c - tok * ratio)];
-                        if (next[u].x == INFINITY) next[u].x = NAN;
-                    }
+                    const int tok = col_tok[u], t = bwd_start<KEYS>(it, b, TOKQ) + tok;
+                    into[u] = make_float2(INFINITY, 0.f);
+                    if (b < it.n && tok < TOKQ && t < T) into[u] = stats[(int64_t)t * p.sh.Hq + it.g * ratio + (u * 32 + lane - tok * ratio)];
                 }
             };
-            if (KEYS) ask(0);
+            if (KEYS) {
+#pragma unroll
+                for (int k = 0; k < BLOCKS_AHEAD; ++k) ask(k, ahead[k]);
+            }
             for (int b = 0; b < it.n; ++b, ++pos) {
                 const uint32_t st = pos % C::STAGES;
                 if (!mbar_wait_warp(&sm.empty[st], ((pos / C::STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
@@ -230,10 +232,12 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                     const bool masked = bwd_masked<KEYS>(it, b, TOKQ);
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
+                        const float2 x = ahead[0][u];
+                        const bool there = col_tok[u] < TOKQ && bwd_start<KEYS>(it, b, TOKQ) + col_tok[u] < T;
                         // where some row does not have the column, statistics that are not finite go the way of such values
-                        const bool bad = masked && next[u].x != INFINITY && !(fabsf(next[u].x) < INFINITY && fabsf(next[u].y) < INFINITY);
-                        sm.lse[st][u * 32 + lane] = bad ? 0.f : -next[u].x;
-                        sm.delta[st][u * 32 + lane] = bad ? 0.f : -next[u].y;
+                        const bool bad = masked && there && !(fabsf(x.x) < INFINITY && fabsf(x.y) < INFINITY);
+                        sm.lse[st][u * 32 + lane] = bad ? 0.f : there && x.x == INFINITY ? NAN : -x.x;
+                        sm.delta[st][u * 32 + lane] = bad ? 0.f : -x.y;
                         const uint32_t all = __ballot_sync(0xffffffffu, bad);
                         if (lane == 0) sm.bad_stats[st][u] = all;
                     }
@@ -252,7 +256,11 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                     }
                 }
                 __syncwarp();
-                if (KEYS) ask(b + 1);
+                if (KEYS) {
+#pragma unroll
+                    for (int k = 0; k + 1 < BLOCKS_AHEAD; ++k) { ahead[k][0] = ahead[k + 1][0]; ahead[k][1] = ahead[k + 1][1]; }
+                    ask(b + BLOCKS_AHEAD, ahead[BLOCKS_AHEAD - 1]);
+                }
             }
         }
         if (!ok) {                                // let the copies in flight land before the block's shared memory goes away
