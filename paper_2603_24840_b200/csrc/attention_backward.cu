@@ -234,8 +234,9 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                     for (int u = 0; u < 2; ++u) {
                         const float2 x = ahead[0][u];
                         const bool there = col_tok[u] < TOKQ && bwd_start<KEYS>(it, b, TOKQ) + col_tok[u] < T;
-                        // where some row does not have the column, statistics that are not finite go the way of such values
-                        const bool bad = masked && there && !(fabsf(x.x) < INFINITY && fabsf(x.y) < INFINITY);
+                        // where some row does not have the column, statistics that are not finite go the way of such values; rows behind the last token
+                        // have none and may hold anything
+                        const bool bad = masked && col_tok[u] < TOKQ && !(there && fabsf(x.x) < INFINITY && fabsf(x.y) < INFINITY);
                         sm.lse[st][u * 32 + lane] = bad ? 0.f : there && x.x == INFINITY ? NAN : -x.x;
                         sm.delta[st][u * 32 + lane] = bad ? 0.f : -x.y;
                         const uint32_t all = __ballot_sync(0xffffffffu, bad);
@@ -343,7 +344,9 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
         }
         __syncwarp();
     } else if (warp == 2) {
-        // ---- scanner: in a block that some row does not have all of, what a masked 0 would meet in the second products must be finite
+        // ---- scanner: in a block that some row does not have all of, what a masked 0 would meet in the second products must be finite.
+        // A query row or its d_o that is not leaves statistics that are not (its lse is a sum over its scores, its delta a sum over d_o), so query rows
+        // are looked over only where some statistics are not finite, or missing; keys always.
         uint32_t c = 0;
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
@@ -355,7 +358,10 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
             for (int b = 0; b < blocks; ++b) {
                 const uint32_t cur = c + b, st = cur % C::STAGES;
                 if (!mbar_wait_warp(&sm.full[st], (cur / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
-                if (bwd_masked<KEYS>(it, b, TOKQ)) {
+                const bool masked = bwd_masked<KEYS>(it, b, TOKQ);
+                if (KEYS && masked && (sm.bad_stats[st][0] | sm.bad_stats[st][1]) == 0u) {
+                    if (lane < 2) sm.bad[st][lane] = 0u;
+                } else if (masked) {
 #pragma unroll 1
                     for (int r = 0; r < 2; ++r) {
                         bool bad = false;
