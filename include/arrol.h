@@ -325,7 +325,8 @@ int arrol_lm_head_backward(arrol_ctx* ctx, const void* hidden, const void* W_voc
  * decreasing; d_num [2] int64 = {S, T} on the device, clamped to S_max and T_max: the outputs of arrol_compact.  Sequences and prompts may
  * be empty.  Without prompts give NULL for prompt_k, prompt_v, cu_prompts and 0 for prompt_rows, P.
  * Rows >= T of the outputs, and rows of dprompt_k / dprompt_v outside the prompts, are not written; inputs there may hold anything, and an
- * infinity or NaN in one row reaches only what attends to that row.  Of rows that do attend to one, o and the gradients are not finite.
+ * infinity or NaN in one row reaches only what attends to that row (through the gradients, what that attends to).  What does attend to one is not
+ * finite where the formulas are not, but in which of a row's entries, and whether infinity or NaN, is not defined.
  * Supported: D a multiple of 8, 8 <= D <= 128; Hq a multiple of Hkv, Hq / Hkv <= 64; T_max, prompt_rows < 2^31 - 512.
  * Products of bf16 with fp32 sums; probabilities and ds are rounded to bf16 before the second contractions; sums, maxima and lse are
  * fp32; every sum has a fixed order, so equal calls give equal bits.

@@ -212,6 +212,36 @@ def test_not_a_number_reaches_only_what_attends_to_it(ctx, where, value):
         assert not torch.isfinite(out["dq"][130, 1]).all()
 
 
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 4, 2), (128, 4, 2), (128, 6, 1), (96, 3, 3)])
+@pytest.mark.parametrize("at", [0, 5, 127, 128, 300, 511, 699])
+def test_not_a_number_in_a_long_sequence(ctx, D, Hq, Hkv, at):
+    """Blocks that some rows see whole and others in part, or not at all: NaN in one value (key, query row) of a sequence between two others."""
+    make = lambda: Problem([200, 700, 333], [150, 260], [0, 1, 4], 4, Hq, Hkv, D, seed=18)  # noqa: E731
+    good = make().run(ctx)
+    for where in ("v", "k", "q", "d_o"):
+        p = make()
+        getattr(p, where)[200 + at, 0, D // 2] = math.nan
+        out = p.run(ctx)
+        rows = torch.zeros(1233, dtype=torch.bool, device="cuda")
+        keys, prompts = rows.clone(), torch.zeros(410, dtype=torch.bool, device="cuda")
+        prompts[:150] = True
+        if where in ("k", "v"):
+            rows[200 + at:900], keys[200:900] = True, True
+        else:
+            rows[200 + at], keys[200:201 + at] = True, True
+        for name, may in (("o", rows), ("dq", rows), ("dk", keys), ("dv", keys), ("dprompt_k", prompts), ("dprompt_v", prompts)):
+            if where == "d_o" and name == "o":
+                may = torch.zeros_like(may)
+            assert torch.equal(out[name][~may], good[name][~may]), (where, name)
+        r = Hq // Hkv
+        if where != "d_o":
+            heads = slice(0, r) if where in ("k", "v") else slice(0, 1)
+            last = 900 if where in ("k", "v") else 201 + at
+            shown = out["o"][200 + at:last, heads]
+            assert not torch.isfinite(shown[..., D // 2]).any(), where
+        assert not torch.isfinite(out["dk"][200:201 + at, 0]).all(-1).any(), where
+
+
 def test_same_bits_every_time_and_on_another_stream(ctx):
     p = Problem([300, 500, 20, 260], [200, 130], [0, 1, 5, 6], 4, 8, 2, 128, seed=7)
     first = p.run(ctx)
@@ -303,3 +333,52 @@ def test_refuses_a_workspace_that_is_too_small(ctx):
             call(ctx, out, ws[:-256])
         assert e.value.code == -3
     assert (out["o"].float() == -7).all()
+
+
+def test_empty_prompts_and_sequences_without_an_index(ctx):
+    """Prompts that are all empty; every rollout present (no survivor_idx); a single prompt row."""
+    p = Problem([30, 200], [0, 0], [0, 5], 4, 4, 2, 64, seed=13)
+    p.check(p.run(ctx))
+    p = Problem([30, 0, 70, 129], [5, 66], None, 2, 4, 2, 64, seed=14)
+    p.check(p.run(ctx))
+    p = Problem([300], [1], [3], 4, 8, 1, 128, seed=15)
+    p.check(p.run(ctx))
+
+
+def test_no_tokens_at_all(ctx):
+    p = Problem([], [40, 3], [], 4, 4, 2, 64)
+    out = p.run(ctx)
+    assert (out["dprompt_k"] == 0).all() and (out["dprompt_v"] == 0).all()
+    p = Problem([], None, None, 1, 4, 2, 64)
+    p.run(ctx)
+
+
+def test_a_prompt_whose_tokens_are_split_into_parts(ctx):
+    """Few tiles and many tokens that pass by them: the prompt's gradients come from parts of the tokens that are added up, in one order."""
+    p = Problem([700, 650, 720, 30], [200], [0, 1, 2, 3], 4, 8, 2, 64, seed=16)
+    out = p.run(ctx)
+    p.check(out)
+    again = p.run(ctx)
+    assert torch.equal(out["dprompt_k"], again["dprompt_k"]) and torch.equal(out["dprompt_v"], again["dprompt_v"])
+
+
+def test_gradients_agree_with_differences(ctx):
+    """The loss changes by gradient times step: coarse, as q, k, v are bf16, but of the kernel's own forward."""
+    p = Problem([90, 60], [40], [0, 1], 2, 4, 2, 64, seed=17)
+    out = p.run(ctx)
+    g = torch.Generator("cuda").manual_seed(1)
+    for name, grad in (("q", "dq"), ("k", "dk"), ("v", "dv"), ("pk", "dprompt_k"), ("pv", "dprompt_v")):
+        x = getattr(p, name)
+        old = x.clone()
+        step = (torch.randn(x.shape, generator=g, device="cuda") * 0.05).to(BF)
+        losses = []
+        for sign in (1, -1):
+            x.copy_((old.float() + sign * step.float()).to(BF))
+            moved = (x.double() - old.double())
+            o = p.run(ctx, backward=False)["o"]
+            losses.append(((o.double() * p.d_o.double()).sum().item(), (moved * out[grad].double()).sum().item()))
+        x.copy_(old)
+        found, expected = losses[0][0] - losses[1][0], losses[0][1] - losses[1][1]
+        # what the roundings of o (2^-8 of each, of either sign) and of the gradient leave of a difference of two sums
+        noise = 2 * 2.0 ** -8 * ((out["o"].double() * p.d_o.double()) ** 2).sum().sqrt().item() * 2
+        assert abs(found - expected) <= noise + 0.02 * abs(expected), (name, found, expected, noise)

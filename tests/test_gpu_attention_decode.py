@@ -189,3 +189,39 @@ def test_lse_is_optional(ctx):
     p.call(ctx, o2, None, p.workspace(ctx))
     torch.cuda.synchronize()
     assert torch.equal(o, o2)
+
+
+def test_nothing_kept_and_no_rollouts(ctx):
+    p = Problem([10, 20], [30], 2, 4, 2, 64, [0, 0])
+    o, lse = p.run(ctx)
+    assert (o.float() == -7).all() and (lse == -7).all()
+    p = Problem([], None, 1, 4, 2, 64)
+    p.run(ctx)
+
+
+def test_empty_caches_and_empty_prompts(ctx):
+    """No cache rows at all, prompts alone; prompts that are all empty."""
+    p = Problem([0, 0], [70], 2, 4, 2, 64, seed=10, gap=0)
+    p.check(*p.run(ctx))
+    p = Problem([5, 90, 0], [0], 3, 4, 2, 128, seed=11, gap=0)
+    p.check(*p.run(ctx))
+
+
+def test_caches_may_share_rows(ctx):
+    """Rollouts that were forked read the same rows."""
+    p = Problem([200, 90, 90], None, 1, 8, 2, 64, seed=12)
+    p.off = [p.off[0], p.off[0] + 10, p.off[0] + 10]
+    p.d_off.copy_(torch.tensor(p.off))
+    o, lse = p.run(ctx)
+    p.check(o, lse)
+
+
+def test_large_scores(ctx):
+    """One key takes nearly all of the weight; maxima change from tile to tile."""
+    p = Problem([900, 300], [500], 2, 8, 2, 64, seed=13, q_scale=60.0)
+    o, lse = p.run(ctx)
+    ro, tol, rl = R.decode(p.q, p.k, p.v, p.off, p.lengths, None, p.pk, p.pv, p.cup, p.G, p.scale)
+    zmax = (p.q.float().norm(dim=-1).max() * max(p.k.float().norm(dim=-1).max(), p.pk.float().norm(dim=-1).max()) * p.scale).item()
+    extra = zmax * 2.0 ** -20          # the exponent's error: 64 products summed in fp32
+    assert ((o.double() - ro).abs() <= tol + 2 * extra * p.v.abs().max().double()).all()
+    assert ((lse.double() - rl).abs() <= 2e-5 * (1 + rl.abs()) + extra).all()
