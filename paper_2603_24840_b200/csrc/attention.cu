@@ -133,6 +133,7 @@ constexpr int FWD_BLOCK = 128;
 constexpr int FWD_THREADS = 384;             // producer, MMA issuer, scanner, second MMA issuer or a spare warp; two softmax groups of four warps
 constexpr int FWD_SLOTS = 2;                 // work items announced ahead
 constexpr uint32_t HALF_BYTES = 128 * 128;   // 128 rows x 64 dimensions
+constexpr int APART_FROM = 16, APART_CYCLES = 1200;        // blocks of an item, cycles
 constexpr float RESCALE_AT = 8.0f;           // the running maximum follows once it is 2^8 behind
 
 struct FwdTile {
@@ -587,6 +588,12 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     len = min(max(len, 0), FWD_BLOCK - lo);
                 }
                 if (!mbar_wait_warp(&sm.s_full[i], s_count & 1u, abort_flag)) { ok = false; break; }
+                if (C::AHEAD && i == 1 && !have_o && it.n >= APART_FROM) {
+                    // half a block behind the other tile, once: in step, both groups would want the exponentials' unit at the same time and
+                    // leave it idle at the same time
+                    const long long c0 = clock64();
+                    while (clock64() - c0 < APART_CYCLES) {}
+                }
                 tcgen05_fence_after();
                 uint32_t s[4][32];
                 __syncwarp();
