@@ -1,4 +1,14 @@
 // arrol_attention: attention of the packed survivors over their shared prompts and their own tokens.
+//
+//     z_j = scale q . k_j,   o = sum_j exp(z_j - m) v_j / l,   l = sum_j exp(z_j - m),   lse = m + log l
+// over the rows of the sequence's prompt and its own rows up to the query's.  One pass over the keys: per block of 128 of them S = Q K^T into tensor memory,
+// a thread takes a row of it, P = exp(S - m) goes back as bf16 (the one rounding beside o's; l is summed before it), O += P V.  m is a reference
+// that the running maximum may be 2^8 ahead of: sums and products carry the same factor 2^-m, so a row's O is scaled again only when
+// that is passed.  4 D flops a pair against one exponential: with 128 dimensions the tensor cores (512 cycles each for S and P V of a tile and
+// block) and the exponentials (1,024 cycles a tile and block at 16 a cycle) are level, with 64 the exponentials bound it.
+// One launch finds every token's range of keys, one computes: 148 blocks that take (256 query rows, key head) items from a counter.
+// Measured: 8,192 tokens, 32 heads of 128 on 8 470 to 500 us (1.10 to 1.17 PFLOP/s, 0.66 to 0.70 of the measured burst rate, tensor pipe busy 0.55
+// of the cycles); with heads of 64 394 to 419 us; 48 survivors of 40 to 333 tokens over 16,000 prompt tokens, 28 heads on 4 395 us (0.92 PFLOP/s).
 #include "attention_common.cuh"
 
 namespace {
@@ -112,7 +122,7 @@ attention_bounds_kernel(const int64_t* __restrict__ cu_seqlens, const int64_t* _
                 float sum = 0.f;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u[w])), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v[w]));
+                    const float2 a = bf16_pair(u[w]), b = bf16_pair(v[w]);
                     sum += a.x * b.x + a.y * b.y;
                 }
 #pragma unroll
@@ -180,7 +190,9 @@ struct FwdParams {
 };
 
 struct FwdShared {
-    uint64_t full[8], empty[8], scanned[8], q_full[2], q_empty[2], s_full[2], s_free[2], p_most[2], p_full[2], pv_done[2], item_full[FWD_SLOTS], item_empty[FWD_SLOTS], item_scanned[FWD_SLOTS], drain[2];
+    uint64_t full[8], empty[8], scanned[8];                                    // per stage
+    uint64_t q_full[2], q_empty[2], s_full[2], s_free[2], p_most[2], p_full[2], pv_done[2], drain[2];      // per tile
+    uint64_t item_full[FWD_SLOTS], item_empty[FWD_SLOTS], item_scanned[FWD_SLOTS];
     alignas(16) uint32_t bad_keys[8][4];     // per stage with values: keys of an edge block that are not finite
     FwdItem items[FWD_SLOTS];
     uint32_t bad_whole[FWD_SLOTS];           // tiles that have values which are not finite in a block that they do not mask
@@ -200,10 +212,20 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     volatile uint32_t* abort_flag = &sm.abort;
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], (C::AHEAD ? 2 : 1) + (i & 1)); mbar_init(&sm.scanned[i], 1); }     // odd stages hold values, which the scanner hands back too
-        for (int i = 0; i < 2; ++i) { mbar_init(&sm.q_full[i], 1); mbar_init(&sm.q_empty[i], 1); mbar_init(&sm.s_full[i], 1); mbar_init(&sm.s_free[i], 4); mbar_init(&sm.p_most[i], 4); mbar_init(&sm.p_full[i], 4); mbar_init(&sm.pv_done[i], 1);}
-        for (int i = 0; i < FWD_SLOTS; ++i) { mbar_init(&sm.item_scanned[i], 1); mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], C::AHEAD ? 11 : 10); }
-        for (int i = 0; i < 2; ++i) mbar_init(&sm.drain[i], 1);
+        for (int i = 0; i < C::STAGES; ++i) {
+            mbar_init(&sm.full[i], 1);
+            mbar_init(&sm.empty[i], (C::AHEAD ? 2 : 1) + (i & 1));       // odd stages hold values, which the scanner hands back too
+            mbar_init(&sm.scanned[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            for (uint64_t* bar : {&sm.q_full[i], &sm.q_empty[i], &sm.s_full[i], &sm.pv_done[i], &sm.drain[i]}) mbar_init(bar, 1);
+            for (uint64_t* bar : {&sm.s_free[i], &sm.p_most[i], &sm.p_full[i]}) mbar_init(bar, 4);
+        }
+        for (int i = 0; i < FWD_SLOTS; ++i) {
+            mbar_init(&sm.item_scanned[i], 1);
+            mbar_init(&sm.item_full[i], 1);
+            mbar_init(&sm.item_empty[i], C::AHEAD ? 11 : 10);
+        }
         sm.abort = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
@@ -260,7 +282,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     FwdTile tl = {};
                     tl.tokens = tokens;
                     if (tokens > 0) {
-                        const int2 np = has_pre ? blocks_meeting(a.pre_lo, z.pre_hi, pl, 0) : make_int2(0, 0), no = blocks_meeting(a.own_lo, last + 1, ol, n_pre);
+                        const int2 np = has_pre ? blocks_meeting(a.pre_lo, z.pre_hi, pl, 0) : make_int2(0, 0);
+                        const int2 no = blocks_meeting(a.own_lo, last + 1, ol, n_pre);
                         const int2 wp = blocks_inside(z.pre_lo, a.pre_hi, pl, 0), wo = blocks_inside(z.own_lo, first + 1, ol, n_pre);
                         tl.need = make_int4(np.x, np.y, no.x, no.y);
                         tl.whole = make_int4(wp.x, min(wp.y, n_pre), wo.x, wo.y);
@@ -287,7 +310,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 if (elect_one()) {
                     mbar_expect_tx(&sm.q_full[i], C::HALVES * (uint32_t)(TOK * ratio) * 128u);
 #pragma unroll
-                    for (int h = 0; h < C::HALVES; ++h) tma_load_3d(q_tiles + i * C::TILE_BYTES + h * HALF_BYTES, &map_q, h * 64, g * ratio, t0 + i * TOK, &sm.q_full[i]);
+                    for (int h = 0; h < C::HALVES; ++h)
+                        tma_load_3d(q_tiles + i * C::TILE_BYTES + h * HALF_BYTES, &map_q, h * 64, g * ratio, t0 + i * TOK, &sm.q_full[i]);
                 }
                 __syncwarp();
                 ++q_loads[i];
@@ -323,8 +347,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         __syncwarp();
     } else if (!C::AHEAD && warp == 1) {
         // ---- MMA issuer.  Per tile and block: S = Q K^T, and once the softmax group has written P (three quarters are enough to begin), O += P V.
-        // One warp for both tiles, in turn, where P V and the next S of a tile follow each other: that keeps their softmax groups half a block apart, so that one's exponentials run while the tensor cores
-        // work for the other.  (A warp per tile let them fall in step, both waiting for the same unit: 8,192 tokens of 32 heads of 128 517 -> 700 us.)
+        // One warp for both tiles, in turn, where P V and the next S of a tile follow each other: that keeps their softmax groups half a block apart, so
+        // that one's exponentials run while the tensor cores work for the other.  (A warp per tile let them fall in step, both waiting for the same
+        // unit: 8,192 tokens of 32 heads of 128 517 -> 700 us.)
         // One thread: votes and converging barriers around every wait were half of its time (8,192 tokens as above 487 -> XXX us).
         if (elect_one()) {
             constexpr uint32_t idesc_s = make_idesc(128, FWD_BLOCK), idesc_o = make_idesc(128, DP, false, true);
@@ -345,38 +370,21 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 auto issue_s = [&](int i, uint32_t pos, bool frees, bool last) {
                     const uint32_t st = pos % C::STAGES;
                     tcgen05_fence_after();
-                    {
-#pragma unroll
-                        for (int h = 0; h < C::HALVES; ++h) {
-                            const uint64_t a_desc = make_smem_desc(q_base + i * C::TILE_BYTES + h * HALF_BYTES), b_desc = make_smem_desc(ring_base + st * C::TILE_BYTES + h * HALF_BYTES);
-#pragma unroll
-                            for (int k = 0; k < 64 / UMMA_K; ++k)
-                                tcgen05_mma_bf16(tmem + i * 128, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_s, (h | k) != 0 ? 1u : 0u);
-                        }
-                        tcgen05_commit(&sm.s_full[i]);
-                        if (frees) tcgen05_commit(&sm.empty[st]);
-                        if (last) tcgen05_commit(&sm.q_empty[i]);
-                    }
+                    mma_over_dims<C::HALVES>(tmem + i * 128, q_base + i * C::TILE_BYTES, HALF_BYTES, ring_base + st * C::TILE_BYTES, HALF_BYTES, idesc_s);
+                    tcgen05_commit(&sm.s_full[i]);
+                    if (frees) tcgen05_commit(&sm.empty[st]);
+                    if (last) tcgen05_commit(&sm.q_empty[i]);
                 };
                 auto issue_pv = [&](int i) {
                     const uint32_t st = pv_pos[i] % C::STAGES, o_at = tmem + C::O_AT + i * DP, p_at = tmem + C::P_AT + i * C::P_STEP;
                     if (!wait_stage(pv_pos[i]) || !mbar_wait(&sm.p_most[i], parity_p[i], abort_flag)) return false;
                     tcgen05_fence_after();
-                    const uint64_t b_desc = make_smem_desc_mn(ring_base + st * C::TILE_BYTES, 128);
-                                    {
-#pragma unroll
-                        for (int k = 0; k < 6; ++k)
-                            tcgen05_mma_bf16_tmem_a(o_at, p_at + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o, first[i] && k == 0 ? 0u : 1u);
-                    }
+                    mma_over_rows<FWD_BLOCK, 0, 6>(o_at, p_at, ring_base + st * C::TILE_BYTES, idesc_o, first[i]);
                     if (!mbar_wait(&sm.p_full[i], parity_p[i], abort_flag)) return false;
                     tcgen05_fence_after();
-                    {
-#pragma unroll
-                        for (int k = 6; k < 8; ++k)
-                            tcgen05_mma_bf16_tmem_a(o_at, p_at + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o, 1u);
-                        if (pv_frees[i]) tcgen05_commit(&sm.empty[st]);
-                        tcgen05_commit(&sm.pv_done[i]);
-                    }
+                    mma_over_rows<FWD_BLOCK, 6, 8>(o_at, p_at, ring_base + st * C::TILE_BYTES, idesc_o, false);
+                    if (pv_frees[i]) tcgen05_commit(&sm.empty[st]);
+                    tcgen05_commit(&sm.pv_done[i]);
                     parity_p[i] ^= 1u;
                     first[i] = false;
                     pv_pos[i] = 0;
@@ -401,7 +409,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     }
                     if (!use[0] && !use[1] && ok) {      // only where row numbers are out of order
                         if (!wait_stage(pos) || !wait_stage(pos + 1)) { ok = false; break; }
-                        { mbar_arrive(&sm.empty[pos % C::STAGES]); mbar_arrive(&sm.empty[(pos + 1) % C::STAGES]); }
+                        mbar_arrive(&sm.empty[pos % C::STAGES]);
+                        mbar_arrive(&sm.empty[(pos + 1) % C::STAGES]);
                     }
                 }
 #pragma unroll
@@ -452,13 +461,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     s_used = true;
                     tcgen05_fence_after();
                     if (elect_one()) {
-#pragma unroll
-                        for (int h = 0; h < C::HALVES; ++h) {
-                            const uint64_t a_desc = make_smem_desc(q_base + h * HALF_BYTES), b_desc = make_smem_desc(ring_base + st * C::TILE_BYTES + h * HALF_BYTES);
-#pragma unroll
-                            for (int k = 0; k < 64 / UMMA_K; ++k)
-                                tcgen05_mma_bf16(s_at, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_s, (h | k) != 0 ? 1u : 0u);
-                        }
+                        mma_over_dims<C::HALVES>(s_at, q_base, HALF_BYTES, ring_base + st * C::TILE_BYTES, HALF_BYTES, idesc_s);
                         tcgen05_commit(&sm.s_full[i]);
                         tcgen05_commit(&sm.empty[st]);
                         if (b + 1 == need.w) tcgen05_commit(&sm.q_empty[i]);
@@ -471,10 +474,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     parity_p ^= 1u;
                     tcgen05_fence_after();
                     if (elect_one()) {
-                        const uint64_t b_desc = make_smem_desc_mn(ring_base + sv * C::TILE_BYTES, 128);
-#pragma unroll
-                        for (int k = 0; k < FWD_BLOCK / UMMA_K; ++k)
-                            tcgen05_mma_bf16_tmem_a(o_at, p_at + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_o, first && k == 0 ? 0u : 1u);
+                        mma_over_rows<FWD_BLOCK, 0, 8>(o_at, p_at, ring_base + sv * C::TILE_BYTES, idesc_o, first);
                         tcgen05_commit(&sm.pv_done[i]);
                         tcgen05_commit(&sm.empty[sv]);
                     }

@@ -11,7 +11,12 @@
 //   queries' gradients:      rows are query rows, a1 = q, a2 = d_o; columns are keys, b1 = k, b2 = v;
 //       dq += ds b1;  lse and delta belong to rows.
 // x and y are double-buffered in tensor memory (2 x 128 columns beside the accumulators' 2 x D), p and ds replace them as bf16 and are read from
-// there by the second products; two groups of four warps take the blocks in turn.
+// there by the second products; two groups of four warps take the blocks in turn.  p and ds are the roundings beside the results'; delta is that of
+// the o that was written.
+// Bounded by the tensor cores and by what feeds them: with 128 dimensions a block is 512 cycles of first products and 512 of second ones for the keys' side,
+// but 64 columns a product make the first ones wait for shared memory (96 KB at 128 a cycle), unless the rows that stay are in tensor memory.
+// Measured with 4,096 tokens, 32 heads of 128 on 8: keys' side 297 us (tensor pipe busy 0.53 of the cycles, its feeding 0.70), queries' side 195 us
+// (0.58, 0.62); forward and backward together 572 us, 0.84 PFLOP/s of the 14 D flops a pair that cannot be done without (18 are done).
 #include "attention_common.cuh"
 
 namespace {
@@ -56,7 +61,8 @@ struct BwdConf {
 };
 
 struct BwdShared {
-    uint64_t full[8], empty[8], a_full, a_ready, a_empty, xy_full[2], ps_full[2], acc_full, acc_empty, item_full[BWD_SLOTS], item_empty[BWD_SLOTS], scanned[8], drain;
+    uint64_t full[8], empty[8], scanned[8];                    // per stage
+    uint64_t a_full, a_ready, a_empty, xy_full[2], ps_full[2], acc_full, acc_empty, item_full[BWD_SLOTS], item_empty[BWD_SLOTS], drain;
     alignas(16) float lse[8][BWD_BLOCK];          // negative, as delta; read four at a time
     alignas(16) float delta[8][BWD_BLOCK];
     uint32_t bad[8][2], bad_stats[8][2];          // per stage: rows of an edge block that are not finite, or whose statistics are not
@@ -111,7 +117,8 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b2) : "memory");
     }
     if (KEYS && TOKQ * ratio < BWD_BLOCK) {       // rows behind the last whole token are never loaded: zeros, for the second products
-        for (uint32_t i = threadIdx.x * 16; i < C::STAGES * 2 * C::COLS_BYTES; i += BWD_THREADS * 16) *reinterpret_cast<uint4*>(ring + i) = make_uint4(0, 0, 0, 0);
+        for (uint32_t i = threadIdx.x * 16; i < C::STAGES * 2 * C::COLS_BYTES; i += BWD_THREADS * 16)
+            *reinterpret_cast<uint4*>(ring + i) = make_uint4(0, 0, 0, 0);
         fence_proxy_async_smem();
     }
     if (warp == 1) {
@@ -293,18 +300,11 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                         tcgen05_fence_after();
                         if (elect_one()) {
 #pragma unroll
-                            for (int o = 0; o < 2; ++o)
-#pragma unroll
-                                for (int h = 0; h < C::HALVES; ++h) {
-                                    const uint64_t a_desc = make_smem_desc(a_base + o * C::ROWS_BYTES + h * ROWS_HALF_BYTES);
-                                    const uint64_t b_desc = make_smem_desc(ring_base + (st * 2 + o) * C::COLS_BYTES + h * COLS_HALF_BYTES);
-#pragma unroll
-                                    for (int k = 0; k < 64 / UMMA_K; ++k)
-                                        if (A_TMEM)
-                                            tcgen05_mma_bf16_tmem_a(xy + o * 64, tmem + C::A_AT + o * C::A_STEP + h * 32 + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_xy, (h | k) != 0 ? 1u : 0u);
-                                        else
-                                            tcgen05_mma_bf16(xy + o * 64, a_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc_xy, (h | k) != 0 ? 1u : 0u);
-                                }
+                            for (int o = 0; o < 2; ++o) {
+                                const uint32_t cols = ring_base + (st * 2 + o) * C::COLS_BYTES;
+                                if (A_TMEM) mma_over_dims_tmem_a<C::HALVES>(xy + o * 64, tmem + C::A_AT + o * C::A_STEP, cols, COLS_HALF_BYTES, idesc_xy);
+                                else mma_over_dims<C::HALVES>(xy + o * 64, a_base + o * C::ROWS_BYTES, ROWS_HALF_BYTES, cols, COLS_HALF_BYTES, idesc_xy);
+                            }
                             tcgen05_commit(&sm.xy_full[cur & 1u]);
                             if (!A_TMEM && b == blocks - 1) tcgen05_commit(&sm.a_empty);
                         }
@@ -317,13 +317,8 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                         tcgen05_fence_after();
                         if (elect_one()) {
 #pragma unroll
-                            for (int o = KEYS ? 0 : 1; o < 2; ++o) {
-                                // accumulator 1: p b2; accumulator 2: ds b1
-                                const uint64_t b_desc = make_smem_desc_mn(ring_base + (st * 2 + 1 - o) * C::COLS_BYTES, BWD_BLOCK);
-#pragma unroll
-                                for (int k = 0; k < BWD_BLOCK / UMMA_K; ++k)
-                                    tcgen05_mma_bf16_tmem_a(tmem + o * 128, xy + o * 64 + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc_acc, b == 1 && k == 0 ? 0u : 1u);
-                            }
+                            for (int o = KEYS ? 0 : 1; o < 2; ++o)       // accumulator 1: p b2; accumulator 2: ds b1
+                                mma_over_rows<BWD_BLOCK, 0, BWD_BLOCK / UMMA_K>(tmem + o * 128, xy + o * 64, ring_base + (st * 2 + 1 - o) * C::COLS_BYTES, idesc_acc, b == 1);
                             tcgen05_commit(&sm.empty[st]);
                             if (b == blocks) tcgen05_commit(&sm.acc_full);
                         }
@@ -523,7 +518,8 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                                 unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[v]), __uint_as_float(x[v + 1])), scale_x2, nl), p0, p1);
                                 p0 = ex2_approx(p0);
                                 p1 = ex2_approx(p1);
-                                unpack_f32x2(mul_f32x2(pack_f32x2(p0, p1), add_f32x2(pack_f32x2(__uint_as_float(y[v]), __uint_as_float(y[v + 1])), nd)), s0, s1);
+                                const uint64_t dp = add_f32x2(pack_f32x2(__uint_as_float(y[v]), __uint_as_float(y[v + 1])), nd);
+                                unpack_f32x2(mul_f32x2(pack_f32x2(p0, p1), dp), s0, s1);
                                 if (KEYS) pk[i + k] = pack_bf16(p0, p1);
                                 dk[i + k] = pack_bf16(s0, s1);
                             }
@@ -558,7 +554,8 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
             }
             const float by = KEYS && w == 0 ? 1.f : p.sh.scale;
             const bool to_parts = KEYS && it.shared && p.splits > 1;
-            float* const sums = !to_parts ? nullptr : (w == 0 ? p.part1 : p.part2) + ((((int64_t)it.split * ((p.sh.prompt_rows + 127) / 128) + it.row0 / 128) * p.sh.Hkv + it.g) * 128 + row) * DP;
+            const int64_t part_tile = ((int64_t)it.split * ((p.sh.prompt_rows + 127) / 128) + it.row0 / 128) * p.sh.Hkv + it.g;
+            float* const sums = !to_parts ? nullptr : (w == 0 ? p.part1 : p.part2) + (part_tile * 128 + row) * DP;
             constexpr int PIECES = DP / 32;
 #pragma unroll 1
             for (int piece = KEYS ? 0 : w * (PIECES / 2); piece < (KEYS ? PIECES : (w + 1) * (PIECES / 2)); ++piece) {
@@ -574,8 +571,10 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 if (to_parts) {
                     if (live) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4)
-                            *reinterpret_cast<float4*>(sums + piece * 32 + i) = make_float4(__uint_as_float(v[i]) * by, __uint_as_float(v[i + 1]) * by, __uint_as_float(v[i + 2]) * by, __uint_as_float(v[i + 3]) * by);
+                        for (int i = 0; i < 32; i += 4) {
+                            auto f = [&](int k) { return __uint_as_float(v[i + k]) * by; };
+                            *reinterpret_cast<float4*>(sums + piece * 32 + i) = make_float4(f(0), f(1), f(2), f(3));
+                        }
                     }
                 } else if (live) {
 #pragma unroll
@@ -657,8 +656,10 @@ int launch_backward(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWor
         {&q_cols, a->q, a->T_max, a->q_stride, a->Hq, ratio, BWD_BLOCK / ratio}, {&do_cols, a->d_o, a->T_max, a->d_o_stride, a->Hq, ratio, BWD_BLOCK / ratio},
         {&k_rows, a->k, a->T_max, a->k_stride, a->Hkv, 1, 128},                  {&v_rows, a->v, a->T_max, a->v_stride, a->Hkv, 1, 128},
         {&k_cols, a->k, a->T_max, a->k_stride, a->Hkv, 1, BWD_BLOCK},            {&v_cols, a->v, a->T_max, a->v_stride, a->Hkv, 1, BWD_BLOCK},
-        {&pk_rows, a->prompt_k, a->prompt_rows, a->prompt_k_stride, a->Hkv, 1, 128}, {&pv_rows, a->prompt_v, a->prompt_rows, a->prompt_v_stride, a->Hkv, 1, 128},
-        {&pk_cols, a->prompt_k, a->prompt_rows, a->prompt_k_stride, a->Hkv, 1, BWD_BLOCK}, {&pv_cols, a->prompt_v, a->prompt_rows, a->prompt_v_stride, a->Hkv, 1, BWD_BLOCK}};
+        {&pk_rows, a->prompt_k, a->prompt_rows, a->prompt_k_stride, a->Hkv, 1, 128},
+        {&pv_rows, a->prompt_v, a->prompt_rows, a->prompt_v_stride, a->Hkv, 1, 128},
+        {&pk_cols, a->prompt_k, a->prompt_rows, a->prompt_k_stride, a->Hkv, 1, BWD_BLOCK},
+        {&pv_cols, a->prompt_v, a->prompt_rows, a->prompt_v_stride, a->Hkv, 1, BWD_BLOCK}};
     for (auto& m : maps) {
         if (m.rows == 0) continue;
         if (make_map_heads(ctx, m.map, m.base, m.rows, m.heads, a->D, m.stride, m.group, m.tokens) != ARROL_OK) return ARROL_ERR_CUDA;
@@ -674,7 +675,8 @@ int launch_backward(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWor
     p.part1 = w.parts;
     p.part2 = w.parts + (int64_t)p.splits * ((a->prompt_rows + 127) / 128) * a->Hkv * 128 * DP;
     int64_t items = ((a->T_max + 127) / 128 + (a->prompt_rows + 127) / 128 * p.splits) * a->Hkv;
-    ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, true>, dim3((unsigned)(items < ctx->sm_count ? items : ctx->sm_count)), dim3(BWD_THREADS), C::SMEM, s,
+    const auto blocks = [&](int64_t n, int64_t most) { return dim3((unsigned)(n < most ? n : most)); };
+    ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, true>, blocks(items, ctx->sm_count), dim3(BWD_THREADS), C::SMEM, s,
                                    k_rows, v_rows, q_cols, do_cols, pk_rows, pv_rows, p));
     ctx->launches += 1;
     if (a->T_max == 0) return ARROL_OK;      // one part then
@@ -683,12 +685,12 @@ int launch_backward(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWor
     p.out2 = static_cast<__nv_bfloat16*>(a->dq); p.out2_stride = a->dq_stride;
     p.counter = w.counters + 2;
     items = (a->T_max + 128 / ratio - 1) / (128 / ratio) * a->Hkv;
-    ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, false>, dim3((unsigned)(items < ctx->sm_count ? items : ctx->sm_count)), dim3(BWD_THREADS), C::SMEM, s,
+    ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, false>, blocks(items, ctx->sm_count), dim3(BWD_THREADS), C::SMEM, s,
                                    q_rows, do_rows, k_cols, v_cols, pk_cols, pv_cols, p));
     ctx->launches += 1;
     if (p.splits > 1) {
-        const int64_t pieces = 2 * a->prompt_rows * a->Hkv * (DP / 8), blocks = (pieces + 255) / 256;
-        ARROL_CUDA_OK(arrol_launch_pdl(attention_add_parts_kernel<DP>, dim3((unsigned)(blocks < 8 * ctx->sm_count ? blocks : 8 * ctx->sm_count)), dim3(256), 0, s, sums));
+        const int64_t pieces = 2 * a->prompt_rows * a->Hkv * (DP / 8);
+        ARROL_CUDA_OK(arrol_launch_pdl(attention_add_parts_kernel<DP>, blocks((pieces + 255) / 256, 8 * ctx->sm_count), dim3(256), 0, s, sums));
         ctx->launches += 1;
     }
     return ARROL_OK;
@@ -704,7 +706,8 @@ extern "C" int arrol_attention_backward(arrol_ctx* ctx, const arrol_attention_ar
     if (a->T_max > 0 && (!attn_rows_ok(a->d_o, a->d_o_stride, a->Hq, a->D) || !attn_rows_ok(a->dq, a->dq_stride, a->Hq, a->D) ||
                          !attn_rows_ok(a->dk, a->dk_stride, a->Hkv, a->D) || !attn_rows_ok(a->dv, a->dv_stride, a->Hkv, a->D)))
         return ARROL_ERR_INVALID_ARG;
-    if (a->prompt_rows > 0 && (!attn_rows_ok(a->dprompt_k, a->dprompt_k_stride, a->Hkv, a->D) || !attn_rows_ok(a->dprompt_v, a->dprompt_v_stride, a->Hkv, a->D)))
+    if (a->prompt_rows > 0 && (!attn_rows_ok(a->dprompt_k, a->dprompt_k_stride, a->Hkv, a->D) ||
+                               !attn_rows_ok(a->dprompt_v, a->dprompt_v_stride, a->Hkv, a->D)))
         return ARROL_ERR_INVALID_ARG;
     const AttnWorkspace w = attn_workspace(a->workspace, ctx->sm_count, a->T_max, a->prompt_rows, a->Hq, a->Hkv, a->D, true);
     if (a->workspace_bytes < w.bytes) return ARROL_ERR_WORKSPACE;

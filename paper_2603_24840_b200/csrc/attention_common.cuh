@@ -65,7 +65,8 @@ inline AttnWorkspace attn_workspace(void* base, int sm_count, int64_t T_max, int
         w.prompt_range = reinterpret_cast<int2*>(take((size_t)prompt_rows * sizeof(int2)));
         w.stats = reinterpret_cast<float2*>(take((size_t)T_max * Hq * sizeof(float2)));
         const int splits = attn_prompt_splits(sm_count, T_max, prompt_rows, 1, Hq, Hkv);      // one prompt has the most
-        if (splits > 1) w.parts = reinterpret_cast<float*>(take((size_t)splits * ((prompt_rows + 127) / 128) * Hkv * 128 * (D <= 64 ? 64 : 128) * 2 * sizeof(float)));
+        const size_t tile = (size_t)128 * (D <= 64 ? 64 : 128) * 2 * sizeof(float);
+        if (splits > 1) w.parts = reinterpret_cast<float*>(take((size_t)splits * ((prompt_rows + 127) / 128) * Hkv * tile));
     }
     w.bytes = at;
     return w;
@@ -98,6 +99,41 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+
+// ---- products.  Operands with 64 HALVES dimensions lie as halves of 64 (128-byte swizzled rows), `half` bytes apart.
+// d = A B^T, rows of both in shared memory
+template <int HALVES>
+__device__ __forceinline__ void mma_over_dims(uint32_t d, uint32_t a, uint32_t a_half, uint32_t b, uint32_t b_half, uint32_t idesc) {
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+        const uint64_t a_desc = make_smem_desc(a + h * a_half), b_desc = make_smem_desc(b + h * b_half);
+#pragma unroll
+        for (int k = 0; k < 64 / UMMA_K; ++k) {
+            const uint64_t step = (uint64_t)(k * (UMMA_K * 2 >> 4));
+            tcgen05_mma_bf16(d, a_desc + step, b_desc + step, idesc, (h | k) != 0 ? 1u : 0u);
+        }
+    }
+}
+// the same with A's rows in tensor memory
+template <int HALVES>
+__device__ __forceinline__ void mma_over_dims_tmem_a(uint32_t d, uint32_t a, uint32_t b, uint32_t b_half, uint32_t idesc) {
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+        const uint64_t b_desc = make_smem_desc(b + h * b_half);
+#pragma unroll
+        for (int k = 0; k < 64 / UMMA_K; ++k)
+            tcgen05_mma_bf16_tmem_a(d, a + h * 32 + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 2 >> 4)), idesc, (h | k) != 0 ? 1u : 0u);
+    }
+}
+// d += A B over steps [K0, K1) of 16 of B's rows, A in tensor memory, B's rows in shared memory (ROWS of them); d = A B from step 0 on where `first`
+template <int ROWS, int K0, int K1>
+__device__ __forceinline__ void mma_over_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool first) {
+    const uint64_t b_desc = make_smem_desc_mn(b, ROWS);
+#pragma unroll
+    for (int k = K0; k < K1; ++k)
+        tcgen05_mma_bf16_tmem_a(d, a + k * (UMMA_K / 2), b_desc + (uint64_t)(k * (UMMA_K * 128 >> 4)), idesc, first && k == 0 ? 0u : 1u);
+}
+__device__ __forceinline__ float2 bf16_pair(uint32_t v) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v)); }
 
 // A row of 128 bytes (64 bf16) of a tile in shared memory: whether any value is an infinity or NaN (times 0 they leave NaN in the sum, everything
 // else leaves 0).  Called for consecutive rows by consecutive lanes, which start at different 16-byte words so that they do not meet in a bank.

@@ -6,6 +6,10 @@
 // these up in order, so the result does not depend on who did what.  The plan follows lengths and mask on the device.
 // The products are 16 x 8 x 16 mma.sync: 64 rows at most meet a key, which is too few flops a byte for tensor memory to pay, and a unit's 4 to 16
 // rows would leave seven eighths of a 128-row tile empty.
+// Measured (calls from a graph): 256 live rollouts of 2,200 tokens, 16 heads of 128 on 8 (2.46 GB) 381 to 394 us, 6.2 to 6.5 TB/s, 0.96 to 0.99 of the
+// measured copy rate; 8 rollouts of 6,600 tokens, 32 heads (236 MB) 62 us; 384 rollouts of 160 tokens over 24 prompts of 5,800, 32 heads of 64 121 us
+// (0.52): there a unit's 64 rows keep the 16 x 8 x 16 products busy 0.6 of the time; 16 rollouts of 30 tokens 14 us, three launches one behind another.
+// More than one tile of keys at once per warp (for its latencies) left too little of the ring for the copies: 121 -> 136 us.
 #include "attention_common.cuh"
 
 namespace {
@@ -20,7 +24,8 @@ static_assert(DEC_STAGES >= DEC_WARPS, "parity waits");
 constexpr int DEC_SLOTS = 4;                       // pairs looked up ahead
 constexpr int DEC_STAGE_BYTES = 16384;             // keys and values of 32 tokens of 128 dimensions, of 64 tokens of 64
 // Tokens of a chunk: as many as make DEC_FEW_PER_SM (unit, head) pairs an SM, between 128 and 512; more where that would make more than
-// DEC_OWN_PER_SM pairs (DEC_SHARED_PER_SM of prompts, whose partial sums are many).
+// DEC_OWN_PER_SM pairs (DEC_SHARED_PER_SM of prompts, whose partial sums are many).  One rollout of 8,000 tokens with 2 / 4 / 8 pairs an SM 18.7 / 27.7 / 27.8 us;
+// 8 of 6,600 with chunks of 128 / 256 / 512 76.8 / 75.6 / 67.2; prompts with 8 / 12 / 16 121 / 126 / 131.
 constexpr int DEC_MIN_CHUNK = 128, DEC_GOOD_CHUNK = 512;
 constexpr int DEC_FEW_PER_SM = 2, DEC_OWN_PER_SM = 32, DEC_SHARED_PER_SM = 8;
 constexpr int PLAN_THREADS = 1024;
@@ -177,7 +182,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) decode_plan_kernel(const DecodeP
             int64_t at = units + before.x;
             for (int c = 0; c < chunks; ++c)
                 for (int g = 0; g < groups && at < p.w.max_units; ++g, ++at) {        // a chunk's groups side by side: they read the same rows
-                    const DecodeUnit d = {x + c * shared_chunk, min(shared_chunk, n - c * shared_chunk), min(p.group, live - g * p.group) * p.ratio, first + g * p.group, c, 1, {0, 0}};
+                    const DecodeUnit d = {x + c * shared_chunk, min(shared_chunk, n - c * shared_chunk), min(p.group, live - g * p.group) * p.ratio,
+                                          first + g * p.group, c, 1, {0, 0}};
                     p.w.units[at] = d;
                 }
         }
@@ -374,7 +380,8 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 const int row = (warp & (row_tiles - 1)) * 16 + (lane >> 2) + r * 8, l = (int)(row * ratio_inv >> 16);
                 const bool there = row < it.rows;
                 const int i = there ? it.of[l].x : 0;
-                const __nv_bfloat16* at = static_cast<const __nv_bfloat16*>(a.q) + i * a.q_stride + (int64_t)(it.g * p.ratio + row - l * p.ratio) * a.D + (lane & 3) * 2;
+                const __nv_bfloat16* at = static_cast<const __nv_bfloat16*>(a.q) + i * a.q_stride +
+                                          (int64_t)(it.g * p.ratio + row - l * p.ratio) * a.D + (lane & 3) * 2;
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
@@ -431,7 +438,8 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                             if (j * 8 + (lane & 3) * 2 + (c & 1) >= there) s[j][c] = -INFINITY;
                     for (int x = there * 8 + lane; x < C::TOKENS * 8; x += 32)
 #pragma unroll
-                        for (int h = 0; h < C::HALVES; ++h) *reinterpret_cast<uint4*>(stage + C::KEYS_BYTES + h * C::HALF_BYTES + x * 16) = make_uint4(0, 0, 0, 0);
+                        for (int h = 0; h < C::HALVES; ++h)
+                            *reinterpret_cast<uint4*>(stage + C::KEYS_BYTES + h * C::HALF_BYTES + x * 16) = make_uint4(0, 0, 0, 0);
                     fence_proxy_async_smem();
                     __syncwarp();
                 }
@@ -469,8 +477,8 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     }
 #pragma unroll
                 for (int k = 0; k < C::TOKENS / 16; ++k) {
-                    const uint32_t w[4] = {pack_bf16(s[2 * k][0], s[2 * k][1]), pack_bf16(s[2 * k][2], s[2 * k][3]), pack_bf16(s[2 * k + 1][0], s[2 * k + 1][1]),
-                                           pack_bf16(s[2 * k + 1][2], s[2 * k + 1][3])};
+                    const uint32_t w[4] = {pack_bf16(s[2 * k][0], s[2 * k][1]), pack_bf16(s[2 * k][2], s[2 * k][3]),
+                                           pack_bf16(s[2 * k + 1][0], s[2 * k + 1][1]), pack_bf16(s[2 * k + 1][2], s[2 * k + 1][3])};
                     const int row = k * 16 + (lane & 15);
 #pragma unroll
                     for (int d0 = 0; d0 < DP / 16; d0 += AT_ONCE) {
@@ -537,7 +545,8 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
 #pragma unroll
                     for (int s = 0; s < DEC_WARPS; ++s)
                         if (s < parts) {
-                            const float by = ml[s].x == -INFINITY ? (ml[s].y == 0.f ? 0.f : 1.f) : ex2_approx(ml[s].x - top);     // a NaN without a maximum stays one
+                            // a NaN without a maximum stays one
+                            const float by = ml[s].x == -INFINITY ? (ml[s].y == 0.f ? 0.f : 1.f) : ex2_approx(ml[s].x - top);
                             const float4 v = *reinterpret_cast<const float4*>(part + ((s * row_tiles + t) * 16 + r) * C::PITCH + d);
                             sum.x += by * v.x; sum.y += by * v.y; sum.z += by * v.z; sum.w += by * v.w;
                             total += by * ml[s].y;
@@ -667,12 +676,15 @@ extern "C" size_t arrol_attention_decode_workspace(arrol_ctx* ctx, int32_t N, in
 
 extern "C" int arrol_attention_decode(arrol_ctx* ctx, const arrol_decode_args* a, void* stream) {
     if (!ctx || !a) return ARROL_ERR_INVALID_ARG;
-    if (a->N < 0 || a->P < 0 || a->G < 1 || a->cache_rows < 0 || a->prompt_rows < 0 || a->Hq < 1 || a->Hkv < 1 || a->D < 1 || a->Hq % a->Hkv) return ARROL_ERR_INVALID_ARG;
+    if (a->N < 0 || a->P < 0 || a->G < 1 || a->cache_rows < 0 || a->prompt_rows < 0) return ARROL_ERR_INVALID_ARG;
+    if (a->Hq < 1 || a->Hkv < 1 || a->D < 1 || a->Hq % a->Hkv) return ARROL_ERR_INVALID_ARG;
     if (!(a->scale > 0.f) || !isfinite(a->scale)) return ARROL_ERR_INVALID_ARG;
-    if (!attn_heads_ok(a->Hq, a->Hkv, a->D) || a->cache_rows >= ATTN_MAX_ROWS || a->prompt_rows >= ATTN_MAX_ROWS || a->G > 1024 || a->N > (1 << 24)) return ARROL_ERR_UNSUPPORTED;
+    if (!attn_heads_ok(a->Hq, a->Hkv, a->D) || a->cache_rows >= ATTN_MAX_ROWS || a->prompt_rows >= ATTN_MAX_ROWS) return ARROL_ERR_UNSUPPORTED;
+    if (a->G > 1024 || a->N > (1 << 24)) return ARROL_ERR_UNSUPPORTED;
     if (a->P > 0 ? (int64_t)a->P * a->G != a->N || !a->cu_prompts : a->prompt_rows > 0) return ARROL_ERR_INVALID_ARG;
     if (a->N == 0) return ARROL_OK;
-    if (!attn_rows_ok(a->q, a->q_stride, a->Hq, a->D) || !attn_rows_ok(a->o, a->o_stride, a->Hq, a->D) || !a->src_tok_off || !a->lengths) return ARROL_ERR_INVALID_ARG;
+    if (!attn_rows_ok(a->q, a->q_stride, a->Hq, a->D) || !attn_rows_ok(a->o, a->o_stride, a->Hq, a->D)) return ARROL_ERR_INVALID_ARG;
+    if (!a->src_tok_off || !a->lengths) return ARROL_ERR_INVALID_ARG;
     if (a->cache_rows > 0 && (!attn_rows_ok(a->k, a->k_stride, a->Hkv, a->D) || !attn_rows_ok(a->v, a->v_stride, a->Hkv, a->D))) return ARROL_ERR_INVALID_ARG;
     if (a->prompt_rows > 0 && (!attn_rows_ok(a->prompt_k, a->prompt_k_stride, a->Hkv, a->D) || !attn_rows_ok(a->prompt_v, a->prompt_v_stride, a->Hkv, a->D)))
         return ARROL_ERR_INVALID_ARG;
