@@ -153,9 +153,8 @@ struct FwdTile {
     int4 whole;                              // blocks whose keys every row has, likewise
 };
 struct alignas(16) FwdItem {
-    int t0, g, valid;
+    int t0, g, valid, split;
     int pre0, n_pre, own0, n;                // block b < n_pre: prompt rows pre0 + 128 b .., then own rows own0 + 128 (b - n_pre) ..
-    int pad;
     FwdTile tile[2];
 };
 __device__ __forceinline__ bool in_ranges(const int4& r, int b) { return (b >= r.x && b < r.y) || (b >= r.z && b < r.w); }
@@ -187,6 +186,9 @@ struct FwdParams {
     uint32_t* counter;
     uint32_t* status;
     int tile_tokens;                         // TOK
+    int splits;                              // parts of an item's keys, each an item; with more than one their sums go to
+    float* part_o;                           // [splits][T_max][Hq][D] and
+    float2* part_ml;                         // [splits][T_max][Hq]: the reference that the sums are taken against, l
 };
 
 struct FwdShared {
@@ -199,7 +201,7 @@ struct FwdShared {
     uint32_t tmem, abort;
 };
 
-template <int DP>
+template <int DP, bool SPLIT>
 __global__ void __launch_bounds__(FWD_THREADS, 1)
 attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                  const __grid_constant__ CUtensorMap map_pk, const __grid_constant__ CUtensorMap map_pv, const FwdParams p) {
@@ -245,7 +247,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     const int T = clamp_row(*pdl_acquire(p.sh.d_num + 1), 0, p.sh.T_max);
     const int ratio = p.sh.ratio, TOK = p.tile_tokens;
     const int pairs = (T + 2 * TOK - 1) / (2 * TOK);
-    const int64_t items = (int64_t)pairs * p.sh.Hkv;
+    const int64_t items = (int64_t)pairs * p.sh.Hkv * (SPLIT ? p.splits : 1);
 
     if (warp == 0) {
         // ---- producer: fetches work items, announces them, loads queries, keys and values
@@ -262,7 +264,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             const bool valid = (int64_t)idx < items;
             if (valid) {
                 // last tokens first: theirs are the longest ranges of a long sequence
-                const int t0 = (pairs - 1 - (int)(idx / (uint32_t)p.sh.Hkv)) * 2 * TOK;
+                const uint32_t head_item = SPLIT ? idx / (uint32_t)p.splits : idx;
+                const int split = SPLIT ? (int)(idx - head_item * (uint32_t)p.splits) : 0;
+                const int t0 = (pairs - 1 - (int)(head_item / (uint32_t)p.sh.Hkv)) * 2 * TOK;
                 TokenBounds a = {0, 0, 0, 0}, z = a;     // of the tile's first and last live token; lane = tile
                 int tokens = 0, last = 0;
                 const int first = t0 + lane * TOK;
@@ -277,7 +281,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const int pl = __reduce_min_sync(0xffffffffu, has_pre ? a.pre_lo : INT_MAX), ph = __reduce_max_sync(0xffffffffu, has_pre ? z.pre_hi : 0);
                 const int ol = __reduce_min_sync(0xffffffffu, tokens > 0 ? a.own_lo : INT_MAX), oh = __reduce_max_sync(0xffffffffu, tokens > 0 ? last + 1 : 0);
                 const int n_pre = ph > pl ? (ph - pl + FWD_BLOCK - 1) / FWD_BLOCK : 0;
-                const int n_own = (oh - ol + FWD_BLOCK - 1) / FWD_BLOCK;
+                const int n_own = (oh - ol + FWD_BLOCK - 1) / FWD_BLOCK, n_all = n_pre + n_own;
+                // this part's blocks: [from, to) of all of them, numbered from 0
+                const int each = SPLIT ? (n_all + p.splits - 1) / p.splits : n_all, from = SPLIT ? min(split * each, n_all) : 0, to = min(from + each, n_all);
                 if (lane < 2) {
                     FwdTile tl = {};
                     tl.tokens = tokens;
@@ -285,18 +291,30 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         const int2 np = has_pre ? blocks_meeting(a.pre_lo, z.pre_hi, pl, 0) : make_int2(0, 0);
                         const int2 no = blocks_meeting(a.own_lo, last + 1, ol, n_pre);
                         const int2 wp = blocks_inside(z.pre_lo, a.pre_hi, pl, 0), wo = blocks_inside(z.own_lo, first + 1, ol, n_pre);
-                        tl.need = make_int4(np.x, np.y, no.x, no.y);
-                        tl.whole = make_int4(wp.x, min(wp.y, n_pre), wo.x, wo.y);
+                        if constexpr (SPLIT) {
+                            auto cut = [&](int2 r) {
+                                r = make_int2(max(r.x, from) - from, min(r.y, to) - from);
+                                return r.x < r.y ? r : make_int2(0, 0);
+                            };
+                            const int2 cp = cut(np), co = cut(no), whole_p = cut(make_int2(wp.x, min(wp.y, n_pre))), whole_o = cut(wo);
+                            // where there are no own blocks the prompt's take their place: a tile's last block is the one before need.w
+                            tl.need = co.y > co.x ? make_int4(cp.x, cp.y, co.x, co.y) : make_int4(0, 0, cp.x, cp.y);
+                            tl.whole = make_int4(whole_p.x, whole_p.y, whole_o.x, whole_o.y);
+                        } else {
+                            tl.need = make_int4(np.x, np.y, no.x, no.y);
+                            tl.whole = make_int4(wp.x, min(wp.y, n_pre), wo.x, wo.y);
+                        }
                     }
                     it.tile[lane] = tl;
                 }
                 if (lane == 0) {
                     it.t0 = t0;
-                    it.g = (int)(idx % (uint32_t)p.sh.Hkv);
-                    it.pre0 = pl;
-                    it.n_pre = n_pre;
-                    it.own0 = ol;
-                    it.n = n_pre + n_own;
+                    it.g = (int)(head_item % (uint32_t)p.sh.Hkv);
+                    it.split = split;
+                    it.n_pre = SPLIT ? max(min(n_pre, to) - from, 0) : n_pre;
+                    it.pre0 = pl + from * FWD_BLOCK;
+                    it.own0 = SPLIT ? ol + max(from - n_pre, 0) * FWD_BLOCK : ol;
+                    it.n = to - from;
                 }
             }
             if (lane == 0) it.valid = valid;
@@ -335,6 +353,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     __syncwarp();
                 }
             }
+            // a part without blocks: every item has its queries loaded, the issuers wait for them and hand them back
+            if (SPLIT && ok && blocks == 0) ok = load_q(0) && load_q(1);
         }
         if (!ok) {                           // let the copies in flight land before the block's shared memory goes away
             for (uint32_t i = 1; i <= C::STAGES && i <= pos; ++i)
@@ -731,6 +751,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const int h = it.g * ratio + head;
                 const float inv = 1.f / l;
                 __nv_bfloat16* out = p.o + (int64_t)t * p.o_stride + (int64_t)h * p.sh.D;
+                const int64_t part_row = ((int64_t)it.split * p.sh.T_max + t) * p.sh.Hq + h;
 #pragma unroll 1
                 for (int c = 0; c < DP / 32; ++c) {
                     uint32_t v[32];
@@ -738,22 +759,31 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     tcgen05_ld_32x32_issue(o_at + c * 32, v);
                     tcgen05_ld_wait(v);
                     if (live) {
+                        if constexpr (SPLIT) {
 #pragma unroll
-                        for (int j = 0; j < 32; j += 8)
-                            if (c * 32 + j < p.sh.D) {
-                                uint4 w;
-                                w.x = pack_bf16(__uint_as_float(v[j]) * inv, __uint_as_float(v[j + 1]) * inv);
-                                w.y = pack_bf16(__uint_as_float(v[j + 2]) * inv, __uint_as_float(v[j + 3]) * inv);
-                                w.z = pack_bf16(__uint_as_float(v[j + 4]) * inv, __uint_as_float(v[j + 5]) * inv);
-                                w.w = pack_bf16(__uint_as_float(v[j + 6]) * inv, __uint_as_float(v[j + 7]) * inv);
-                                *reinterpret_cast<uint4*>(out + c * 32 + j) = w;
-                            }
+                            for (int j = 0; j < 32; j += 4)
+                                if (c * 32 + j < p.sh.D)
+                                    *reinterpret_cast<uint4*>(p.part_o + part_row * p.sh.D + c * 32 + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; j += 8)
+                                if (c * 32 + j < p.sh.D) {
+                                    uint4 w;
+                                    w.x = pack_bf16(__uint_as_float(v[j]) * inv, __uint_as_float(v[j + 1]) * inv);
+                                    w.y = pack_bf16(__uint_as_float(v[j + 2]) * inv, __uint_as_float(v[j + 3]) * inv);
+                                    w.z = pack_bf16(__uint_as_float(v[j + 4]) * inv, __uint_as_float(v[j + 5]) * inv);
+                                    w.w = pack_bf16(__uint_as_float(v[j + 6]) * inv, __uint_as_float(v[j + 7]) * inv);
+                                    *reinterpret_cast<uint4*>(out + c * 32 + j) = w;
+                                }
+                        }
                     }
                 }
                 __syncwarp();
                 tcgen05_fence_before();
-                if (live) p.lse[(int64_t)t * p.sh.Hq + h] = (m + log2f(l)) * LN2;
+                if (!SPLIT && live) p.lse[(int64_t)t * p.sh.Hq + h] = (m + log2f(l)) * LN2;
             }
+            if (SPLIT && live)           // a part without a key of this tile: nothing for the join
+                p.part_ml[((int64_t)it.split * p.sh.T_max + t) * p.sh.Hq + it.g * ratio + head] = have_o ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
             __syncwarp();
             if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
             __syncwarp();
@@ -768,12 +798,44 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     }
 }
 
+// The parts of a row, in order: a warp per (token, query head), four dimensions a lane.
+__global__ void __launch_bounds__(256) attention_join_kernel(const FwdParams p) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int T = clamp_row(*pdl_acquire(p.sh.d_num + 1), 0, p.sh.T_max), lane = threadIdx.x & 31, d = lane * 4;
+    const int64_t rows = (int64_t)T * p.sh.Hq, step = (int64_t)p.sh.T_max * p.sh.Hq;
+    for (int64_t i = blockIdx.x * (int64_t)8 + (threadIdx.x >> 5); i < rows; i += (int64_t)gridDim.x * 8) {
+        const float2* ml = pdl_acquire(p.part_ml) + i;
+        const float* o = pdl_acquire(p.part_o) + i * p.sh.D + d;
+        float top = -INFINITY, l = 0.f;
+        for (int s = 0; s < p.splits; ++s) top = fmaxf(top, ml[s * step].x);
+        float4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = 0; s < p.splits; ++s) {
+            const float2 x = ml[s * step];
+            if (x.x == -INFINITY && x.y == 0.f) continue;            // no key; its sums were not written
+            const float by = x.x == -INFINITY ? 1.f : ex2_approx(x.x - top);       // a NaN without a reference stays one
+            l += by * x.y;
+            if (d < p.sh.D) {
+                const float4 v = *reinterpret_cast<const float4*>(o + s * step * p.sh.D);
+                sum.x += by * v.x; sum.y += by * v.y; sum.z += by * v.z; sum.w += by * v.w;
+            }
+        }
+        const float inv = 1.f / l;
+        const int64_t t = i / p.sh.Hq;
+        if (d < p.sh.D)
+            *reinterpret_cast<uint2*>(p.o + t * p.o_stride + (i - t * p.sh.Hq) * p.sh.D + d) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
+        if (lane == 0) p.lse[i] = (top + log2f(l)) * LN2;
+    }
+}
+
 template <int DP>
 int launch_attention(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWorkspace& w, cudaStream_t s) {
     using C = FwdConf<DP>;
     bool& set = ctx->attention_smem_set[DP == 128];
     if (!set) {
-        ARROL_CUDA_OK(cudaFuncSetAttribute(attention_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+        ARROL_CUDA_OK(cudaFuncSetAttribute(attention_kernel<DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+        ARROL_CUDA_OK(cudaFuncSetAttribute(attention_kernel<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
         set = true;
     }
     FwdParams p = {};
@@ -793,10 +855,19 @@ int launch_attention(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWo
         if (make_map_heads(ctx, &pk, a->prompt_k, a->prompt_rows, a->Hkv, a->D, a->prompt_k_stride, 1, FWD_BLOCK) != ARROL_OK) return ARROL_ERR_CUDA;
         if (make_map_heads(ctx, &pv, a->prompt_v, a->prompt_rows, a->Hkv, a->D, a->prompt_v_stride, 1, FWD_BLOCK) != ARROL_OK) return ARROL_ERR_CUDA;
     }
-    int64_t items = (a->T_max + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens) * a->Hkv;
+    // A form of its own: with the parts' arithmetic in one form for both, heads of 128 spilled 56 bytes of registers a thread instead of 32.
+    p.splits = attn_key_splits(ctx->sm_count, a->T_max, a->prompt_rows, a->P, a->S_max, a->Hq, a->Hkv);
+    p.part_o = w.part_o;
+    p.part_ml = w.part_ml;
+    int64_t items = (a->T_max + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens) * a->Hkv * p.splits;
     const unsigned grid = (unsigned)(items < ctx->sm_count ? items : ctx->sm_count);
-    ARROL_CUDA_OK(arrol_launch_pdl(attention_kernel<DP>, dim3(grid), dim3(FWD_THREADS), C::SMEM, s, q, k, v, pk, pv, p));
+    ARROL_CUDA_OK(arrol_launch_pdl(p.splits > 1 ? attention_kernel<DP, true> : attention_kernel<DP, false>, dim3(grid), dim3(FWD_THREADS), C::SMEM, s, q, k, v, pk, pv, p));
     ctx->launches += 1;
+    if (p.splits > 1) {
+        const int64_t blocks = (a->T_max * a->Hq + 7) / 8;
+        ARROL_CUDA_OK(arrol_launch_pdl(attention_join_kernel, dim3((unsigned)(blocks < 8 * ctx->sm_count ? blocks : 8 * ctx->sm_count)), dim3(256), 0, s, p));
+        ctx->launches += 1;
+    }
     return ARROL_OK;
 }
 

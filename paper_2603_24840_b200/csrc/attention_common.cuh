@@ -18,6 +18,8 @@ struct AttnWorkspace {
     int2* prompt_range;
     float2* stats;                // per packed token and query head: lse log2(e), d_o . o
     float* parts;                 // partial sums of the prompts' gradients
+    float* part_o;                // of o, where an item's keys are split, with
+    float2* part_ml;              // their references and sums
     size_t bytes;
 };
 
@@ -54,6 +56,19 @@ inline int attn_prompt_splits(int sm_count, int64_t T_max, int64_t prompt_rows, 
     return (int)(n < 1 ? 1 : n > 16 ? 16 : n);
 }
 
+// Parts of an item's keys in the forward: as many as give every SM an item, of about four blocks of 128 keys at least (what the arrays' sizes say of a
+// prompt and a sequence on average; the lengths are on the device, and a part may turn out to have none).  Few rows over long keys are bound by one
+// block's walk over them otherwise: 64 tokens over a prompt of 6,000, 4 heads of 128 on one 100 -> 29 us, two prompts of 3,000 with 4 sequences of 30
+// 98 -> 37, one sequence of 4,096 with 4 heads of 64 53 -> 49.  Where half of the SMs have an item already the walk is left whole.
+inline int attn_key_splits(int sm_count, int64_t T_max, int64_t prompt_rows, int P, int S_max, int Hq, int Hkv) {
+    const int64_t tokens = 2 * (128 / (Hq / Hkv)), items = (T_max + tokens - 1) / tokens * Hkv;
+    if (items == 0 || items * 2 > sm_count) return 1;
+    const int64_t blocks = (prompt_rows / (P > 0 ? P : 1) + T_max / (S_max > 0 ? S_max : 1) / 2) / 128;
+    int64_t n = sm_count / items;
+    if (n > blocks / 4) n = blocks / 4;
+    return (int)(n < 1 ? 1 : n > 32 ? 32 : n);
+}
+
 inline AttnWorkspace attn_workspace(void* base, int sm_count, int64_t T_max, int64_t prompt_rows, int Hq, int Hkv, int D, bool backward) {
     AttnWorkspace w = {};
     uint8_t* p = static_cast<uint8_t*>(base);
@@ -61,6 +76,11 @@ inline AttnWorkspace attn_workspace(void* base, int sm_count, int64_t T_max, int
     auto take = [&](size_t n) { uint8_t* q = p + at; at += attn_round(n); return q; };
     w.counters = reinterpret_cast<uint32_t*>(take(256));
     w.bounds = reinterpret_cast<TokenBounds*>(take((size_t)T_max * sizeof(TokenBounds)));
+    const int key_splits = attn_key_splits(sm_count, T_max, prompt_rows, 1, 1, Hq, Hkv);       // one prompt, one sequence: the most
+    if (key_splits > 1) {
+        w.part_ml = reinterpret_cast<float2*>(take((size_t)key_splits * T_max * Hq * sizeof(float2)));
+        w.part_o = reinterpret_cast<float*>(take((size_t)key_splits * T_max * Hq * D * sizeof(float)));
+    }
     if (backward) {
         w.prompt_range = reinterpret_cast<int2*>(take((size_t)prompt_rows * sizeof(int2)));
         w.stats = reinterpret_cast<float2*>(take((size_t)T_max * Hq * sizeof(float2)));

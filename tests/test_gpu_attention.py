@@ -362,6 +362,85 @@ def test_a_prompt_whose_tokens_are_split_into_parts(ctx):
     assert torch.equal(out["dprompt_k"], again["dprompt_k"]) and torch.equal(out["dprompt_v"], again["dprompt_v"])
 
 
+# Few query rows and many keys: the keys are split over blocks and joined.  Parts without a key (their number comes from the arrays' sizes, the lengths
+# from the device), parts of the prompt alone and of own keys alone, and parts that only one of a pair of tiles needs.
+SPLIT = [
+    # lens, prompts, index, G, Hq, Hkv, D
+    ([64], [6000], [0], 1, 4, 1, 128),
+    ([1], [5000], [0], 1, 2, 1, 64),
+    ([30, 25, 31, 28], [3000, 2900], [0, 1, 2, 3], 2, 8, 2, 64),
+    ([100, 3], [4500, 1], [0, 1], 1, 4, 2, 128),
+    ([3, 100], [1, 4500], [0, 1], 1, 4, 2, 64),
+    ([2, 200], [0, 5000], [0, 1], 1, 7, 1, 96),
+    ([3000], None, None, 1, 1, 1, 128),
+    ([3001], None, None, 1, 2, 1, 64),
+    ([2500, 900], [1500, 10], [0, 1], 1, 2, 1, 72),
+    ([40] * 6, [700] * 6, [0, 1, 2, 3, 4, 5], 1, 4, 4, 8),
+]
+
+
+@pytest.mark.parametrize("lens,prompts,index,G,Hq,Hkv,D", SPLIT)
+def test_few_rows_whose_keys_are_split(ctx, lens, prompts, index, G, Hq, Hkv, D):
+    p = Problem(lens, prompts, index, G, Hq, Hkv, D, seed=len(lens) + D, spare=5, fill=math.nan)
+    out = p.run(ctx)
+    p.check(out)
+    again = p.run(ctx)
+    assert all(torch.equal(out[n][:1], again[n][:1]) for n in out) and torch.equal(out["o"][:p.T], again["o"][:p.T])
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 4, 1), (128, 4, 2), (128, 7, 1)])
+@pytest.mark.parametrize("at", [0, 127, 128, 1500, 2559])
+def test_not_a_number_where_the_keys_are_split(ctx, D, Hq, Hkv, at):
+    """One key or value of a shared prompt: every row of its sequences has it, and no row of the others."""
+    make = lambda: Problem([60, 70, 50], [2560, 900], [0, 1, 3], 2, Hq, Hkv, D, seed=21)  # noqa: E731
+    good = make().run(ctx, backward=False)
+    for where, value in (("pv", math.nan), ("pv", math.inf), ("pk", math.nan)):
+        p = make()
+        getattr(p, where)[at, 0, D // 2] = value
+        out = p.run(ctx, backward=False)
+        assert torch.equal(out["o"][130:], good["o"][130:]) and torch.equal(out["lse"][130:], good["lse"][130:])
+        assert not torch.isfinite(out["o"][:130, :Hq // Hkv, D // 2]).any(), where
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_split_keys_captured_and_replayed_with_other_lengths(ctx, D):
+    """The number of parts is the launch's; a replay with short prompts leaves most of them without a key, one with none and no rows all of them."""
+    p = Problem([64, 40], [3500, 2000], [0, 1], 1, 4, 2, D, seed=22, spare=20)
+    others = [Problem([1, 70], [3, 130], [0, 1], 1, 4, 2, D, seed=23, spare=5420), Problem([0, 0], [0, 0], [0, 1], 1, 4, 2, D, seed=24, spare=6000),
+              Problem([100, 2], [100, 5000], [0, 1], 1, 4, 2, D, seed=25, spare=450)]
+    out, ws = p.outputs(), p.workspace(ctx, False)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.forward(ctx, out, ws)
+    for q in [None] + others:
+        if q is not None:
+            for n in ("q", "k", "v", "pk", "pv", "d_cu", "d_num", "d_cup", "d_idx"):
+                getattr(p, n).copy_(getattr(q, n)[:getattr(p, n).shape[0]])
+            p.T, p.cu, p.index, p.cu_prompts, p.seqs = q.T, q.cu, q.index, q.cu_prompts, q.seqs
+        for t in out.values():
+            t.fill_(-7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert B.arrol_poll_status(ctx) == 0
+        if p.T:
+            p.check({"o": out["o"], "lse": out["lse"]}, backward=False)
+        else:
+            assert (out["o"].float() == -7).all() and (out["lse"] == -7).all()
+
+
+def test_large_scores_where_the_keys_are_split(ctx):
+    """Parts whose maxima lie hundreds apart."""
+    p = Problem([50], [4000], [0], 1, 4, 1, 64, seed=26, q_scale=60.0)
+    p.pk *= torch.linspace(0, 1, 4000, device="cuda").view(-1, 1, 1).to(BF)
+    out = p.run(ctx, backward=False)
+    res, tol = p.reference(False)
+    # as above: sums of 64 products in fp32, |z| 2^-20
+    extra = (p.q.float().norm(dim=-1).max() * max(p.k.float().norm(dim=-1).max(), p.pk.float().norm(dim=-1).max()) * p.scale).item() * 2.0 ** -20
+    spread = max(p.v.abs().max(), p.pv.abs().max()).double()
+    assert ((out["o"].double() - res["o"]).abs() <= tol["o"] + 2 * extra * spread).all()
+    assert ((out["lse"].double() - res["lse"]).abs() <= tol["lse"] + extra).all()
+
+
 def test_gradients_agree_with_differences(ctx):
     """The loss changes by gradient times step: coarse, as q, k, v are bf16, but of the kernel's own forward."""
     p = Problem([90, 60], [40], [0, 1], 2, 4, 2, 64, seed=17)
