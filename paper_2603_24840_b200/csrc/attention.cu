@@ -5,10 +5,12 @@
 // a thread takes a row of it, P = exp(S - m) goes back as bf16 (the one rounding beside o's; l is summed before it), O += P V.  m is a reference
 // that the running maximum may be 2^8 ahead of: sums and products carry the same factor 2^-m, so a row's O is scaled again only when
 // that is passed.  4 D flops a pair against one exponential: with 128 dimensions the tensor cores (512 cycles each for S and P V of a tile and
-// block) and the exponentials (1,024 cycles a tile and block at 16 a cycle) are level, with 64 the exponentials bound it.
+// block) and the exponentials (1,024 cycles a tile and block at 16 a cycle) are level, with 64 the exponentials are the longer.  Neither unit is full: with
+// 128 both are busy about half of the cycles, with 64 0.53 and 0.28; the rest is the way between them.
 // One launch finds every token's range of keys, one computes: 148 blocks that take (256 query rows, key head) items from a counter.
 // Measured: 8,192 tokens, 32 heads of 128 on 8 470 to 500 us (1.10 to 1.17 PFLOP/s, 0.66 to 0.70 of the measured burst rate, tensor pipe busy 0.55
-// of the cycles); with heads of 64 394 to 419 us; 48 survivors of 40 to 333 tokens over 16,000 prompt tokens, 28 heads on 4 395 us (0.92 PFLOP/s).
+// of the cycles); with heads of 64 370 to 419 us; 48 survivors of 40 to 333 tokens over 16,000 prompt tokens, 28 heads on 4 395 to 440 us (0.82 to
+// 0.92 PFLOP/s).  Where few rows leave most blocks without an item, an item's keys are split and a third launch joins the parts (attn_key_splits).
 #include "attention_common.cuh"
 
 namespace {
