@@ -333,8 +333,9 @@ int arrol_lm_head_backward(arrol_ctx* ctx, const void* hidden, const void* W_voc
  * Row numbers out of order or outside (cu_seqlens, cu_prompts, survivor_idx) are not followed; ARROL_DEV_BAD_INDEX is recorded and the
  * outputs are undefined.
  * workspace: arrol_attention_workspace(...) bytes, 256-byte aligned; `backward` != 0 for arrol_attention_backward (a larger one that serves
- * both).  Contents need not be initialised or kept.  The calls use nothing of the context's buffers: they may be in flight on several
- * streams, each with a workspace and outputs of its own, and may be captured. */
+ * both); one for the largest T_max and prompt_rows serves smaller calls with the same heads.  Contents need not be initialised or kept.  The
+ * calls use nothing of the context's buffers: they may be in flight on several streams, each with a workspace and outputs of its own, and may
+ * be captured. */
 typedef struct arrol_attention_args {
     const void *q, *k, *v;
     int64_t q_stride, k_stride, v_stride;

@@ -56,6 +56,16 @@ inline int attn_prompt_splits(int sm_count, int64_t T_max, int64_t prompt_rows, 
     return (int)(n < 1 ? 1 : n > 16 ? 16 : n);
 }
 
+// The most tiles of partial sums that a call of up to so many tokens and prompt rows has, so that a workspace for the largest call serves the smaller
+// ones, which may have more parts.  With n > 1 parts n <= ceil(4 SMs / tiles), so there are fewer than 4 SMs tiles and less than 4 SMs + tiles parts.
+inline int64_t attn_prompt_parts(int sm_count, int64_t T_max, int64_t prompt_rows, int Hq, int Hkv) {
+    const int64_t blocks = T_max * (Hq / Hkv) / 64, tiles = (prompt_rows + 127) / 128 * Hkv, all = 4 * (int64_t)sm_count;
+    const int64_t n = (blocks + 47) / 48 > blocks / 4 ? (blocks + 47) / 48 : blocks / 4;
+    if (n <= 1) return 0;
+    const int64_t few = (n < 16 ? n : 16) * tiles, many = all + (tiles < all ? tiles : all);
+    return few < many ? few : many;
+}
+
 // Parts of an item's keys in the forward: as many as give every SM an item, of about four blocks of 128 keys at least (what the arrays' sizes say of a
 // prompt and a sequence on average; the lengths are on the device, and a part may turn out to have none).  Few rows over long keys are bound by one
 // block's walk over them otherwise: 64 tokens over a prompt of 6,000, 4 heads of 128 on one 100 -> 29 us, two prompts of 3,000 with 4 sequences of 30
@@ -69,6 +79,14 @@ inline int attn_key_splits(int sm_count, int64_t T_max, int64_t prompt_rows, int
     return (int)(n < 1 ? 1 : n > 32 ? 32 : n);
 }
 
+// The most rows (part, token) of partial sums, likewise: n parts of `items` give n items <= SMs.
+inline int64_t attn_key_parts(int sm_count, int64_t T_max, int64_t prompt_rows, int Hq, int Hkv) {
+    const int64_t n = (prompt_rows + T_max / 2) / 512, most = sm_count / Hkv * (int64_t)(2 * (128 / (Hq / Hkv)));
+    if (n <= 1 || sm_count / Hkv < 2) return 0;
+    const int64_t few = (n < 32 ? n : 32) * T_max;
+    return few < most ? few : most;
+}
+
 inline AttnWorkspace attn_workspace(void* base, int sm_count, int64_t T_max, int64_t prompt_rows, int Hq, int Hkv, int D, bool backward) {
     AttnWorkspace w = {};
     uint8_t* p = static_cast<uint8_t*>(base);
@@ -76,17 +94,14 @@ inline AttnWorkspace attn_workspace(void* base, int sm_count, int64_t T_max, int
     auto take = [&](size_t n) { uint8_t* q = p + at; at += attn_round(n); return q; };
     w.counters = reinterpret_cast<uint32_t*>(take(256));
     w.bounds = reinterpret_cast<TokenBounds*>(take((size_t)T_max * sizeof(TokenBounds)));
-    const int key_splits = attn_key_splits(sm_count, T_max, prompt_rows, 1, 1, Hq, Hkv);       // one prompt, one sequence: the most
-    if (key_splits > 1) {
-        w.part_ml = reinterpret_cast<float2*>(take((size_t)key_splits * T_max * Hq * sizeof(float2)));
-        w.part_o = reinterpret_cast<float*>(take((size_t)key_splits * T_max * Hq * D * sizeof(float)));
-    }
+    const size_t key_rows = (size_t)attn_key_parts(sm_count, T_max, prompt_rows, Hq, Hkv) * Hq;
+    w.part_ml = reinterpret_cast<float2*>(take(key_rows * sizeof(float2)));
+    w.part_o = reinterpret_cast<float*>(take(key_rows * D * sizeof(float)));
     if (backward) {
         w.prompt_range = reinterpret_cast<int2*>(take((size_t)prompt_rows * sizeof(int2)));
         w.stats = reinterpret_cast<float2*>(take((size_t)T_max * Hq * sizeof(float2)));
-        const int splits = attn_prompt_splits(sm_count, T_max, prompt_rows, 1, Hq, Hkv);      // one prompt has the most
         const size_t tile = (size_t)128 * (D <= 64 ? 64 : 128) * 2 * sizeof(float);
-        if (splits > 1) w.parts = reinterpret_cast<float*>(take((size_t)splits * ((prompt_rows + 127) / 128) * Hkv * tile));
+        w.parts = reinterpret_cast<float*>(take((size_t)attn_prompt_parts(sm_count, T_max, prompt_rows, Hq, Hkv) * tile));
     }
     w.bytes = at;
     return w;

@@ -441,6 +441,26 @@ def test_large_scores_where_the_keys_are_split(ctx):
     assert ((out["lse"].double() - res["lse"]).abs() <= tol["lse"] + extra).all()
 
 
+def test_a_workspace_for_the_largest_call_serves_the_smaller_ones(ctx):
+    """Fewer tokens may mean more parts, but never more bytes."""
+    for Hq, Hkv, D in ((4, 1, 128), (8, 2, 64), (32, 8, 128), (7, 1, 96), (200, 100, 8)):
+        for backward in (False, True):
+            ask = lambda T, rows: A.arrol_attention_workspace(ctx, 4, T, rows, Hq, Hkv, D, backward)  # noqa: E731
+            tokens, prompts = (1, 64, 65, 300, 1000, 2500, 8192, 40000, 300000), (0, 1, 500, 2600, 6000, 30000, 200000)
+            for rows in prompts:
+                sizes = [ask(T, rows) for T in tokens]
+                assert sizes == sorted(sizes), (Hq, Hkv, D, backward, rows, sizes)
+            for T in tokens:
+                sizes = [ask(T, rows) for rows in prompts]
+                assert sizes == sorted(sizes), (Hq, Hkv, D, backward, T, sizes)
+    p = Problem([64], [6000], [0], 1, 4, 1, 128, seed=27)
+    ws, out = torch.full((A.arrol_attention_workspace(ctx, 1, 8192, 6000, 4, 1, 128, True),), 0xAB, dtype=torch.uint8, device="cuda"), p.outputs()
+    p.forward(ctx, out, ws)
+    p.backward(ctx, out, ws)
+    torch.cuda.synchronize()
+    p.check(out)
+
+
 def test_gradients_agree_with_differences(ctx):
     """The loss changes by gradient times step: coarse, as q, k, v are bf16, but of the kernel's own forward."""
     p = Problem([90, 60], [40], [0, 1], 2, 4, 2, 64, seed=17)
