@@ -80,8 +80,10 @@ def _ints(name: str, t: Optional[torch.Tensor], dtype, count: int = 0):
 
 def _prompts(prompt_k, prompt_v, cu_prompts, Hkv: int, D: int):
     """(rows, prompts, k, v, k stride, v stride, cu)"""
-    if prompt_k is None:
+    if prompt_k is None and prompt_v is None:
         return 0, 0, None, None, 0, 0, None
+    if prompt_k is None or prompt_v is None or cu_prompts is None:
+        raise ValueError("prompts are given by prompt_k, prompt_v and cu_prompts")
     rows = prompt_k.shape[0]
     k, k_stride = _rows(prompt_k, rows, Hkv, D)
     v, v_stride = _rows(prompt_v, rows, Hkv, D)

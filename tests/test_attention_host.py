@@ -166,3 +166,18 @@ def test_binding_refuses_other_layouts():
         A._ints("lengths", torch.zeros(3, dtype=torch.int32), torch.int32, 4)
     with pytest.raises(ValueError):
         A._ints("lengths", torch.zeros(4, dtype=torch.int64), torch.int32, 4)
+
+
+def test_binding_refuses_prompts_in_part():
+    class Ctx:
+        handle = 0
+
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    q, k, lse = bf(4, 4, 64), bf(4, 2, 64), torch.zeros(4, 4)
+    cu, num, ws = torch.tensor([0, 4]), torch.tensor([1, 4]), torch.zeros(1 << 12, dtype=torch.uint8)
+    pk, cup = bf(6, 2, 64), torch.tensor([0, 6])
+    for prompts in (dict(prompt_k=pk, prompt_v=pk), dict(prompt_k=pk, cu_prompts=cup), dict(prompt_v=pk, cu_prompts=cup), dict(prompt_v=pk)):
+        with pytest.raises(ValueError):
+            A.arrol_attention(Ctx, q, k, k, cu, num, q, lse, ws, **prompts)
+        with pytest.raises(ValueError):
+            A.arrol_attention_decode(Ctx, q, k, k, torch.zeros(4, dtype=torch.int64), torch.zeros(4, dtype=torch.int32), q, lse, ws, G=4, **prompts)
