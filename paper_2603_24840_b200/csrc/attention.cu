@@ -700,9 +700,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     __syncwarp();
                 };
                 if (masked) {
-                    // the values have been looked over before P V may begin
-                    const uint32_t pos = pos0 + 2 * b + 1, st = pos % C::STAGES;
-                    if (!mbar_wait_warp(&sm.scanned[st], (pos / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                    // The values have been looked over before P V may begin.  The stage is waited for first: S needs the keys alone, and while the values that
+                    // had the stage before are still being looked over, their phase's parity is what the second wait would take for this one's.
+                    const uint32_t pos = pos0 + 2 * b + 1, st = pos % C::STAGES, parity = (pos / C::STAGES) & 1u;
+                    if (!mbar_wait_warp(&sm.full[st], parity, abort_flag) || !mbar_wait_warp(&sm.scanned[st], parity, abort_flag)) { ok = false; break; }
                     const uint4 bad = *reinterpret_cast<const uint4*>(sm.bad_keys[st]);
                     if ((bad.x & on[0]) | (bad.y & on[1]) | (bad.z & on[2]) | (bad.w & on[3])) l = NAN;
                     __syncwarp();

@@ -481,3 +481,31 @@ def test_gradients_agree_with_differences(ctx):
         # what the roundings of o (2^-8 of each, of either sign) and of the gradient leave of a difference of two sums
         noise = 2 * 2.0 ** -8 * ((out["o"].double() * p.d_o.double()) ** 2).sum().sqrt().item() * 2
         assert abs(found - expected) <= noise + 0.02 * abs(expected), (name, found, expected, noise)
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,first,rows", [(64, 32, 8, 8, 75), (64, 32, 8, 8, 80), (64, 32, 8, 8, 64), (64, 32, 8, 16, 33), (40, 28, 4, 6, 90), (128, 32, 8, 8, 40)])
+def test_many_values_that_are_not_finite_beside_another_prompt(ctx, D, Hq, Hkv, first, rows):
+    """The first tile of an item holds short sequences whose prompts, several blocks in all, are full of NaN; the second tile's prompt begins behind them,
+    inside a block, and so keeps its values from a stage that those blocks had before it.  Its rows are those of a clean call, bit for bit."""
+    tile = 128 // (Hq // Hkv)
+    lens, prompts, clean = [], [], []
+    for _ in range(3):                          # three items
+        each = [tile // first] * first
+        each[-1] += tile - sum(each)
+        lens += each + [tile]
+        prompts += [rows] * first + [100]
+        clean += [False] * first + [True]
+    make = lambda: Problem(lens, prompts, list(range(len(lens))), 1, Hq, Hkv, D, seed=31)  # noqa: E731
+    good, p = make().run(ctx), make()
+    for i, c in enumerate(clean):
+        if not c:
+            p.pv[p.cu_prompts[i]:p.cu_prompts[i + 1], :, ::3] = math.nan
+    keep = torch.tensor([c for c, n in zip(clean, lens) for _ in range(n)], device="cuda")
+    kept_prompts = torch.tensor([c for c, n in zip(clean, prompts) for _ in range(n)], device="cuda")
+    for _ in range(20):
+        out = p.run(ctx)
+        for name in ("o", "lse", "dq", "dk", "dv"):
+            assert torch.equal(out[name][keep], good[name][keep]), name
+        for name in ("dprompt_k", "dprompt_v"):
+            assert torch.equal(out[name][kept_prompts], good[name][kept_prompts]), name
+        assert not torch.isfinite(out["o"][~keep][..., 0]).any()

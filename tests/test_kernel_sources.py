@@ -62,3 +62,18 @@ def test_kernels_wait_for_their_asynchronous_copies_on_every_way_out(path):
 def test_the_rule_finds_the_kernels():
     found = {name for p in SOURCES for name, _ in _kernels(_code(p))}
     assert {"combine_splits_kernel", "token_logprob_kernel", "prune_fused_kernel", "column_sum_kernel"} <= found
+
+
+@pytest.mark.parametrize("name", ["attention.cu", "attention_backward.cu"])
+def test_a_scanned_stage_is_waited_for_behind_its_filling(name):
+    """A wait for a phase knows only its parity, so a phase that is two ahead passes for one that is over.  A stage is filled again only once the scanner
+    has handed it back, so whoever waits for the scanner waits for the filling first, whatever else it has waited for."""
+    code = _code(os.path.join(CSRC, name))
+    roles = re.split(r"\n    (?:\} else )?if \([^\n]*warp [=>]=? ?\d", code)
+    waits = 0
+    for role in roles:
+        for m in re.finditer(r"mbar_wait\w*\(&sm\.scanned\[(\w+)\]", role):
+            waits += 1
+            loop = role.rindex(" while (" if name == "attention.cu" else " for (int b = 0;", 0, m.start())
+            assert re.search(r"mbar_wait\w*\(&sm\.full\[%s\]" % m.group(1), role[loop:m.start()]), name
+    assert waits == 1
