@@ -630,7 +630,7 @@ __global__ void __launch_bounds__(256) decode_merge_kernel(const DecodeParams p)
             sum.x += by * v[k].x; sum.y += by * v[k].y; sum.z += by * v[k].z; sum.w += by * v[k].w;
         }
     }
-    const bool none = total == 0.f;
+    const bool none = rec.count == 0;        // no key; a sum of nothing over keys that are there (scores of minus infinity) gives NaN, as the formula does
     const float inv = none ? 0.f : 1.f / total;
     if (d < a.D)
         *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + i * a.o_stride + (int64_t)h * a.D + d) =

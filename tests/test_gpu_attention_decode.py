@@ -225,3 +225,46 @@ def test_large_scores(ctx):
     extra = zmax * 2.0 ** -20          # the exponent's error: 64 products summed in fp32
     assert ((o.double() - ro).abs() <= tol + 2 * extra * p.v.abs().max().double()).all()
     assert ((lse.double() - rl).abs() <= 2e-5 * (1 + rl.abs()) + extra).all()
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 4, 2), (128, 8, 1), (72, 3, 3)])
+def test_keys_whose_scores_are_minus_infinity_are_keys(ctx, D, Hq, Hkv):
+    """A softmax over scores of minus infinity alone is not a number; no key at all gives zeros.  One key, several chunks of them, a prompt's."""
+    make = lambda: Problem([1, 400, 0, 60, 0], [0, 90, 0, 0, 130], 1, Hq, Hkv, D, seed=14)  # noqa: E731
+    good, p = make().run(ctx), make()
+    p.q[:, :, 0] = 1.0
+    for i in (0, 1):
+        p.k[p.off[i]:p.off[i] + p.lengths[i], :, 0] = -math.inf
+    for i in (1, 4):
+        p.pk[p.cup[i]:p.cup[i + 1], :, 0] = -math.inf
+    o, lse = p.run(ctx)
+    for i in (0, 1, 4):
+        assert not torch.isfinite(o[i]).any() and not torch.isfinite(lse[i]).any(), i
+    assert (o[2] == 0).all() and (lse[2] == -math.inf).all()
+    assert torch.isfinite(o[3]).all() and torch.isfinite(lse[3]).all()
+    # beside a key with a score they weigh nothing
+    p = make()
+    p.q[:, :, 0] = 1.0
+    clean = p.run(ctx)
+    p.k[p.off[1]:p.off[1] + 300, :, 0] = -math.inf
+    p.pk[p.cup[4]:p.cup[5] - 1, :, 0] = -math.inf
+    o, lse = p.run(ctx)
+    assert torch.isfinite(o).all() and torch.isfinite(lse[[0, 1, 3, 4]]).all()
+    assert all(torch.equal(x[[0, 2, 3]], y[[0, 2, 3]]) for x, y in zip(clean, (o, lse)))
+    assert torch.equal(o[4], p.pv[p.cup[5] - 1].repeat_interleave(Hq // Hkv, 0))
+    assert good[0].shape == o.shape
+
+
+@pytest.mark.parametrize("where,value", [("pk", math.nan), ("pv", math.nan), ("pv", math.inf), ("pk", math.inf), ("pk", -math.inf), ("k", math.inf), ("k", -math.inf)])
+def test_not_a_number_in_a_prompt_or_a_key_reaches_its_rollouts_alone(ctx, where, value):
+    p = Problem([100, 150, 30, 64], [65, 40], 2, 4, 2, 64, seed=15)
+    p.q[:, :, 5] = 1.0
+    good = p.run(ctx)
+    at, reached = (70, [2, 3]) if where[0] == "p" else (p.off[1] + 149, [1])
+    getattr(p, where)[at, 0, 5] = value
+    bad = p.run(ctx)
+    others = [i for i in range(4) if i not in reached]
+    for x, y in zip(good, bad):
+        assert torch.equal(x[others], y[others]) and torch.equal(x[reached, 2:], y[reached, 2:])
+    if value != -math.inf:                     # a key of no weight is all that a score of minus infinity makes
+        assert not torch.isfinite(bad[0][reached, :2, 5]).any()
