@@ -80,7 +80,7 @@ def _ints(name: str, t: Optional[torch.Tensor], dtype, count: int = 0):
 
 def _prompts(prompt_k, prompt_v, cu_prompts, Hkv: int, D: int):
     """(rows, prompts, k, v, k stride, v stride, cu)"""
-    if prompt_k is None and prompt_v is None:
+    if prompt_k is None and prompt_v is None and cu_prompts is None:
         return 0, 0, None, None, 0, 0, None
     if prompt_k is None or prompt_v is None or cu_prompts is None:
         raise ValueError("prompts are given by prompt_k, prompt_v and cu_prompts")
@@ -132,7 +132,9 @@ def arrol_attention_backward(ctx: B.Context, q, k, v, cu_seqlens, d_num, o, lse,
     """Gradients (overwritten) of arrol_attention's o; o and lse are what that call wrote."""
     (T, Hq, D), Hkv, rows = q.shape, k.shape[1], 0 if prompt_k is None else prompt_k.shape[0]
     grads = _rows(d_o, T, Hq, D) + _rows(dq, T, Hq, D) + _rows(dk, T, Hkv, D) + _rows(dv, T, Hkv, D)
-    grads += (None, 0) * 2 if prompt_k is None else _rows(dprompt_k, rows, Hkv, D) + _rows(dprompt_v, rows, Hkv, D)
+    if prompt_k is None and (dprompt_k is not None or dprompt_v is not None):
+        raise ValueError("dprompt_k and dprompt_v are the gradients of prompt_k and prompt_v")
+    grads += _rows(dprompt_k, rows, Hkv, D) + _rows(dprompt_v, rows, Hkv, D)
     a = _packed(q, k, v, cu_seqlens, d_num, o, lse, workspace, scale, prompt_k, prompt_v, cu_prompts, survivor_idx, G, grads)
     B._check(_lib().arrol_attention_backward(ctx.handle, C.byref(a), B._stream(stream)), "arrol_attention_backward")
 

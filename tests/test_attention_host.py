@@ -181,3 +181,20 @@ def test_binding_refuses_prompts_in_part():
             A.arrol_attention(Ctx, q, k, k, cu, num, q, lse, ws, **prompts)
         with pytest.raises(ValueError):
             A.arrol_attention_decode(Ctx, q, k, k, torch.zeros(4, dtype=torch.int64), torch.zeros(4, dtype=torch.int32), q, lse, ws, G=4, **prompts)
+
+
+def test_binding_refuses_what_belongs_to_prompts_without_them():
+    class Ctx:
+        handle = 0
+
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    q, k, lse = bf(4, 4, 64), bf(4, 2, 64), torch.zeros(4, 4)
+    cu, num, ws = torch.tensor([0, 4]), torch.tensor([1, 4]), torch.zeros(1 << 12, dtype=torch.uint8)
+    pk, cup = bf(6, 2, 64), torch.tensor([0, 6])
+    with pytest.raises(ValueError):
+        A.arrol_attention(Ctx, q, k, k, cu, num, q, lse, ws, cu_prompts=cup)
+    with pytest.raises(ValueError):
+        A.arrol_attention_decode(Ctx, q, k, k, torch.zeros(4, dtype=torch.int64), torch.zeros(4, dtype=torch.int32), q, lse, ws, G=4, cu_prompts=cup)
+    for prompts in (dict(cu_prompts=cup), dict(dprompt_k=pk), dict(dprompt_v=pk), dict(dprompt_k=pk, dprompt_v=pk)):
+        with pytest.raises(ValueError):
+            A.arrol_attention_backward(Ctx, q, k, k, cu, num, q, lse, q, q, k, k, ws, **prompts)
