@@ -4,7 +4,8 @@
 // queries', 7 products of 2 D flops a pair where 5 would do with sums of dq in memory.  Those sums would be atomics, whose order would change the
 // result; this way each tile of gradients has one block that adds in a fixed order in tensor memory.
 //
-// One kernel, two uses.  128 rows stay (two operands a1, a2), 64 rows a block stream past (b1, b2):
+// One kernel, two sides: a block takes items of the keys' side until there are none, then of the queries' side, which needs nothing of the other.
+// 128 rows stay (two operands a1, a2), 64 rows a block stream past (b1, b2):
 //     x = a1 b1^T,  y = a2 b2^T  (128 x 64),  p = exp(scale x - lse),  ds = p (y - delta),
 //   keys' gradients (KEYS):  rows are keys, a1 = k, a2 = v; columns are query rows (tokens x heads of the group), b1 = q, b2 = d_o;
 //       dv += p b2,  dk += ds b1;  lse and delta belong to columns;
@@ -15,8 +16,9 @@
 // the o that was written.
 // Bounded by the tensor cores and by what feeds them: with 128 dimensions a block is 512 cycles of first products and 512 of second ones for the keys' side,
 // but 64 columns a product make the first ones wait for shared memory (96 KB at 128 a cycle), unless the rows that stay are in tensor memory.
-// Measured with 4,096 tokens, 32 heads of 128 on 8: keys' side 297 us (tensor pipe busy 0.53 of the cycles, its feeding 0.70), queries' side 195 us
-// (0.58, 0.62); forward and backward together 572 us, 0.84 PFLOP/s of the 14 D flops a pair that cannot be done without (18 are done).
+// Measured with 4,096 tokens, 32 heads of 128 on 8: the sides as launches of their own 297 us (keys; tensor pipe busy 0.53 of the cycles, its feeding 0.70)
+// and 195 us (queries; 0.58, 0.62); forward and backward together 571 us from a graph, 0.84 PFLOP/s of the 14 D flops a pair that cannot be done without (18
+// are done).
 #include "attention_common.cuh"
 
 namespace {
@@ -32,14 +34,18 @@ struct BwdParams {
     const float2* stats;                          // [T_max, Hq]: lse log2(e), delta
     const int64_t* cu_prompts;
     int P;
-    __nv_bfloat16 *out1, *out2;                   // dv and dk; dq in out2
-    int64_t out1_stride, out2_stride;
+    __nv_bfloat16 *dv, *dk, *dq;
+    int64_t dv_stride, dk_stride, dq_stride;
     __nv_bfloat16 *shared1, *shared2;             // dprompt_v, dprompt_k
     int64_t shared1_stride, shared2_stride;
     int splits;                                   // parts of the tokens that pass by a prompt's tile, each an item; with more than one their sums go to
     float *part1, *part2;                         // [splits][prompt tiles][Hkv][128][DP]
-    uint32_t* counter;
+    uint32_t* counter[2];                         // of the queries' items, the keys' items
     uint32_t* status;
+};
+
+struct BwdMaps {
+    CUtensorMap q_rows, do_rows, q_cols, do_cols, k_rows, v_rows, k_cols, v_cols, pk_rows, pv_rows, pk_cols, pv_cols;
 };
 
 struct BwdItem {
@@ -56,13 +62,17 @@ struct BwdConf {
     static constexpr int STAGES = DP == 128 ? 4 : 8;
     // The rows that stay are put into tensor memory where there is room (not for keys' gradients of 128 dimensions): read from shared memory, 128 of them
     // with every 64 columns, they make the first products wait for its bandwidth (96 KB at 128 a cycle against 512 cycles of products).
+    template <bool KEYS> static constexpr bool A_IN_TMEM = !(KEYS && DP == 128);
     static constexpr uint32_t A_AT = DP == 128 ? 0 : 64, A_STEP = DP == 128 ? 64 : 128;
     static constexpr size_t SMEM = 1024 + 2 * (size_t)ROWS_BYTES + STAGES * 2 * (size_t)COLS_BYTES;
 };
 
-struct BwdShared {
+struct BwdBarriers {
     uint64_t full[8], empty[8], scanned[8];                    // per stage
     uint64_t a_full, a_ready, a_empty, xy_full[2], ps_full[2], acc_full, acc_empty, item_full[BWD_SLOTS], item_empty[BWD_SLOTS], drain;
+};
+struct BwdShared {
+    BwdBarriers of[2];                            // of the queries' side, the keys' side: the last arrivals of one may come while the other begins
     alignas(16) float lse[8][BWD_BLOCK];          // negative, as delta; read four at a time
     alignas(16) float delta[8][BWD_BLOCK];
     uint32_t bad[8][2], bad_stats[8][2];          // per stage: rows of an edge block that are not finite, or whose statistics are not
@@ -84,55 +94,32 @@ __device__ __forceinline__ bool bwd_masked(const BwdItem& it, int b, int TOKQ) {
 }
 
 template <int DP, bool KEYS>
-__global__ void __launch_bounds__(BWD_THREADS, 1)
-attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_a2,
-                          const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2,
-                          const __grid_constant__ CUtensorMap map_p1, const __grid_constant__ CUtensorMap map_p2, const BwdParams p) {
-    // the prompts' keys and values (p1, p2) are rows of KEYS items, columns otherwise
+__device__ __forceinline__ void init_barriers(BwdBarriers& bar) {
     using C = BwdConf<DP>;
-    constexpr bool A_TMEM = !(KEYS && DP == 128);
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ BwdShared sm;
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    for (int i = 0; i < C::STAGES; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.empty[i], 2); mbar_init(&bar.scanned[i], 1); }
+    mbar_init(&bar.a_full, 1);
+    mbar_init(&bar.a_ready, 8);
+    mbar_init(&bar.a_empty, C::template A_IN_TMEM<KEYS> ? 8 : 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(&bar.xy_full[i], 1); mbar_init(&bar.ps_full[i], 4); }
+    mbar_init(&bar.acc_full, 1);
+    mbar_init(&bar.acc_empty, 8);
+    for (int i = 0; i < BWD_SLOTS; ++i) { mbar_init(&bar.item_full[i], 1); mbar_init(&bar.item_empty[i], 10); }
+    mbar_init(&bar.drain, 1);
+}
+
+// All items of one side that this block gets.  The prompts' keys and values (p1, p2) are rows of KEYS items, columns otherwise.
+template <int DP, bool KEYS>
+__device__ __forceinline__ void backward_side(const CUtensorMap& map_a1, const CUtensorMap& map_a2, const CUtensorMap& map_b1, const CUtensorMap& map_b2,
+                                              const CUtensorMap& map_p1, const CUtensorMap& map_p2, const BwdParams& p, BwdShared& sm, uint8_t* const smem,
+                                              const uint32_t tmem) {
+    using C = BwdConf<DP>;
+    constexpr bool A_TMEM = C::template A_IN_TMEM<KEYS>;
+    BwdBarriers& bar = sm.of[KEYS];
     uint8_t* const rows_a = smem;
     uint8_t* const ring = smem + 2 * C::ROWS_BYTES;
     volatile uint32_t* abort_flag = &sm.abort;
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int ratio = p.sh.ratio, TOK = 128 / ratio, TOKQ = BWD_BLOCK / ratio;
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 2); mbar_init(&sm.scanned[i], 1); }
-        mbar_init(&sm.a_full, 1);
-        mbar_init(&sm.a_ready, 8);
-        mbar_init(&sm.a_empty, A_TMEM ? 8 : 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&sm.xy_full[i], 1); mbar_init(&sm.ps_full[i], 4); }
-        mbar_init(&sm.acc_full, 1);
-        mbar_init(&sm.acc_empty, 8);
-        for (int i = 0; i < BWD_SLOTS; ++i) { mbar_init(&sm.item_full[i], 1); mbar_init(&sm.item_empty[i], 10); }
-        mbar_init(&sm.drain, 1);
-        sm.abort = 0u;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a1) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a2) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b1) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b2) : "memory");
-    }
-    if (KEYS && TOKQ * ratio < BWD_BLOCK) {       // rows behind the last whole token are never loaded: zeros, for the second products
-        for (uint32_t i = threadIdx.x * 16; i < C::STAGES * 2 * C::COLS_BYTES; i += BWD_THREADS * 16)
-            *reinterpret_cast<uint4*>(ring + i) = make_uint4(0, 0, 0, 0);
-        fence_proxy_async_smem();
-    }
-    if (warp == 1) {
-        tcgen05_alloc(&sm.tmem, 512);
-        tcgen05_relinquish();
-    }
-    tcgen05_fence_before();
-    __syncthreads();
-    tcgen05_fence_after();
-    const uint32_t tmem = uniform(sm.tmem);                // accumulators 1 and 2 at columns 0 and 128; x, y of buffer i at 256 + 128 i and + 64
-    // The queries' launch needs nothing of the keys' launch before it, only what that one has waited for, so it starts as soon as that one's blocks are all
-    // there and takes the SMs that they leave; it waits for them before it ends, so that what follows it has both.
-    if (KEYS) pdl_wait();
-    pdl_launch_dependents();
     const int T = clamp_row(*pdl_acquire(p.sh.d_num + 1), 0, p.sh.T_max);
     const int live_prompt = KEYS && p.P > 0 ? clamp_row(pdl_acquire(p.cu_prompts)[p.P], 0, p.sh.prompt_rows) : 0;
     const TokenBounds* bounds = pdl_acquire(p.sh.bounds);
@@ -149,9 +136,9 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % BWD_SLOTS, use = n / BWD_SLOTS;
-            if (!mbar_wait_warp(&sm.item_empty[slot], (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+            if (!mbar_wait_warp(&bar.item_empty[slot], (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
             uint32_t idx = 0;
-            if (lane == 0) idx = atomicAdd(p.counter, 1u);
+            if (lane == 0) idx = atomicAdd(p.counter[KEYS], 1u);
             idx = __shfl_sync(0xffffffffu, idx, 0);
             BwdItem it = {};
             it.valid = (int64_t)idx < items;
@@ -200,19 +187,19 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
             }
             if (lane == 0) sm.items[slot] = it;
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.item_full[slot]);
+            if (lane == 0) mbar_arrive(&bar.item_full[slot]);
             __syncwarp();
             if (!it.valid) break;
             if (it.n == 0) continue;              // a prompt without survivors: nothing is loaded
-            if (!mbar_wait_warp(&sm.a_empty, (a_loads & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+            if (!mbar_wait_warp(&bar.a_empty, (a_loads & 1u) ^ 1u, abort_flag)) { ok = false; break; }
             if (elect_one()) {
-                mbar_expect_tx(&sm.a_full, 2u * C::HALVES * (KEYS ? 128u : (uint32_t)(TOK * ratio)) * 128u);
+                mbar_expect_tx(&bar.a_full, 2u * C::HALVES * (KEYS ? 128u : (uint32_t)(TOK * ratio)) * 128u);
 #pragma unroll
                 for (int o = 0; o < 2; ++o) {
                     const CUtensorMap* m = KEYS && it.shared ? (o ? &map_p2 : &map_p1) : (o ? &map_a2 : &map_a1);
 #pragma unroll
                     for (int h = 0; h < C::HALVES; ++h)
-                        tma_load_3d(rows_a + o * C::ROWS_BYTES + h * ROWS_HALF_BYTES, m, h * 64, KEYS ? it.g : it.g * ratio, it.row0, &sm.a_full);
+                        tma_load_3d(rows_a + o * C::ROWS_BYTES + h * ROWS_HALF_BYTES, m, h * 64, KEYS ? it.g : it.g * ratio, it.row0, &bar.a_full);
                 }
             }
             __syncwarp();
@@ -234,7 +221,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
             }
             for (int b = 0; b < it.n; ++b, ++pos) {
                 const uint32_t st = pos % C::STAGES;
-                if (!mbar_wait_warp(&sm.empty[st], ((pos / C::STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                if (!mbar_wait_warp(&bar.empty[st], ((pos / C::STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
                 if (KEYS) {
                     const bool masked = bwd_masked<KEYS>(it, b, TOKQ);
 #pragma unroll
@@ -254,13 +241,13 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 if (elect_one()) {
                     const bool pre = !KEYS && b < it.n_pre;
                     const int row = bwd_start<KEYS>(it, b, TOKQ);
-                    mbar_expect_tx(&sm.full[st], 2u * C::HALVES * (KEYS ? (uint32_t)(TOKQ * ratio) : (uint32_t)BWD_BLOCK) * 128u);
+                    mbar_expect_tx(&bar.full[st], 2u * C::HALVES * (KEYS ? (uint32_t)(TOKQ * ratio) : (uint32_t)BWD_BLOCK) * 128u);
 #pragma unroll
                     for (int o = 0; o < 2; ++o) {
                         const CUtensorMap* m = pre ? (o ? &map_p2 : &map_p1) : (o ? &map_b2 : &map_b1);
 #pragma unroll
                         for (int h = 0; h < C::HALVES; ++h)
-                            tma_load_3d(ring + (st * 2 + o) * C::COLS_BYTES + h * COLS_HALF_BYTES, m, h * 64, KEYS ? it.g * ratio : it.g, row, &sm.full[st]);
+                            tma_load_3d(ring + (st * 2 + o) * C::COLS_BYTES + h * COLS_HALF_BYTES, m, h * 64, KEYS ? it.g * ratio : it.g, row, &bar.full[st]);
                     }
                 }
                 __syncwarp();
@@ -274,10 +261,10 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
         if (!ok) {                                // let the copies in flight land before the block's shared memory goes away
             for (uint32_t i = 1; i <= C::STAGES && i <= pos; ++i)
                 for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
-                    if (mbar_try_wait(&sm.full[(pos - i) % C::STAGES], ((pos - i) / C::STAGES) & 1u)) break;
+                    if (mbar_try_wait(&bar.full[(pos - i) % C::STAGES], ((pos - i) / C::STAGES) & 1u)) break;
             if (a_loads > 0)
                 for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
-                    if (mbar_try_wait(&sm.a_full, (a_loads - 1u) & 1u)) break;
+                    if (mbar_try_wait(&bar.a_full, (a_loads - 1u) & 1u)) break;
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -288,15 +275,15 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % BWD_SLOTS;
-            if (!mbar_wait_warp(&sm.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
+            if (!mbar_wait_warp(&bar.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
             if (!sm.items[slot].valid) break;
             const int blocks = uniform(sm.items[slot].n);
             if (blocks > 0) {
-                if (!mbar_wait_warp(A_TMEM ? &sm.a_ready : &sm.a_full, with_blocks & 1u, abort_flag)) { ok = false; break; }
+                if (!mbar_wait_warp(A_TMEM ? &bar.a_ready : &bar.a_full, with_blocks & 1u, abort_flag)) { ok = false; break; }
                 for (int b = 0; b <= blocks; ++b) {
                     if (b < blocks) {
                         const uint32_t cur = c + b, st = cur % C::STAGES, xy = tmem + 256 + (cur & 1u) * 128;
-                        if (!mbar_wait_warp(&sm.full[st], (cur / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                        if (!mbar_wait_warp(&bar.full[st], (cur / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
                         tcgen05_fence_after();
                         if (elect_one()) {
 #pragma unroll
@@ -305,22 +292,22 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                                 if (A_TMEM) mma_over_dims_tmem_a<C::HALVES>(xy + o * 64, tmem + C::A_AT + o * C::A_STEP, cols, COLS_HALF_BYTES, idesc_xy);
                                 else mma_over_dims<C::HALVES>(xy + o * 64, a_base + o * C::ROWS_BYTES, ROWS_HALF_BYTES, cols, COLS_HALF_BYTES, idesc_xy);
                             }
-                            tcgen05_commit(&sm.xy_full[cur & 1u]);
-                            if (!A_TMEM && b == blocks - 1) tcgen05_commit(&sm.a_empty);
+                            tcgen05_commit(&bar.xy_full[cur & 1u]);
+                            if (!A_TMEM && b == blocks - 1) tcgen05_commit(&bar.a_empty);
                         }
                         __syncwarp();
                     }
                     if (b > 0) {
                         const uint32_t cur = c + b - 1, st = cur % C::STAGES, xy = tmem + 256 + (cur & 1u) * 128;
-                        if (b == 1 && !mbar_wait_warp(&sm.acc_empty, (with_blocks & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-                        if (!mbar_wait_warp(&sm.ps_full[cur & 1u], (cur >> 1) & 1u, abort_flag)) { ok = false; break; }
+                        if (b == 1 && !mbar_wait_warp(&bar.acc_empty, (with_blocks & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                        if (!mbar_wait_warp(&bar.ps_full[cur & 1u], (cur >> 1) & 1u, abort_flag)) { ok = false; break; }
                         tcgen05_fence_after();
                         if (elect_one()) {
 #pragma unroll
                             for (int o = KEYS ? 0 : 1; o < 2; ++o)       // accumulator 1: p b2; accumulator 2: ds b1
                                 mma_over_rows<BWD_BLOCK, 0, BWD_BLOCK / UMMA_K>(tmem + o * 128, xy + o * 64, ring_base + (st * 2 + 1 - o) * C::COLS_BYTES, idesc_acc, b == 1);
-                            tcgen05_commit(&sm.empty[st]);
-                            if (b == blocks) tcgen05_commit(&sm.acc_full);
+                            tcgen05_commit(&bar.empty[st]);
+                            if (b == blocks) tcgen05_commit(&bar.acc_full);
                         }
                         __syncwarp();
                     }
@@ -328,14 +315,14 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 c += blocks;
                 ++with_blocks;
             }
-            if (ok && elect_one()) mbar_arrive(&sm.item_empty[slot]);
+            if (ok && elect_one()) mbar_arrive(&bar.item_empty[slot]);
             __syncwarp();
         }
         if (!ok) {
-            if (elect_one()) tcgen05_commit(&sm.drain);
+            if (elect_one()) tcgen05_commit(&bar.drain);
             __syncwarp();
             for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
-                if (mbar_try_wait(&sm.drain, 0u)) break;
+                if (mbar_try_wait(&bar.drain, 0u)) break;
         }
         __syncwarp();
     } else if (warp == 2) {
@@ -346,13 +333,13 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % BWD_SLOTS;
-            if (!mbar_wait_warp(&sm.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) break;
+            if (!mbar_wait_warp(&bar.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) break;
             const BwdItem& it = sm.items[slot];
             if (!it.valid) break;
             const int blocks = it.n;
             for (int b = 0; b < blocks; ++b) {
                 const uint32_t cur = c + b, st = cur % C::STAGES;
-                if (!mbar_wait_warp(&sm.full[st], (cur / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                if (!mbar_wait_warp(&bar.full[st], (cur / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
                 const bool masked = bwd_masked<KEYS>(it, b, TOKQ);
                 if (KEYS && masked && (sm.bad_stats[st][0] | sm.bad_stats[st][1]) == 0u) {
                     if (lane < 2) sm.bad[st][lane] = 0u;
@@ -375,13 +362,13 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 }
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(&sm.scanned[st]);
-                    mbar_arrive(&sm.empty[st]);
+                    mbar_arrive(&bar.scanned[st]);
+                    mbar_arrive(&bar.empty[st]);
                 }
                 __syncwarp();
             }
             c += blocks;
-            if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
+            if (lane == 0) mbar_arrive(&bar.item_empty[slot]);
             __syncwarp();
         }
     } else if (warp >= 4) {
@@ -398,9 +385,9 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
         auto prepare = [&](uint32_t n) {
             if (!A_TMEM) return true;
             const uint32_t slot = n % BWD_SLOTS;
-            if (!mbar_wait_warp(&sm.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) return false;
+            if (!mbar_wait_warp(&bar.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) return false;
             if (!sm.items[slot].valid || sm.items[slot].n == 0) return true;
-            if (!mbar_wait_warp(&sm.a_full, prepared++ & 1u, abort_flag)) return false;
+            if (!mbar_wait_warp(&bar.a_full, prepared++ & 1u, abort_flag)) return false;
 #pragma unroll 1
             for (int h = 0; h < C::HALVES; ++h) {
                 const uint8_t* at = rows_a + w * C::ROWS_BYTES + h * ROWS_HALF_BYTES + row * 128;
@@ -417,8 +404,8 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
             tcgen05_fence_before();
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(&sm.a_ready);
-                mbar_arrive(&sm.a_empty);
+                mbar_arrive(&bar.a_ready);
+                mbar_arrive(&bar.a_empty);
             }
             __syncwarp();
             return true;
@@ -426,7 +413,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
         ok = prepare(0);
         for (uint32_t n = 0; ok; ++n) {
             const uint32_t slot = n % BWD_SLOTS;
-            if (!mbar_wait_warp(&sm.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
+            if (!mbar_wait_warp(&bar.item_full[slot], (n / BWD_SLOTS) & 1u, abort_flag)) { ok = false; break; }
             const BwdItem& it = sm.items[slot];
             if (!it.valid) break;
             const int blocks = it.n, tok = KEYS ? row : row / ratio, head = it.g * ratio + (KEYS ? 0 : row - tok * ratio);
@@ -464,13 +451,13 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                     }
                     if (!live || len < 0) len = 0;
                 }
-                if (!mbar_wait_warp(&sm.full[st], (cur / C::STAGES) & 1u, abort_flag) ||      // the columns' statistics
-                    !mbar_wait_warp(&sm.xy_full[w], (cur >> 1) & 1u, abort_flag)) { ok = false; break; }
+                if (!mbar_wait_warp(&bar.full[st], (cur / C::STAGES) & 1u, abort_flag) ||      // the columns' statistics
+                    !mbar_wait_warp(&bar.xy_full[w], (cur >> 1) & 1u, abort_flag)) { ok = false; break; }
                 tcgen05_fence_after();
                 uint32_t on[2] = {0xffffffffu, 0xffffffffu}, bad[2] = {0u, 0u};
                 bool select = false, none_of_it = false;
                 if (masked) {
-                    if (!mbar_wait_warp(&sm.scanned[st], (cur / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                    if (!mbar_wait_warp(&bar.scanned[st], (cur / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         const int a = min(max(first - u * 32, 0), 32), z = min(max(first + len - u * 32, 0), 32);
@@ -532,25 +519,25 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
                 tcgen05_st_wait();
                 tcgen05_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sm.ps_full[w]);
+                if (lane == 0) mbar_arrive(&bar.ps_full[w]);
                 __syncwarp();
             }
             if (!ok) break;
             c += blocks;
             // KEYS: group 0 writes dv, group 1 dk; else each half of dq
             if (blocks > 0) {
-                if (!mbar_wait_warp(&sm.acc_full, with_blocks & 1u, abort_flag)) { ok = false; break; }
+                if (!mbar_wait_warp(&bar.acc_full, with_blocks & 1u, abort_flag)) { ok = false; break; }
                 tcgen05_fence_after();
                 ++with_blocks;
             }
             if (!prepare(n + 1)) { ok = false; break; }
             __nv_bfloat16* out;
             if (KEYS) {
-                out = w == 0 ? (it.shared ? p.shared1 + j * p.shared1_stride : p.out1 + j * p.out1_stride)
-                             : (it.shared ? p.shared2 + j * p.shared2_stride : p.out2 + j * p.out2_stride);
+                out = w == 0 ? (it.shared ? p.shared1 + j * p.shared1_stride : p.dv + j * p.dv_stride)
+                             : (it.shared ? p.shared2 + j * p.shared2_stride : p.dk + j * p.dk_stride);
                 out += (int64_t)it.g * p.sh.D;
             } else {
-                out = p.out2 + j * p.out2_stride + (int64_t)head * p.sh.D;
+                out = p.dq + j * p.dq_stride + (int64_t)head * p.sh.D;
             }
             const float by = KEYS && w == 0 ? 1.f : p.sh.scale;
             const bool to_parts = KEYS && it.shared && p.splits > 1;
@@ -593,20 +580,57 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_a1, const __gr
             tcgen05_fence_before();
             __syncwarp();
             if (lane == 0) {
-                if (blocks > 0) mbar_arrive(&sm.acc_empty);
-                mbar_arrive(&sm.item_empty[slot]);
+                if (blocks > 0) mbar_arrive(&bar.acc_empty);
+                mbar_arrive(&bar.item_empty[slot]);
             }
             __syncwarp();
         }
     }
+}
+
+template <int DP>
+__global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(const __grid_constant__ BwdMaps maps, const BwdParams p) {
+    using C = BwdConf<DP>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ BwdShared sm;
+    uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int warp = uniform((int)threadIdx.x >> 5);
+    if (threadIdx.x == 0) {
+        init_barriers<DP, true>(sm.of[1]);
+        init_barriers<DP, false>(sm.of[0]);
+        sm.abort = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (const CUtensorMap* m : {&maps.k_rows, &maps.v_rows, &maps.q_cols, &maps.do_cols}) asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+    }
+    if (BWD_BLOCK / p.sh.ratio * p.sh.ratio < BWD_BLOCK) {       // rows behind the last whole token are never loaded: zeros, for the keys' second products
+        for (uint32_t i = threadIdx.x * 16; i < C::STAGES * 2 * C::COLS_BYTES; i += BWD_THREADS * 16)
+            *reinterpret_cast<uint4*>(smem + 2 * C::ROWS_BYTES + i) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+    }
+    if (warp == 1) {
+        tcgen05_alloc(&sm.tmem, 512);
+        tcgen05_relinquish();
+    }
     tcgen05_fence_before();
     __syncthreads();
-    if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, ARROL_DEV_WAIT_EXPIRED);
+    tcgen05_fence_after();
+    const uint32_t tmem = uniform(sm.tmem);                // accumulators 1 and 2 at columns 0 and 128; x, y of buffer i at 256 + 128 i and + 64
+    pdl_launch_dependents();
+    pdl_wait();
+    // The queries' side needs nothing of the keys' side, so a block goes on to it as soon as it finds no more of the keys' items.
+    backward_side<DP, true>(maps.k_rows, maps.v_rows, maps.q_cols, maps.do_cols, maps.pk_rows, maps.pv_rows, p, sm, smem, tmem);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    if (!*static_cast<volatile uint32_t*>(&sm.abort))
+        backward_side<DP, false>(maps.q_rows, maps.do_rows, maps.k_cols, maps.v_cols, maps.pk_cols, maps.pv_cols, p, sm, smem, tmem);
+    tcgen05_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && *static_cast<volatile uint32_t*>(&sm.abort)) atomicOr(p.status, ARROL_DEV_WAIT_EXPIRED);
     if (warp == 1) {
         tcgen05_fence_after();
         tcgen05_dealloc(tmem, 512);
     }
-    if (!KEYS) pdl_wait();
 }
 
 // The parts of a prompt tile's sums, in order.
@@ -639,8 +663,7 @@ int launch_backward(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWor
     using C = BwdConf<DP>;
     bool& set = ctx->attention_backward_smem_set[DP == 128];
     if (!set) {
-        ARROL_CUDA_OK(cudaFuncSetAttribute(attention_backward_kernel<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
-        ARROL_CUDA_OK(cudaFuncSetAttribute(attention_backward_kernel<DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+        ARROL_CUDA_OK(cudaFuncSetAttribute(attention_backward_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
         set = true;
     }
     const int ratio = a->Hq / a->Hkv;
@@ -650,47 +673,40 @@ int launch_backward(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWor
     p.cu_prompts = a->cu_prompts;
     p.P = a->P;
     p.status = ctx->d_status;
-    CUtensorMap q_cols, do_cols, q_rows, do_rows, k_cols, v_cols, k_rows, v_rows, pk_cols, pv_cols, pk_rows, pv_rows;
+    BwdMaps m;
     struct { CUtensorMap* map; const void* base; int64_t rows, stride; int heads, group, tokens; } maps[] = {
-        {&q_rows, a->q, a->T_max, a->q_stride, a->Hq, ratio, 128 / ratio},       {&do_rows, a->d_o, a->T_max, a->d_o_stride, a->Hq, ratio, 128 / ratio},
-        {&q_cols, a->q, a->T_max, a->q_stride, a->Hq, ratio, BWD_BLOCK / ratio}, {&do_cols, a->d_o, a->T_max, a->d_o_stride, a->Hq, ratio, BWD_BLOCK / ratio},
-        {&k_rows, a->k, a->T_max, a->k_stride, a->Hkv, 1, 128},                  {&v_rows, a->v, a->T_max, a->v_stride, a->Hkv, 1, 128},
-        {&k_cols, a->k, a->T_max, a->k_stride, a->Hkv, 1, BWD_BLOCK},            {&v_cols, a->v, a->T_max, a->v_stride, a->Hkv, 1, BWD_BLOCK},
-        {&pk_rows, a->prompt_k, a->prompt_rows, a->prompt_k_stride, a->Hkv, 1, 128},
-        {&pv_rows, a->prompt_v, a->prompt_rows, a->prompt_v_stride, a->Hkv, 1, 128},
-        {&pk_cols, a->prompt_k, a->prompt_rows, a->prompt_k_stride, a->Hkv, 1, BWD_BLOCK},
-        {&pv_cols, a->prompt_v, a->prompt_rows, a->prompt_v_stride, a->Hkv, 1, BWD_BLOCK}};
-    for (auto& m : maps) {
-        if (m.rows == 0) continue;
-        if (make_map_heads(ctx, m.map, m.base, m.rows, m.heads, a->D, m.stride, m.group, m.tokens) != ARROL_OK) return ARROL_ERR_CUDA;
+        {&m.q_rows, a->q, a->T_max, a->q_stride, a->Hq, ratio, 128 / ratio},       {&m.do_rows, a->d_o, a->T_max, a->d_o_stride, a->Hq, ratio, 128 / ratio},
+        {&m.q_cols, a->q, a->T_max, a->q_stride, a->Hq, ratio, BWD_BLOCK / ratio}, {&m.do_cols, a->d_o, a->T_max, a->d_o_stride, a->Hq, ratio, BWD_BLOCK / ratio},
+        {&m.k_rows, a->k, a->T_max, a->k_stride, a->Hkv, 1, 128},                  {&m.v_rows, a->v, a->T_max, a->v_stride, a->Hkv, 1, 128},
+        {&m.k_cols, a->k, a->T_max, a->k_stride, a->Hkv, 1, BWD_BLOCK},            {&m.v_cols, a->v, a->T_max, a->v_stride, a->Hkv, 1, BWD_BLOCK},
+        {&m.pk_rows, a->prompt_k, a->prompt_rows, a->prompt_k_stride, a->Hkv, 1, 128},
+        {&m.pv_rows, a->prompt_v, a->prompt_rows, a->prompt_v_stride, a->Hkv, 1, 128},
+        {&m.pk_cols, a->prompt_k, a->prompt_rows, a->prompt_k_stride, a->Hkv, 1, BWD_BLOCK},
+        {&m.pv_cols, a->prompt_v, a->prompt_rows, a->prompt_v_stride, a->Hkv, 1, BWD_BLOCK}};
+    for (auto& x : maps) {
+        if (x.rows == 0) continue;
+        if (make_map_heads(ctx, x.map, x.base, x.rows, x.heads, a->D, x.stride, x.group, x.tokens) != ARROL_OK) return ARROL_ERR_CUDA;
     }
-    if (a->prompt_rows == 0) { pk_rows = k_rows; pv_rows = v_rows; pk_cols = k_cols; pv_cols = v_cols; }     // never read then
-    if (a->T_max == 0) { q_cols = do_cols = k_rows = v_rows = pk_rows; }
-    p.out1 = static_cast<__nv_bfloat16*>(a->dv); p.out1_stride = a->dv_stride;
-    p.out2 = static_cast<__nv_bfloat16*>(a->dk); p.out2_stride = a->dk_stride;
+    // never read then
+    if (a->prompt_rows == 0) { m.pk_rows = m.k_rows; m.pv_rows = m.v_rows; m.pk_cols = m.k_cols; m.pv_cols = m.v_cols; }
+    if (a->T_max == 0) { m.q_rows = m.do_rows = m.q_cols = m.do_cols = m.k_rows = m.v_rows = m.k_cols = m.v_cols = m.pk_rows; }
+    p.dv = static_cast<__nv_bfloat16*>(a->dv); p.dv_stride = a->dv_stride;
+    p.dk = static_cast<__nv_bfloat16*>(a->dk); p.dk_stride = a->dk_stride;
+    p.dq = static_cast<__nv_bfloat16*>(a->dq); p.dq_stride = a->dq_stride;
     p.shared1 = static_cast<__nv_bfloat16*>(a->dprompt_v); p.shared1_stride = a->dprompt_v_stride;
     p.shared2 = static_cast<__nv_bfloat16*>(a->dprompt_k); p.shared2_stride = a->dprompt_k_stride;
-    p.counter = w.counters + 1;
+    p.counter[0] = w.counters + 2;
+    p.counter[1] = w.counters + 1;
     p.splits = attn_prompt_splits(ctx->sm_count, a->T_max, a->prompt_rows, a->P, a->Hq, a->Hkv);
     p.part1 = w.parts;
     p.part2 = w.parts + (int64_t)p.splits * ((a->prompt_rows + 127) / 128) * a->Hkv * 128 * DP;
-    int64_t items = ((a->T_max + 127) / 128 + (a->prompt_rows + 127) / 128 * p.splits) * a->Hkv;
+    const int64_t items = ((a->T_max + 127) / 128 + (a->prompt_rows + 127) / 128 * p.splits + (a->T_max + 128 / ratio - 1) / (128 / ratio)) * a->Hkv;
     const auto blocks = [&](int64_t n, int64_t most) { return dim3((unsigned)(n < most ? n : most)); };
-    ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, true>, blocks(items, ctx->sm_count), dim3(BWD_THREADS), C::SMEM, s,
-                                   k_rows, v_rows, q_cols, do_cols, pk_rows, pv_rows, p));
-    ctx->launches += 1;
-    if (a->T_max == 0) return ARROL_OK;      // one part then
-    BwdParams sums = p;
-    p.out1 = nullptr;
-    p.out2 = static_cast<__nv_bfloat16*>(a->dq); p.out2_stride = a->dq_stride;
-    p.counter = w.counters + 2;
-    items = (a->T_max + 128 / ratio - 1) / (128 / ratio) * a->Hkv;
-    ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP, false>, blocks(items, ctx->sm_count), dim3(BWD_THREADS), C::SMEM, s,
-                                   q_rows, do_rows, k_cols, v_cols, pk_cols, pv_cols, p));
+    ARROL_CUDA_OK(arrol_launch_pdl(attention_backward_kernel<DP>, blocks(items, ctx->sm_count), dim3(BWD_THREADS), C::SMEM, s, m, p));
     ctx->launches += 1;
     if (p.splits > 1) {
         const int64_t pieces = 2 * a->prompt_rows * a->Hkv * (DP / 8);
-        ARROL_CUDA_OK(arrol_launch_pdl(attention_add_parts_kernel<DP>, blocks((pieces + 255) / 256, 8 * ctx->sm_count), dim3(256), 0, s, sums));
+        ARROL_CUDA_OK(arrol_launch_pdl(attention_add_parts_kernel<DP>, blocks((pieces + 255) / 256, 8 * ctx->sm_count), dim3(256), 0, s, p));
         ctx->launches += 1;
     }
     return ARROL_OK;

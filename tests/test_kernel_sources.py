@@ -72,8 +72,26 @@ def test_a_scanned_stage_is_waited_for_behind_its_filling(name):
     roles = re.split(r"\n    (?:\} else )?if \([^\n]*warp [=>]=? ?\d", code)
     waits = 0
     for role in roles:
-        for m in re.finditer(r"mbar_wait\w*\(&sm\.scanned\[(\w+)\]", role):
+        for m in re.finditer(r"mbar_wait\w*\(&\w+\.scanned\[(\w+)\]", role):
             waits += 1
             loop = role.rindex(" while (" if name == "attention.cu" else " for (int b = 0;", 0, m.start())
-            assert re.search(r"mbar_wait\w*\(&sm\.full\[%s\]" % m.group(1), role[loop:m.start()]), name
+            assert re.search(r"mbar_wait\w*\(&\w+\.full\[%s\]" % m.group(1), role[loop:m.start()]), name
     assert waits == 1
+
+
+@pytest.mark.parametrize("path", SOURCES, ids=os.path.basename)
+def test_kernels_that_start_early_wait_before_they_touch_what_others_wrote(path):
+    """Only a grid that waits itself is promised what the grids before it wrote; that the one in between has waited does not do.  So the wait is every
+    thread's, at the outermost level, and comes before anything that is asked for through pdl_acquire() or added to."""
+    for name, body in _kernels(_code(path)):
+        if "pdl_wait()" not in body:
+            continue
+        depth, wait = 0, 0
+        for m in re.finditer(r"[{}]|\bpdl_wait\(\)", body):
+            depth += {"{": 1, "}": -1}.get(m.group(), 0)
+            if m.group().startswith("pdl_wait"):
+                wait = m.start()
+                break
+        assert depth == 0, name
+        assert re.search(r"[;{}]\s*$", body[:wait]), "%s: the wait stands under a condition" % name
+        assert not re.search(r"\b(pdl_acquire|atomic\w+)\(", body[:wait]), name
