@@ -218,7 +218,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::STAGES; ++i) {
             mbar_init(&sm.full[i], 1);
-            mbar_init(&sm.empty[i], (C::AHEAD ? 2 : 1) + (i & 1));       // odd stages hold values, which the scanner hands back too
+            mbar_init(&sm.empty[i], C::AHEAD ? 3 : 1 + (i & 1));         // odd stages hold values, which the scanner hands back too (and keys, see there)
             mbar_init(&sm.scanned[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -561,6 +561,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(&sm.scanned[st]);
+                    // keys too: S of the block that has the stage next then says that the values which had its values' stage have been looked over
+                    if (C::AHEAD) mbar_arrive(&sm.empty[(pos - 1) % C::STAGES]);
                     mbar_arrive(&sm.empty[st]);
                 }
                 __syncwarp();
@@ -700,10 +702,13 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     __syncwarp();
                 };
                 if (masked) {
-                    // The values have been looked over before P V may begin.  The stage is waited for first: S needs the keys alone, and while the values that
-                    // had the stage before are still being looked over, their phase's parity is what the second wait would take for this one's.
+                    // The values have been looked over before P V may begin.  Nothing here may wait for the scanner while it is still at the values that had the
+                    // stage before: their phase's parity is what the wait would take for this one's, and S needs the keys alone.  A stage that has been
+                    // filled again rules it out; where S runs ahead the keys' stage does, which the scanner hands back with the values (there 413 us with
+                    // this wait, 399 with that; with heads of 128 458 with this, 472 to 487 with that).
                     const uint32_t pos = pos0 + 2 * b + 1, st = pos % C::STAGES, parity = (pos / C::STAGES) & 1u;
-                    if (!mbar_wait_warp(&sm.full[st], parity, abort_flag) || !mbar_wait_warp(&sm.scanned[st], parity, abort_flag)) { ok = false; break; }
+                    if (!C::AHEAD && !mbar_wait_warp(&sm.full[st], parity, abort_flag)) { ok = false; break; }
+                    if (!mbar_wait_warp(&sm.scanned[st], parity, abort_flag)) { ok = false; break; }
                     const uint4 bad = *reinterpret_cast<const uint4*>(sm.bad_keys[st]);
                     if ((bad.x & on[0]) | (bad.y & on[1]) | (bad.z & on[2]) | (bad.w & on[3])) l = NAN;
                     __syncwarp();

@@ -77,6 +77,10 @@ def test_a_scanned_stage_is_waited_for_behind_its_filling(name):
             loop = role.rindex(" while (" if name == "attention.cu" else " for (int b = 0;", 0, m.start())
             assert re.search(r"mbar_wait\w*\(&\w+\.full\[%s\]" % m.group(1), role[loop:m.start()]), name
     assert waits == 1
+    if name == "attention.cu":       # where S runs ahead the wait is for the keys, whose stage the scanner hands back with the values
+        assert "if (!C::AHEAD && !mbar_wait_warp(&sm.full[st], parity" in code
+        assert "if (C::AHEAD) mbar_arrive(&sm.empty[(pos - 1) % C::STAGES]);" in code
+        assert "mbar_init(&sm.empty[i], C::AHEAD ? 3 : 1 + (i & 1));" in code
 
 
 @pytest.mark.parametrize("path", SOURCES, ids=os.path.basename)
