@@ -448,6 +448,7 @@ __device__ __forceinline__ void backward_side(const CUtensorMap& map_a1, const C
                         first = (pre ? pre_lo : lo) - c0;
                         len = (pre ? pre_hi - pre_lo : hi - lo);
                         if (first < 0) { len += first; first = 0; }
+                        len = min(len, BWD_BLOCK - first);        // of this block: a whole block's number is what leaves the selection out below
                     }
                     if (!live || len < 0) len = 0;
                 }

@@ -509,3 +509,12 @@ def test_many_values_that_are_not_finite_beside_another_prompt(ctx, D, Hq, Hkv, 
         for name in ("dprompt_k", "dprompt_v"):
             assert torch.equal(out[name][kept_prompts], good[name][kept_prompts]), name
         assert not torch.isfinite(out["o"][~keep][..., 0]).any()
+
+
+@pytest.mark.parametrize("n", [32, 64, 128])
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 4, 4), (128, 4, 2), (16, 1, 1), (128, 32, 1), (64, 64, 1)])
+def test_prompts_and_sequences_as_long_as_a_block(ctx, D, Hq, Hkv, n):
+    """Ranges of keys as long as a block of them, but not at its beginning: the first token's prompt begins the blocks, a prompt and a sequence of exactly n
+    rows follow at odd places, so that every row of a warp has n keys of which some are in the block."""
+    p = Problem([37, 150, n, n + 1, 200, n], [29, n, n, 1, n], [0, 1, 1, 2, 3, 4], 1, Hq, Hkv, D, seed=32)
+    p.check(p.run(ctx))
