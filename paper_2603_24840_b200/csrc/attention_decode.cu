@@ -441,7 +441,6 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
 #pragma unroll
                         for (int h = 0; h < C::HALVES; ++h)
                             *reinterpret_cast<uint4*>(stage + C::KEYS_BYTES + h * C::HALF_BYTES + x * 16) = make_uint4(0, 0, 0, 0);
-                    fence_proxy_async_smem();
                     __syncwarp();
                 }
                 // The reference is let fall up to 2^8 behind the maximum, which changes nothing (sums and products carry the same factor): only where
@@ -496,6 +495,9 @@ decode_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         }
                     }
                 }
+                // The next copy into the stage is the async proxy's: the arrival alone does not keep it behind this warp's reads (and zeros).  Without the
+                // fence the last values were now and then those of the copy that followed.
+                fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_n(&sm.empty[st], (uint32_t)parts);     // row_tiles warps read it: DEC_WARPS in all
                 __syncwarp();

@@ -268,3 +268,22 @@ def test_not_a_number_in_a_prompt_or_a_key_reaches_its_rollouts_alone(ctx, where
         assert torch.equal(x[others], y[others]) and torch.equal(x[reached, 2:], y[reached, 2:])
     if value != -math.inf:                     # a key of no weight is all that a score of minus infinity makes
         assert not torch.isfinite(bad[0][reached, :2, 5]).any()
+
+
+@pytest.mark.parametrize("lengths,prompts,G,Hq,Hkv,D", [
+    ([0, 226, 0, 834, 156, 705, 550, 757, 0, 547, 1, 0, 1, 24, 595, 0, 1, 0, 0, 96, 0, 1, 1, 0, 0, 1, 0, 170, 205, 0, 0, 0, 1, 565, 1, 0, 219, 140, 281, 193, 462, 188, 24, 177,
+      771, 157, 651, 387, 379, 0, 1, 83, 74, 86, 268, 1, 392, 3, 281, 1], [55, 178, 0, 142], 15, 32, 8, 64),
+    ([700, 30, 608, 250] * 10, [227, 80, 1, 300], 10, 64, 8, 128),
+    ([33, 64, 407, 851] * 14, None, 1, 128, 8, 128),
+])
+def test_same_bits_over_many_calls(ctx, lengths, prompts, G, Hq, Hkv, D):
+    """The stages of the ring change hands between readers and copies thousands of times: calls one behind another, all results compared on the device."""
+    p = Problem(lengths, prompts, G, Hq, Hkv, D, seed=16, gap=70, fill=math.nan)
+    o, lse = p.run(ctx)
+    p.check(o, lse)
+    ws, other = p.workspace(ctx), torch.zeros((), dtype=torch.bool, device="cuda")
+    for _ in range(1500):
+        again = p.outputs()
+        p.call(ctx, *again, ws)
+        other |= (again[0] != o).any() | (again[1] != lse).any()
+    assert B.arrol_poll_status(ctx) == 0 and not other.item()

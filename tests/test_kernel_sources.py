@@ -99,3 +99,17 @@ def test_kernels_that_start_early_wait_before_they_touch_what_others_wrote(path)
         assert depth == 0, name
         assert re.search(r"[;{}]\s*$", body[:wait]), "%s: the wait stands under a condition" % name
         assert not re.search(r"\b(pdl_acquire|atomic\w+)\(", body[:wait]), name
+
+
+def test_stages_read_by_warps_are_handed_back_behind_a_proxy_fence():
+    """Reads of shared memory by instructions and the copies that refill it belong to different proxies, and an arrival orders nothing between them: a warp that has
+    read a stage through ldmatrix fences before it arrives, every lane, and the lanes meet before the one arrives for all."""
+    found = 0
+    for path in SOURCES:
+        code = re.sub(r"\s+", " ", _code(path))
+        if "ldmatrix_x4" not in code or "mbar_arrive" not in code:
+            continue
+        for m in re.finditer(r"if \(lane == 0\) mbar_arrive\w*\(&sm\.empty\[", code):
+            found += 1
+            assert code[:m.start()].endswith("fence_proxy_async_smem(); __syncwarp(); "), os.path.basename(path)
+    assert found == 1
