@@ -5,12 +5,13 @@
 // a thread takes a row of it, P = exp(S - m) goes back as bf16 (the one rounding beside o's; l is summed before it), O += P V.  m is a reference
 // that the running maximum may be 2^8 ahead of: sums and products carry the same factor 2^-m, so a row's O is scaled again only when
 // that is passed.  4 D flops a pair against one exponential: with 128 dimensions the tensor cores (512 cycles each for S and P V of a tile and
-// block) and the exponentials (1,024 cycles a tile and block at 16 a cycle) are level, with 64 the exponentials are the longer.  Neither unit is full: with
-// 128 both are busy about half of the cycles, with 64 0.53 and 0.28; the rest is the way between them.
+// block) and the exponentials (1,024 cycles a tile and block at 16 a cycle) are level, with 64 the exponentials are the longer.  By the counters neither unit is
+// full: with 128 both are busy about half of the cycles, with 64 0.53 and 0.28.  What fills the rest was not measured; the way between them is what is left.
 // One launch finds every token's range of keys, one computes: 148 blocks that take (256 query rows, key head) items from a counter.
-// Measured: 8,192 tokens, 32 heads of 128 on 8 470 to 500 us (1.10 to 1.17 PFLOP/s, 0.66 to 0.70 of the measured burst rate, tensor pipe busy 0.55
-// of the cycles); with heads of 64 370 to 419 us; 48 survivors of 40 to 333 tokens over 16,000 prompt tokens, 28 heads on 4 395 to 440 us (0.82 to
-// 0.92 PFLOP/s).  Where few rows leave most blocks without an item, an item's keys are split and a third launch joins the parts (attn_key_splits).
+// Measured, calls from a graph: 8,192 tokens, 32 heads of 128 on 8 458 to 479 us (1.15 to 1.20 PFLOP/s, 0.68 to 0.71 of the measured burst rate, tensor
+// pipe busy 0.55 of the cycles); with heads of 64 379 us; 48 survivors of 40 to 333 tokens over 16,000 prompt tokens, 28 heads on 4 394 to 422 us (0.86 to
+// 0.92 PFLOP/s).  Calls from the host one by one: 535 to 554, and 440 to 445 us.  Where few rows leave most blocks without an item, an item's keys are
+// split and a third launch joins the parts (attn_key_splits).
 #include "attention_common.cuh"
 
 namespace {
@@ -429,7 +430,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                             pv_frees[i] = i == 1 || !use[1];
                         }
                     }
-                    if (!use[0] && !use[1] && ok) {      // only where row numbers are out of order
+                    if (!use[0] && !use[1] && ok) {      // keys of prompts between the tiles' that have no survivors, or row numbers out of order
                         if (!wait_stage(pos) || !wait_stage(pos + 1)) { ok = false; break; }
                         mbar_arrive(&sm.empty[pos % C::STAGES]);
                         mbar_arrive(&sm.empty[(pos + 1) % C::STAGES]);
@@ -863,7 +864,7 @@ int launch_attention(arrol_ctx* ctx, const arrol_attention_args* a, const AttnWo
         if (make_map_heads(ctx, &pk, a->prompt_k, a->prompt_rows, a->Hkv, a->D, a->prompt_k_stride, 1, FWD_BLOCK) != ARROL_OK) return ARROL_ERR_CUDA;
         if (make_map_heads(ctx, &pv, a->prompt_v, a->prompt_rows, a->Hkv, a->D, a->prompt_v_stride, 1, FWD_BLOCK) != ARROL_OK) return ARROL_ERR_CUDA;
     }
-    // A form of its own: with the parts' arithmetic in one form for both, heads of 128 spilled 56 bytes of registers a thread instead of 32.
+    // A form of its own: the parts' arithmetic spills 56 bytes of registers a thread with heads of 128 and 92 with 64, the form of whole keys 32 and none.
     p.splits = attn_key_splits(ctx->sm_count, a->T_max, a->prompt_rows, a->P, a->S_max, a->Hq, a->Hkv);
     p.part_o = w.part_o;
     p.part_ml = w.part_ml;

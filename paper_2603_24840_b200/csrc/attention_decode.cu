@@ -7,7 +7,7 @@
 // The products are 16 x 8 x 16 mma.sync: 64 rows at most meet a key, which is too few flops a byte for tensor memory to pay, and a unit's 4 to 16
 // rows would leave seven eighths of a 128-row tile empty.
 // Measured (calls from a graph): 256 live rollouts of 2,200 tokens, 16 heads of 128 on 8 (2.46 GB) 381 to 394 us, 6.2 to 6.5 TB/s, 0.96 to 0.99 of the
-// measured copy rate; 8 rollouts of 6,600 tokens, 32 heads (236 MB) 62 us; 384 rollouts of 160 tokens over 24 prompts of 5,800, 32 heads of 64 121 us
+// measured copy rate; 8 rollouts of 6,600 tokens, 32 heads (236 MB) 61 us; 384 rollouts of 160 tokens over 24 prompts of 5,800, 32 heads of 64 121 to 124 us
 // (0.52): there it is latency, with 64 rows' products behind every key and eight consuming warps an SM (the products' pipe is active 0.30 of the cycles, a
 // scheduler issues 0.33 instructions a cycle, no pipe is full); 16 rollouts of 30 tokens 14 us, three launches one behind another.
 // More than one tile of keys at once per warp (for its latencies) left too little of the ring for the copies: 121 -> 136 us.
