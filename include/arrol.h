@@ -409,6 +409,137 @@ typedef struct arrol_decode_args {
 size_t arrol_attention_decode_workspace(arrol_ctx* ctx, int32_t N, int32_t P, int32_t Hq, int32_t Hkv, int32_t D);
 int arrol_attention_decode(arrol_ctx* ctx, const arrol_decode_args* args, void* stream);
 
+/* ---- Rotary positions (what the policy does to queries and keys before attention) -------------------------------------------
+ * The first R dimensions of every head are R / 2 pairs: (i, i + R / 2), or (2 i, 2 i + 1) where `interleaved` != 0.  Pair i of a row at position p turns by
+ * a = p frequencies[i], with cosine and sine multiplied by `factor`:
+ *     y1 = factor (x1 cos a - x2 sin a),   y2 = factor (x2 cos a + x1 sin a);   dimensions from R on stay as they are.
+ * arrol_rotary_backward gives the gradients: it takes d loss / d y in q, k and writes d loss / d x (the same with -a) to q_out, k_out.
+ * Rows are packed tokens.  positions [T_max] int32 says where each is, any integer; or, where it is NULL, token t of survivor s, row cu_seqlens[s] + t, is at
+ * t plus the length of its prompt, cu_prompts[p + 1] - cu_prompts[p], p = survivor_idx[s] / G (s / G when survivor_idx is NULL; t alone when cu_prompts is NULL and
+ * P = 0): the outputs of arrol_compact as they are, [S_max + 1], [P + 1], [S_max].  d_num [2] int64 = {S, T} on the device, clamped to S_max and T_max; with
+ * positions it may be NULL (all T_max rows).  Rows >= T are not written.
+ * frequencies: device double [R / 2], radians per position (arrol_rotary_frequencies).  Angles are formed in 64 bits and reduced before cosine and sine, which are fp32
+ * like the products; results are rounded once to bf16.
+ * q, q_out [T_max, Hq, D]; k, k_out [T_max, Hkv, D] bf16, layouts and alignment as in the attention calls; q_out may be q and k_out k (same stride, in place), otherwise
+ * outputs overlap nothing.  Hq or Hkv may be 0 (NULL pointers).  D a multiple of 8, 8 <= D <= 256; R even, 2 <= R <= D; T_max < 2^31 - 512.
+ * Row numbers out of order or outside are not followed; ARROL_DEV_BAD_INDEX is recorded and the outputs are undefined.  No workspace; the calls use nothing of the
+ * context's buffers and may be captured.
+ *
+ * arrol_rotary_frequencies (host): frequencies[i] = base^(-2 i / R), [R / 2] in host memory, for longer contexts changed by `kind`, in double:
+ *   ARROL_ROTARY_PLAIN   as they are;
+ *   ARROL_ROTARY_LINEAR  divided by `stretch` (positions interpolated);
+ *   ARROL_ROTARY_BANDS   by wave length: pair i makes n = original frequencies[i] / (2 pi) turns in `original` positions; divided by stretch where n <= low, unchanged
+ *                        where n >= high, between these (1 - s) f / stretch + s f with s = (n - low) / (high - low);
+ *   ARROL_ROTARY_RAMP    by pair number: i(n) = R log(original / (2 pi n)) / (2 log base) is the pair that makes n turns; s rises from 0 at floor(i(high)) to 1 at
+ *                        ceil(i(low)) (both kept within 0 .. R - 1, at least 0.001 apart), the frequency is (1 - s) f + s f / stretch.
+ * low, high, original are for the last two kinds.  A longer base (a change of base) needs no kind.  *factor (may be NULL) receives the factor on cosine and sine:
+ * 0.1 log(stretch) + 1 for ARROL_ROTARY_RAMP with stretch > 1, else 1.  INVALID_ARG for R odd or < 2, base <= 1, stretch <= 0, original <= 0, low <= 0, high <= low or values
+ * that are not finite. */
+#define ARROL_ROTARY_PLAIN 0
+#define ARROL_ROTARY_LINEAR 1
+#define ARROL_ROTARY_BANDS 2
+#define ARROL_ROTARY_RAMP 3
+int arrol_rotary_frequencies(int32_t R, double base, int32_t kind, double stretch, double low, double high, double original,
+                             double* frequencies, double* factor);
+typedef struct arrol_rotary_args {
+    const void *q, *k;
+    int64_t q_stride, k_stride;
+    void *q_out, *k_out;
+    int64_t q_out_stride, k_out_stride;
+    const double* frequencies;
+    const int32_t* positions;
+    const int64_t* cu_seqlens;
+    const int64_t* d_num;
+    const int64_t* cu_prompts;
+    const int32_t* survivor_idx;
+    int64_t T_max;
+    int32_t S_max, P, G, Hq, Hkv, D, R, interleaved;
+    float factor;
+    int32_t reserved;
+} arrol_rotary_args;
+int arrol_rotary(arrol_ctx* ctx, const arrol_rotary_args* args, void* stream);
+int arrol_rotary_backward(arrol_ctx* ctx, const arrol_rotary_args* args, void* stream);
+
+/* ---- A paged cache of keys and values in 8 bits (Algorithm 1, backend: generation) ---------------------------------------------
+ * A pool of `pages` pages, each of `page` tokens (16, 32, 64 or 128) of all key heads: k_cache, v_cache hold e4m3 numbers, [Hkv, page, D] of a page side by side, pages
+ * `k_page_stride` / `v_page_stride` bytes apart (a multiple of 16, at least Hkv * page * D; keys and values of one buffer may alternate); k_scale, v_scale float hold one
+ * scale per page and key head, pages `k_scale_stride` / `v_scale_stride` floats apart.  An entry stands for its e4m3 number times its page's and head's scale, a power of
+ * two: the least one, not below 2^-100, that brings the largest finite entry of the page and head to 448 or less.  As powers of two the scales cost no precision, and a
+ * scale may grow with the page's tokens without rounding them again (numbers that the larger scale makes subnormal excepted).  Infinities and NaN are stored as NaN.
+ * Token j of sequence i lies in slot j % page of page page_table[i * table_stride + j / page]; page_table int32, `table_pages` entries a row.
+ *
+ * arrol_cache_append writes new tokens' keys and values, with rotary positions applied on the way:
+ *   cu_new == NULL: one token per sequence, row i of q, k, v (rows = N), generation;  else rows cu_new[i] .. cu_new[i + 1] - 1 (cu_new [N + 1] int64, from 0, not
+ *   decreasing, at most `rows`), prompts or pieces of them; none is fine.
+ *   lengths [N] int32: tokens that sequence i has WITH the new ones, which are its last.  They are written over whatever the slots hold, so the same call again leaves the
+ *   same cache (a page's scale excepted where other tokens were in those slots).  A page's scale is taken anew by the call that writes its slot 0; other calls let it
+ *   grow, and the tokens before theirs with it.  Slots behind the last token stay as they are.
+ *   The position of token j is j, plus prompt_lengths[i / G] where prompt_lengths [P] int32 is given (N = P G; otherwise NULL and P = 0): a rollout's own cache begins
+ *   behind its group's prompt.  k and, where q is given, q are turned as by arrol_rotary (frequencies, R, interleaved, factor; frequencies NULL and R = 0: not at all).
+ *   q_out [rows, Hq, D] receives q; k_out [rows, Hkv, D], if not NULL, k, both bf16; k is stored from its fp32 value.  In place as in arrol_rotary.
+ *   keep [N] uint8 or NULL: sequences with 0 are left out, their pages and output rows untouched, their lengths and tables not followed.
+ *   Pages that receive tokens belong to one sequence of the call; pages that are only read (forked prefixes) may be shared.
+ *
+ * arrol_cache_attention is attention of one token per rollout, as arrol_attention_decode, over such a cache: rollout i < N with keep[i] != 0 attends with q[i] (bf16) to
+ * the prompt_lengths[p] tokens of its group's prompt, p = i / G, pages prompt_table[p * prompt_table_stride + ...], and to its own lengths[i] tokens:
+ *     z_j = scale q[i, h] . k_j[g];   o[i, h] = sum_j exp(z_j - lse[i, h]) v_j[g];   lse[i, h] = log sum_j exp(z_j),   g = h / (Hq / Hkv).
+ * A rollout without any key gets o = 0, lse = -inf; rows of rollouts that are not kept are not written.  A prompt's pages are read once for all of its live rollouts (up to
+ * 64 query rows, rollouts x Hq / Hkv, per key head).  Without prompts: prompt_table, prompt_lengths NULL, P = 0.  Products of q and e4m3 numbers are exact (q is split in
+ * two 8-bit parts; entries below 2^-22 of their row's largest are cut there), sums fp32; probabilities are rounded to fp16 before the product with values.  Every sum
+ * has a fixed order, so equal calls give equal bits.
+ *
+ * D a multiple of 16, 16 <= D <= 128; Hq a multiple of Hkv, Hq / Hkv <= 64; G <= 1024, N <= 2^24; pages, page_table entries < 2^31; scale finite, above 0; bf16 tensors as in
+ * the attention calls.  A length that is negative or more than its table row holds, fewer tokens than new ones, or a page number outside [0, pages) is not followed (in
+ * attention a sequence or prompt with such a length counts as empty, and what rollouts over such pages get is not defined) and ARROL_DEV_BAD_INDEX is recorded.  The calls use nothing of the context's buffers and may be captured;
+ * workspace: arrol_cache_attention_workspace(...) bytes, 256-byte aligned, contents need not be initialised or kept. */
+typedef struct arrol_cache {
+    void *k_cache, *v_cache;
+    int64_t k_page_stride, v_page_stride;
+    float *k_scale, *v_scale;
+    int64_t k_scale_stride, v_scale_stride;
+    int32_t pages, page, Hkv, D;
+} arrol_cache;
+typedef struct arrol_cache_append_args {
+    arrol_cache cache;
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    void *q_out, *k_out;
+    int64_t q_out_stride, k_out_stride;
+    const int32_t* page_table;
+    int64_t table_stride;
+    const int32_t* lengths;
+    const int64_t* cu_new;
+    const uint8_t* keep;
+    const int32_t* prompt_lengths;
+    const double* frequencies;
+    int64_t rows;
+    int32_t table_pages, N, P, G, Hq, R, interleaved;
+    float factor;
+} arrol_cache_append_args;
+int arrol_cache_append(arrol_ctx* ctx, const arrol_cache_append_args* args, void* stream);
+typedef struct arrol_cache_attention_args {
+    arrol_cache cache;
+    const void* q;
+    int64_t q_stride;
+    const int32_t* page_table;
+    int64_t table_stride;
+    const int32_t* lengths;
+    const uint8_t* keep;
+    const int32_t* prompt_table;
+    int64_t prompt_table_stride;
+    const int32_t* prompt_lengths;
+    int32_t table_pages, prompt_table_pages, N, P, G, Hq;
+    float scale;
+    int32_t reserved;
+    void* o;
+    int64_t o_stride;
+    float* lse;
+    void* workspace;
+    size_t workspace_bytes;
+} arrol_cache_attention_args;
+size_t arrol_cache_attention_workspace(arrol_ctx* ctx, int32_t N, int32_t P, int32_t G, int32_t Hq, int32_t Hkv, int32_t D);
+int arrol_cache_attention(arrol_ctx* ctx, const arrol_cache_attention_args* args, void* stream);
+
 /* ---- Trace confidence (Section 3 "Trace Confidence") ---------------------------------------------------------
  * arrol_token_logprob_conf: arrol_token_logprob with one more output from the same launch, the token confidence
  *     token_conf[t] = H_t = - sum_{v < V} log P_t(v) = V lse[t] - sum_v z_{t,v}     (float [T_max], rows t < T)

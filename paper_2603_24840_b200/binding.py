@@ -30,6 +30,8 @@ EXPORTS = [
     "arrol_token_logprob_gathered", "arrol_token_logprob_gathered_workspace",
     "arrol_attention_workspace", "arrol_attention", "arrol_attention_backward", "arrol_attention_decode_workspace",
     "arrol_attention_decode",
+    "arrol_rotary_frequencies", "arrol_rotary", "arrol_rotary_backward", "arrol_cache_append", "arrol_cache_attention_workspace",
+    "arrol_cache_attention",
 ]
 
 

@@ -1,0 +1,347 @@
+// arrol_cache_append: new tokens' keys and values into the paged 8-bit cache, keys and queries turned by their positions on the way.
+//
+// Bound by HBM where there are many tokens (bf16 in, 8 bits out, queries in and out), by one launch and a chain of dependent loads (length, page number, scale) where
+// there are few.  A page's scale needs the largest entry of all of its new tokens before the first can be rounded, so a page and head belong to one block
+// (append_runs_kernel: runs of tokens) or one warp (append_one_kernel: a token per sequence), which holds the turned values in registers in between: nothing is read
+// twice, and no atomics take part.
+#include "cache_common.cuh"
+#include "rotary_common.cuh"
+
+namespace {
+
+constexpr int ONE_WARPS = 4;
+constexpr int64_t APPEND_MAX_ROWS = ((int64_t)1 << 31) - 512;
+
+struct AppendParams {
+    arrol_cache_append_args a;
+    RotaryPairs pairs;
+    int units;                     // of a head (append_runs_kernel)
+    int passes;                    // of a block over a page's units
+    uint32_t* status;
+};
+
+// Page and first new token of a sequence whose new tokens are `fresh`; false where there is nothing to write.
+__device__ __forceinline__ bool append_start(const arrol_cache_append_args& a, int i, int64_t fresh, int64_t& start, int& len, bool& bad) {
+    len = cache_tokens(a.lengths, i, a.table_pages, a.cache.page, bad);
+    start = len - fresh;
+    if (start < 0) { bad = true; return false; }
+    return fresh > 0;
+}
+__device__ __forceinline__ bool append_page(const arrol_cache_append_args& a, int i, int64_t ordinal, int& page, bool& bad) {
+    page = a.page_table[(int64_t)i * a.table_stride + ordinal];
+    if (page < 0 || page >= a.cache.pages) { bad = true; return false; }
+    return true;
+}
+__device__ __forceinline__ int64_t append_offset(const arrol_cache_append_args& a, int i) { return a.prompt_lengths ? a.prompt_lengths[i / a.G] : 0; }
+
+// Numbers of `bytes` bytes (a multiple of 16) times 2^-shift, by threads `at`, `at + step`, ...: exact but for those that become subnormal.
+__device__ __forceinline__ void append_rescale(uint8_t* page, int bytes, float by, int at, int step) {
+    for (int x = at * 16; x < bytes; x += step * 16) {
+        uint4 w = *reinterpret_cast<uint4*>(page + x);
+        uint32_t* u = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 a = e4m3_pair_to_float((uint16_t)u[j]), b = e4m3_pair_to_float((uint16_t)(u[j] >> 16));
+            u[j] = e4m3_pair(a.x * by, a.y * by) | (uint32_t)e4m3_pair(b.x * by, b.y * by) << 16;
+        }
+        *reinterpret_cast<uint4*>(page + x) = w;
+    }
+}
+// Scale of a page and head whose new entries are `amax` at most, `old` before: the exponent, and whether what the page holds moves to it.
+__device__ __forceinline__ int append_exponent(float amax, int slot, float old, bool& grows) {
+    const int e = cache_exponent(amax);
+    grows = false;
+    if (slot == 0) return e;
+    const int had = (int)(__float_as_uint(old) >> 23 & 255u) - 127;
+    if (had >= e) return had > 127 ? 127 : had;              // 127: not a scale that was written here
+    grows = true;
+    return e;
+}
+
+// ---- one token per sequence: a warp per (sequence, head of q, k or v), four dimensions a lane
+__global__ void __launch_bounds__(32 * ONE_WARPS) append_one_kernel(const AppendParams p) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const arrol_cache_append_args& a = p.a;
+    const int lane = threadIdx.x & 31, tasks = 2 * a.cache.Hkv + (a.q ? a.Hq : 0), D = a.cache.D;
+    const int64_t item = (int64_t)blockIdx.x * ONE_WARPS + (threadIdx.x >> 5);
+    const int64_t seq = item / tasks;
+    if (seq >= a.N) return;
+    const int i = (int)seq, task = (int)(item - seq * tasks);
+    if (a.keep && !a.keep[i]) return;
+    // keys, then values, then queries
+    const bool value = task >= a.cache.Hkv && task < 2 * a.cache.Hkv, query = task >= 2 * a.cache.Hkv;
+    const int h = query ? task - 2 * a.cache.Hkv : value ? task - a.cache.Hkv : task;
+    const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(query ? a.q : value ? a.v : a.k) + (query ? a.q_stride : value ? a.v_stride : a.k_stride) * i + (int64_t)h * D;
+    const int d0 = lane * 4;
+    float y[4] = {0.f, 0.f, 0.f, 0.f};
+    if (d0 < D) chunk_to_floats<4>(*reinterpret_cast<const uint2*>(x + d0), y);
+    float partner[4];
+    bool turns[4];
+    const int R = value ? 0 : p.pairs.R;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int d = d0 + j;
+        turns[j] = d < R;
+        partner[j] = turns[j] ? __bfloat162float(x[p.pairs.interleaved ? d ^ 1 : d < R / 2 ? d + R / 2 : d - R / 2]) : 0.f;
+    }
+    bool bad = false;
+    int64_t start;
+    int len, page = 0;
+    bool ok = append_start(a, i, 1, start, len, bad);
+    const int64_t position = start + append_offset(a, i);
+    if (ok && !query) ok = append_page(a, i, start / a.cache.page, page, bad);
+    if (bad && lane == 0) atomicOr(p.status, ARROL_DEV_BAD_INDEX);
+    if (!ok) return;
+    const int slot = (int)(start % a.cache.page);
+    float* const scale = query ? nullptr : value ? a.cache.v_scale + page * a.cache.v_scale_stride + h : a.cache.k_scale + page * a.cache.k_scale_stride + h;
+    const float old = query || slot == 0 ? 0.f : *scale;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (turns[j]) {
+            const int d = d0 + j;
+            const bool first = p.pairs.interleaved ? (d & 1) == 0 : d < R / 2;
+            const float2 cs = rotary_cos_sin(p.pairs, p.pairs.interleaved ? d >> 1 : first ? d : d - R / 2, position);
+            y[j] = first ? rotary_first(y[j], partner[j], cs) : rotary_second(partner[j], y[j], cs);
+        }
+    __syncwarp();                                            // in place: every lane has read its partners
+    if (query || (!value && a.k_out)) {
+        __nv_bfloat16* to = query ? static_cast<__nv_bfloat16*>(a.q_out) + a.q_out_stride * i : static_cast<__nv_bfloat16*>(a.k_out) + a.k_out_stride * i;
+        if (d0 < D) *reinterpret_cast<uint2*>(to + (int64_t)h * D + d0) = floats_to_chunk<4>(y);
+    }
+    if (query) return;
+    float amax = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) amax = finite_max(amax, y[j]);
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
+    bool grows;
+    const int e = append_exponent(amax, slot, old, grows);
+    uint8_t* const codes = static_cast<uint8_t*>(value ? a.cache.v_cache : a.cache.k_cache) + page * (value ? a.cache.v_page_stride : a.cache.k_page_stride) +
+                           (int64_t)h * a.cache.page * D;
+    if (grows) append_rescale(codes, slot * D, old * cache_power(-e), lane, 32);
+    const float by = cache_power(-e);
+    if (d0 < D)
+        *reinterpret_cast<uint32_t*>(codes + slot * D + d0) = e4m3_pair(y[0] * by, y[1] * by) | (uint32_t)e4m3_pair(y[2] * by, y[3] * by) << 16;
+    if (lane == 0 && (slot == 0 || grows)) *scale = cache_power(e);
+}
+
+// ---- runs of tokens: a block per page that gets some (and part of the heads); a thread has one unit of one token, its angles in registers, and goes through the heads
+// A unit of token `tok` of the page, turned; nothing where the token is none of the run's.
+template <int V>
+__device__ __forceinline__ void append_load(const AppendParams& p, const RotaryUnit<V>& unit, const __nv_bfloat16* row, bool turn, float (&x)[V], float (&y)[V]) {
+    typedef typename Bf16Chunk<V>::type Chunk;
+    chunk_to_floats<V>(*reinterpret_cast<const Chunk*>(row + unit.a), x);
+    chunk_to_floats<V>(*reinterpret_cast<const Chunk*>(row + unit.b), y);
+    if (turn) unit.turn(p.pairs, x, y);
+}
+template <int V>
+__device__ __forceinline__ void append_codes(uint8_t* to, const float (&x)[V], float by) {
+    if constexpr (V == 1) {
+        *to = (uint8_t)e4m3_pair(x[0] * by, 0.f);
+    } else if constexpr (V == 2) {
+        *reinterpret_cast<uint16_t*>(to) = e4m3_pair(x[0] * by, x[1] * by);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; j += 4)
+            *reinterpret_cast<uint32_t*>(to + j) = e4m3_pair(x[j] * by, x[j + 1] * by) | (uint32_t)e4m3_pair(x[j + 2] * by, x[j + 3] * by) << 16;
+    }
+}
+template <>
+__device__ __forceinline__ void append_codes<8>(uint8_t* to, const float (&x)[8], float by) {
+    uint2 w;
+    w.x = e4m3_pair(x[0] * by, x[1] * by) | (uint32_t)e4m3_pair(x[2] * by, x[3] * by) << 16;
+    w.y = e4m3_pair(x[4] * by, x[5] * by) | (uint32_t)e4m3_pair(x[6] * by, x[7] * by) << 16;
+    *reinterpret_cast<uint2*>(to) = w;
+}
+
+template <int V, int THREADS>
+__global__ void __launch_bounds__(THREADS) append_runs_kernel(const AppendParams p) {
+    typedef typename Bf16Chunk<V>::type Chunk;
+    __shared__ float2 most[2][32];                           // per warp: largest of the keys, of the values
+    pdl_launch_dependents();
+    pdl_wait();
+    const arrol_cache_append_args& a = p.a;
+    const int page_size = a.cache.page, D = a.cache.D, Hkv = a.cache.Hkv, warps = blockDim.x >> 5;
+    const int64_t* cu = pdl_acquire(a.cu_new);
+    // Sequence i has the blocks from cu[i] / page + 2 i on: a run of n tokens touches n / page + 2 pages at most, whatever slot it begins in.
+    const int64_t u = blockIdx.x;
+    const int64_t i64 = block_search(a.N, [&](int64_t i) { return cu[i + 1] / page_size + 2 * (i + 1) <= u; });
+    if (i64 >= a.N) return;
+    const int i = (int)i64;
+    if (a.keep && !a.keep[i]) return;
+    const int64_t row0 = cu[i], fresh = cu[i + 1] - row0;
+    bool bad = false;
+    int64_t start = 0;
+    int len = 0, page = 0;
+    bool ok = row0 >= 0 && fresh >= 0 && row0 + fresh <= a.rows;
+    if (!ok) bad = true;
+    ok = ok && append_start(a, i, fresh, start, len, bad);
+    const int64_t ordinal = start / page_size + u - (row0 / page_size + 2 * i64);
+    const int64_t from = ordinal * page_size > start ? ordinal * page_size : start, to = (ordinal + 1) * page_size < len ? (ordinal + 1) * page_size : len;
+    ok = ok && ordinal >= 0 && from < to;
+    if (ok) ok = append_page(a, i, ordinal, page, bad);
+    if (bad && threadIdx.x == 0) atomicOr(p.status, ARROL_DEV_BAD_INDEX);
+    if (!ok) return;
+    const int slot0 = (int)(from - ordinal * page_size), tokens = (int)(to - from);
+    const int64_t first_row = row0 + (from - start), first_position = from + append_offset(a, i);
+    // unit `x` of the page's tokens * units: token x / units
+    const int items = tokens * p.units;
+    int tok = threadIdx.x / p.units;
+    RotaryUnit<V> unit(p.pairs, threadIdx.x - tok * p.units);
+    bool mine = (int)threadIdx.x < items;
+    auto pass_to = [&](int pass) {                           // only where a page's units are more than the block's threads
+        const int x = threadIdx.x + pass * blockDim.x;
+        tok = x / p.units;
+        unit = RotaryUnit<V>(p.pairs, x - tok * p.units);
+        mine = x < items;
+        if (mine) unit.at(p.pairs, first_position + tok);
+    };
+    if (mine) unit.at(p.pairs, first_position + tok);
+    const __nv_bfloat16* const k = static_cast<const __nv_bfloat16*>(a.k) + first_row * a.k_stride;
+    const __nv_bfloat16* const v = static_cast<const __nv_bfloat16*>(a.v) + first_row * a.v_stride;
+    int turn = 0;
+    for (int h = blockIdx.y; h < Hkv; h += gridDim.y, turn ^= 1) {
+        float kx[V], ky[V], vx[V], vy[V];
+        float2 m = {0.f, 0.f};
+        float* const k_scale = a.cache.k_scale + page * a.cache.k_scale_stride + h;
+        float* const v_scale = a.cache.v_scale + page * a.cache.v_scale_stride + h;
+        const float2 old = slot0 ? make_float2(*k_scale, *v_scale) : make_float2(0.f, 0.f);
+        for (int pass = 0; pass < p.passes; ++pass) {
+            if (p.passes > 1) pass_to(pass);
+            if (mine) {
+                append_load<V>(p, unit, k + tok * a.k_stride + (int64_t)h * D, true, kx, ky);
+                append_load<V>(p, unit, v + tok * a.v_stride + (int64_t)h * D, false, vx, vy);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    m.x = finite_max(finite_max(m.x, kx[j]), ky[j]);
+                    m.y = finite_max(finite_max(m.y, vx[j]), vy[j]);
+                }
+            }
+        }
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1) {
+            m.x = fmaxf(m.x, __shfl_xor_sync(0xffffffffu, m.x, s));
+            m.y = fmaxf(m.y, __shfl_xor_sync(0xffffffffu, m.y, s));
+        }
+        if ((threadIdx.x & 31) == 0) most[turn][threadIdx.x >> 5] = m;
+        __syncthreads();                                     // the other of the two buffers is the next head's: one barrier a head
+        for (int w = 0; w < warps; ++w) {
+            const float2 o = most[turn][w];
+            m.x = fmaxf(m.x, o.x);
+            m.y = fmaxf(m.y, o.y);
+        }
+        bool k_grows, v_grows;
+        const int ke = append_exponent(m.x, slot0, old.x, k_grows), ve = append_exponent(m.y, slot0, old.y, v_grows);
+        uint8_t* const kc = static_cast<uint8_t*>(a.cache.k_cache) + page * a.cache.k_page_stride + (int64_t)h * page_size * D;
+        uint8_t* const vc = static_cast<uint8_t*>(a.cache.v_cache) + page * a.cache.v_page_stride + (int64_t)h * page_size * D;
+        const float kb = cache_power(-ke), vb = cache_power(-ve);
+        if (k_grows) append_rescale(kc, slot0 * D, old.x * kb, threadIdx.x, blockDim.x);
+        if (v_grows) append_rescale(vc, slot0 * D, old.y * vb, threadIdx.x, blockDim.x);
+        for (int pass = 0; pass < p.passes; ++pass) {
+            if (p.passes > 1) {
+                pass_to(pass);
+                if (mine) {
+                    append_load<V>(p, unit, k + tok * a.k_stride + (int64_t)h * D, true, kx, ky);
+                    append_load<V>(p, unit, v + tok * a.v_stride + (int64_t)h * D, false, vx, vy);
+                }
+            }
+            if (mine) {
+                const int at = (slot0 + tok) * D;
+                append_codes<V>(kc + at + unit.a, kx, kb);
+                append_codes<V>(kc + at + unit.b, ky, kb);
+                append_codes<V>(vc + at + unit.a, vx, vb);
+                append_codes<V>(vc + at + unit.b, vy, vb);
+                if (a.k_out) {
+                    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.k_out) + (first_row + tok) * a.k_out_stride + (int64_t)h * D;
+                    *reinterpret_cast<Chunk*>(out + unit.a) = floats_to_chunk<V>(kx);
+                    *reinterpret_cast<Chunk*>(out + unit.b) = floats_to_chunk<V>(ky);
+                }
+            }
+        }
+        if (threadIdx.x == 0) {
+            if (slot0 == 0 || k_grows) *k_scale = cache_power(ke);
+            if (slot0 == 0 || v_grows) *v_scale = cache_power(ve);
+        }
+    }
+    if (!a.q) return;
+    for (int pass = 0; pass < p.passes; ++pass) {
+        if (p.passes > 1) pass_to(pass);
+        if (!mine) continue;
+        const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.q) + (first_row + tok) * a.q_stride;
+        __nv_bfloat16* const qo = static_cast<__nv_bfloat16*>(a.q_out) + (first_row + tok) * a.q_out_stride;
+        constexpr int AT_ONCE = 4;
+        for (int h = blockIdx.y; h < a.Hq; h += gridDim.y * AT_ONCE) {
+            Chunk ca[AT_ONCE], cb[AT_ONCE];
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int hh = h + j * gridDim.y;
+                if (hh < a.Hq) {
+                    ca[j] = *reinterpret_cast<const Chunk*>(q + (int64_t)hh * D + unit.a);
+                    cb[j] = *reinterpret_cast<const Chunk*>(q + (int64_t)hh * D + unit.b);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int hh = h + j * gridDim.y;
+                if (hh < a.Hq) {
+                    float x[V], y[V];
+                    chunk_to_floats<V>(ca[j], x);
+                    chunk_to_floats<V>(cb[j], y);
+                    unit.turn(p.pairs, x, y);
+                    *reinterpret_cast<Chunk*>(qo + (int64_t)hh * D + unit.a) = floats_to_chunk<V>(x);
+                    *reinterpret_cast<Chunk*>(qo + (int64_t)hh * D + unit.b) = floats_to_chunk<V>(y);
+                }
+            }
+        }
+    }
+}
+
+}  // namespace
+
+extern "C" int arrol_cache_append(arrol_ctx* ctx, const arrol_cache_append_args* a, void* stream) {
+    if (!ctx || !a) return ARROL_ERR_INVALID_ARG;
+    const int cache = cache_check(a->cache);
+    if (cache == ARROL_ERR_INVALID_ARG) return cache;
+    if (a->N < 0 || a->P < 0 || a->rows < 0 || a->table_pages < 0 || a->table_stride < a->table_pages || a->R < 0 || a->R % 2 || a->R > a->cache.D || !isfinite(a->factor))
+        return ARROL_ERR_INVALID_ARG;
+    if ((a->R > 0) != (a->frequencies != nullptr) || !arrol_aligned(a->frequencies, 8)) return ARROL_ERR_INVALID_ARG;
+    if (a->P > 0 ? a->G < 1 || (int64_t)a->P * a->G != a->N || !a->prompt_lengths : a->prompt_lengths != nullptr) return ARROL_ERR_INVALID_ARG;
+    if (!a->cu_new && a->rows != a->N) return ARROL_ERR_INVALID_ARG;
+    if ((a->q != nullptr) != (a->q_out != nullptr) || (a->q && a->Hq < 1)) return ARROL_ERR_INVALID_ARG;
+    if (cache != ARROL_OK || a->N > (1 << 24) || a->rows >= APPEND_MAX_ROWS || (a->q && a->Hq > 65536)) return ARROL_ERR_UNSUPPORTED;
+    if (a->N == 0 || a->rows == 0) return ARROL_OK;
+    const int D = a->cache.D, Hkv = a->cache.Hkv;
+    if (a->cache.pages == 0 || !a->page_table || !a->lengths || a->table_pages == 0) return ARROL_ERR_INVALID_ARG;
+    if (!cache_rows_ok(a->k, a->k_stride, Hkv, D) || !cache_rows_ok(a->v, a->v_stride, Hkv, D)) return ARROL_ERR_INVALID_ARG;
+    if (a->q && (!cache_rows_ok(a->q, a->q_stride, a->Hq, D) || !cache_rows_ok(a->q_out, a->q_out_stride, a->Hq, D))) return ARROL_ERR_INVALID_ARG;
+    if (a->k_out && !cache_rows_ok(a->k_out, a->k_out_stride, Hkv, D)) return ARROL_ERR_INVALID_ARG;
+    if ((a->q && a->q == a->q_out && a->q_stride != a->q_out_stride) || (a->k_out == a->k && a->k_stride != a->k_out_stride)) return ARROL_ERR_INVALID_ARG;
+    AppendParams p = {};
+    p.a = *a;
+    p.pairs = {a->frequencies, a->R, a->interleaved != 0, a->factor, 1.0f};
+    p.status = ctx->d_status;
+    ArrolDeviceGuard guard(ctx->device);
+    if (!guard.ok) return ARROL_ERR_CUDA;
+    if (!a->cu_new) {
+        const int64_t warps = (int64_t)a->N * (2 * Hkv + (a->q ? a->Hq : 0));
+        if ((warps + ONE_WARPS - 1) / ONE_WARPS >= ((int64_t)1 << 31)) return ARROL_ERR_UNSUPPORTED;
+        ARROL_CUDA_OK(arrol_launch_pdl(append_one_kernel, dim3((unsigned)((warps + ONE_WARPS - 1) / ONE_WARPS)), dim3(32 * ONE_WARPS), 0, (cudaStream_t)stream, p));
+    } else {
+        const int V = rotary_vector(D, a->R);
+        p.units = D / (2 * V);
+        const int items = a->cache.page * p.units, threads = items > 1024 ? 1024 : (items + 31) & ~31;
+        p.passes = (items + threads - 1) / threads;
+        const int64_t pages = a->rows / a->cache.page + 2 * (int64_t)a->N;
+        // Enough blocks for two an SM at 512 threads each; as many heads a block as that leaves, for the angles are formed once a block.
+        const int most = a->q && a->Hq > Hkv ? a->Hq : Hkv;
+        int64_t split = (int64_t)(4 * ctx->sm_count) * 512 / threads / (a->rows / a->cache.page + 1);
+        split = split < 1 ? 1 : split > most ? most : split;
+        void (*kernel)(AppendParams);
+        if (threads <= 512) kernel = V == 8 ? append_runs_kernel<8, 512> : V == 4 ? append_runs_kernel<4, 512> : V == 2 ? append_runs_kernel<2, 512> : append_runs_kernel<1, 512>;
+        else kernel = V == 8 ? append_runs_kernel<8, 1024> : V == 4 ? append_runs_kernel<4, 1024> : V == 2 ? append_runs_kernel<2, 1024> : append_runs_kernel<1, 1024>;
+        ARROL_CUDA_OK(arrol_launch_pdl(kernel, dim3((unsigned)pages, (unsigned)split), dim3(threads), 0, (cudaStream_t)stream, p));
+    }
+    ctx->launches += 1;
+    return ARROL_OK;
+}
