@@ -16,12 +16,14 @@
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int CA_WARPS = 4, CA_THREADS = 32 * CA_WARPS;
+constexpr int CA_WARPS = 4, CA_THREADS = 32 * (CA_WARPS + 1);      // consumers; one more warp brings their pieces
 constexpr int CA_PER_SM = 2;                       // blocks
 constexpr int CA_ROWS = 64;                        // query rows of a shared unit
 constexpr int CA_ALONE = 16;                       // query rows up to which a unit is a warp's
-constexpr int CA_TOKENS = 32;                      // a warp's piece; a shared one is CA_WARPS of them
-constexpr int CA_SHARED_COST = 5;                  // of a shared piece, in single ones
+constexpr int CA_TOKENS = 32;                      // a single piece; a shared one is four of them, two for more than 32 rows, so that a warp has two to compute
+// The line that the work is cut along, in single pieces: what a shared piece costs, and what a unit costs before its first piece (queries, results) in pieces of its kind.
+constexpr int CA_SHARED_COST = 11, CA_SHARED_SETUP = 1, CA_SINGLE_SETUP = 3;
+constexpr int CA_SCANNED = 1024;                   // entries that a block keeps in shared memory between the two passes of its scan
 constexpr float CA_RESCALE_AT = 8.0f;              // the running maximum follows once it is 2^8 behind
 constexpr float CA_P_SCALE = 128.0f;               // probabilities up to 2^8 times 2^7 stay below fp16's largest
 
@@ -31,8 +33,8 @@ struct alignas(16) CacheEntry {
 };
 
 struct CacheWorkspace {
-    long long* head;           // [0] pieces of the shared line, [1] of the single one
-    long long* where;          // [entries]: where an entry's pieces begin on its line
+    long long* head;           // [0] length of the shared line, [1] of the single one, [2] cost that a block takes
+    int2* owners;              // [entries][Hkv]: the first and the last block (warp) that has some of the unit
     CacheEntry* shared;        // entries with pieces, in order
     CacheEntry* single;
     float2* ml;                // per record row: reference (of scores log2 e), sum
@@ -57,7 +59,7 @@ inline CacheWorkspace cache_workspace(void* base, int sm_count, int N, int P, in
     auto take = [&](size_t n) { uint8_t* q = p + at; at += (n + 255) & ~(size_t)255; return q; };
     const int64_t rows = w.rows_own + w.rows_prompt + w.rows_shared;
     w.head = reinterpret_cast<long long*>(take(256));
-    w.where = reinterpret_cast<long long*>(take((size_t)entries * sizeof(long long)));
+    w.owners = reinterpret_cast<int2*>(take((size_t)entries * Hkv * sizeof(int2)));
     w.shared = reinterpret_cast<CacheEntry*>(take((size_t)entries * sizeof(CacheEntry)));
     w.single = reinterpret_cast<CacheEntry*>(take((size_t)entries * sizeof(CacheEntry)));
     w.ml = reinterpret_cast<float2*>(take((size_t)rows * sizeof(float2)));
@@ -77,20 +79,19 @@ struct CacheParams {
 
 // ---- the line of pieces
 struct Line {
-    long long shared, single;      // pieces
+    long long shared, single;      // lengths: units' pieces and setups
     long long per;                 // cost that a block takes
 };
 __device__ __forceinline__ Line make_line(long long shared, long long single, int grid) {
     const long long cost = shared * CA_SHARED_COST + single;
     return {shared, single, cost <= grid ? 1 : (cost + grid - 1) / grid};
 }
-// shared pieces from there on are block b's or a later one's
+// the shared line from there on is block b's or a later one's
 __device__ __forceinline__ long long shared_begin(const Line& l, long long b) {
     const long long x = (b * l.per + CA_SHARED_COST - 1) / CA_SHARED_COST;
     return x < l.shared ? x : l.shared;
 }
-__device__ __forceinline__ long long shared_block(const Line& l, long long x) { return x * CA_SHARED_COST / l.per; }
-// single pieces of block b, before they are cut to those that there are, and of each of its warps
+// block b's part of the single line, before it is cut to what there is, and that of each of its warps
 __device__ __forceinline__ void single_range(const Line& l, long long b, long long& lo, long long& each) {
     const long long at = l.shared * CA_SHARED_COST;
     lo = b * l.per - at;
@@ -107,13 +108,6 @@ __device__ __forceinline__ void warp_range(const Line& l, long long warp, long l
     y0 = lo + k * each;
     y1 = y0 + each < hi ? y0 + each : hi;
 }
-__device__ __forceinline__ long long single_warp(const Line& l, long long y) {
-    const long long b = (l.shared * CA_SHARED_COST + y) / l.per;
-    long long lo, each;
-    single_range(l, b, lo, each);
-    return b * CA_WARPS + (y - lo) / each;
-}
-
 // Live rollouts of group p.
 __device__ __forceinline__ int live_of(const CacheParams& p, int q) {
     const int G = p.a.G;
@@ -129,27 +123,34 @@ __device__ __forceinline__ int live_of(const CacheParams& p, int q) {
     for (; i < G; ++i) n += keep[i] != 0;
     return n;
 }
-__device__ __forceinline__ CacheEntry make_entry(const CacheParams& p, int e, bool& bad) {
+// Parts of 32 tokens of a piece.
+__device__ __forceinline__ int piece_parts(int rows) { return rows > 32 ? 2 : rows > CA_ALONE ? 4 : 1; }
+__device__ __forceinline__ int entry_pieces(int rows, int tokens) {
+    const int of = CA_TOKENS * piece_parts(rows);             // a power of two
+    return (int)(((int64_t)tokens + of - 1) / of);
+}
+__device__ __forceinline__ int unit_setup(int rows) { return rows > CA_ALONE ? CA_SHARED_SETUP : CA_SINGLE_SETUP; }
+// {tokens, rows} of an entry; no rows where it is left out.
+__device__ __forceinline__ int2 entry_size(const CacheParams& p, int e, bool& bad) {
     const arrol_cache_attention_args& a = p.a;
-    CacheEntry x = {e, 0, 0, 0};
     if (e < p.prompts) {
         const int q = e / p.blocks, rollouts = min(live_of(p, q) - (e - q * p.blocks) * p.group, p.group);
-        if (rollouts <= 0) return x;
-        x.rows = rollouts * p.ratio;
-        x.tokens = cache_tokens(a.prompt_lengths, q, a.prompt_table_pages, a.cache.page, bad);
-    } else {
-        const int i = e - p.prompts;
-        if (a.keep && !a.keep[i]) return x;
-        x.rows = p.ratio;
-        x.tokens = cache_tokens(a.lengths, i, a.table_pages, a.cache.page, bad);
+        bool wrong = false;
+        const int tokens = cache_tokens(a.prompt_lengths, q, a.prompt_table_pages, a.cache.page, wrong);
+        if (rollouts <= 0) return make_int2(0, 0);
+        bad |= wrong;
+        return make_int2(tokens, rollouts * p.ratio);
     }
-    const int of = x.rows > CA_ALONE ? CA_TOKENS * CA_WARPS : CA_TOKENS;
-    x.pieces = (int)(((int64_t)x.tokens + of - 1) / of);
-    return x;
+    const int i = e - p.prompts;
+    bool wrong = false;
+    const int tokens = cache_tokens(a.lengths, i, a.table_pages, a.cache.page, wrong);      // asked for with the mask, not behind it
+    if (a.keep && !a.keep[i]) return make_int2(0, 0);
+    bad |= wrong;
+    return make_int2(tokens, p.ratio);
 }
 
 struct ScanSums {
-    long long shared, single;      // pieces
+    long long shared, single;      // lengths of the lines
     int shared_entries, single_entries;
 };
 __device__ __forceinline__ ScanSums operator+(const ScanSums& a, const ScanSums& b) {
@@ -160,31 +161,49 @@ __device__ __forceinline__ ScanSums shfl_up(const ScanSums& a, int d) {
             __shfl_up_sync(0xffffffffu, a.single_entries, d)};
 }
 
+// Where a block (warp) begins: an entry, its number in the list, how much of it lies before.
 struct Start {
-    int entry;                     // number in the list
-    long long offset;              // pieces of it before
+    CacheEntry e;
+    long long offset;
+    int number;
 };
 
-__device__ __forceinline__ void cp_async_zfill_16(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+// bytes that the barrier's phase waits for, without an arrival
+__device__ __forceinline__ void mbar_expect_bytes(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void cp_async_zfill_8(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(there ? 8 : 0) : "memory");
+__device__ __forceinline__ void mbar_arrive_n(uint64_t* bar, uint32_t n) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(n) : "memory");
 }
-__device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int y, int z, int w, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// Four 8 x 16 byte matrices as they lie: a lane (g, t) gets bytes 4 t .. 4 t + 3 of row g of each.
+__device__ __forceinline__ void ldmatrix_rows(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// Two 16 x 16 byte matrices transposed: a lane gets bytes g and g + 8 of rows 4 t .. 4 t + 3, a register each.
+__device__ __forceinline__ void ldmatrix_columns(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
 
-__device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// An 8 x 8 matrix of pairs of halves transposed: from (row g, columns 2 t and the next) to (column g, rows 2 t and the next).
+__device__ __forceinline__ uint32_t transpose_halves(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+// Four numbers of each of two registers as an operand of sixteen rows: (row g, first two), (row g + 8, first two), (row g, others), (row g + 8, others).
+__device__ __forceinline__ void widen(uint32_t (&a)[4], uint32_t v0, uint32_t v1) {
+    a[0] = e4m3_pair_to_half((uint16_t)v0);
+    a[1] = e4m3_pair_to_half((uint16_t)v1);
+    a[2] = e4m3_pair_to_half((uint16_t)(v0 >> 16));
+    a[3] = e4m3_pair_to_half((uint16_t)(v1 >> 16));
 }
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     uint32_t r;
@@ -192,306 +211,339 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     return r;
 }
 
-// What a warp copies and reads of 32 tokens.  Keys: a lane (g, t) = (lane / 4, lane % 4) has, of the tokens 8 j + g, the 16-byte chunks t and t + 4 of their rows; as the
-// order of a product's dimensions is free as long as q has the same, these are the operand registers of two (DP = 64) or four products.  Values: of the tokens that the
-// lane's own columns of the scores are, 8 j + 2 t and the next, the dimensions VB g .. VB g + VB - 1.  Each lane reads what it copied, 16 (8) bytes beside its neighbours'.
+// A stage: 32 tokens' keys, then their values, as rows of DP bytes, swizzled by the copies over as many (chunk c of 16 bytes of row r lies where c ^ swizzle(r) would), and
+// the four scales (keys' of the first and the second 16 tokens, values') in front of the ring.
 template <int DP>
 struct CacheConf {
-    static constexpr int CHUNKS = DP / 64;                        // of keys, per token and lane
-    static constexpr int VB = DP / 8;                             // bytes of a token's values, per lane
-    static constexpr int KEYS = CA_TOKENS * DP, BYTES = 2 * KEYS + 128;      // scales behind: keys' of the first and second 16 tokens, values'
+    static constexpr int KEYS = CA_TOKENS * DP, BYTES = 2 * KEYS;
     static constexpr int STAGES = DP == 128 ? 3 : 4;
-    static constexpr int NT = DP / 8;
-    static constexpr size_t SMEM = (size_t)STAGES * CA_WARPS * BYTES;
+    static constexpr int CHUNKS = DP / 16;
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * CA_WARPS * BYTES;
+    static __device__ __forceinline__ uint32_t at(int row, int chunk) { return row * DP + ((chunk ^ (DP == 128 ? row & 7 : row >> 1 & 3)) << 4); }
 };
 
-// Walks over a line's pieces.  What comes next is asked for before it is needed.
+// Walks over a part of a line, piece by piece.  What comes next is asked for before it is needed.
 struct Cursor {
     CacheEntry e, next;
     const CacheEntry* list;
+    long long left;                // of the part, from the piece that the cursor is at on
     int number, last;              // of the list's entries
-    int head, piece;
+    int head, piece, setup;
     __device__ __forceinline__ void fetch() {
         if (number + 1 <= last) next = list[number + 1];
     }
-    __device__ __forceinline__ void begin(const CacheEntry* l, const Start& s, int n) {
+    __device__ __forceinline__ void begin(const CacheEntry* l, const Start& s, int entries, long long length) {
         list = l;
-        number = s.entry;
-        last = n - 1;
-        e = list[number];
-        head = (int)(s.offset / e.pieces);
-        piece = (int)(s.offset - (long long)head * e.pieces);
+        e = s.e;
+        number = s.number;
+        last = entries - 1;
+        left = length;
+        setup = unit_setup(e.rows);
+        head = (int)(s.offset / (e.pieces + setup));
+        piece = (int)(s.offset - (long long)head * (e.pieces + setup)) - setup;
+        if (piece < 0) { left += piece; piece = 0; }
         fetch();
     }
     __device__ __forceinline__ void advance(int heads) {
+        --left;
         if (++piece < e.pieces) return;
         piece = 0;
+        left -= setup;
         if (++head < heads) return;
         head = 0;
         e = next;
         ++number;
         fetch();
     }
+    // whether the piece is the part's last one
+    __device__ __forceinline__ bool is_last() const { return left == 1 || (piece == e.pieces - 1 && left <= 1 + setup); }
 };
 
-// The rows of the page table that an entry follows.
-__device__ __forceinline__ const int32_t* entry_table(const CacheParams& p, int e) {
-    return e < p.prompts ? p.a.prompt_table + (int64_t)(e / p.blocks) * p.a.prompt_table_stride : p.a.page_table + (int64_t)(e - p.prompts) * p.a.table_stride;
-}
+// Pages of the first and the second 16 tokens from `tok` on, -1 where there are none.
 struct PagePair {
-    int first, second;             // pages of the piece's first and second 16 tokens, -1 where there are none
+    int first, second;
 };
 __device__ __forceinline__ PagePair find_pages(const CacheParams& p, const Cursor& c, int tok) {
-    const int32_t* table = entry_table(p, c.e.entry);
+    const int32_t* table = c.e.entry < p.prompts ? p.a.prompt_table + (int64_t)(c.e.entry / p.blocks) * p.a.prompt_table_stride
+                                                 : p.a.page_table + (int64_t)(c.e.entry - p.prompts) * p.a.table_stride;
     PagePair g = {-1, -1};
     if (tok < c.e.tokens) g.first = table[tok >> p.page_shift];
-    if (tok + 16 < c.e.tokens) g.second = table[(tok + 16) >> p.page_shift];
+    if (tok + 16 < c.e.tokens) g.second = p.page_shift > 4 ? g.first : table[(tok >> 4) + 1];
     return g;
 }
 
-template <int DP>
-__device__ __forceinline__ void copy_piece(const CacheParams& p, const Cursor& c, int tok, PagePair pages, uint8_t* stage, int lane) {
-    using C = CacheConf<DP>;
-    const arrol_cache& cache = p.a.cache;
-    const int D = cache.D, g = lane >> 2, t = lane & 3, there = c.e.tokens - tok, in_page = cache.page - 1;
-    if ((pages.first < 0 && there > 0) || pages.first >= cache.pages || (pages.second < 0 && there > 16) || pages.second >= cache.pages) {
-        if (lane == 0) atomicOr(p.status, ARROL_DEV_BAD_INDEX);
-        if ((unsigned)pages.first >= (unsigned)cache.pages) pages.first = -1;
-        if ((unsigned)pages.second >= (unsigned)cache.pages) pages.second = -1;
-    }
-    const uint32_t to = smem_u32(stage) + lane * 16;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int page = half ? pages.second : pages.first, slot = (tok + half * 16) & in_page, left = there - half * 16;
-        const bool is = page >= 0;
-        const int64_t at = (int64_t)c.head * cache.page * D + slot * D;
-        const uint8_t* const none = reinterpret_cast<const uint8_t*>(p.w.head);       // of a copy that reads nothing
-        const uint8_t* k = is ? static_cast<const uint8_t*>(cache.k_cache) + page * cache.k_page_stride + at : none;
-        const uint8_t* v = is ? static_cast<const uint8_t*>(cache.v_cache) + page * cache.v_page_stride + at : none;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int token = 8 * j + g;
-            const bool copy = is && token < left;
-#pragma unroll
-            for (int x = 0; x < C::CHUNKS; ++x)
-                if ((t + 4 * x) * 16 < D) cp_async_zfill_16(to + ((half * 2 + j) * C::CHUNKS + x) * 512, k + (copy ? token * D + (t + 4 * x) * 16 : 0), copy);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int token = (j >> 1) * 8 + 2 * t + (j & 1);
-            const bool copy = is && token < left;
-            if (g * C::VB < D) {
-                const uint8_t* from = v + (copy ? token * D + g * C::VB : 0);
-                if (C::VB == 16) cp_async_zfill_16(to + C::KEYS + (half * 4 + j) * 512, from, copy);
-                else cp_async_zfill_8(smem_u32(stage) + C::KEYS + (half * 4 + j) * 256 + lane * 8, from, copy);
-            }
-        }
-        if (lane < 2) {                                       // lane 0 the keys' scale, lane 1 the values'
-            uint8_t* s = stage + 2 * C::KEYS + lane * 8 + half * 4;
-            if (is) cp_async_4(smem_u32(s), lane ? cache.v_scale + page * cache.v_scale_stride + c.head : cache.k_scale + page * cache.k_scale_stride + c.head);
-            else *reinterpret_cast<float*>(s) = lane ? 0.f : -1.f;
-        }
-    }
-}
+// What a consumer has to know of a piece.
+struct alignas(16) PieceInfo {
+    float scales[4];               // of the keys of the first and the second 16 tokens (below 0: none there), of the values
+    int entry, head, there, flags; // there: tokens from its first one to the entry's end
+};
+// The first and the last of a unit in this block or warp; of the unit; no piece, but the end; query rows from bit 8 on.
+constexpr int PIECE_FIRST = 1, PIECE_LAST = 2, PIECE_BEGIN = 4, PIECE_END = 8, PIECE_NONE = 16, PIECE_ROWS = 8;
 
-// A tile of up to 16 query rows against the pieces of its unit.  Rows g and g + 8 of the tile are this lane's.
+// A piece on its way: first its page numbers are asked for, then, a piece later, its scales, then its copies.
+struct Fetch {
+    PagePair pages;
+    int tok;
+    PieceInfo info;
+    __device__ __forceinline__ void find(const CacheParams& p, const Cursor& c, int token, bool first) {
+        tok = token;
+        pages = find_pages(p, c, token);
+        info.entry = c.e.entry;
+        info.head = c.head;
+        info.there = c.e.tokens - token;
+        info.flags = (first || c.piece == 0 ? PIECE_FIRST : 0) | (c.piece == 0 ? PIECE_BEGIN : 0) | (c.piece == c.e.pieces - 1 ? PIECE_LAST | PIECE_END : 0) |
+                     (c.is_last() ? PIECE_LAST : 0) | c.e.rows << PIECE_ROWS;
+    }
+    __device__ __forceinline__ void find_scales(const CacheParams& p) {
+        const arrol_cache& c = p.a.cache;
+        if ((pages.first < 0 && info.there > 0) || pages.first >= c.pages || (pages.second < 0 && info.there > 16) || pages.second >= c.pages) {
+            atomicOr(p.status, ARROL_DEV_BAD_INDEX);
+            if (pages.first >= c.pages) pages.first = -1;
+            if (pages.second >= c.pages) pages.second = -1;
+        }
+        info.scales[0] = info.scales[1] = -1.f;
+        info.scales[2] = info.scales[3] = 0.f;
+        if (pages.first >= 0) {
+            info.scales[0] = c.k_scale[pages.first * c.k_scale_stride + info.head];
+            info.scales[2] = c.v_scale[pages.first * c.v_scale_stride + info.head];
+        }
+        if (pages.second >= 0) {
+            info.scales[1] = c.k_scale[pages.second * c.k_scale_stride + info.head];
+            info.scales[3] = c.v_scale[pages.second * c.v_scale_stride + info.head];
+        }
+    }
+    // The copies; the arrival that lets the stage be read is the caller's.
+    template <int DP>
+    __device__ __forceinline__ void copy(const CacheParams& p, const CUtensorMap* map_k, const CUtensorMap* map_v, uint32_t to, uint64_t* full) const {
+        using C = CacheConf<DP>;
+        const bool whole = p.page_shift > 4;                  // 32 tokens side by side
+        if (pages.first >= 0) {
+            const int slot = tok & (p.a.cache.page - 1);
+            mbar_expect_bytes(full, whole ? C::BYTES : C::KEYS);
+            tma_load_4d(to, map_k, slot, info.head, pages.first, full);
+            tma_load_4d(to + C::KEYS, map_v, slot, info.head, pages.first, full);
+        }
+        if (!whole && pages.second >= 0) {
+            mbar_expect_bytes(full, C::KEYS);
+            tma_load_4d(to + C::KEYS / 2, map_k, 0, info.head, pages.second, full);
+            tma_load_4d(to + C::KEYS + C::KEYS / 2, map_v, 0, info.head, pages.second, full);
+        }
+    }
+};
+
+// A tile of up to 16 query rows against the pieces of its unit, transposed: tokens (and dimensions) are the sixteen rows of a product, query rows its eight columns, so that eight
+// query heads waste nothing.  A lane (g, t) = (lane / 4, lane % 4) has the scores of query rows 2 t and 2 t + 1 (of each eight) with tokens g and, of the second eight of
+// sixteen, 8 + (g + 4) % 8: in that order eight rows of keys, and the sixteen of values that a lane's four scores belong to, are read without two in a bank.
 template <int DP>
 struct RowTile {
     using C = CacheConf<DP>;
-    uint32_t q[2][DP / 32][4];        // rows 0 .. 7 and 8 .. 15 as operands: upper parts above, lower parts below
-    float by[2];                      // what a product's sum times the key's scale is multiplied by
-    float o[C::NT][4], m[2], l[2];
+    uint32_t q[C::CHUNKS][2][2];      // per 16 dimensions and eight rows: row g's dimensions 4 t .. 4 t + 3
+    float by[2][2];                   // what a product's sum times the key's scale is multiplied by
+    float o[C::CHUNKS][2][4], m[2][2], l[2][2];
     float v_scale;                    // largest scale of the values so far: o is in units of it / CA_P_SCALE
 
-    __device__ __forceinline__ void load(const CacheParams& p, int lane, const __nv_bfloat16* row0, const __nv_bfloat16* row1) {
+    // `row`: this lane's row g, or null; r: of the first or the second eight
+    __device__ __forceinline__ void load(const CacheParams& p, int lane, const __nv_bfloat16* row, int r) {
         const int t = lane & 3, D = p.a.cache.D;
+        uint2 raw[C::CHUNKS];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const __nv_bfloat16* row = r ? row1 : row0;
-            uint32_t raw[C::CHUNKS][8];
+        for (int x = 0; x < C::CHUNKS; ++x) raw[x] = row && x * 16 < D ? *reinterpret_cast<const uint2*>(row + x * 16 + t * 4) : make_uint2(0, 0);
+        {
             float most = 0.f, odd = 0.f;
 #pragma unroll
-            for (int x = 0; x < C::CHUNKS; ++x) {
-                const bool there = row && (t + 4 * x) * 16 < D;
+            for (int x = 0; x < C::CHUNKS; ++x)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const uint4 w = there ? *reinterpret_cast<const uint4*>(row + (t + 4 * x) * 16 + y * 8) : make_uint4(0, 0, 0, 0);
-                    raw[x][y * 4] = w.x; raw[x][y * 4 + 1] = w.y; raw[x][y * 4 + 2] = w.z; raw[x][y * 4 + 3] = w.w;
-                }
-#pragma unroll
-                for (int y = 0; y < 8; ++y) {
-                    const float a = __uint_as_float(raw[x][y] << 16), b = __uint_as_float(raw[x][y] & 0xFFFF0000u);
+                    const uint32_t w = y ? raw[x].y : raw[x].x;
+                    const float a = __uint_as_float(w << 16), b = __uint_as_float(w & 0xFFFF0000u);
                     most = finite_max(finite_max(most, a), b);
                     odd += (a - a) + (b - b);                 // NaN where one is not finite
                 }
-            }
 #pragma unroll
             for (int s = 1; s < 4; s <<= 1) {
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
                 odd += __shfl_xor_sync(0xffffffffu, odd, s);
             }
-            const int e = cache_exponent(most);
-            const float down = cache_power(-e);
-            by[r] = cache_power(e) * p.scale_log2 + odd;      // a query that is not finite makes its scores NaN
+            const int e = cache_exponent(most) - 5;           // up to 448 x 2^5 = 14,336, a quarter of fp16's largest
+            const float down = cache_power(-e), mine = cache_power(e) * p.scale_log2 + odd;      // a query that is not finite makes its scores NaN
+            by[r][0] = __shfl_sync(0xffffffffu, mine, t * 8);
+            by[r][1] = __shfl_sync(0xffffffffu, mine, t * 8 + 4);
 #pragma unroll
             for (int x = 0; x < C::CHUNKS; ++x)
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {                 // four dimensions: registers (2 x + y / 2), rows above and below
-                    uint32_t upper = 0, lower = 0;
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const uint32_t w = raw[x][y * 2 + z];
-                        const float a = __uint_as_float(w << 16) * down, b = __uint_as_float(w & 0xFFFF0000u) * down;
-                        const uint16_t hi = e4m3_pair(a, b);
-                        const float2 h = e4m3_pair_to_float(hi);
-                        upper |= (uint32_t)hi << (z * 16);
-                        lower |= (uint32_t)e4m3_pair((a - h.x) * 16.f, (b - h.y) * 16.f) << (z * 16);
-                    }
-                    q[r][2 * x + (y >> 1)][(y & 1) * 2] = upper;
-                    q[r][2 * x + (y >> 1)][(y & 1) * 2 + 1] = lower;
+                for (int y = 0; y < 2; ++y) {
+                    const uint32_t w = y ? raw[x].y : raw[x].x;
+                    q[x][r][y] = pack_half(__uint_as_float(w << 16) * down, __uint_as_float(w & 0xFFFF0000u) * down);
                 }
         }
 #pragma unroll
-        for (int d = 0; d < C::NT; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f;
-        m[0] = m[1] = -INFINITY;
-        l[0] = l[1] = 0.f;
+        for (int c = 0; c < C::CHUNKS; ++c) o[c][r][0] = o[c][r][1] = o[c][r][2] = o[c][r][3] = 0.f;
+        m[r][0] = m[r][1] = -INFINITY;
+        l[r][0] = l[r][1] = 0.f;
         v_scale = 0.f;
     }
 
-    // `there` tokens of the piece (at least one).  BOTH: rows 8 .. 15 are there.
-    template <bool BOTH>
-    __device__ __forceinline__ void piece(const uint8_t* stage, int there, int lane) {
-        constexpr int ROWS = BOTH ? 2 : 1;
-        const int t = lane & 3;
-        const uint8_t* const mine = stage + lane * 16;
-        const float4 scales = *reinterpret_cast<const float4*>(stage + 2 * C::KEYS);
-        float s[ROWS][4][2];
+    // A piece with at least one token, ROWS x 8 query rows.
+    template <int ROWS>
+    __device__ __forceinline__ void piece(uint8_t* stage, const PieceInfo& info, int lane) {
+        const int g = lane >> 2, there = info.there;
+        const float4 scales = *reinterpret_cast<const float4*>(info.scales);
+        const uint32_t keys = smem_u32(stage), values = keys + C::KEYS;
+        const int later = (lane >> 3) & 1, row = later * 8 + ((lane + 4 * later) & 7);
+        float s[2][ROWS][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float acc[ROWS][4];
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) acc[r][0] = acc[r][1] = acc[r][2] = acc[r][3] = 0.f;
+            for (int r = 0; r < ROWS; ++r) s[half][r][0] = s[half][r][1] = s[half][r][2] = s[half][r][3] = 0.f;
 #pragma unroll
-            for (int x = 0; x < C::CHUNKS; ++x) {
-                const uint4 w = *reinterpret_cast<const uint4*>(mine + (j * C::CHUNKS + x) * 512);
+        for (int c = 0; c < C::CHUNKS; c += 2)
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) mma_e4m3(acc[r], q[r][2 * x], w.x, w.y);
+            for (int half = 0; half < 2; ++half) {
+                uint32_t w[4], a[4];
+                ldmatrix_rows(keys + C::at(half * 16 + row, c + (lane >> 4)), w);
+                widen(a, w[0], w[1]);
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) mma_e4m3(acc[r], q[r][2 * x + 1], w.z, w.w);
+                for (int r = 0; r < ROWS; ++r) mma_f16(s[half][r], a, q[c][r][0], q[c][r][1]);
+                widen(a, w[2], w[3]);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) mma_f16(s[half][r], a, q[c + 1][r][0], q[c + 1][r][1]);
             }
-            const float ks = j < 2 ? scales.x : scales.y;
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                const float f = by[r] * ks;
-                s[r][j][0] = fmaf(acc[r][2], 0.0625f, acc[r][0]) * f;
-                s[r][j][1] = fmaf(acc[r][3], 0.0625f, acc[r][1]) * f;
-            }
-        }
-        if (there < CA_TOKENS || scales.x < 0.f || scales.y < 0.f) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (8 * j + 2 * t + c >= there || (j < 2 ? scales.x : scales.y) < 0.f)
-#pragma unroll
-                        for (int r = 0; r < ROWS; ++r) s[r][j][c] = -INFINITY;
-        }
-        // The reference is let fall up to 2^8 behind the maximum: only where some row is further behind do its four lanes settle on a new one.
-        float mx[2] = {-INFINITY, -INFINITY};
+        float f[2][ROWS][2];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mx[r] = fmaxf(mx[r], fmaxf(s[r][j][0], s[r][j][1]));
+            for (int b = 0; b < 2; ++b) { f[0][r][b] = by[r][b] * scales.x; f[1][r][b] = by[r][b] * scales.y; }
+        if (there < CA_TOKENS || scales.x < 0.f || scales.y < 0.f) {
+            // tokens behind the unit's last, or on a page that is none: no weight, and nothing that 0 times it would not make 0
+            const int most[2] = {scales.x < 0.f ? 0 : there, scales.y < 0.f ? 0 : there};      // tokens below these are there, in either half
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (half * 16 + (x ? 8 + ((g + 4) & 7) : g) >= most[half])
+#pragma unroll
+                        for (int r = 0; r < ROWS; ++r) s[half][r][2 * x] = s[half][r][2 * x + 1] = -INFINITY;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)              // minus infinity stays that
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) f[half][r][b] = f[half][r][b] <= 0.f ? 1e-37f : f[half][r][b];
+            for (int x = lane; x < CA_TOKENS * C::CHUNKS; x += 32) {
+                const int token = x / C::CHUNKS;
+                if (token >= most[token >> 4]) *reinterpret_cast<uint4*>(stage + C::KEYS + x * 16) = make_uint4(0, 0, 0, 0);
+            }
+            __syncwarp();
+        }
+        // The reference is let fall up to 2^8 behind the maximum: only where some row is further behind do its eight lanes settle on a new one.
+        float mx[ROWS][2];
+        bool behind = false;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                mx[r][b] = fmaxf(fmaxf(s[0][r][b], s[0][r][2 + b]) * f[0][r][b], fmaxf(s[1][r][b], s[1][r][2 + b]) * f[1][r][b]);
+                behind |= mx[r][b] > m[r][b] + CA_RESCALE_AT;
+            }
         const float vs = fmaxf(scales.z, scales.w);
-        if (vs > v_scale || __any_sync(0xffffffffu, mx[0] > m[0] + CA_RESCALE_AT || mx[1] > m[1] + CA_RESCALE_AT)) {
+        if (__any_sync(0xffffffffu, behind || vs > v_scale)) {
             const float shrink = vs > v_scale ? v_scale / vs : 1.f;
             v_scale = fmaxf(vs, v_scale);
-            float up[2] = {1.f, 1.f};
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    float top = mx[r][b], up = shrink;
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    if (top > m[r][b] + CA_RESCALE_AT) {
+                        const float fall = ex2_approx(m[r][b] - top);
+                        m[r][b] = top;
+                        l[r][b] *= fall;
+                        up *= fall;
+                    }
+#pragma unroll
+                    for (int c = 0; c < C::CHUNKS; ++c) { o[c][r][b] *= up; o[c][r][2 + b] *= up; }
+                }
+        }
+        const float inv = v_scale > 0.f ? CA_P_SCALE / v_scale : 0.f, w[2] = {scales.z * inv, scales.w * inv};
+        uint32_t pt[2][ROWS][2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
-                mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
-                mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
-                if (mx[r] > m[r] + CA_RESCALE_AT) {
-                    up[r] = ex2_approx(m[r] - mx[r]);
-                    m[r] = mx[r];
-                    l[r] *= up[r];
+                float e[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const float sub = m[r][x & 1] == -INFINITY ? 0.f : m[r][x & 1];
+                    e[x] = ex2_approx(fmaf(s[half][r][x], f[half][r][x & 1], -sub));
+                    l[r][x & 1] += e[x];
                 }
-                up[r] *= shrink;
+                pt[half][r][0] = transpose_halves(pack_half(e[0] * w[half], e[1] * w[half]));
+                pt[half][r][1] = transpose_halves(pack_half(e[2] * w[half], e[3] * w[half]));
             }
+        // row i of 16: tokens 2 t and the next (i % 4 < 2) and their likes of the second eight, t = i / 4
+        const int i = lane & 15, of = (i >> 2) * 2 + (i & 1), token = i & 2 ? 8 + ((of + 4) & 7) : of;
 #pragma unroll
-            for (int d = 0; d < C::NT; ++d) { o[d][0] *= up[0]; o[d][1] *= up[0]; o[d][2] *= up[1]; o[d][3] *= up[1]; }
-        }
-        const float inv = v_scale > 0.f ? CA_P_SCALE / v_scale : 0.f, w0 = scales.z * inv, w1 = scales.w * inv;
-        uint32_t a[2][4];
+        for (int c = 0; c < C::CHUNKS; c += 2)
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            const float sub = m[r] == -INFINITY ? 0.f : m[r];
+            for (int half = 0; half < 2; ++half) {
+                uint32_t v[4], a[4];
+                ldmatrix_columns(values + C::at(half * 16 + token, c + (lane >> 4)), v);
+                widen(a, v[0], v[1]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float e0 = ex2_approx(s[r][j][0] - sub), e1 = ex2_approx(s[r][j][1] - sub), w = j < 2 ? w0 : w1;
-                l[r] += e0 + e1;
-                a[j >> 1][(j & 1) * 2 + r] = pack_half(e0 * w, e1 * w);
+                for (int r = 0; r < ROWS; ++r) mma_f16(o[c][r], a, pt[half][r][0], pt[half][r][1]);
+                widen(a, v[2], v[3]);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) mma_f16(o[c + 1][r], a, pt[half][r][0], pt[half][r][1]);
             }
-        }
-        if (!BOTH) a[0][1] = a[0][3] = a[1][1] = a[1][3] = 0u;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            uint32_t v[4][C::VB / 4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (C::VB == 16) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(mine + C::KEYS + (half * 4 + j) * 512);
-                    v[j][0] = w.x; v[j][1] = w.y; v[j][C::VB / 4 - 2] = w.z; v[j][C::VB / 4 - 1] = w.w;
-                } else {
-                    const uint2 w = *reinterpret_cast<const uint2*>(stage + C::KEYS + (half * 4 + j) * 256 + lane * 8);
-                    v[j][0] = w.x; v[j][1] = w.y;
-                }
-            }
-#pragma unroll
-            for (int x = 0; x < C::VB / 4; ++x)
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {                  // dimensions 4 x + 2 y and the next: their numbers of two tokens side by side
-                    const uint32_t b0 = __byte_perm(v[0][x], v[1][x], y ? 0x7362 : 0x5140), b1 = __byte_perm(v[2][x], v[3][x], y ? 0x7362 : 0x5140);
-                    mma_f16(o[4 * x + 2 * y], a[half], e4m3_pair_to_half((uint16_t)b0), e4m3_pair_to_half((uint16_t)b1));
-                    mma_f16(o[4 * x + 2 * y + 1], a[half], e4m3_pair_to_half((uint16_t)(b0 >> 16)), e4m3_pair_to_half((uint16_t)(b1 >> 16)));
-                }
-        }
     }
 
-    // Sums of the tile's first `rows` rows to record rows `at`, ...
-    __device__ __forceinline__ void store(const CacheParams& p, int64_t at, int rows, int lane) {
-        const int t = lane & 3, D = p.a.cache.D;
+    // Sums of the first or the second eight rows, as far as the tile has them, to record rows `at`, ...
+    __device__ __forceinline__ void store(const CacheParams& p, int64_t at, int rows, int lane, int r) {
+        const int g = lane >> 2, t = lane & 3, D = p.a.cache.D;
         const float unit = v_scale * (1.f / CA_P_SCALE);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-            const int row = (lane >> 2) + 8 * r;
-            if (row >= rows) continue;
-            float* out = p.w.o + (at + row) * D + t * 2 * C::VB;      // columns 2 t and 2 t + 1 of the products: dimensions VB 2 t .. + 2 VB
+            for (int b = 0; b < 2; ++b) {
+                float sum = l[r][b];
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-                if ((2 * t + c) * C::VB < D)
+                for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                const int row = 8 * r + 2 * t + b;
+                if (row < rows) {
+                    float* out = p.w.o + (at + row) * D + g;
 #pragma unroll
-                    for (int d = 0; d < C::VB; d += 4)
-                        *reinterpret_cast<float4*>(out + c * C::VB + d) =
-                            make_float4(o[d][2 * r + c] * unit, o[d + 1][2 * r + c] * unit, o[d + 2][2 * r + c] * unit, o[d + 3][2 * r + c] * unit);
-            if (t == 0) p.w.ml[at + row] = make_float2(m[r], l[r]);
-        }
+                    for (int c = 0; c < C::CHUNKS; ++c)
+                        if (c * 16 < D) {
+                            out[c * 16] = o[c][r][b] * unit;
+                            out[c * 16 + 8] = o[c][r][2 + b] * unit;
+                        }
+                    if (g == 0) p.w.ml[at + row] = make_float2(m[r][b], sum);
+                }
+            }
     }
 };
 
 struct CacheShared {
-    ScanSums warp_sums[CA_WARPS];
+    PieceInfo info[4][CA_WARPS];       // per stage and warp, as the barriers
+    uint64_t full[4][CA_WARPS], empty[4][CA_WARPS];
+    ScanSums warp_sums[CA_WARPS + 1];
     Start shared, single[CA_WARPS];
     int live[CA_WARPS][CA_ROWS];       // rollouts of a prompt entry, per warp
+    int2 sizes[CA_SCANNED];            // the entries' tokens and rows
+    uint32_t abort;
 };
 
-// Query rows `row0`, `row0` + 8 of the entry's unit (rows of them), for this lane.
-__device__ __forceinline__ const __nv_bfloat16* query_row(const CacheParams& p, const CacheEntry& e, int head, const int* live, int row) {
-    if (row >= e.rows) return nullptr;
+// Who has the unit's first and last piece, for the merge.
+__device__ __forceinline__ void tell_owner(const CacheParams& p, const PieceInfo& e, int owner) {
+    int2* const at = p.w.owners + (int64_t)e.entry * p.a.cache.Hkv + e.head;
+    if (e.flags & PIECE_BEGIN) at->x = owner;
+    if (e.flags & PIECE_END) at->y = owner;
+}
+// Query row `row` of an entry's unit, if it has so many.
+__device__ __forceinline__ const __nv_bfloat16* query_row(const CacheParams& p, const PieceInfo& e, const int* live, int row) {
+    if (row >= e.flags >> PIECE_ROWS) return nullptr;
     const int of = row / p.ratio, i = e.entry < p.prompts ? live[of] : e.entry - p.prompts;
-    return static_cast<const __nv_bfloat16*>(p.a.q) + i * p.a.q_stride + (int64_t)(head * p.ratio + row - of * p.ratio) * p.a.cache.D;
+    return static_cast<const __nv_bfloat16*>(p.a.q) + i * p.a.q_stride + (int64_t)(e.head * p.ratio + row - of * p.ratio) * p.a.cache.D;
 }
 // The live rollouts of a prompt entry, in order; by a warp.
 __device__ __forceinline__ void find_live(const CacheParams& p, int e, int* live, int lane) {
@@ -510,28 +562,40 @@ __device__ __forceinline__ void find_live(const CacheParams& p, int e, int* live
 }
 
 template <int DP>
-__global__ void __launch_bounds__(CA_THREADS, CA_PER_SM) cache_units_kernel(const CacheParams p) {
+__global__ void __launch_bounds__(CA_THREADS, CA_PER_SM) cache_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const CacheParams p) {
     using C = CacheConf<DP>;
-    extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ CacheShared sm;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(16) CacheShared sm;
+    uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    volatile uint32_t* abort_flag = &sm.abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, Hkv = p.a.cache.Hkv;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::STAGES * CA_WARPS; ++i) {
+            mbar_init(&sm.full[i / CA_WARPS][i % CA_WARPS], 1);
+            mbar_init(&sm.empty[i / CA_WARPS][i % CA_WARPS], CA_WARPS);
+        }
+        sm.abort = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
     pdl_launch_dependents();
     pdl_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, Hkv = p.a.cache.Hkv, D = p.a.cache.D;
     const long long b = blockIdx.x;
-    // dimensions that no copy fills are zeros
-    if (D < DP)
-        for (int x = threadIdx.x * 16; x < (int)C::SMEM; x += CA_THREADS * 16) *reinterpret_cast<uint4*>(ring + x) = make_uint4(0, 0, 0, 0);
 
-    // ---- the scan: a thread has `each` entries in a row, twice (sums, then what is this block's)
+    // ---- the scan: sizes of the entries, side by side; then a thread has `each` entries in a row, twice (sums, and what is this block's)
+    bool bad = false;
+    for (int e = threadIdx.x; e < min(p.entries, CA_SCANNED); e += CA_THREADS) sm.sizes[e] = entry_size(p, e, bad);
+    __syncthreads();
     const int each = (p.entries + CA_THREADS - 1) / CA_THREADS;
     const int e0 = min((int)threadIdx.x * each, p.entries), e1 = min(e0 + each, p.entries);
-    bool bad = false;
+    auto size = [&](int e) { return e < CA_SCANNED ? sm.sizes[e] : entry_size(p, e, bad); };
+    auto length = [&](int2 x) { return (long long)(entry_pieces(x.y, x.x) + unit_setup(x.y)) * Hkv; };
     ScanSums mine = {0, 0, 0, 0};
     for (int e = e0; e < e1; ++e) {
-        const CacheEntry x = make_entry(p, e, bad);
-        if (x.pieces == 0) continue;
-        if (x.rows > CA_ALONE) { mine.shared += (long long)x.pieces * Hkv; ++mine.shared_entries; }
-        else { mine.single += (long long)x.pieces * Hkv; ++mine.single_entries; }
+        const int2 x = size(e);
+        if (x.x == 0) continue;
+        if (x.y > CA_ALONE) { mine.shared += length(x); ++mine.shared_entries; }
+        else { mine.single += length(x); ++mine.single_entries; }
     }
     if (bad && b == 0) atomicOr(p.status, ARROL_DEV_BAD_INDEX);
     ScanSums sum = mine;
@@ -544,159 +608,167 @@ __global__ void __launch_bounds__(CA_THREADS, CA_PER_SM) cache_units_kernel(cons
     __syncthreads();
     ScanSums total = {0, 0, 0, 0}, at = {sum.shared - mine.shared, sum.single - mine.single, sum.shared_entries - mine.shared_entries, sum.single_entries - mine.single_entries};
 #pragma unroll
-    for (int w = 0; w < CA_WARPS; ++w) {
+    for (int w = 0; w < CA_WARPS + 1; ++w) {
         if (w < warp) at = at + sm.warp_sums[w];
         total = total + sm.warp_sums[w];
     }
     const Line line = make_line(total.shared, total.single, p.grid);
-    if (b == 0 && threadIdx.x == 0) { p.w.head[0] = total.shared; p.w.head[1] = total.single; }
+    if (b == 0 && threadIdx.x == 0) { p.w.head[0] = line.shared; p.w.head[1] = line.single; p.w.head[2] = line.per; }
     const long long x0 = shared_begin(line, b), x1 = shared_begin(line, b + 1);
-    long long y0, y1, block_y0, block_y1;
-    warp_range(line, b * CA_WARPS + warp, y0, y1);
-    {
-        long long other;
-        warp_range(line, b * CA_WARPS, block_y0, other);
-        block_y1 = (b + 1) * line.per - line.shared * CA_SHARED_COST;
-        if (block_y1 > line.single) block_y1 = line.single;
-    }
-    const bool tell = (int)(threadIdx.x % gridDim.x) == (int)b;            // where the entries' pieces begin, for the merge: each thread's by one block
-    for (int e = e0; e < e1; ++e) {
-        const CacheEntry x = make_entry(p, e, bad);
-        if (x.pieces == 0) continue;
-        const long long n = (long long)x.pieces * Hkv;
-        if (x.rows > CA_ALONE) {
-            if (tell) p.w.where[e] = at.shared;
-            if (at.shared < x1 && at.shared + n > x0) p.w.shared[at.shared_entries] = x;      // neighbours write the same
-            if (at.shared <= x0 && at.shared + n > x0) sm.shared = {at.shared_entries, x0 - at.shared};
+    long long y0[CA_WARPS], y1[CA_WARPS];
+#pragma unroll
+    for (int w = 0; w < CA_WARPS; ++w) warp_range(line, b * CA_WARPS + w, y0[w], y1[w]);
+    const long long block_y1 = max(max(y1[0], y1[1]), max(y1[2], y1[3]));
+    if (mine.shared > 0 && at.shared < x1 && at.shared + mine.shared > x0)
+        for (int e = e0; e < e1; ++e) {
+            const int2 x = size(e);
+            if (x.x == 0 || x.y <= CA_ALONE) continue;
+            const long long n = length(x);
+            const CacheEntry entry = {e, x.x, x.y, entry_pieces(x.y, x.x)};
+            if (at.shared < x1 && at.shared + n > x0) p.w.shared[at.shared_entries] = entry;                 // neighbours write the same
+            if (at.shared <= x0 && at.shared + n > x0) sm.shared = {entry, x0 - at.shared, at.shared_entries};
             at.shared += n;
             ++at.shared_entries;
-        } else {
-            if (tell) p.w.where[e] = at.single;
-            if (at.single < block_y1 && at.single + n > block_y0) p.w.single[at.single_entries] = x;
+        }
+    if (mine.single > 0 && at.single < block_y1 && at.single + mine.single > y0[0])
+        for (int e = e0; e < e1; ++e) {
+            const int2 x = size(e);
+            if (x.x == 0 || x.y > CA_ALONE) continue;
+            const long long n = length(x);
+            if (at.single < block_y1 && at.single + n > y0[0]) {
+                const CacheEntry entry = {e, x.x, x.y, entry_pieces(x.y, x.x)};
+                p.w.single[at.single_entries] = entry;
 #pragma unroll
-            for (int w = 0; w < CA_WARPS; ++w) {
-                long long w0, w1;
-                warp_range(line, b * CA_WARPS + w, w0, w1);
-                if (w0 < w1 && at.single <= w0 && at.single + n > w0) sm.single[w] = {at.single_entries, w0 - at.single};
+                for (int w = 0; w < CA_WARPS; ++w)
+                    if (at.single <= y0[w] && at.single + n > y0[w]) sm.single[w] = {entry, y0[w] - at.single, at.single_entries};
             }
             at.single += n;
             ++at.single_entries;
         }
-    }
     __syncthreads();
 
-    // ---- shared pieces: four warps, a tile of 16 rows each; with two tiles two warps share a tile's tokens
-    RowTile<DP> tile;
-    if (x0 < x1) {
-        Cursor ahead, now;
-        ahead.begin(p.w.shared, sm.shared, total.shared_entries);
-        now = ahead;
-        long long left = x1 - x0;                             // pieces to copy
-        PagePair pages = find_pages(p, ahead, (ahead.piece * CA_WARPS + warp) * CA_TOKENS);
-        uint32_t slot = 0;
-        auto copy = [&](uint32_t to) {
-            if (left > 0) {
-                copy_piece<DP>(p, ahead, (ahead.piece * CA_WARPS + warp) * CA_TOKENS, pages, ring + (size_t)(to * CA_WARPS + warp) * C::BYTES, lane);
-                if (--left > 0) {
-                    ahead.advance(Hkv);
-                    pages = find_pages(p, ahead, (ahead.piece * CA_WARPS + warp) * CA_TOKENS);
+    // Stages are filled and read in turn, from the first shared piece to the last single one, behind which comes one that says so.  A consumer of shared pieces waits for all
+    // four parts of a stage, those that it does not read too: a later wait for one of them by its parity alone would otherwise pass for a filling that is two ahead.
+    auto stage = [&](uint32_t n, int w) { return ring + (size_t)(n % C::STAGES * CA_WARPS + w) * C::BYTES; };
+    bool ok = true;
+    if (warp == CA_WARPS) {
+        // ---- the producer: a lane for each consumer
+        uint32_t n = 0;
+        if (lane < CA_WARPS) {
+            for (int phase = 0; phase < 2 && ok; ++phase) {
+                long long from, to;
+                warp_range(line, b * CA_WARPS + lane, from, to);
+                if (phase == 0) { from = x0; to = x1; }
+                if (from >= to) continue;
+                Cursor c;
+                c.begin(phase ? p.w.single : p.w.shared, phase ? sm.single[lane] : sm.shared, phase ? total.single_entries : total.shared_entries, to - from);
+                if (c.left <= 0) continue;
+                // a part that its piece does not have begins where no tokens are
+                auto token = [&] { const int parts = piece_parts(c.e.rows); return phase ? c.piece * CA_TOKENS : lane < parts ? (c.piece * parts + lane) * CA_TOKENS : c.e.tokens; };
+                Fetch now, next;
+                now.find(p, c, token(), true);
+                c.advance(Hkv);
+                bool more = c.left > 0;
+                if (more) next.find(p, c, token(), false);
+                now.find_scales(p);
+                for (;; ++n) {
+                    const uint32_t st = n % C::STAGES;
+                    if (!mbar_wait(&sm.empty[st][lane], ((n / C::STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+                    now.copy<DP>(p, &map_k, &map_v, smem_u32(stage(n, lane)), &sm.full[st][lane]);
+                    bool after_next = false;
+                    Fetch after;
+                    if (more) {
+                        c.advance(Hkv);
+                        after_next = c.left > 0;
+                        if (after_next) after.find(p, c, token(), false);
+                    }
+                    sm.info[st][lane] = now.info;
+                    mbar_arrive(&sm.full[st][lane]);
+                    if (!more) { ++n; break; }
+                    now = next;
+                    now.find_scales(p);
+                    next = after;
+                    more = after_next;
                 }
             }
-            cp_async_commit();
-        };
-#pragma unroll
-        for (int i = 0; i < C::STAGES - 1; ++i) copy(i);
-        bool first = true;
-        for (long long x = x0; x < x1; ++x) {
-            const int row_tiles = now.e.rows <= 32 ? 2 : 4, mine_tile = warp & (row_tiles - 1), share = warp / row_tiles;
-            if (first || now.piece == 0) {
-                if (now.e.entry < p.prompts) find_live(p, now.e.entry, sm.live[warp], lane);
-                const int row = mine_tile * 16 + (lane >> 2);
-                tile.load(p, lane, query_row(p, now.e, now.head, sm.live[warp], row), query_row(p, now.e, now.head, sm.live[warp], row + 8));
-                first = false;
+            if (ok && mbar_wait(&sm.empty[n % C::STAGES][lane], ((n / C::STAGES) & 1u) ^ 1u, abort_flag)) {
+                sm.info[n % C::STAGES][lane].flags = PIECE_NONE;
+                mbar_arrive(&sm.full[n % C::STAGES][lane]);
+            } else {
+                // let the copies in flight land before the block's shared memory goes away (all have, unless a wait ran out)
+                for (uint32_t i = n > C::STAGES ? n - C::STAGES : 0; i < n; ++i)
+                    for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
+                        if (mbar_try_wait(&sm.full[i % C::STAGES][lane], (i / C::STAGES) & 1u)) break;
             }
-            cp_async_wait<C::STAGES - 2>();
-            __syncthreads();
-            copy(slot == 0 ? C::STAGES - 1 : slot - 1);       // the stage that every warp has left before the barrier
-            if (mine_tile * 16 < now.e.rows)
-                for (int w = share; w < CA_WARPS; w += CA_WARPS / row_tiles) {
-                    const int there = now.e.tokens - (now.piece * CA_WARPS + w) * CA_TOKENS;
-                    if (there <= 0) break;
-                    tile.template piece<true>(ring + (size_t)(slot * CA_WARPS + w) * C::BYTES, there, lane);
-                }
-            if (now.piece == now.e.pieces - 1 || x == x1 - 1) {
-                const int64_t record = ((int64_t)now.e.entry * Hkv + now.head + b) * CA_ROWS + (row_tiles == 2 ? share * 32 : 0) + mine_tile * 16;
-                tile.store(p, p.w.rows_own + p.w.rows_prompt + record, now.e.rows - mine_tile * 16, lane);
-            }
-            if (x < x1 - 1) now.advance(Hkv);
-            slot = slot == C::STAGES - 1 ? 0 : slot + 1;
         }
-        cp_async_wait<0>();
-        __syncthreads();
-    }
-
-    // ---- single pieces: a warp each
-    if (y0 < y1) {
-        const long long global_warp = b * CA_WARPS + warp;
-        Cursor ahead, now;
-        ahead.begin(p.w.single, sm.single[warp], total.single_entries);
-        now = ahead;
-        long long left = y1 - y0;
-        PagePair pages = find_pages(p, ahead, ahead.piece * CA_TOKENS);
-        uint32_t slot = 0;
-        uint8_t* const stages = ring + (size_t)warp * C::BYTES;
-        auto copy = [&](uint32_t to) {
-            if (left > 0) {
-                copy_piece<DP>(p, ahead, ahead.piece * CA_TOKENS, pages, stages + (size_t)to * CA_WARPS * C::BYTES, lane);
-                if (--left > 0) {
-                    ahead.advance(Hkv);
-                    pages = find_pages(p, ahead, ahead.piece * CA_TOKENS);
-                }
+        __syncwarp();
+    } else {
+        RowTile<DP> tile;
+        for (uint32_t n = 0;; ++n) {
+            const uint32_t st = n % C::STAGES, parity = (n / C::STAGES) & 1u;
+            if (!mbar_wait_warp(&sm.full[st][warp], parity, abort_flag)) break;
+            const PieceInfo& e = sm.info[st][warp];
+            const int flags = e.flags, rows = flags >> PIECE_ROWS;
+            if (flags & PIECE_NONE) break;
+            // a shared piece: a tile of 16 rows a warp; with two tiles two warps share a tile's tokens
+            const bool shared = rows > CA_ALONE;
+            const int row_tiles = rows > 32 ? 4 : 2, row0 = shared ? (warp & (row_tiles - 1)) * 16 : 0, left = rows - row0, share = shared ? warp / row_tiles : warp;
+            if (shared) {
+                for (int w = 0; w < CA_WARPS && ok; ++w) ok = mbar_wait_warp(&sm.full[st][w], parity, abort_flag);
+                if (!ok) break;
             }
-            cp_async_commit();
-        };
-#pragma unroll
-        for (int i = 0; i < C::STAGES - 1; ++i) copy(i);
-        bool first = true;
-        for (long long y = y0; y < y1; ++y) {
-            if (first || now.piece == 0) {
-                if (now.e.entry < p.prompts) find_live(p, now.e.entry, sm.live[warp], lane);
-                tile.load(p, lane, query_row(p, now.e, now.head, sm.live[warp], lane >> 2), query_row(p, now.e, now.head, sm.live[warp], (lane >> 2) + 8));
-                first = false;
+            if ((flags & PIECE_FIRST) && left > 0) {
+                if (e.entry < p.prompts) find_live(p, e.entry, sm.live[warp], lane);
+                tile.load(p, lane, query_row(p, e, sm.live[warp], row0 + (lane >> 2)), 0);
+                if (left > 8) tile.load(p, lane, query_row(p, e, sm.live[warp], row0 + 8 + (lane >> 2)), 1);
             }
-            cp_async_wait<C::STAGES - 2>();
+            for (int w = share; w < CA_WARPS; w += shared ? CA_WARPS / row_tiles : CA_WARPS) {
+                const PieceInfo& part = sm.info[st][w];
+                if (part.there <= 0 || left <= 0) break;
+                if (left > 8) tile.template piece<2>(stage(n, w), part, lane);
+                else tile.template piece<1>(stage(n, w), part, lane);
+            }
+            if (lane == 0 && (!shared || warp == 0)) tell_owner(p, e, (int)(shared ? b : b * CA_WARPS + warp));
+            if ((flags & PIECE_LAST) && left > 0) {
+                const int64_t unit = (int64_t)e.entry * Hkv + e.head, owner = b * CA_WARPS + warp;
+                const int64_t record = shared ? p.w.rows_own + p.w.rows_prompt + (unit + b) * CA_ROWS + (row_tiles == 2 ? share * 32 : 0) + row0
+                                     : e.entry < p.prompts ? p.w.rows_own + (unit + owner) * CA_ALONE : (unit - (int64_t)p.prompts * Hkv + owner) * p.ratio;
+                tile.store(p, record, left, lane, 0);
+                if (left > 8) tile.store(p, record, left, lane, 1);
+            }
+            // what was read by instructions comes before the copies that fill the stage again
+            fence_proxy_async_smem();
             __syncwarp();
-            copy(slot == 0 ? C::STAGES - 1 : slot - 1);
-            const int there = now.e.tokens - now.piece * CA_TOKENS;
-            const uint8_t* stage = stages + (size_t)slot * CA_WARPS * C::BYTES;
-            if (now.e.rows > 8) tile.template piece<true>(stage, there, lane);
-            else tile.template piece<false>(stage, there, lane);
-            if (now.piece == now.e.pieces - 1 || y == y1 - 1) {
-                const int64_t record = now.e.entry < p.prompts ? p.w.rows_own + ((int64_t)now.e.entry * Hkv + now.head + global_warp) * CA_ALONE
-                                                               : ((int64_t)(now.e.entry - p.prompts) * Hkv + now.head + global_warp) * p.ratio;
-                tile.store(p, record, now.e.rows, lane);
-            }
-            if (y < y1 - 1) now.advance(Hkv);
-            slot = slot == C::STAGES - 1 ? 0 : slot + 1;
+            if (shared ? lane < CA_WARPS : lane == 0) mbar_arrive_n(&sm.empty[st][shared ? lane : warp], shared ? 1 : CA_WARPS);
+            __syncwarp();
         }
     }
-    cp_async_wait_all();
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, ARROL_DEV_WAIT_EXPIRED);
 }
 
-// Running sum of records.
+// A warp per (rollout, query head): the prompt's records, then its own, in order; four dimensions a lane.  Records are asked for four at a time.
 struct Merged {
+    static constexpr int AT_ONCE = 4;
     float top, total;
     float4 sum;
-    __device__ __forceinline__ void add(float2 ml, float4 v) {
-        const float next = fmaxf(top, ml.x), up = next == -INFINITY ? 1.f : ex2_approx(top - next);
-        const float by = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : ex2_approx(ml.x - next);      // a NaN without a maximum stays one
-        total = total * up + by * ml.y;
-        sum.x = sum.x * up + by * v.x; sum.y = sum.y * up + by * v.y; sum.z = sum.z * up + by * v.z; sum.w = sum.w * up + by * v.w;
+    __device__ __forceinline__ void add(const float2 (&x)[AT_ONCE], const float4 (&v)[AT_ONCE]) {
+        float next = top;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) next = fmaxf(next, x[k].x);
+        const float up = next == -INFINITY ? 1.f : ex2_approx(top - next);
+        total *= up;
+        sum.x *= up; sum.y *= up; sum.z *= up; sum.w *= up;
         top = next;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const float by = x[k].x == -INFINITY ? (x[k].y == 0.f ? 0.f : 1.f) : ex2_approx(x[k].x - top);      // a NaN without a maximum stays one
+            total += by * x[k].y;
+            sum.x += by * v[k].x; sum.y += by * v[k].y; sum.z += by * v[k].z; sum.w += by * v[k].w;
+        }
     }
 };
 
-// A warp per (rollout, query head): the prompt's records, then its own, in order; four dimensions a lane.
 __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
     pdl_launch_dependents();
     pdl_wait();
@@ -705,46 +777,69 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
     const int64_t row = blockIdx.x * (int64_t)8 + (threadIdx.x >> 5);
     if (row >= (int64_t)a.N * a.Hq) return;
     const int i = (int)(row / a.Hq), hq = (int)(row - (int64_t)i * a.Hq), h = hq / p.ratio, r = hq - h * p.ratio;
-    if (a.keep && !a.keep[i]) return;
     const long long* head = pdl_acquire(p.w.head);
-    const long long* where = pdl_acquire(p.w.where);
+    const int2* owners = pdl_acquire(p.w.owners);
     const float2* ml = pdl_acquire(p.w.ml);
     const float* o = pdl_acquire(p.w.o);
-    const Line line = make_line(head[0], head[1], p.grid);
-    Merged m = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    bool any = false, bad = false;
-    auto record = [&](int64_t at) { m.add(ml[at], d < D ? *reinterpret_cast<const float4*>(o + at * D + d) : make_float4(0.f, 0.f, 0.f, 0.f)); };
-    auto entry = [&](const CacheEntry& e, int row_in) {
-        if (e.pieces == 0) return;
-        any = true;
-        const long long from = where[e.entry] + (long long)h * e.pieces, to = from + e.pieces - 1;
-        if (e.rows > CA_ALONE) {
-            const long long b1 = shared_block(line, to);
-            for (long long b = shared_block(line, from); b <= b1; ++b) {
-                if (shared_begin(line, b) >= shared_begin(line, b + 1)) continue;
-                const int64_t at = p.w.rows_own + p.w.rows_prompt + ((int64_t)e.entry * Hkv + h + b) * CA_ROWS + row_in;
-                record(at);
-                if (e.rows <= 32) record(at + 32);
-            }
-        } else {
-            const long long w1 = single_warp(line, to);
-            for (long long w = single_warp(line, from); w <= w1; ++w) {
-                long long y0, y1;
-                warp_range(line, w, y0, y1);
-                if (y0 >= y1) continue;
-                record(e.entry < p.prompts ? p.w.rows_own + ((int64_t)e.entry * Hkv + h + w) * CA_ALONE + row_in
-                                           : ((int64_t)(e.entry - p.prompts) * Hkv + h + w) * p.ratio + row_in);
-            }
-        }
-    };
+    const Line line = {head[0], head[1], head[2]};
+    bool bad = false;
+    const int own_tokens = cache_tokens(a.lengths, i, a.table_pages, a.cache.page, bad);
+    const int2 own = owners[(int64_t)(p.prompts + i) * Hkv + h];       // not read where there are no tokens
+    int prompt_tokens = 0, prompt_rows = 0, prompt_row = 0, entry = 0;
+    int2 shared = {0, 0};
     if (p.prompts) {
         const int q = i / a.G, G = a.G;
-        int before = 0;                                       // live rollouts of the group before this one
-        for (int j = lane; j < i - q * G; j += 32) before += !a.keep || a.keep[(int64_t)q * G + j];
-        before = __reduce_add_sync(0xffffffffu, before);
-        entry(make_entry(p, q * p.blocks + before / p.group, bad), before % p.group * p.ratio + r);
+        prompt_tokens = cache_tokens(a.prompt_lengths, q, a.prompt_table_pages, a.cache.page, bad);
+        int before = 0, live = 0;                             // live rollouts of the group: before this one, all
+        for (int j0 = 0; j0 < G; j0 += 32) {
+            const int j = j0 + lane;
+            const uint32_t all = __ballot_sync(0xffffffffu, j < G && (!a.keep || a.keep[(int64_t)q * G + j]));
+            const int left = i - q * G - j0;
+            live += __popc(all);
+            before += __popc(left >= 32 ? all : left <= 0 ? 0u : all & ((1u << left) - 1u));
+        }
+        entry = q * p.blocks + before / p.group;
+        prompt_rows = min(live - before / p.group * p.group, p.group) * p.ratio;
+        prompt_row = before % p.group * p.ratio + r;
+        shared = owners[(int64_t)entry * Hkv + h];
     }
-    entry(make_entry(p, p.prompts + i, bad), r);
+    if (a.keep && !a.keep[i]) return;
+    Merged m = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    // `x`: a prompt's entry, or the rollout's own
+    auto unit = [&](bool prompt, int rows, int2 of, int row_in) {
+        const int64_t number = prompt ? (int64_t)entry * Hkv + h : (int64_t)i * Hkv + h;
+        const bool in_blocks = rows > CA_ALONE;
+        const int twice = in_blocks && rows <= 32 ? 1 : 0;    // two warps' records a block
+        for (int64_t k0 = (int64_t)of.x << twice; k0 <= ((int64_t)of.y << twice | twice); k0 += Merged::AT_ONCE) {
+            float2 x[Merged::AT_ONCE];
+            float4 v[Merged::AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < Merged::AT_ONCE; ++k) {
+                x[k] = make_float2(-INFINITY, 0.f);
+                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                const int64_t w = (k0 + k) >> twice;
+                bool there = w <= of.y;
+                int64_t at;
+                if (in_blocks) {
+                    there = there && shared_begin(line, w) < shared_begin(line, w + 1);
+                    at = p.w.rows_own + p.w.rows_prompt + ((prompt ? number : (int64_t)(p.prompts + i) * Hkv + h) + w) * CA_ROWS + row_in + ((k0 + k) & twice) * 32;
+                } else {
+                    long long y0, y1;
+                    warp_range(line, w, y0, y1);
+                    there = there && y0 < y1;
+                    at = prompt ? p.w.rows_own + (number + w) * CA_ALONE + row_in : (number + w) * p.ratio + row_in;
+                }
+                if (there) {
+                    x[k] = ml[at];
+                    if (d < D) v[k] = *reinterpret_cast<const float4*>(o + at * D + d);
+                }
+            }
+            m.add(x, v);
+        }
+    };
+    if (prompt_tokens > 0) unit(true, prompt_rows, shared, prompt_row);
+    if (own_tokens > 0) unit(false, p.ratio, own, r);
+    const bool any = prompt_tokens > 0 || own_tokens > 0;     // none: no key
     const float inv = any ? 1.f / m.total : 0.f;
     if (d < D) {
         uint2 w = make_uint2(0u, 0u);
@@ -757,6 +852,18 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
     if (lane == 0 && a.lse) a.lse[row] = any ? (m.top + log2f(m.total)) * LN2 : -INFINITY;
 }
 
+// [pages, Hkv, page, D] numbers as boxes of up to 32 tokens x DP bytes of one page and head, rows of DP bytes in shared memory, swizzled over as many; dimensions past D are zeros.
+int make_map_pages(arrol_ctx* ctx, CUtensorMap* map, const arrol_cache& c, const void* base, int64_t page_stride, int DP) {
+    const cuuint64_t dims[4] = {(cuuint64_t)c.D, (cuuint64_t)c.page, (cuuint64_t)c.Hkv, (cuuint64_t)c.pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)c.D, (cuuint64_t)c.page * c.D, (cuuint64_t)page_stride};
+    const cuuint32_t box[4] = {(cuuint32_t)DP, (cuuint32_t)(c.page < CA_TOKENS ? c.page : CA_TOKENS), 1, 1};
+    const cuuint32_t elem_strides[4] = {1, 1, 1, 1};
+    CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(
+        map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        DP == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? ARROL_OK : ARROL_ERR_CUDA;
+}
+
 template <int DP>
 int launch_cache_attention(arrol_ctx* ctx, const CacheParams& p, cudaStream_t s) {
     using C = CacheConf<DP>;
@@ -765,7 +872,11 @@ int launch_cache_attention(arrol_ctx* ctx, const CacheParams& p, cudaStream_t s)
         ARROL_CUDA_OK(cudaFuncSetAttribute(cache_units_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
         set = true;
     }
-    ARROL_CUDA_OK(arrol_launch_pdl(cache_units_kernel<DP>, dim3((unsigned)p.grid), dim3(CA_THREADS), C::SMEM, s, p));
+    CUtensorMap k = {}, v = {};                              // without pages nothing is copied
+    if (p.a.cache.pages > 0 && (make_map_pages(ctx, &k, p.a.cache, p.a.cache.k_cache, p.a.cache.k_page_stride, DP) != ARROL_OK ||
+                                make_map_pages(ctx, &v, p.a.cache, p.a.cache.v_cache, p.a.cache.v_page_stride, DP) != ARROL_OK))
+        return ARROL_ERR_CUDA;
+    ARROL_CUDA_OK(arrol_launch_pdl(cache_units_kernel<DP>, dim3((unsigned)p.grid), dim3(CA_THREADS), C::SMEM, s, k, v, p));
     ARROL_CUDA_OK(arrol_launch_pdl(cache_merge_kernel, dim3((unsigned)(((int64_t)p.a.N * p.a.Hq + 7) / 8)), dim3(256), 0, s, p));
     ctx->launches += 2;
     return ARROL_OK;
