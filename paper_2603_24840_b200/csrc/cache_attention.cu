@@ -10,6 +10,8 @@
 // (shared pieces first: a chunk of 128 tokens for more than 16 query rows, four warps a row tile each; then single ones: 32 tokens for 16 rows or less, a warp each).
 // Pieces of a unit (rows x key head) that fall to different blocks or warps leave partial sums, which cache_merge_kernel adds up in order, so the result does not
 // depend on who was first.
+#include <type_traits>
+
 #include "cache_common.cuh"
 #include "tc_common.cuh"
 
@@ -255,6 +257,16 @@ struct Cursor {
         ++number;
         fetch();
     }
+    // so many pieces on, or past the part's end
+    __device__ __forceinline__ void skip(int n, int heads) {
+        if (left > 0 && piece + n < e.pieces) {
+            piece += n;
+            left -= n;
+            return;
+        }
+#pragma unroll 1
+        for (; n > 0 && left > 0; --n) advance(heads);
+    }
     // whether the piece is the part's last one
     __device__ __forceinline__ bool is_last() const { return left == 1 || (piece == e.pieces - 1 && left <= 1 + setup); }
 };
@@ -413,7 +425,7 @@ struct RowTile {
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
             for (int b = 0; b < 2; ++b) { f[0][r][b] = by[r][b] * scales.x; f[1][r][b] = by[r][b] * scales.y; }
-        if (there < CA_TOKENS || scales.x < 0.f || scales.y < 0.f) {
+        if (__builtin_expect(there < CA_TOKENS || scales.x < 0.f || scales.y < 0.f, 0)) {
             // tokens behind the unit's last, or on a page that is none: no weight, and nothing that 0 times it would not make 0
             const int most[2] = {scales.x < 0.f ? 0 : there, scales.y < 0.f ? 0 : there};      // tokens below these are there, in either half
 #pragma unroll
@@ -446,7 +458,7 @@ struct RowTile {
                 behind |= mx[r][b] > m[r][b] + CA_RESCALE_AT;
             }
         const float vs = fmaxf(scales.z, scales.w);
-        if (__any_sync(0xffffffffu, behind || vs > v_scale)) {
+        if (__builtin_expect(__any_sync(0xffffffffu, behind || vs > v_scale), 0)) {
             const float shrink = vs > v_scale ? v_scale / vs : 1.f;
             v_scale = fmaxf(vs, v_scale);
 #pragma unroll
@@ -652,95 +664,134 @@ __global__ void __launch_bounds__(CA_THREADS, CA_PER_SM) cache_units_kernel(cons
     auto stage = [&](uint32_t n, int w) { return ring + (size_t)(n % C::STAGES * CA_WARPS + w) * C::BYTES; };
     bool ok = true;
     if (warp == CA_WARPS) {
-        // ---- the producer: a lane for each consumer
-        uint32_t n = 0;
-        if (lane < CA_WARPS) {
-            for (int phase = 0; phase < 2 && ok; ++phase) {
-                long long from, to;
-                warp_range(line, b * CA_WARPS + lane, from, to);
-                if (phase == 0) { from = x0; to = x1; }
-                if (from >= to) continue;
-                Cursor c;
-                c.begin(phase ? p.w.single : p.w.shared, phase ? sm.single[lane] : sm.shared, phase ? total.single_entries : total.shared_entries, to - from);
-                if (c.left <= 0) continue;
-                // a part that its piece does not have begins where no tokens are
-                auto token = [&] { const int parts = piece_parts(c.e.rows); return phase ? c.piece * CA_TOKENS : lane < parts ? (c.piece * parts + lane) * CA_TOKENS : c.e.tokens; };
-                Fetch now, next;
-                now.find(p, c, token(), true);
-                c.advance(Hkv);
-                bool more = c.left > 0;
-                if (more) next.find(p, c, token(), false);
+        // ---- the producer: eight lanes for each consumer, which look up eight pieces at once, the next eight while these are copied, and copy one after another
+        const int of = lane >> 3, k = lane & 7;
+        const uint32_t eight = 0xFFu << (of * 8);
+        uint32_t n = 0, asked = 0;                            // pieces of this consumer before the eight, asked for so far
+        for (int phase = 0; phase < 2 && ok; ++phase) {
+            long long from, to;
+            warp_range(line, b * CA_WARPS + of, from, to);
+            if (phase == 0) { from = x0; to = x1; }
+            Cursor c;
+            c.left = 0;
+            if (from < to) c.begin(phase ? p.w.single : p.w.shared, phase ? sm.single[of] : sm.shared, phase ? total.single_entries : total.shared_entries, to - from);
+            // a part that its piece does not have begins where no tokens are
+            auto token = [&] { const int parts = piece_parts(c.e.rows); return phase ? c.piece * CA_TOKENS : of < parts ? (c.piece * parts + of) * CA_TOKENS : c.e.tokens; };
+            for (int i = 0; i < k && c.left > 0; ++i) c.advance(Hkv);
+            Fetch now, next;
+            bool there = c.left > 0, more = false;
+            if (there) {
+                now.find(p, c, token(), k == 0);
                 now.find_scales(p);
-                for (;; ++n) {
-                    const uint32_t st = n % C::STAGES;
-                    if (!mbar_wait(&sm.empty[st][lane], ((n / C::STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-                    now.copy<DP>(p, &map_k, &map_v, smem_u32(stage(n, lane)), &sm.full[st][lane]);
-                    bool after_next = false;
-                    Fetch after;
-                    if (more) {
-                        c.advance(Hkv);
-                        after_next = c.left > 0;
-                        if (after_next) after.find(p, c, token(), false);
-                    }
-                    sm.info[st][lane] = now.info;
-                    mbar_arrive(&sm.full[st][lane]);
-                    if (!more) { ++n; break; }
-                    now = next;
-                    now.find_scales(p);
-                    next = after;
-                    more = after_next;
-                }
             }
-            if (ok && mbar_wait(&sm.empty[n % C::STAGES][lane], ((n / C::STAGES) & 1u) ^ 1u, abort_flag)) {
-                sm.info[n % C::STAGES][lane].flags = PIECE_NONE;
-                mbar_arrive(&sm.full[n % C::STAGES][lane]);
+            // Each consumer's eight lanes go on by themselves: `at` is the lane whose turn it is, a stage that is not free yet is asked for again in the next round.
+            int at = 8;
+            uint32_t fresh = 0;                               // rounds without any progress
+            bool begun = false;
+            for (;;) {
+                const uint32_t all = __ballot_sync(0xffffffffu, there) & eight;
+                if (at == 8 || at >= __popc(all)) {           // the next eight
+                    if (begun) {
+                        n += __popc(all);
+                        there = more;
+                        now = next;
+                    }
+                    begun = true;
+                    at = 0;
+                    c.skip(8, Hkv);
+                    more = there && c.left > 0;
+                    if (more) next.find(p, c, token(), false);
+                }
+                if (!__any_sync(0xffffffffu, there)) break;
+                const uint32_t mine = n + k, st = mine % C::STAGES;
+                const bool turn = there && k == at, go = turn && mbar_try_wait(&sm.empty[st][of], ((mine / C::STAGES) & 1u) ^ 1u);
+                if (go) {
+                    now.copy<DP>(p, &map_k, &map_v, smem_u32(stage(mine, of)), &sm.full[st][of]);
+                    sm.info[st][of] = now.info;
+                    mbar_arrive(&sm.full[st][of]);
+                    if (phase || of == 0) tell_owner(p, now.info, (int)(phase ? b * CA_WARPS + of : b));
+                }
+                const uint32_t went = __ballot_sync(0xffffffffu, go);
+                if (went & eight) {
+                    ++at;
+                    ++asked;
+                    if (at == 4 && more) next.find_scales(p);
+                }
+                fresh = went ? 0 : fresh + 1;
+                if (fresh > SPIN_LIMIT || ((fresh & 1023u) == 1023u && __any_sync(0xffffffffu, *abort_flag != 0u))) { *abort_flag = 1u; ok = false; break; }
+            }
+        }
+        if (k == 0) {
+            if (ok && mbar_wait(&sm.empty[n % C::STAGES][of], ((n / C::STAGES) & 1u) ^ 1u, abort_flag)) {
+                sm.info[n % C::STAGES][of].flags = PIECE_NONE;
+                mbar_arrive(&sm.full[n % C::STAGES][of]);
             } else {
                 // let the copies in flight land before the block's shared memory goes away (all have, unless a wait ran out)
-                for (uint32_t i = n > C::STAGES ? n - C::STAGES : 0; i < n; ++i)
+                for (uint32_t i = asked > C::STAGES ? asked - C::STAGES : 0; i < asked; ++i)
                     for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
-                        if (mbar_try_wait(&sm.full[i % C::STAGES][lane], (i / C::STAGES) & 1u)) break;
+                        if (mbar_try_wait(&sm.full[i % C::STAGES][of], (i / C::STAGES) & 1u)) break;
             }
         }
         __syncwarp();
     } else {
+        // Units one behind another.  What a unit's pieces have in common stands outside their loop, which is kept short: a warp that jumps over code that it seldom needs waits
+        // for instructions each time.
         RowTile<DP> tile;
-        for (uint32_t n = 0;; ++n) {
-            const uint32_t st = n % C::STAGES, parity = (n / C::STAGES) & 1u;
-            if (!mbar_wait_warp(&sm.full[st][warp], parity, abort_flag)) break;
-            const PieceInfo& e = sm.info[st][warp];
-            const int flags = e.flags, rows = flags >> PIECE_ROWS;
-            if (flags & PIECE_NONE) break;
+        for (uint32_t n = 0; ok;) {
+            if (!mbar_wait_warp(&sm.full[n % C::STAGES][warp], (n / C::STAGES) & 1u, abort_flag)) break;
+            const PieceInfo& e = sm.info[n % C::STAGES][warp];
+            const int rows = e.flags >> PIECE_ROWS, entry = e.entry, head = e.head;
+            if (e.flags & PIECE_NONE) break;
             // a shared piece: a tile of 16 rows a warp; with two tiles two warps share a tile's tokens
             const bool shared = rows > CA_ALONE;
             const int row_tiles = rows > 32 ? 4 : 2, row0 = shared ? (warp & (row_tiles - 1)) * 16 : 0, left = rows - row0, share = shared ? warp / row_tiles : warp;
-            if (shared) {
-                for (int w = 0; w < CA_WARPS && ok; ++w) ok = mbar_wait_warp(&sm.full[st][w], parity, abort_flag);
-                if (!ok) break;
-            }
-            if ((flags & PIECE_FIRST) && left > 0) {
-                if (e.entry < p.prompts) find_live(p, e.entry, sm.live[warp], lane);
+            if (left > 0) {
+                if (entry < p.prompts) find_live(p, entry, sm.live[warp], lane);
                 tile.load(p, lane, query_row(p, e, sm.live[warp], row0 + (lane >> 2)), 0);
                 if (left > 8) tile.load(p, lane, query_row(p, e, sm.live[warp], row0 + 8 + (lane >> 2)), 1);
             }
-            for (int w = share; w < CA_WARPS; w += shared ? CA_WARPS / row_tiles : CA_WARPS) {
-                const PieceInfo& part = sm.info[st][w];
-                if (part.there <= 0 || left <= 0) break;
-                if (left > 8) tile.template piece<2>(stage(n, w), part, lane);
-                else tile.template piece<1>(stage(n, w), part, lane);
+            auto single_pieces = [&](auto eights) {
+                for (;;) {
+                    const uint32_t st = n % C::STAGES;
+                    const PieceInfo& piece = sm.info[st][warp];
+                    tile.template piece<decltype(eights)::value>(stage(n, warp), piece, lane);
+                    const bool last = piece.flags & PIECE_LAST;
+                    // what was read by instructions comes before the copies that fill the stage again
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_n(&sm.empty[st][warp], CA_WARPS);
+                    ++n;
+                    if (last) break;
+                    if (!mbar_wait_warp(&sm.full[n % C::STAGES][warp], (n / C::STAGES) & 1u, abort_flag)) { ok = false; break; }
+                }
+            };
+            if (shared) {
+                for (;;) {
+                    const uint32_t st = n % C::STAGES, parity = (n / C::STAGES) & 1u;
+                    for (int w = 0; w < CA_WARPS && ok; ++w) ok = mbar_wait_warp(&sm.full[st][w], parity, abort_flag);
+                    if (!ok) break;
+                    for (int w = share; w < CA_WARPS; w += CA_WARPS / row_tiles)
+                        if (sm.info[st][w].there > 0 && left > 0) tile.template piece<2>(stage(n, w), sm.info[st][w], lane);
+                    const bool last = sm.info[st][warp].flags & PIECE_LAST;
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane < CA_WARPS) mbar_arrive(&sm.empty[st][lane]);
+                    ++n;
+                    if (last) break;
+                }
+            } else if (left > 8) {
+                single_pieces(std::integral_constant<int, 2>());
+            } else {
+                single_pieces(std::integral_constant<int, 1>());
             }
-            if (lane == 0 && (!shared || warp == 0)) tell_owner(p, e, (int)(shared ? b : b * CA_WARPS + warp));
-            if ((flags & PIECE_LAST) && left > 0) {
-                const int64_t unit = (int64_t)e.entry * Hkv + e.head, owner = b * CA_WARPS + warp;
+            if (!ok) break;
+            if (left > 0) {
+                const int64_t unit = (int64_t)entry * Hkv + head, owner = b * CA_WARPS + warp;
                 const int64_t record = shared ? p.w.rows_own + p.w.rows_prompt + (unit + b) * CA_ROWS + (row_tiles == 2 ? share * 32 : 0) + row0
-                                     : e.entry < p.prompts ? p.w.rows_own + (unit + owner) * CA_ALONE : (unit - (int64_t)p.prompts * Hkv + owner) * p.ratio;
+                                     : entry < p.prompts ? p.w.rows_own + (unit + owner) * CA_ALONE : (unit - (int64_t)p.prompts * Hkv + owner) * p.ratio;
                 tile.store(p, record, left, lane, 0);
                 if (left > 8) tile.store(p, record, left, lane, 1);
             }
-            // what was read by instructions comes before the copies that fill the stage again
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (shared ? lane < CA_WARPS : lane == 0) mbar_arrive_n(&sm.empty[st][shared ? lane : warp], shared ? 1 : CA_WARPS);
-            __syncwarp();
         }
     }
     __syncthreads();
