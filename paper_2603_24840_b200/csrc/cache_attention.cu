@@ -19,13 +19,12 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int CA_WARPS = 4, CA_THREADS = 32 * (CA_WARPS + 1);      // consumers; one more warp brings their pieces
-constexpr int CA_PER_SM = 2;                       // blocks
 constexpr int CA_ROWS = 64;                        // query rows of a shared unit
 constexpr int CA_ALONE = 16;                       // query rows up to which a unit is a warp's
 constexpr int CA_TOKENS = 32;                      // a single piece; a shared one is four of them, two for more than 32 rows, so that a warp has two to compute
 // The line that the work is cut along, in single pieces: what a shared piece costs, and what a unit costs before its first piece (queries, results) in pieces of its kind.
-constexpr int CA_SHARED_COST = 11, CA_SHARED_SETUP = 1, CA_SINGLE_SETUP = 3;
-constexpr int CA_SCANNED = 1024;                   // entries that a block keeps in shared memory between the two passes of its scan
+constexpr int CA_SHARED_COST = 13, CA_SHARED_SETUP = 1, CA_SINGLE_SETUP = 3;
+constexpr int CA_SCANNED = 768;                    // entries that a block keeps in shared memory between the two passes of its scan
 constexpr float CA_RESCALE_AT = 8.0f;              // the running maximum follows once it is 2^8 behind
 constexpr float CA_P_SCALE = 128.0f;               // probabilities up to 2^8 times 2^7 stay below fp16's largest
 
@@ -45,12 +44,13 @@ struct CacheWorkspace {
     size_t bytes;
 };
 
+inline int ca_per_sm(int D) { return D <= 64 ? 3 : 2; }                            // blocks
 inline int ca_group(int ratio) { return CA_ROWS / ratio; }                         // rollouts a prompt entry
 inline int ca_blocks(int G, int ratio) { return (G + ca_group(ratio) - 1) / ca_group(ratio); }
 
 inline CacheWorkspace cache_workspace(void* base, int sm_count, int N, int P, int G, int Hq, int Hkv, int D) {
     const int ratio = Hq / Hkv;
-    const int64_t grid = (int64_t)sm_count * CA_PER_SM, prompts = P > 0 ? (int64_t)P * ca_blocks(G, ratio) : 0, entries = prompts + N;
+    const int64_t grid = (int64_t)sm_count * ca_per_sm(D), prompts = P > 0 ? (int64_t)P * ca_blocks(G, ratio) : 0, entries = prompts + N;
     CacheWorkspace w = {};
     // a unit has one record, and one more for every border between blocks (warps) that falls into it: numbers unit + block (warp)
     w.rows_own = ratio <= CA_ALONE ? ((int64_t)N * Hkv + grid * CA_WARPS) * ratio : 0;
@@ -218,7 +218,7 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 template <int DP>
 struct CacheConf {
     static constexpr int KEYS = CA_TOKENS * DP, BYTES = 2 * KEYS;
-    static constexpr int STAGES = DP == 128 ? 3 : 4;
+    static constexpr int STAGES = 3, PER_SM = DP == 128 ? 2 : 3;
     static constexpr int CHUNKS = DP / 16;
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * CA_WARPS * BYTES;
     static __device__ __forceinline__ uint32_t at(int row, int chunk) { return row * DP + ((chunk ^ (DP == 128 ? row & 7 : row >> 1 & 3)) << 4); }
@@ -402,11 +402,15 @@ struct RowTile {
         const float4 scales = *reinterpret_cast<const float4*>(info.scales);
         const uint32_t keys = smem_u32(stage), values = keys + C::KEYS;
         const int later = (lane >> 3) & 1, row = later * 8 + ((lane + 4 * later) & 7);
-        float s[2][ROWS][4];
+        // every other product of eight rows adds up by itself: one after the other they would wait for one another
+        constexpr int CHAINS = ROWS == 1 ? 2 : 1;
+        float s[2][ROWS][4], chain[CHAINS][2][ROWS][4];
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int i = 0; i < CHAINS; ++i)
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) s[half][r][0] = s[half][r][1] = s[half][r][2] = s[half][r][3] = 0.f;
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) chain[i][half][r][0] = chain[i][half][r][1] = chain[i][half][r][2] = chain[i][half][r][3] = 0.f;
 #pragma unroll
         for (int c = 0; c < C::CHUNKS; c += 2)
 #pragma unroll
@@ -415,11 +419,17 @@ struct RowTile {
                 ldmatrix_rows(keys + C::at(half * 16 + row, c + (lane >> 4)), w);
                 widen(a, w[0], w[1]);
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) mma_f16(s[half][r], a, q[c][r][0], q[c][r][1]);
+                for (int r = 0; r < ROWS; ++r) mma_f16(chain[0][half][r], a, q[c][r][0], q[c][r][1]);
                 widen(a, w[2], w[3]);
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) mma_f16(s[half][r], a, q[c + 1][r][0], q[c + 1][r][1]);
+                for (int r = 0; r < ROWS; ++r) mma_f16(chain[CHAINS - 1][half][r], a, q[c + 1][r][0], q[c + 1][r][1]);
             }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) s[half][r][x] = CHAINS == 2 ? chain[0][half][r][x] + chain[CHAINS - 1][half][r][x] : chain[0][half][r][x];
         float f[2][ROWS][2];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
@@ -574,7 +584,7 @@ __device__ __forceinline__ void find_live(const CacheParams& p, int e, int* live
 }
 
 template <int DP>
-__global__ void __launch_bounds__(CA_THREADS, CA_PER_SM) cache_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const CacheParams p) {
+__global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const CacheParams p) {
     using C = CacheConf<DP>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) CacheShared sm;
@@ -768,7 +778,7 @@ __global__ void __launch_bounds__(CA_THREADS, CA_PER_SM) cache_units_kernel(cons
             if (shared) {
                 for (;;) {
                     const uint32_t st = n % C::STAGES, parity = (n / C::STAGES) & 1u;
-                    for (int w = 0; w < CA_WARPS && ok; ++w) ok = mbar_wait_warp(&sm.full[st][w], parity, abort_flag);
+                    ok = mbar_wait_warp(&sm.full[st][lane % CA_WARPS], parity, abort_flag);       // all four at once, a lane each
                     if (!ok) break;
                     for (int w = share; w < CA_WARPS; w += CA_WARPS / row_tiles)
                         if (sm.info[st][w].there > 0 && left > 0) tile.template piece<2>(stage(n, w), sm.info[st][w], lane);
@@ -969,7 +979,7 @@ extern "C" int arrol_cache_attention(arrol_ctx* ctx, const arrol_cache_attention
     p.prompts = a->P * p.blocks;
     p.entries = p.prompts + a->N;
     p.page_shift = __builtin_ctz((unsigned)a->cache.page);
-    p.grid = ctx->sm_count * CA_PER_SM;
+    p.grid = ctx->sm_count * ca_per_sm(a->cache.D);
     p.scale_log2 = a->scale * LOG2E;
     p.status = ctx->d_status;
     ArrolDeviceGuard guard(ctx->device);
