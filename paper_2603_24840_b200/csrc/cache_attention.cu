@@ -34,7 +34,6 @@ struct alignas(16) CacheEntry {
 };
 
 struct CacheWorkspace {
-    long long* head;           // [0] length of the shared line, [1] of the single one, [2] cost that a block takes
     int2* owners;              // [entries][Hkv]: the first and the last block (warp) that has some of the unit
     CacheEntry* shared;        // entries with pieces, in order
     CacheEntry* single;
@@ -60,7 +59,6 @@ inline CacheWorkspace cache_workspace(void* base, int sm_count, int N, int P, in
     size_t at = 0;
     auto take = [&](size_t n) { uint8_t* q = p + at; at += (n + 255) & ~(size_t)255; return q; };
     const int64_t rows = w.rows_own + w.rows_prompt + w.rows_shared;
-    w.head = reinterpret_cast<long long*>(take(256));
     w.owners = reinterpret_cast<int2*>(take((size_t)entries * Hkv * sizeof(int2)));
     w.shared = reinterpret_cast<CacheEntry*>(take((size_t)entries * sizeof(CacheEntry)));
     w.single = reinterpret_cast<CacheEntry*>(take((size_t)entries * sizeof(CacheEntry)));
@@ -84,32 +82,26 @@ struct Line {
     long long shared, single;      // lengths: units' pieces and setups
     long long per;                 // cost that a block takes
 };
+// Shares are such that every block (warp) between the first and the last that has some of a unit has one of its pieces: a share holds a shared piece, and the single
+// line begins where four warps have as much of it each.
+__device__ __forceinline__ long long single_begin(long long shared) { return (shared * CA_SHARED_COST + CA_WARPS - 1) / CA_WARPS * CA_WARPS; }
 __device__ __forceinline__ Line make_line(long long shared, long long single, int grid) {
-    const long long cost = shared * CA_SHARED_COST + single;
-    return {shared, single, cost <= grid ? 1 : (cost + grid - 1) / grid};
+    const long long each = (single_begin(shared) + single + grid - 1) / grid;
+    return {shared, single, (max(each, (long long)(shared > 0 ? CA_SHARED_COST : 1)) + CA_WARPS - 1) / CA_WARPS * CA_WARPS};
 }
 // the shared line from there on is block b's or a later one's
 __device__ __forceinline__ long long shared_begin(const Line& l, long long b) {
     const long long x = (b * l.per + CA_SHARED_COST - 1) / CA_SHARED_COST;
     return x < l.shared ? x : l.shared;
 }
-// block b's part of the single line, before it is cut to what there is, and that of each of its warps
-__device__ __forceinline__ void single_range(const Line& l, long long b, long long& lo, long long& each) {
-    const long long at = l.shared * CA_SHARED_COST;
-    lo = b * l.per - at;
-    if (lo < 0) lo = 0;
-    const long long hi = (b + 1) * l.per - at;
-    each = hi > lo ? (hi - lo + CA_WARPS - 1) / CA_WARPS : 0;
-}
+// a warp's part of the single line, from y0 to y1 (none where that is not more); warps are counted over all blocks
 __device__ __forceinline__ void warp_range(const Line& l, long long warp, long long& y0, long long& y1) {
-    long long lo, each;
-    const long long b = warp / CA_WARPS, k = warp % CA_WARPS;
-    single_range(l, b, lo, each);
-    long long hi = (b + 1) * l.per - l.shared * CA_SHARED_COST;
-    if (hi > l.single) hi = l.single;
+    const long long begin = single_begin(l.shared), b = warp / CA_WARPS, k = warp % CA_WARPS;
+    const long long lo = max(b * l.per - begin, 0ll), each = max((b + 1) * l.per - begin - lo, 0ll) / CA_WARPS;
     y0 = lo + k * each;
-    y1 = y0 + each < hi ? y0 + each : hi;
+    y1 = min(y0 + each, l.single);
 }
+
 // Live rollouts of group p.
 __device__ __forceinline__ int live_of(const CacheParams& p, int q) {
     const int G = p.a.G;
@@ -635,7 +627,6 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
         total = total + sm.warp_sums[w];
     }
     const Line line = make_line(total.shared, total.single, p.grid);
-    if (b == 0 && threadIdx.x == 0) { p.w.head[0] = line.shared; p.w.head[1] = line.single; p.w.head[2] = line.per; }
     const long long x0 = shared_begin(line, b), x1 = shared_begin(line, b + 1);
     long long y0[CA_WARPS], y1[CA_WARPS];
 #pragma unroll
@@ -808,9 +799,9 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
     if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, ARROL_DEV_WAIT_EXPIRED);
 }
 
-// A warp per (rollout, query head): the prompt's records, then its own, in order; four dimensions a lane.  Records are asked for four at a time.
+// A warp per (rollout, query head): the prompt's records, then its own, in order; four dimensions a lane.  Records are asked for eight at a time.
 struct Merged {
-    static constexpr int AT_ONCE = 4;
+    static constexpr int AT_ONCE = 8;
     float top, total;
     float4 sum;
     __device__ __forceinline__ void add(const float2 (&x)[AT_ONCE], const float4 (&v)[AT_ONCE]) {
@@ -838,11 +829,9 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
     const int64_t row = blockIdx.x * (int64_t)8 + (threadIdx.x >> 5);
     if (row >= (int64_t)a.N * a.Hq) return;
     const int i = (int)(row / a.Hq), hq = (int)(row - (int64_t)i * a.Hq), h = hq / p.ratio, r = hq - h * p.ratio;
-    const long long* head = pdl_acquire(p.w.head);
     const int2* owners = pdl_acquire(p.w.owners);
     const float2* ml = pdl_acquire(p.w.ml);
     const float* o = pdl_acquire(p.w.o);
-    const Line line = {head[0], head[1], head[2]};
     bool bad = false;
     const int own_tokens = cache_tokens(a.lengths, i, a.table_pages, a.cache.page, bad);
     const int2 own = owners[(int64_t)(p.prompts + i) * Hkv + h];       // not read where there are no tokens
@@ -866,31 +855,18 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
     }
     if (a.keep && !a.keep[i]) return;
     Merged m = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    // `x`: a prompt's entry, or the rollout's own
-    auto unit = [&](bool prompt, int rows, int2 of, int row_in) {
-        const int64_t number = prompt ? (int64_t)entry * Hkv + h : (int64_t)i * Hkv + h;
-        const bool in_blocks = rows > CA_ALONE;
-        const int twice = in_blocks && rows <= 32 ? 1 : 0;    // two warps' records a block
-        for (int64_t k0 = (int64_t)of.x << twice; k0 <= ((int64_t)of.y << twice | twice); k0 += Merged::AT_ONCE) {
+    // records of the blocks (warps) that have some of a unit, `step` rows apart; of shared units of up to 32 rows two each, CA_ROWS / 2 apart
+    auto unit = [&](int rows, int2 of, int64_t first, int step) {
+        const int twice = rows > CA_ALONE && rows <= 32 ? 1 : 0;
+        for (int w = of.x << twice; w <= (of.y << twice | twice); w += Merged::AT_ONCE) {
             float2 x[Merged::AT_ONCE];
             float4 v[Merged::AT_ONCE];
 #pragma unroll
             for (int k = 0; k < Merged::AT_ONCE; ++k) {
                 x[k] = make_float2(-INFINITY, 0.f);
                 v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                const int64_t w = (k0 + k) >> twice;
-                bool there = w <= of.y;
-                int64_t at;
-                if (in_blocks) {
-                    there = there && shared_begin(line, w) < shared_begin(line, w + 1);
-                    at = p.w.rows_own + p.w.rows_prompt + ((prompt ? number : (int64_t)(p.prompts + i) * Hkv + h) + w) * CA_ROWS + row_in + ((k0 + k) & twice) * 32;
-                } else {
-                    long long y0, y1;
-                    warp_range(line, w, y0, y1);
-                    there = there && y0 < y1;
-                    at = prompt ? p.w.rows_own + (number + w) * CA_ALONE + row_in : (number + w) * p.ratio + row_in;
-                }
-                if (there) {
+                if (w + k <= (of.y << twice | twice)) {
+                    const int64_t at = first + (int64_t)((w + k) >> twice) * step + ((w + k) & twice) * (CA_ROWS / 2);
                     x[k] = ml[at];
                     if (d < D) v[k] = *reinterpret_cast<const float4*>(o + at * D + d);
                 }
@@ -898,8 +874,15 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
             m.add(x, v);
         }
     };
-    if (prompt_tokens > 0) unit(true, prompt_rows, shared, prompt_row);
-    if (own_tokens > 0) unit(false, p.ratio, own, r);
+    const int64_t own_number = (int64_t)i * Hkv + h, prompt_number = (int64_t)entry * Hkv + h, shared_rows = p.w.rows_own + p.w.rows_prompt;
+    if (prompt_tokens > 0) {
+        if (prompt_rows > CA_ALONE) unit(prompt_rows, shared, shared_rows + prompt_number * CA_ROWS + prompt_row, CA_ROWS);
+        else unit(prompt_rows, shared, p.w.rows_own + prompt_number * CA_ALONE + prompt_row, CA_ALONE);
+    }
+    if (own_tokens > 0) {
+        if (p.ratio > CA_ALONE) unit(p.ratio, own, shared_rows + ((int64_t)p.prompts * Hkv + own_number) * CA_ROWS + r, CA_ROWS);
+        else unit(p.ratio, own, own_number * p.ratio + r, p.ratio);
+    }
     const bool any = prompt_tokens > 0 || own_tokens > 0;     // none: no key
     const float inv = any ? 1.f / m.total : 0.f;
     if (d < D) {
