@@ -23,7 +23,13 @@ constexpr int CA_ROWS = 64;                        // query rows of a shared uni
 constexpr int CA_ALONE = 16;                       // query rows up to which a unit is a warp's
 constexpr int CA_TOKENS = 32;                      // a single piece; a shared one is four of them, two for more than 32 rows, so that a warp has two to compute
 // The line that the work is cut along, in single pieces: what a shared piece costs, and what a unit costs before its first piece (queries, results) in pieces of its kind.
-constexpr int CA_SHARED_COST = 13, CA_SHARED_SETUP = 1, CA_SINGLE_SETUP = 3;
+// From clocks around the parts (cycles with heads up to 64 and above): a shared piece 4,000 and 6,300 to 8,400 of four warps, a single one 1,640 and 2,700 of one; a single unit's
+// queries, first wait and results 5,800 and 7,000 to 9,000.
+constexpr int CA_SHARED_SETUP = 1;
+struct LineCosts {
+    int shared, single_setup;
+};
+__host__ __device__ inline LineCosts line_costs(int D) { return D <= 64 ? LineCosts{10, 4} : LineCosts{12, 3}; }
 constexpr int CA_SCANNED = 768;                    // entries that a block keeps in shared memory between the two passes of its scan
 constexpr float CA_RESCALE_AT = 8.0f;              // the running maximum follows once it is 2^8 behind
 constexpr float CA_P_SCALE = 128.0f;               // probabilities up to 2^8 times 2^7 stay below fp16's largest
@@ -73,6 +79,7 @@ struct CacheParams {
     CacheWorkspace w;
     int ratio, group, blocks, prompts, entries;    // rollouts a prompt entry, entries a prompt, prompt entries, all
     int page_shift, grid;
+    LineCosts costs;
     float scale_log2;
     uint32_t* status;
 };
@@ -81,22 +88,23 @@ struct CacheParams {
 struct Line {
     long long shared, single;      // lengths: units' pieces and setups
     long long per;                 // cost that a block takes
+    int cost;                      // of a shared piece
 };
 // Shares are such that every block (warp) between the first and the last that has some of a unit has one of its pieces: a share holds a shared piece, and the single
 // line begins where four warps have as much of it each.
-__device__ __forceinline__ long long single_begin(long long shared) { return (shared * CA_SHARED_COST + CA_WARPS - 1) / CA_WARPS * CA_WARPS; }
-__device__ __forceinline__ Line make_line(long long shared, long long single, int grid) {
-    const long long each = (single_begin(shared) + single + grid - 1) / grid;
-    return {shared, single, (max(each, (long long)(shared > 0 ? CA_SHARED_COST : 1)) + CA_WARPS - 1) / CA_WARPS * CA_WARPS};
+__device__ __forceinline__ long long single_begin(long long shared, int cost) { return (shared * cost + CA_WARPS - 1) / CA_WARPS * CA_WARPS; }
+__device__ __forceinline__ Line make_line(long long shared, long long single, int grid, int cost) {
+    const long long each = (single_begin(shared, cost) + single + grid - 1) / grid;
+    return {shared, single, (max(each, (long long)(shared > 0 ? cost : 1)) + CA_WARPS - 1) / CA_WARPS * CA_WARPS, cost};
 }
 // the shared line from there on is block b's or a later one's
 __device__ __forceinline__ long long shared_begin(const Line& l, long long b) {
-    const long long x = (b * l.per + CA_SHARED_COST - 1) / CA_SHARED_COST;
+    const long long x = (b * l.per + l.cost - 1) / l.cost;
     return x < l.shared ? x : l.shared;
 }
 // a warp's part of the single line, from y0 to y1 (none where that is not more); warps are counted over all blocks
 __device__ __forceinline__ void warp_range(const Line& l, long long warp, long long& y0, long long& y1) {
-    const long long begin = single_begin(l.shared), b = warp / CA_WARPS, k = warp % CA_WARPS;
+    const long long begin = single_begin(l.shared, l.cost), b = warp / CA_WARPS, k = warp % CA_WARPS;
     const long long lo = max(b * l.per - begin, 0ll), each = max((b + 1) * l.per - begin - lo, 0ll) / CA_WARPS;
     y0 = lo + k * each;
     y1 = min(y0 + each, l.single);
@@ -123,7 +131,7 @@ __device__ __forceinline__ int entry_pieces(int rows, int tokens) {
     const int of = CA_TOKENS * piece_parts(rows);             // a power of two
     return (int)(((int64_t)tokens + of - 1) / of);
 }
-__device__ __forceinline__ int unit_setup(int rows) { return rows > CA_ALONE ? CA_SHARED_SETUP : CA_SINGLE_SETUP; }
+__device__ __forceinline__ int unit_setup(const CacheParams& p, int rows) { return rows > CA_ALONE ? CA_SHARED_SETUP : p.costs.single_setup; }
 // {tokens, rows} of an entry; no rows where it is left out.
 __device__ __forceinline__ int2 entry_size(const CacheParams& p, int e, bool& bad) {
     const arrol_cache_attention_args& a = p.a;
@@ -226,13 +234,13 @@ struct Cursor {
     __device__ __forceinline__ void fetch() {
         if (number + 1 <= last) next = list[number + 1];
     }
-    __device__ __forceinline__ void begin(const CacheEntry* l, const Start& s, int entries, long long length) {
+    __device__ __forceinline__ void begin(const CacheParams& p, const CacheEntry* l, const Start& s, int entries, long long length) {
         list = l;
         e = s.e;
         number = s.number;
         last = entries - 1;
         left = length;
-        setup = unit_setup(e.rows);
+        setup = unit_setup(p, e.rows);
         head = (int)(s.offset / (e.pieces + setup));
         piece = (int)(s.offset - (long long)head * (e.pieces + setup)) - setup;
         if (piece < 0) { left += piece; piece = 0; }
@@ -603,7 +611,7 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
     const int each = (p.entries + CA_THREADS - 1) / CA_THREADS;
     const int e0 = min((int)threadIdx.x * each, p.entries), e1 = min(e0 + each, p.entries);
     auto size = [&](int e) { return e < CA_SCANNED ? sm.sizes[e] : entry_size(p, e, bad); };
-    auto length = [&](int2 x) { return (long long)(entry_pieces(x.y, x.x) + unit_setup(x.y)) * Hkv; };
+    auto length = [&](int2 x) { return (long long)(entry_pieces(x.y, x.x) + unit_setup(p, x.y)) * Hkv; };
     ScanSums mine = {0, 0, 0, 0};
     for (int e = e0; e < e1; ++e) {
         const int2 x = size(e);
@@ -626,7 +634,7 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
         if (w < warp) at = at + sm.warp_sums[w];
         total = total + sm.warp_sums[w];
     }
-    const Line line = make_line(total.shared, total.single, p.grid);
+    const Line line = make_line(total.shared, total.single, p.grid, p.costs.shared);
     const long long x0 = shared_begin(line, b), x1 = shared_begin(line, b + 1);
     long long y0[CA_WARPS], y1[CA_WARPS];
 #pragma unroll
@@ -675,7 +683,7 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
             if (phase == 0) { from = x0; to = x1; }
             Cursor c;
             c.left = 0;
-            if (from < to) c.begin(phase ? p.w.single : p.w.shared, phase ? sm.single[of] : sm.shared, phase ? total.single_entries : total.shared_entries, to - from);
+            if (from < to) c.begin(p, phase ? p.w.single : p.w.shared, phase ? sm.single[of] : sm.shared, phase ? total.single_entries : total.shared_entries, to - from);
             // a part that its piece does not have begins where no tokens are
             auto token = [&] { const int parts = piece_parts(c.e.rows); return phase ? c.piece * CA_TOKENS : of < parts ? (c.piece * parts + of) * CA_TOKENS : c.e.tokens; };
             for (int i = 0; i < k && c.left > 0; ++i) c.advance(Hkv);
@@ -963,6 +971,7 @@ extern "C" int arrol_cache_attention(arrol_ctx* ctx, const arrol_cache_attention
     p.entries = p.prompts + a->N;
     p.page_shift = __builtin_ctz((unsigned)a->cache.page);
     p.grid = ctx->sm_count * ca_per_sm(a->cache.D);
+    p.costs = line_costs(a->cache.D);
     p.scale_log2 = a->scale * LOG2E;
     p.status = ctx->d_status;
     ArrolDeviceGuard guard(ctx->device);
