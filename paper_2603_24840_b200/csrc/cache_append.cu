@@ -4,6 +4,8 @@
 // there are few.  A page's scale needs the largest entry of all of its new tokens before the first can be rounded, so a page and head belong to one block
 // (append_runs_kernel: runs of tokens) or one warp (append_one_kernel: a token per sequence), which holds the turned values in registers in between: nothing is read
 // twice, and no atomics take part.
+#include <type_traits>
+
 #include "cache_common.cuh"
 #include "rotary_common.cuh"
 
@@ -126,44 +128,40 @@ __global__ void __launch_bounds__(32 * ONE_WARPS) append_one_kernel(const Append
     if (lane == 0 && (slot == 0 || grows)) *scale = cache_power(e);
 }
 
-// ---- runs of tokens: a block per page that gets some (and part of the heads); a thread has one unit of one token, its angles in registers, and goes through the heads
-// A unit of token `tok` of the page, turned; nothing where the token is none of the run's.
+// ---- runs of tokens: a block per page that gets some, for keys and queries or for values (and part of the heads); a thread has one unit of one token, its angles in
+// registers, and goes through the heads
 template <int V>
-__device__ __forceinline__ void append_load(const AppendParams& p, const RotaryUnit<V>& unit, const __nv_bfloat16* row, bool turn, float (&x)[V], float (&y)[V]) {
-    typedef typename Bf16Chunk<V>::type Chunk;
-    chunk_to_floats<V>(*reinterpret_cast<const Chunk*>(row + unit.a), x);
-    chunk_to_floats<V>(*reinterpret_cast<const Chunk*>(row + unit.b), y);
-    if (turn) unit.turn(p.pairs, x, y);
+__device__ __forceinline__ void not_finite_to_nan(float (&x)[V], float (&y)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) { x[j] += x[j] - x[j]; y[j] += y[j] - y[j]; }
 }
+// V numbers times `by`, none of them infinite.
 template <int V>
 __device__ __forceinline__ void append_codes(uint8_t* to, const float (&x)[V], float by) {
     if constexpr (V == 1) {
-        *to = (uint8_t)e4m3_pair(x[0] * by, 0.f);
+        *to = (uint8_t)e4m3_pair_finite(x[0] * by, 0.f);
     } else if constexpr (V == 2) {
-        *reinterpret_cast<uint16_t*>(to) = e4m3_pair(x[0] * by, x[1] * by);
+        *reinterpret_cast<uint16_t*>(to) = e4m3_pair_finite(x[0] * by, x[1] * by);
     } else {
+        uint32_t w[V / 4];
 #pragma unroll
-        for (int j = 0; j < V; j += 4)
-            *reinterpret_cast<uint32_t*>(to + j) = e4m3_pair(x[j] * by, x[j + 1] * by) | (uint32_t)e4m3_pair(x[j + 2] * by, x[j + 3] * by) << 16;
+        for (int j = 0; j < V / 4; ++j)
+            w[j] = e4m3_pair_finite(x[4 * j] * by, x[4 * j + 1] * by) | (uint32_t)e4m3_pair_finite(x[4 * j + 2] * by, x[4 * j + 3] * by) << 16;
+        if constexpr (V == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t*>(to) = w[0];
     }
-}
-template <>
-__device__ __forceinline__ void append_codes<8>(uint8_t* to, const float (&x)[8], float by) {
-    uint2 w;
-    w.x = e4m3_pair(x[0] * by, x[1] * by) | (uint32_t)e4m3_pair(x[2] * by, x[3] * by) << 16;
-    w.y = e4m3_pair(x[4] * by, x[5] * by) | (uint32_t)e4m3_pair(x[6] * by, x[7] * by) << 16;
-    *reinterpret_cast<uint2*>(to) = w;
 }
 
 template <int V, int THREADS>
-__global__ void __launch_bounds__(THREADS) append_runs_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_runs_kernel(const AppendParams p) {
     typedef typename Bf16Chunk<V>::type Chunk;
-    __shared__ float2 most[2][32];                           // per warp: largest of the keys, of the values
+    __shared__ uint32_t most[3];                             // largest of a head, as bits: in turn
     pdl_launch_dependents();
     pdl_wait();
     const arrol_cache_append_args& a = p.a;
-    const int page_size = a.cache.page, D = a.cache.D, Hkv = a.cache.Hkv, warps = blockDim.x >> 5;
+    const int page_size = a.cache.page, D = a.cache.D, Hkv = a.cache.Hkv, lane = threadIdx.x & 31;
     const int64_t* cu = pdl_acquire(a.cu_new);
+    if (threadIdx.x < 3) most[threadIdx.x] = 0u;             // published by the search's barriers
     // Sequence i has the blocks from cu[i] / page + 2 i on: a run of n tokens touches n / page + 2 pages at most, whatever slot it begins in.
     const int64_t u = blockIdx.x;
     const int64_t i64 = block_search(a.N, [&](int64_t i) { return cu[i + 1] / page_size + 2 * (i + 1) <= u; });
@@ -190,87 +188,113 @@ __global__ void __launch_bounds__(THREADS) append_runs_kernel(const AppendParams
     int tok = threadIdx.x / p.units;
     RotaryUnit<V> unit(p.pairs, threadIdx.x - tok * p.units);
     bool mine = (int)threadIdx.x < items;
+    const int passes = THREADS == 512 ? 1 : p.passes;        // a small block's page always fits
     auto pass_to = [&](int pass) {                           // only where a page's units are more than the block's threads
         const int x = threadIdx.x + pass * blockDim.x;
         tok = x / p.units;
         unit = RotaryUnit<V>(p.pairs, x - tok * p.units);
         mine = x < items;
-        if (mine) unit.at(p.pairs, first_position + tok);
+        if (mine && blockIdx.z == 0) unit.at(p.pairs, first_position + tok);
     };
-    if (mine) unit.at(p.pairs, first_position + tok);
-    const __nv_bfloat16* const k = static_cast<const __nv_bfloat16*>(a.k) + first_row * a.k_stride;
-    const __nv_bfloat16* const v = static_cast<const __nv_bfloat16*>(a.v) + first_row * a.v_stride;
-    int turn = 0;
-    for (int h = blockIdx.y; h < Hkv; h += gridDim.y, turn ^= 1) {
-        float kx[V], ky[V], vx[V], vy[V];
-        float2 m = {0.f, 0.f};
-        float* const k_scale = a.cache.k_scale + page * a.cache.k_scale_stride + h;
-        float* const v_scale = a.cache.v_scale + page * a.cache.v_scale_stride + h;
-        const float2 old = slot0 ? make_float2(*k_scale, *v_scale) : make_float2(0.f, 0.f);
-        for (int pass = 0; pass < p.passes; ++pass) {
-            if (p.passes > 1) pass_to(pass);
-            if (mine) {
-                append_load<V>(p, unit, k + tok * a.k_stride + (int64_t)h * D, true, kx, ky);
-                append_load<V>(p, unit, v + tok * a.v_stride + (int64_t)h * D, false, vx, vy);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    m.x = finite_max(finite_max(m.x, kx[j]), ky[j]);
-                    m.y = finite_max(finite_max(m.y, vx[j]), vy[j]);
+    if (mine && blockIdx.z == 0) unit.at(p.pairs, first_position + tok);
+    const bool values = blockIdx.z != 0;
+    const __nv_bfloat16* const rows = static_cast<const __nv_bfloat16*>(values ? a.v : a.k) + first_row * (values ? a.v_stride : a.k_stride);
+    const int64_t stride = values ? a.v_stride : a.k_stride;
+    float* const scales = values ? a.cache.v_scale + page * a.cache.v_scale_stride : a.cache.k_scale + page * a.cache.k_scale_stride;
+    uint8_t* const codes = static_cast<uint8_t*>(values ? a.cache.v_cache : a.cache.k_cache) + page * (values ? a.cache.v_page_stride : a.cache.k_page_stride);
+    // What was loaded stays as it came, and is turned twice, for the largest and for the codes: as floats it would need twice the registers, and half of the threads would
+    // not fit.  The next head's loads are under way while this one's largest is found.
+    struct Raw { Chunk a, b; };
+    auto load = [&](int h) {
+        Raw r = {};
+        if (mine) {
+            const __nv_bfloat16* row = rows + tok * stride + h * D;
+            r.a = *reinterpret_cast<const Chunk*>(row + unit.a);
+            r.b = *reinterpret_cast<const Chunk*>(row + unit.b);
+        }
+        return r;
+    };
+    auto turned = [&](const Raw& r, float (&x)[V], float (&y)[V]) {
+        chunk_to_floats<V>(r.a, x);
+        chunk_to_floats<V>(r.b, y);
+        if (!values) unit.turn(p.pairs, x, y);
+    };
+    // The largest of all threads' values; what is not finite is left out only where there is an infinity among them (a NaN the maximum passes over by itself).
+    auto largest = [&](float m, int slot) {
+        const uint32_t x = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+        if (lane == 0) atomicMax(&most[slot], x);
+        __syncthreads();
+        return __uint_as_float(most[slot]);
+    };
+    int slot = 0;
+    Raw raw = {};
+    if (passes == 1 && (int)blockIdx.y < Hkv) raw = load(blockIdx.y);
+    for (int h = blockIdx.y; h < Hkv; h += gridDim.y) {
+        const float old = slot0 ? scales[h] : 0.f;
+        auto own_largest = [&](auto finite) {
+            float m = 0.f;
+            for (int pass = 0; pass < passes; ++pass) {
+                if (passes > 1) {
+                    pass_to(pass);
+                    raw = load(h);
                 }
+                float x[V], y[V];
+                turned(raw, x, y);
+#pragma unroll
+                for (int j = 0; j < V; ++j) m = decltype(finite)::value ? finite_max(finite_max(m, x[j]), y[j]) : fmaxf(fmaxf(m, fabsf(x[j])), fabsf(y[j]));
             }
+            return m;
+        };
+        const float own = own_largest(std::false_type());
+        Raw after = {};
+        if (passes == 1 && h + (int)gridDim.y < Hkv) after = load(h + gridDim.y);
+        float m = largest(own, slot);
+        // A word is cleared two meetings before it is used again: all have read it then, in front of the meeting between.
+        auto next_slot = [&] {
+            if (threadIdx.x == 0) most[slot == 0 ? 2 : slot - 1] = 0u;
+            slot = slot == 2 ? 0 : slot + 1;
+        };
+        next_slot();
+        const bool infinite = isinf(m);
+        if (__builtin_expect(infinite, 0)) {
+            m = largest(own_largest(std::true_type()), slot);
+            next_slot();
         }
-#pragma unroll
-        for (int s = 16; s > 0; s >>= 1) {
-            m.x = fmaxf(m.x, __shfl_xor_sync(0xffffffffu, m.x, s));
-            m.y = fmaxf(m.y, __shfl_xor_sync(0xffffffffu, m.y, s));
-        }
-        if ((threadIdx.x & 31) == 0) most[turn][threadIdx.x >> 5] = m;
-        __syncthreads();                                     // the other of the two buffers is the next head's: one barrier a head
-        for (int w = 0; w < warps; ++w) {
-            const float2 o = most[turn][w];
-            m.x = fmaxf(m.x, o.x);
-            m.y = fmaxf(m.y, o.y);
-        }
-        bool k_grows, v_grows;
-        const int ke = append_exponent(m.x, slot0, old.x, k_grows), ve = append_exponent(m.y, slot0, old.y, v_grows);
-        uint8_t* const kc = static_cast<uint8_t*>(a.cache.k_cache) + page * a.cache.k_page_stride + (int64_t)h * page_size * D;
-        uint8_t* const vc = static_cast<uint8_t*>(a.cache.v_cache) + page * a.cache.v_page_stride + (int64_t)h * page_size * D;
-        const float kb = cache_power(-ke), vb = cache_power(-ve);
-        if (k_grows) append_rescale(kc, slot0 * D, old.x * kb, threadIdx.x, blockDim.x);
-        if (v_grows) append_rescale(vc, slot0 * D, old.y * vb, threadIdx.x, blockDim.x);
-        for (int pass = 0; pass < p.passes; ++pass) {
-            if (p.passes > 1) {
+        bool grows;
+        const int e = append_exponent(m, slot0, old, grows);
+        uint8_t* const to_head = codes + (int64_t)h * page_size * D;
+        const float by = cache_power(-e);
+        if (grows) append_rescale(to_head, slot0 * D, old * by, threadIdx.x, blockDim.x);
+        for (int pass = 0; pass < passes; ++pass) {
+            if (passes > 1) {
                 pass_to(pass);
-                if (mine) {
-                    append_load<V>(p, unit, k + tok * a.k_stride + (int64_t)h * D, true, kx, ky);
-                    append_load<V>(p, unit, v + tok * a.v_stride + (int64_t)h * D, false, vx, vy);
-                }
+                raw = load(h);
             }
             if (mine) {
                 const int at = (slot0 + tok) * D;
-                append_codes<V>(kc + at + unit.a, kx, kb);
-                append_codes<V>(kc + at + unit.b, ky, kb);
-                append_codes<V>(vc + at + unit.a, vx, vb);
-                append_codes<V>(vc + at + unit.b, vy, vb);
-                if (a.k_out) {
-                    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.k_out) + (first_row + tok) * a.k_out_stride + (int64_t)h * D;
-                    *reinterpret_cast<Chunk*>(out + unit.a) = floats_to_chunk<V>(kx);
-                    *reinterpret_cast<Chunk*>(out + unit.b) = floats_to_chunk<V>(ky);
+                float x[V], y[V];
+                turned(raw, x, y);
+                if (!values && a.k_out) {
+                    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.k_out) + (first_row + tok) * a.k_out_stride + h * D;
+                    *reinterpret_cast<Chunk*>(out + unit.a) = floats_to_chunk<V>(x);
+                    *reinterpret_cast<Chunk*>(out + unit.b) = floats_to_chunk<V>(y);
                 }
+                if (__builtin_expect(infinite, 0)) not_finite_to_nan<V>(x, y);
+                append_codes<V>(to_head + at + unit.a, x, by);
+                append_codes<V>(to_head + at + unit.b, y, by);
             }
         }
-        if (threadIdx.x == 0) {
-            if (slot0 == 0 || k_grows) *k_scale = cache_power(ke);
-            if (slot0 == 0 || v_grows) *v_scale = cache_power(ve);
-        }
+        if (threadIdx.x == 0 && (slot0 == 0 || grows)) scales[h] = cache_power(e);
+        raw = after;
     }
+    if (values) return;
     if (!a.q) return;
-    for (int pass = 0; pass < p.passes; ++pass) {
-        if (p.passes > 1) pass_to(pass);
+    for (int pass = 0; pass < passes; ++pass) {
+        if (passes > 1) pass_to(pass);
         if (!mine) continue;
         const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.q) + (first_row + tok) * a.q_stride;
         __nv_bfloat16* const qo = static_cast<__nv_bfloat16*>(a.q_out) + (first_row + tok) * a.q_out_stride;
-        constexpr int AT_ONCE = 4;
+        constexpr int AT_ONCE = 2;
         for (int h = blockIdx.y; h < a.Hq; h += gridDim.y * AT_ONCE) {
             Chunk ca[AT_ONCE], cb[AT_ONCE];
 #pragma unroll
@@ -328,7 +352,8 @@ extern "C" int arrol_cache_append(arrol_ctx* ctx, const arrol_cache_append_args*
         if ((warps + ONE_WARPS - 1) / ONE_WARPS >= ((int64_t)1 << 31)) return ARROL_ERR_UNSUPPORTED;
         ARROL_CUDA_OK(arrol_launch_pdl(append_one_kernel, dim3((unsigned)((warps + ONE_WARPS - 1) / ONE_WARPS)), dim3(32 * ONE_WARPS), 0, (cudaStream_t)stream, p));
     } else {
-        const int V = rotary_vector(D, a->R);
+        // Chunks of 4 where a page's units then fit a block: with 8 the values and angles of a thread spill (656 bytes), and of the same bytes half as many threads are there to wait.
+        int V = rotary_vector(D, a->R);
         p.units = D / (2 * V);
         const int items = a->cache.page * p.units, threads = items > 1024 ? 1024 : (items + 31) & ~31;
         p.passes = (items + threads - 1) / threads;
@@ -340,7 +365,7 @@ extern "C" int arrol_cache_append(arrol_ctx* ctx, const arrol_cache_append_args*
         void (*kernel)(AppendParams);
         if (threads <= 512) kernel = V == 8 ? append_runs_kernel<8, 512> : V == 4 ? append_runs_kernel<4, 512> : V == 2 ? append_runs_kernel<2, 512> : append_runs_kernel<1, 512>;
         else kernel = V == 8 ? append_runs_kernel<8, 1024> : V == 4 ? append_runs_kernel<4, 1024> : V == 2 ? append_runs_kernel<2, 1024> : append_runs_kernel<1, 1024>;
-        ARROL_CUDA_OK(arrol_launch_pdl(kernel, dim3((unsigned)pages, (unsigned)split), dim3(threads), 0, (cudaStream_t)stream, p));
+        ARROL_CUDA_OK(arrol_launch_pdl(kernel, dim3((unsigned)pages, (unsigned)split, 2), dim3(threads), 0, (cudaStream_t)stream, p));
     }
     ctx->launches += 1;
     return ARROL_OK;

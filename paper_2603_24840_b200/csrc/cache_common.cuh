@@ -23,12 +23,14 @@ __device__ __forceinline__ int cache_exponent(float amax) {
 __device__ __forceinline__ float cache_power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }       // 2^e, normal
 // The larger of the maximum and |x|, leaving out what is not finite (x - x is then NaN, which fmaxf passes over).
 __device__ __forceinline__ float finite_max(float most, float x) { return fmaxf(most, fabsf(x) + (x - x)); }
-// Two numbers rounded to e4m3, nearest even; infinities become NaN like NaN itself.
-__device__ __forceinline__ uint16_t e4m3_pair(float lo, float hi) {
+// Two numbers rounded to e4m3, nearest even, NaN stays NaN; an infinity would become 448.
+__device__ __forceinline__ uint16_t e4m3_pair_finite(float lo, float hi) {
     uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi + (hi - hi)), "f"(lo + (lo - lo)));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// the same with infinities to NaN
+__device__ __forceinline__ uint16_t e4m3_pair(float lo, float hi) { return e4m3_pair_finite(lo + (lo - lo), hi + (hi - hi)); }
 __device__ __forceinline__ uint32_t e4m3_pair_to_half(uint16_t c) {                                              // exact
     uint32_t r;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(c));
