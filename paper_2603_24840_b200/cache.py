@@ -52,34 +52,36 @@ _CODES = (torch.float8_e4m3fn, torch.uint8)
 
 
 def _pool(k_cache, v_cache, k_scale, v_scale) -> _Cache:
-    shape, strides = k_cache.shape, []
+    # shapes and strides are asked for once a tensor: small calls are bound by the host
+    shape, ks, vs, kss, vss = k_cache.shape, k_cache.stride(), v_cache.stride(), k_scale.stride(), v_scale.stride()
     if len(shape) != 4 or v_cache.shape != shape or k_scale.shape != shape[:2] or v_scale.shape != shape[:2]:
         raise ValueError("k_cache and v_cache are [pages, Hkv, page, D], their scales [pages, Hkv]")
+    if k_cache.dtype not in _CODES or v_cache.dtype not in _CODES:
+        raise TypeError("caches are float8_e4m3fn, or uint8 of the same bits")
+    if k_scale.dtype is not torch.float32 or v_scale.dtype is not torch.float32:
+        raise TypeError("scales are float32")
     pages, Hkv, page, D = shape
-    for t in (k_cache, v_cache):
-        if t.dtype not in _CODES:
-            raise TypeError("caches are float8_e4m3fn, or uint8 of the same bits")
-        s = t.stride()
-        if t.numel() and (s[3] != 1 or s[2] != D and page > 1 or s[1] != page * D and Hkv > 1):
-            raise ValueError("a page's heads, tokens and dimensions lie side by side")
-        strides.append(s[0] if pages > 1 else Hkv * page * D)
-    for t in (k_scale, v_scale):
-        if t.dtype is not torch.float32:
-            raise TypeError("scales are float32")
-        s = t.stride()
-        if t.numel() and s[1] != 1 and Hkv > 1:
-            raise ValueError("a page's scales lie side by side")
-        strides.append(s[0] if pages > 1 else Hkv)
-    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), strides[0], strides[1], k_scale.data_ptr(), v_scale.data_ptr(), strides[2], strides[3], pages, page, Hkv, D)
+    inner = (page * D, D, 1)
+    if ks[1:] != inner or vs[1:] != inner:      # heads, tokens of which there is one, and empty pools may have any
+        for s in (ks, vs):
+            if pages * Hkv * page * D and (s[3] != 1 or s[2] != D and page > 1 or s[1] != page * D and Hkv > 1):
+                raise ValueError("a page's heads, tokens and dimensions lie side by side")
+    if (kss[1] != 1 or vss[1] != 1) and Hkv > 1 and pages:
+        raise ValueError("a page's scales lie side by side")
+    if pages == 1:
+        ks = vs = (Hkv * page * D,)
+        kss = vss = (Hkv,)
+    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), ks[0], vs[0], k_scale.data_ptr(), v_scale.data_ptr(), kss[0], vss[0], pages, page, Hkv, D)
 
 
 def _table(name: str, t: Optional[torch.Tensor], rows: int):
     """(pointer, stride, entries a row)"""
     if t is None:
         return None, 0, 0
-    if t.dtype is not torch.int32 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] > 1 and t.stride(1) != 1:
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not torch.int32 or len(shape) != 2 or shape[0] != rows or shape[1] > 1 and stride[1] != 1:
         raise ValueError("%s is an int32 tensor [%d, pages]" % (name, rows))
-    return t.data_ptr(), t.stride(0) if rows > 1 else t.shape[1], t.shape[1]
+    return t.data_ptr(), stride[0] if rows > 1 else shape[1], shape[1]
 
 
 def arrol_cache_append(ctx: B.Context, k, v, k_cache, v_cache, k_scale, v_scale, page_table, lengths, cu_new=None, keep=None, q=None, q_out=None, k_out=None,

@@ -1,16 +1,17 @@
 // arrol_rotary, arrol_rotary_backward: queries and keys of packed tokens turned by their positions.
 //
 // Bound by HBM: every entry is read and written once, 4 D bytes a token and head.  A thread has one unit (two chunks, 16 bytes each in the usual case) of one token,
-// forms its cosines and sines once and goes through the heads with them in registers, so that a token's angles are computed once and not once a head, and eight loads
-// are under way at a time.  Where that makes too few threads the heads are split over blocks, each of which forms the angles again.
+// forms its cosines and sines once and goes through the heads with them in registers, so that a token's angles are computed once and not once a head.  Where that makes too few threads the heads are split over blocks, each of which forms the angles again.
 #include <math.h>
 
 #include "rotary_common.cuh"
 
 namespace {
 
-constexpr int ROT_THREADS = 256;
-constexpr int ROT_AT_ONCE = 4;                    // heads loaded before the first is turned
+// Two heads loaded at once and eight blocks of 128 threads an SM: 15,400 tokens of 24 heads of 80 22 us, 138,000 of 24 heads of 128 259.  Four at once take 80 registers:
+// six blocks, 27 and 255 (one of 256 threads at 88 registers 29 and 264).
+constexpr int ROT_THREADS = 128, ROT_PER_SM = 8;
+constexpr int ROT_AT_ONCE = 2;
 constexpr int64_t ROT_MAX_ROWS = ((int64_t)1 << 31) - 512;
 
 struct RotaryParams {
@@ -33,7 +34,7 @@ __device__ __forceinline__ int64_t packed_position(const arrol_rotary_args& a, i
 }
 
 template <int V>
-__global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(const RotaryParams p) {
+__global__ void __launch_bounds__(ROT_THREADS, ROT_PER_SM) rotary_kernel(const RotaryParams p) {
     typedef typename Bf16Chunk<V>::type Chunk;
     pdl_launch_dependents();
     pdl_wait();
@@ -113,7 +114,7 @@ int rotary_call(arrol_ctx* ctx, const arrol_rotary_args* a, float sign, void* st
     p.units = a->D / (2 * V);
     p.status = ctx->d_status;
     const int64_t blocks = (a->T_max * p.units + ROT_THREADS - 1) / ROT_THREADS;
-    // Four blocks an SM or more where the heads allow it, four heads a block at least.
+    // Four blocks an SM or more where the heads allow it, a few heads a block at least: with eight or sixteen the angles cost more than the waiting (22 -> 26, 27 us).
     int64_t split = (4 * (int64_t)ctx->sm_count + blocks - 1) / blocks;
     const int64_t most = (heads + ROT_AT_ONCE - 1) / ROT_AT_ONCE;
     if (split > most) split = most;
