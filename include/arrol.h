@@ -484,11 +484,13 @@ int arrol_rotary_backward(arrol_ctx* ctx, const arrol_rotary_args* args, void* s
  * the prompt_lengths[p] tokens of its group's prompt, p = i / G, pages prompt_table[p * prompt_table_stride + ...], and to its own lengths[i] tokens:
  *     z_j = scale q[i, h] . k_j[g];   o[i, h] = sum_j exp(z_j - lse[i, h]) v_j[g];   lse[i, h] = log sum_j exp(z_j),   g = h / (Hq / Hkv).
  * A rollout without any key gets o = 0, lse = -inf; rows of rollouts that are not kept are not written.  A prompt's pages are read once for all of its live rollouts (up to
- * 64 query rows, rollouts x Hq / Hkv, per key head).  Without prompts: prompt_table, prompt_lengths NULL, P = 0.  Products of q and e4m3 numbers are exact (q is split in
- * two 8-bit parts; entries below 2^-22 of their row's largest are cut there), sums fp32; probabilities are rounded to fp16 before the product with values.  Every sum
+ * 64 query rows, rollouts x Hq / Hkv, per key head).  Without prompts: prompt_table, prompt_lengths NULL, P = 0.  q is scaled by a power of two for each row
+ * and taken as fp16, which is exact for bf16 (entries below 2^-27 of their row's largest are rounded at 2^-39 of it); e4m3 numbers are exact in fp16; sums are fp32; probabilities
+ * are rounded to fp16 before the product with values.  Every sum
  * has a fixed order, so equal calls give equal bits.
  *
- * D a multiple of 16, 16 <= D <= 128; Hq a multiple of Hkv, Hq / Hkv <= 64; G <= 1024, N <= 2^24; pages, page_table entries < 2^31; scale finite, above 0; bf16 tensors as in
+ * D a multiple of 16, 16 <= D <= 128; Hq a multiple of Hkv, Hq / Hkv <= 64; G <= 1024, N <= 2^24; pages, tokens of a table row < 2^31; for the attention N * Hkv * (tokens of
+ * a table row) below 2^34 (2^31 with Hq / Hkv > 16), the same product of prompts (each counted once for every 64 query rows of its group) below 2^31; scale finite, above 0; bf16 tensors as in
  * the attention calls.  A length that is negative or more than its table row holds, fewer tokens than new ones, or a page number outside [0, pages) is not followed (in
  * attention a sequence or prompt with such a length counts as empty, and what rollouts over such pages get is not defined) and ARROL_DEV_BAD_INDEX is recorded.  The calls use nothing of the context's buffers and may be captured;
  * workspace: arrol_cache_attention_workspace(...) bytes, 256-byte aligned, contents need not be initialised or kept. */

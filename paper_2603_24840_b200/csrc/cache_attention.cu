@@ -1,15 +1,20 @@
 // arrol_cache_attention: one generated token per rollout over its group's prompt and its own tokens, both in the paged 8-bit cache.
 //
-// Bound by HBM: every live rollout's pages and every group's prompt pages are read once, half of a bf16 cache's bytes.  The products with keys take the e4m3 numbers as
-// they lie in memory (m16n8k32 mma.sync): a row of q becomes two e4m3 rows, q = 2^e (hi + lo / 16), which is exact for bf16 but for entries below 2^-22 of the row's
-// largest, so eight query rows fill the sixteen of a product and nothing has to be converted.  Probabilities would not survive that (a long tail of keys at 2^-20 of the
-// first's weight carries real weight), so they are fp16 and the values are widened to it, two per instruction, which also brings the two tokens of an operand register
-// together.  With a few rows a key there is too little work for tensor memory to pay.
+// Bound by HBM in the large: every live rollout's pages and every group's prompt pages are read once, half of a bf16 cache's bytes.  Measured (calls one behind another):
+// 256 live rollouts of 2,200 tokens over 32 prompts, 16 heads of 128 on 8 (1.23 GB) 259 us, 4.8 TB/s; with nothing computed the same copies take 233, so the rest is for the
+// start (a scan, then three loads that depend on one another: 8 us), the merge (10) and the products behind the last copies.  8 rollouts of 6,600 tokens, 32 heads (118 MB) 46 to
+// 53 us.  384 rollouts of 160 tokens over 24 prompts of 4,850, 32 heads of 64 (188 MB) 136 us: there it is the work of 64 query rows behind every key.
 //
-// Work is cut without a plan: the lengths make a line of pieces of equal cost, every block takes an equal part of it, and each finds its own by a scan over the lengths
-// (shared pieces first: a chunk of 128 tokens for more than 16 query rows, four warps a row tile each; then single ones: 32 tokens for 16 rows or less, a warp each).
-// Pieces of a unit (rows x key head) that fall to different blocks or warps leave partial sums, which cache_merge_kernel adds up in order, so the result does not
-// depend on who was first.
+// The products are m16n8k16 mma.sync in fp16, transposed: tokens (of S^T = K Q^T) and dimensions (of O^T = V^T P^T) are the sixteen rows, query rows the eight columns, so that
+// eight query heads waste nothing.  e4m3 numbers widen to fp16 exactly, two an instruction, and q, scaled by a power of two for each row, is exact in fp16 too (bf16 has
+// fewer bits; what is below 2^-27 of the row's largest is rounded at 2^-39 of it).  Probabilities are rounded to fp16, which holds a long tail of keys at 2^-20 of the
+// largest one's weight as well as that one.  Scales of pages and heads join the scores and the probabilities.  (Products of e4m3 operands by mma.sync are widened by the
+// compiler, at each use: 12 instructions for one.)
+//
+// Work is cut without a plan: the lengths make a line of pieces and units' setups by their cost, every block takes an equal part of it, and each finds its own by a scan over
+// the lengths.  Shared pieces come first: tokens that more than 16 query rows have in common, four warps a tile of 16 rows each (or two for two tiles); then single ones, 32
+// tokens for 16 rows or less, a warp each.  Pieces of a unit (rows x key head) that fall to different blocks or warps leave partial sums, which cache_merge_kernel adds up in
+// order, so the result does not depend on who was first.
 #include <type_traits>
 
 #include "cache_common.cuh"
@@ -79,33 +84,34 @@ struct CacheParams {
     CacheWorkspace w;
     int ratio, group, blocks, prompts, entries;    // rollouts a prompt entry, entries a prompt, prompt entries, all
     int page_shift, grid;
+    int own_most;                                  // tokens that a row of page_table holds
     LineCosts costs;
     float scale_log2;
     uint32_t* status;
 };
 
-// ---- the line of pieces
+// ---- the line of pieces.  The host sees to it that its length fits 31 bits.
 struct Line {
-    long long shared, single;      // lengths: units' pieces and setups
-    long long per;                 // cost that a block takes
+    int shared, single;      // lengths: units' pieces and setups
+    int per;                 // cost that a block takes
     int cost;                      // of a shared piece
 };
 // Shares are such that every block (warp) between the first and the last that has some of a unit has one of its pieces: a share holds a shared piece, and the single
 // line begins where four warps have as much of it each.
-__device__ __forceinline__ long long single_begin(long long shared, int cost) { return (shared * cost + CA_WARPS - 1) / CA_WARPS * CA_WARPS; }
-__device__ __forceinline__ Line make_line(long long shared, long long single, int grid, int cost) {
-    const long long each = (single_begin(shared, cost) + single + grid - 1) / grid;
-    return {shared, single, (max(each, (long long)(shared > 0 ? cost : 1)) + CA_WARPS - 1) / CA_WARPS * CA_WARPS, cost};
+__device__ __forceinline__ int single_begin(int shared, int cost) { return (shared * cost + CA_WARPS - 1) / CA_WARPS * CA_WARPS; }
+__device__ __forceinline__ Line make_line(int shared, int single, int grid, int cost) {
+    const int each = (single_begin(shared, cost) + single + grid - 1) / grid;
+    return {shared, single, (max(each, (shared > 0 ? cost : 1)) + CA_WARPS - 1) / CA_WARPS * CA_WARPS, cost};
 }
 // the shared line from there on is block b's or a later one's
-__device__ __forceinline__ long long shared_begin(const Line& l, long long b) {
-    const long long x = (b * l.per + l.cost - 1) / l.cost;
+__device__ __forceinline__ int shared_begin(const Line& l, int b) {
+    const int x = (b * l.per + l.cost - 1) / l.cost;
     return x < l.shared ? x : l.shared;
 }
 // a warp's part of the single line, from y0 to y1 (none where that is not more); warps are counted over all blocks
-__device__ __forceinline__ void warp_range(const Line& l, long long warp, long long& y0, long long& y1) {
-    const long long begin = single_begin(l.shared, l.cost), b = warp / CA_WARPS, k = warp % CA_WARPS;
-    const long long lo = max(b * l.per - begin, 0ll), each = max((b + 1) * l.per - begin - lo, 0ll) / CA_WARPS;
+__device__ __forceinline__ void warp_range(const Line& l, int warp, int& y0, int& y1) {
+    const int begin = single_begin(l.shared, l.cost), b = warp / CA_WARPS, k = warp % CA_WARPS;
+    const int lo = max(b * l.per - begin, 0), each = max((b + 1) * l.per - begin - lo, 0) / CA_WARPS;
     y0 = lo + k * each;
     y1 = min(y0 + each, l.single);
 }
@@ -152,7 +158,7 @@ __device__ __forceinline__ int2 entry_size(const CacheParams& p, int e, bool& ba
 }
 
 struct ScanSums {
-    long long shared, single;      // lengths of the lines
+    int shared, single;      // lengths of the lines
     int shared_entries, single_entries;
 };
 __device__ __forceinline__ ScanSums operator+(const ScanSums& a, const ScanSums& b) {
@@ -166,7 +172,7 @@ __device__ __forceinline__ ScanSums shfl_up(const ScanSums& a, int d) {
 // Where a block (warp) begins: an entry, its number in the list, how much of it lies before.
 struct Start {
     CacheEntry e;
-    long long offset;
+    int offset;
     int number;
 };
 
@@ -218,6 +224,7 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 template <int DP>
 struct CacheConf {
     static constexpr int KEYS = CA_TOKENS * DP, BYTES = 2 * KEYS;
+    // Heads up to 64 leave room for a third block (long prompts 191 -> 178 us).  Six consumers a block at 128 registers spill with heads of 128 (283 -> 307 us).
     static constexpr int STAGES = 3, PER_SM = DP == 128 ? 2 : 3;
     static constexpr int CHUNKS = DP / 16;
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * CA_WARPS * BYTES;
@@ -228,13 +235,13 @@ struct CacheConf {
 struct Cursor {
     CacheEntry e, next;
     const CacheEntry* list;
-    long long left;                // of the part, from the piece that the cursor is at on
+    int left;                // of the part, from the piece that the cursor is at on
     int number, last;              // of the list's entries
     int head, piece, setup;
     __device__ __forceinline__ void fetch() {
         if (number + 1 <= last) next = list[number + 1];
     }
-    __device__ __forceinline__ void begin(const CacheParams& p, const CacheEntry* l, const Start& s, int entries, long long length) {
+    __device__ __forceinline__ void begin(const CacheParams& p, const CacheEntry* l, const Start& s, int entries, int length) {
         list = l;
         e = s.e;
         number = s.number;
@@ -242,7 +249,7 @@ struct Cursor {
         left = length;
         setup = unit_setup(p, e.rows);
         head = (int)(s.offset / (e.pieces + setup));
-        piece = (int)(s.offset - (long long)head * (e.pieces + setup)) - setup;
+        piece = (int)(s.offset - head * (e.pieces + setup)) - setup;
         if (piece < 0) { left += piece; piece = 0; }
         fetch();
     }
@@ -292,7 +299,7 @@ struct alignas(16) PieceInfo {
 // The first and the last of a unit in this block or warp; of the unit; no piece, but the end; query rows from bit 8 on.
 constexpr int PIECE_FIRST = 1, PIECE_LAST = 2, PIECE_BEGIN = 4, PIECE_END = 8, PIECE_NONE = 16, PIECE_ROWS = 8;
 
-// A piece on its way: first its page numbers are asked for, then, a piece later, its scales, then its copies.
+// A piece on its way: first its page numbers are asked for, then its scales, then its copies.
 struct Fetch {
     PagePair pages;
     int tok;
@@ -306,13 +313,18 @@ struct Fetch {
         info.flags = (first || c.piece == 0 ? PIECE_FIRST : 0) | (c.piece == 0 ? PIECE_BEGIN : 0) | (c.piece == c.e.pieces - 1 ? PIECE_LAST | PIECE_END : 0) |
                      (c.is_last() ? PIECE_LAST : 0) | c.e.rows << PIECE_ROWS;
     }
-    __device__ __forceinline__ void find_scales(const CacheParams& p) {
+    // pages that are none are reported and left out
+    __device__ __forceinline__ void check(const CacheParams& p) {
         const arrol_cache& c = p.a.cache;
         if ((pages.first < 0 && info.there > 0) || pages.first >= c.pages || (pages.second < 0 && info.there > 16) || pages.second >= c.pages) {
             atomicOr(p.status, ARROL_DEV_BAD_INDEX);
             if (pages.first >= c.pages) pages.first = -1;
             if (pages.second >= c.pages) pages.second = -1;
         }
+    }
+    __device__ __forceinline__ void find_scales(const CacheParams& p) {
+        const arrol_cache& c = p.a.cache;
+        check(p);
         info.scales[0] = info.scales[1] = -1.f;
         info.scales[2] = info.scales[3] = 0.f;
         if (pages.first >= 0) {
@@ -343,8 +355,7 @@ struct Fetch {
     }
 };
 
-// A tile of up to 16 query rows against the pieces of its unit, transposed: tokens (and dimensions) are the sixteen rows of a product, query rows its eight columns, so that eight
-// query heads waste nothing.  A lane (g, t) = (lane / 4, lane % 4) has the scores of query rows 2 t and 2 t + 1 (of each eight) with tokens g and, of the second eight of
+// A tile of up to 16 query rows against the pieces of its unit.  A lane (g, t) = (lane / 4, lane % 4) has the scores of query rows 2 t and 2 t + 1 (of each eight) with tokens g and, of the second eight of
 // sixteen, 8 + (g + 4) % 8: in that order eight rows of keys, and the sixteen of values that a lane's four scores belong to, are read without two in a bank.
 template <int DP>
 struct RowTile {
@@ -402,15 +413,11 @@ struct RowTile {
         const float4 scales = *reinterpret_cast<const float4*>(info.scales);
         const uint32_t keys = smem_u32(stage), values = keys + C::KEYS;
         const int later = (lane >> 3) & 1, row = later * 8 + ((lane + 4 * later) & 7);
-        // every other product of eight rows adds up by itself: one after the other they would wait for one another
-        constexpr int CHAINS = ROWS == 1 ? 2 : 1;
-        float s[2][ROWS][4], chain[CHAINS][2][ROWS][4];
+        float s[2][ROWS][4];
 #pragma unroll
-        for (int i = 0; i < CHAINS; ++i)
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int r = 0; r < ROWS; ++r) chain[i][half][r][0] = chain[i][half][r][1] = chain[i][half][r][2] = chain[i][half][r][3] = 0.f;
+            for (int r = 0; r < ROWS; ++r) s[half][r][0] = s[half][r][1] = s[half][r][2] = s[half][r][3] = 0.f;
 #pragma unroll
         for (int c = 0; c < C::CHUNKS; c += 2)
 #pragma unroll
@@ -419,17 +426,11 @@ struct RowTile {
                 ldmatrix_rows(keys + C::at(half * 16 + row, c + (lane >> 4)), w);
                 widen(a, w[0], w[1]);
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) mma_f16(chain[0][half][r], a, q[c][r][0], q[c][r][1]);
+                for (int r = 0; r < ROWS; ++r) mma_f16(s[half][r], a, q[c][r][0], q[c][r][1]);
                 widen(a, w[2], w[3]);
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) mma_f16(chain[CHAINS - 1][half][r], a, q[c + 1][r][0], q[c + 1][r][1]);
+                for (int r = 0; r < ROWS; ++r) mma_f16(s[half][r], a, q[c + 1][r][0], q[c + 1][r][1]);
             }
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) s[half][r][x] = CHAINS == 2 ? chain[0][half][r][x] + chain[CHAINS - 1][half][r][x] : chain[0][half][r][x];
         float f[2][ROWS][2];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
@@ -598,20 +599,48 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
         }
         sm.abort = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (p.a.cache.pages > 0) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+        }
     }
     __syncthreads();
     pdl_launch_dependents();
     pdl_wait();
-    const long long b = blockIdx.x;
+    const int b = blockIdx.x;
 
     // ---- the scan: sizes of the entries, side by side; then a thread has `each` entries in a row, twice (sums, and what is this block's)
     bool bad = false;
-    for (int e = threadIdx.x; e < min(p.entries, CA_SCANNED); e += CA_THREADS) sm.sizes[e] = entry_size(p, e, bad);
+    constexpr int AT_ONCE = 4;                                // entries of a thread whose lengths are on their way together
+    for (int e0 = threadIdx.x; e0 < min(p.entries, CA_SCANNED); e0 += AT_ONCE * CA_THREADS) {
+        int n[AT_ONCE], kept[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int own = e0 + i * CA_THREADS - p.prompts;
+            n[i] = kept[i] = 0;
+            if (own >= 0 && own < p.a.N) {
+                n[i] = p.a.lengths[own];
+                kept[i] = p.a.keep ? p.a.keep[own] : 1;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int e = e0 + i * CA_THREADS;
+            if (e >= min(p.entries, CA_SCANNED)) break;
+            if (e < p.prompts) {
+                sm.sizes[e] = entry_size(p, e, bad);
+            } else {
+                const bool fits = n[i] >= 0 && n[i] <= p.own_most;
+                bad |= kept[i] && !fits;
+                sm.sizes[e] = kept[i] && fits ? make_int2(n[i], p.ratio) : make_int2(0, 0);
+            }
+        }
+    }
     __syncthreads();
     const int each = (p.entries + CA_THREADS - 1) / CA_THREADS;
     const int e0 = min((int)threadIdx.x * each, p.entries), e1 = min(e0 + each, p.entries);
     auto size = [&](int e) { return e < CA_SCANNED ? sm.sizes[e] : entry_size(p, e, bad); };
-    auto length = [&](int2 x) { return (long long)(entry_pieces(x.y, x.x) + unit_setup(p, x.y)) * Hkv; };
+    auto length = [&](int2 x) { return (entry_pieces(x.y, x.x) + unit_setup(p, x.y)) * Hkv; };
     ScanSums mine = {0, 0, 0, 0};
     for (int e = e0; e < e1; ++e) {
         const int2 x = size(e);
@@ -635,16 +664,16 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
         total = total + sm.warp_sums[w];
     }
     const Line line = make_line(total.shared, total.single, p.grid, p.costs.shared);
-    const long long x0 = shared_begin(line, b), x1 = shared_begin(line, b + 1);
-    long long y0[CA_WARPS], y1[CA_WARPS];
+    const int x0 = shared_begin(line, b), x1 = shared_begin(line, b + 1);
+    int y0[CA_WARPS], y1[CA_WARPS];
 #pragma unroll
     for (int w = 0; w < CA_WARPS; ++w) warp_range(line, b * CA_WARPS + w, y0[w], y1[w]);
-    const long long block_y1 = max(max(y1[0], y1[1]), max(y1[2], y1[3]));
+    const int block_y1 = max(max(y1[0], y1[1]), max(y1[2], y1[3]));
     if (mine.shared > 0 && at.shared < x1 && at.shared + mine.shared > x0)
         for (int e = e0; e < e1; ++e) {
             const int2 x = size(e);
             if (x.x == 0 || x.y <= CA_ALONE) continue;
-            const long long n = length(x);
+            const int n = length(x);
             const CacheEntry entry = {e, x.x, x.y, entry_pieces(x.y, x.x)};
             if (at.shared < x1 && at.shared + n > x0) p.w.shared[at.shared_entries] = entry;                 // neighbours write the same
             if (at.shared <= x0 && at.shared + n > x0) sm.shared = {entry, x0 - at.shared, at.shared_entries};
@@ -655,7 +684,7 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
         for (int e = e0; e < e1; ++e) {
             const int2 x = size(e);
             if (x.x == 0 || x.y > CA_ALONE) continue;
-            const long long n = length(x);
+            const int n = length(x);
             if (at.single < block_y1 && at.single + n > y0[0]) {
                 const CacheEntry entry = {e, x.x, x.y, entry_pieces(x.y, x.x)};
                 p.w.single[at.single_entries] = entry;
@@ -678,7 +707,7 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
         const uint32_t eight = 0xFFu << (of * 8);
         uint32_t n = 0, asked = 0;                            // pieces of this consumer before the eight, asked for so far
         for (int phase = 0; phase < 2 && ok; ++phase) {
-            long long from, to;
+            int from, to;
             warp_range(line, b * CA_WARPS + of, from, to);
             if (phase == 0) { from = x0; to = x1; }
             Cursor c;
@@ -689,8 +718,15 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
             for (int i = 0; i < k && c.left > 0; ++i) c.advance(Hkv);
             Fetch now, next;
             bool there = c.left > 0, more = false;
+            bool copied = false;
             if (there) {
                 now.find(p, c, token(), k == 0);
+                // The very first pieces find their stages free: their copies need not wait for the scales.
+                if (n == 0 && k < C::STAGES) {
+                    now.check(p);
+                    now.copy<DP>(p, &map_k, &map_v, smem_u32(stage(k, of)), &sm.full[k][of]);
+                    copied = true;
+                }
                 now.find_scales(p);
             }
             // Each consumer's eight lanes go on by themselves: `at` is the lane whose turn it is, a stage that is not free yet is asked for again in the next round.
@@ -715,7 +751,8 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
                 const uint32_t mine = n + k, st = mine % C::STAGES;
                 const bool turn = there && k == at, go = turn && mbar_try_wait(&sm.empty[st][of], ((mine / C::STAGES) & 1u) ^ 1u);
                 if (go) {
-                    now.copy<DP>(p, &map_k, &map_v, smem_u32(stage(mine, of)), &sm.full[st][of]);
+                    if (!copied) now.copy<DP>(p, &map_k, &map_v, smem_u32(stage(mine, of)), &sm.full[st][of]);
+                    copied = false;
                     sm.info[st][of] = now.info;
                     mbar_arrive(&sm.full[st][of]);
                     if (phase || of == 0) tell_owner(p, now.info, (int)(phase ? b * CA_WARPS + of : b));
@@ -728,6 +765,11 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
                 }
                 fresh = went ? 0 : fresh + 1;
                 if (fresh > SPIN_LIMIT || ((fresh & 1023u) == 1023u && __any_sync(0xffffffffu, *abort_flag != 0u))) { *abort_flag = 1u; ok = false; break; }
+            }
+            if (!ok && copied) {                              // a copy whose stage nobody has been told of
+                mbar_arrive(&sm.full[k][of]);
+                for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin)
+                    if (mbar_try_wait(&sm.full[k][of], 0u)) break;
             }
         }
         if (k == 0) {
@@ -863,33 +905,36 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
     }
     if (a.keep && !a.keep[i]) return;
     Merged m = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    // records of the blocks (warps) that have some of a unit, `step` rows apart; of shared units of up to 32 rows two each, CA_ROWS / 2 apart
-    auto unit = [&](int rows, int2 of, int64_t first, int step) {
-        const int twice = rows > CA_ALONE && rows <= 32 ? 1 : 0;
-        for (int w = of.x << twice; w <= (of.y << twice | twice); w += Merged::AT_ONCE) {
-            float2 x[Merged::AT_ONCE];
-            float4 v[Merged::AT_ONCE];
-#pragma unroll
-            for (int k = 0; k < Merged::AT_ONCE; ++k) {
-                x[k] = make_float2(-INFINITY, 0.f);
-                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (w + k <= (of.y << twice | twice)) {
-                    const int64_t at = first + (int64_t)((w + k) >> twice) * step + ((w + k) & twice) * (CA_ROWS / 2);
-                    x[k] = ml[at];
-                    if (d < D) v[k] = *reinterpret_cast<const float4*>(o + at * D + d);
-                }
-            }
-            m.add(x, v);
-        }
-    };
+    // The records of a unit: `count` of the blocks (warps) that have some of it, `step` rows apart; of shared units of up to 32 rows two each, CA_ROWS / 2 apart.
+    struct Records { int64_t first; int count, step, twice; };
     const int64_t own_number = (int64_t)i * Hkv + h, prompt_number = (int64_t)entry * Hkv + h, shared_rows = p.w.rows_own + p.w.rows_prompt;
-    if (prompt_tokens > 0) {
-        if (prompt_rows > CA_ALONE) unit(prompt_rows, shared, shared_rows + prompt_number * CA_ROWS + prompt_row, CA_ROWS);
-        else unit(prompt_rows, shared, p.w.rows_own + prompt_number * CA_ALONE + prompt_row, CA_ALONE);
-    }
-    if (own_tokens > 0) {
-        if (p.ratio > CA_ALONE) unit(p.ratio, own, shared_rows + ((int64_t)p.prompts * Hkv + own_number) * CA_ROWS + r, CA_ROWS);
-        else unit(p.ratio, own, own_number * p.ratio + r, p.ratio);
+    auto records = [&](int rows, int2 of, int64_t shared_first, int64_t first, int step) {
+        const bool in_blocks = rows > CA_ALONE;
+        const int twice = in_blocks && rows <= 32 ? 1 : 0;
+        if (in_blocks) { first = shared_first; step = CA_ROWS; }
+        return Records{first + (int64_t)of.x * step, (of.y - of.x + 1) << twice, step, twice};
+    };
+    Records a_prompt = {0, 0, 0, 0}, an_own = {0, 0, 0, 0};
+    if (prompt_tokens > 0)
+        a_prompt = records(prompt_rows, shared, shared_rows + prompt_number * CA_ROWS + prompt_row, p.w.rows_own + prompt_number * CA_ALONE + prompt_row, CA_ALONE);
+    if (own_tokens > 0) an_own = records(p.ratio, own, shared_rows + ((int64_t)p.prompts * Hkv + own_number) * CA_ROWS + r, own_number * p.ratio + r, p.ratio);
+    for (int w = 0; w < a_prompt.count + an_own.count; w += Merged::AT_ONCE) {
+        float2 x[Merged::AT_ONCE];
+        float4 v[Merged::AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < Merged::AT_ONCE; ++k) {
+            x[k] = make_float2(-INFINITY, 0.f);
+            v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (w + k < a_prompt.count + an_own.count) {
+                const bool of_prompt = w + k < a_prompt.count;
+                const Records& u = of_prompt ? a_prompt : an_own;
+                const int number = of_prompt ? w + k : w + k - a_prompt.count;
+                const int64_t at = u.first + (int64_t)(number >> u.twice) * u.step + (number & u.twice) * (CA_ROWS / 2);
+                x[k] = ml[at];
+                if (d < D) v[k] = *reinterpret_cast<const float4*>(o + at * D + d);
+            }
+        }
+        m.add(x, v);
     }
     const bool any = prompt_tokens > 0 || own_tokens > 0;     // none: no key
     const float inv = any ? 1.f / m.total : 0.f;
@@ -972,6 +1017,15 @@ extern "C" int arrol_cache_attention(arrol_ctx* ctx, const arrol_cache_attention
     p.page_shift = __builtin_ctz((unsigned)a->cache.page);
     p.grid = ctx->sm_count * ca_per_sm(a->cache.D);
     p.costs = line_costs(a->cache.D);
+    // The line is counted in 32 bits: with every table full it stays below 2^30.
+    const int64_t own_most = (int64_t)a->table_pages * a->cache.page, prompt_most = (int64_t)a->prompt_table_pages * a->cache.page;
+    auto longest = [&](int64_t units, int64_t tokens, bool shared) {
+        const double pieces = shared ? (double)(tokens / 64 + 2) * p.costs.shared : (double)(tokens / 32 + 1 + p.costs.single_setup);
+        return (double)units * a->cache.Hkv * pieces;
+    };
+    if (own_most > INT32_MAX || prompt_most > INT32_MAX || longest(a->N, own_most, p.ratio > CA_ALONE) + longest(p.prompts, prompt_most, true) >= 1073741824.0)
+        return ARROL_ERR_UNSUPPORTED;
+    p.own_most = (int)own_most;
     p.scale_log2 = a->scale * LOG2E;
     p.status = ctx->d_status;
     ArrolDeviceGuard guard(ctx->device);
