@@ -2,8 +2,11 @@
 //
 // Bound by HBM where there are many tokens (bf16 in, 8 bits out, queries in and out), by one launch and a chain of dependent loads (length, page number, scale) where
 // there are few.  A page's scale needs the largest entry of all of its new tokens before the first can be rounded, so a page and head belong to one block
-// (append_runs_kernel: runs of tokens) or one warp (append_one_kernel: a token per sequence), which holds the turned values in registers in between: nothing is read
-// twice, and no atomics take part.
+// (append_runs_kernel: runs of tokens) or one warp (append_one_kernel: a token per sequence), which keeps what it loaded in registers in between (but for pages that are
+// more than a block can hold, odd sizes only) and needs no atomics in global memory.
+//
+// 38,000 prompt tokens of 16 heads of 128 on 8 (600 MB) 143 us, 4.2 TB/s: the meeting of a block for each head, and the turning twice, are not all hidden.  One token each of
+// 512 live rollouts, 32 heads on 8 (12 MB), 18 us.
 #include <type_traits>
 
 #include "cache_common.cuh"
@@ -352,8 +355,8 @@ extern "C" int arrol_cache_append(arrol_ctx* ctx, const arrol_cache_append_args*
         if ((warps + ONE_WARPS - 1) / ONE_WARPS >= ((int64_t)1 << 31)) return ARROL_ERR_UNSUPPORTED;
         ARROL_CUDA_OK(arrol_launch_pdl(append_one_kernel, dim3((unsigned)((warps + ONE_WARPS - 1) / ONE_WARPS)), dim3(32 * ONE_WARPS), 0, (cudaStream_t)stream, p));
     } else {
-        // Chunks of 4 where a page's units then fit a block: with 8 the values and angles of a thread spill (656 bytes), and of the same bytes half as many threads are there to wait.
-        int V = rotary_vector(D, a->R);
+        // The widest chunks that the sizes allow: 4 numbers and twice the threads take 200 to 247 us instead of 143 for 38,000 prompt tokens.
+        const int V = rotary_vector(D, a->R);
         p.units = D / (2 * V);
         const int items = a->cache.page * p.units, threads = items > 1024 ? 1024 : (items + 31) & ~31;
         p.passes = (items + threads - 1) / threads;

@@ -8,8 +8,8 @@
 // The products are m16n8k16 mma.sync in fp16, transposed: tokens (of S^T = K Q^T) and dimensions (of O^T = V^T P^T) are the sixteen rows, query rows the eight columns, so that
 // eight query heads waste nothing.  e4m3 numbers widen to fp16 exactly, two an instruction, and q, scaled by a power of two for each row, is exact in fp16 too (bf16 has
 // fewer bits; what is below 2^-27 of the row's largest is rounded at 2^-39 of it).  Probabilities are rounded to fp16, which holds a long tail of keys at 2^-20 of the
-// largest one's weight as well as that one.  Scales of pages and heads join the scores and the probabilities.  (Products of e4m3 operands by mma.sync are widened by the
-// compiler, at each use: 12 instructions for one.)
+// largest one's weight as well as that one; its smallest steps are 2^-31 of that weight.  Scales of pages and heads join the scores and the probabilities.  (Products of
+// e4m3 operands by mma.sync are widened by the compiler, at each use: 12 instructions for one.)
 //
 // Work is cut without a plan: the lengths make a line of pieces and units' setups by their cost, every block takes an equal part of it, and each finds its own by a scan over
 // the lengths.  Shared pieces come first: tokens that more than 16 query rows have in common, four warps a tile of 16 rows each (or two for two tiles); then single ones, 32
@@ -884,7 +884,7 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
     const float* o = pdl_acquire(p.w.o);
     bool bad = false;
     const int own_tokens = cache_tokens(a.lengths, i, a.table_pages, a.cache.page, bad);
-    const int2 own = owners[(int64_t)(p.prompts + i) * Hkv + h];       // not read where there are no tokens
+    const int2 own = owners[(int64_t)(p.prompts + i) * Hkv + h];       // nothing known where there are no tokens: not used there
     int prompt_tokens = 0, prompt_rows = 0, prompt_row = 0, entry = 0;
     int2 shared = {0, 0};
     if (p.prompts) {
@@ -912,7 +912,9 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
         const bool in_blocks = rows > CA_ALONE;
         const int twice = in_blocks && rows <= 32 ? 1 : 0;
         if (in_blocks) { first = shared_first; step = CA_ROWS; }
-        return Records{first + (int64_t)of.x * step, (of.y - of.x + 1) << twice, step, twice};
+        // inside the workspace even where a wait ran out, so that nobody told of the unit
+        const int most = (in_blocks ? p.grid : p.grid * CA_WARPS) - 1, from = min(max(of.x, 0), most), to = min(max(of.y, from - 1), most);
+        return Records{first + (int64_t)from * step, (to - from + 1) << twice, step, twice};
     };
     Records a_prompt = {0, 0, 0, 0}, an_own = {0, 0, 0, 0};
     if (prompt_tokens > 0)

@@ -43,7 +43,7 @@ __device__ __forceinline__ float2 e4m3_pair_to_float(uint16_t c) {
     return f;
 }
 
-// Tokens of sequence i, -1 where it is left out; none where its length is not one that its table row can hold.
+// Tokens of sequence i; none where its length is not one that its table row can hold.
 __device__ __forceinline__ int cache_tokens(const int32_t* lengths, int i, int table_pages, int page, bool& bad) {
     const int n = lengths[i];
     if (n < 0 || n > (int64_t)table_pages * page) { bad = true; return 0; }

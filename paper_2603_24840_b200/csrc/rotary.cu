@@ -1,7 +1,8 @@
 // arrol_rotary, arrol_rotary_backward: queries and keys of packed tokens turned by their positions.
 //
 // Bound by HBM: every entry is read and written once, 4 D bytes a token and head.  A thread has one unit (two chunks, 16 bytes each in the usual case) of one token,
-// forms its cosines and sines once and goes through the heads with them in registers, so that a token's angles are computed once and not once a head.  Where that makes too few threads the heads are split over blocks, each of which forms the angles again.
+// forms its cosines and sines once and goes through the heads with them in registers, so that a token's angles are computed once and not once a head.  Where that
+// makes too few threads the heads are split over blocks, each of which forms the angles again.
 #include <math.h>
 
 #include "rotary_common.cuh"

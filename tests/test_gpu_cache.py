@@ -319,6 +319,41 @@ def test_forked_rollouts_share_pages(ctx):
     p.check(*p.run(ctx))
 
 
+def _spread(pool, stride):
+    """The pool with its pages this many bytes apart, keys and values in one buffer."""
+    shape, size = pool.k.shape, pool.Hkv * pool.page * pool.D
+    buffer = torch.full(((pool.pages - 1) * stride + 2 * size,), 0x7F, dtype=torch.uint8, device="cuda")
+    for at, name in ((0, "k"), (size, "v")):
+        far = buffer[at:].as_strided(shape, (stride,) + pool.k[0].contiguous().stride())
+        far.copy_(getattr(pool, name).view(torch.uint8))
+        setattr(pool, name, far)
+
+
+def test_pages_beyond_32_bit_offsets(ctx):
+    p = Attend([70, 33, 1], [40], 3, 4, 2, 64, 32, seed=20)
+    stride = -(-(1 << 33) // p.pool.pages) // 16 * 16
+    want = p.run(ctx)
+    _spread(p.pool, stride)
+    assert all(torch.equal(x, y) for x, y in zip(want, p.run(ctx)))
+    for new in (None, [9, 40, 1]):
+        p = Append([70, 41, 17], new, page=32, seed=21)
+        p.pool.k, p.pool.v = p.pool.k.view(torch.uint8), p.pool.v.view(torch.uint8)
+        _spread(p.pool, stride)
+        p.check(p.run(ctx))
+
+
+def test_a_workspace_for_more_serves_less(ctx):
+    """Of the same heads: with fewer rollouts, prompts or rollouts a prompt; what an earlier call left there does not matter."""
+    big = Attend([50, 300] * 20, [100, 9, 0, 400], 10, 8, 2, 64, 16, seed=22)
+    ws = big.workspace(ctx)
+    for x in (big, Attend([7, 0, 900], None, 1, 8, 2, 64, 16, seed=23), Attend([20] * 6, [500, 3], 3, 8, 2, 64, 16, [1, 1, 0, 1, 0, 0], seed=24), big, Attend([3000], [70], 1, 8, 2, 64, 16, seed=25)):
+        out = x.outputs()
+        assert x.workspace(ctx).numel() <= ws.numel()
+        x.call(ctx, *out, ws)
+        torch.cuda.synchronize()
+        x.check(*out)
+
+
 # ---- appends ----------------------------------------------------------------------------------------------------------------------------------
 
 class Append:
@@ -541,6 +576,33 @@ def test_appends_captured_and_replayed(ctx):
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(p.snapshot(), q.snapshot())) and torch.equal(p.q_out, q.q_out)
+
+
+def test_appends_at_once_on_two_streams(ctx):
+    """Into different pages of one pool, as two batches that are served side by side."""
+    def pair():
+        x, y = Append([200] * 30, [70] * 30, page=32, seed=11), Append([64, 33, 17], None, page=32, seed=12)
+        both = Pool(x.pool.pages + y.pool.pages, 2, 32, 64)
+        n = x.pool.pages
+        for part, p in ((slice(0, n), x.pool), (slice(n, None), y.pool)):
+            for name in ("k", "v"):
+                getattr(both, name).view(torch.uint8)[part] = getattr(p, name).view(torch.uint8)
+            both.ks[part], both.vs[part] = p.ks, p.vs
+        y.table = torch.where(y.table >= 0, y.table + n, y.table)
+        x.pool = y.pool = both
+        return x, y
+    x, y = pair()
+    x.run(ctx)
+    y.run(ctx)
+    u, w = pair()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for p, s in zip((u, w), streams):
+        p.call(ctx, stream=s)
+    torch.cuda.synchronize()
+    assert B.arrol_poll_status(ctx) == 0
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(x.snapshot(), u.snapshot()))
+    assert torch.equal(x.q_out, u.q_out) and torch.equal(y.q_out, w.q_out) and torch.equal(x.k_out, u.k_out) and torch.equal(y.k_out, w.k_out)
 
 
 # ---- all of it ------------------------------------------------------------------------------------------------------------------------------------

@@ -232,6 +232,9 @@ def test_attention_refuses_pools(lib, over, code):
     (dict(P=1), -1), (dict(G=0), -1), (dict(N=-1), -1), (dict(Hq=6), -1), (dict(Hq=0), -1), (dict(scale=0.0), -1), (dict(scale=-1.0), -1), (dict(scale=math.nan), -1),
     (dict(scale=math.inf), -1), (dict(Hq=4 * 65), -2), (dict(G=2048, P=1, N=2048), -2), (dict(N=(1 << 24) + 4, P=(1 << 22) + 1), -2),
     (dict(workspace=None), -3), (dict(workspace=ADDR + 64), -3), (dict(workspace_bytes=255), -3),
+    # tables whose tokens, all of them there, would be more pieces than 32 bits count
+    (dict(table_pages=1 << 28, table_stride=1 << 28, workspace_bytes=1 << 40), -2), (dict(prompt_table_pages=1 << 28, prompt_table_stride=1 << 28, workspace_bytes=1 << 40), -2),
+    (dict(table_pages=1 << 26, table_stride=1 << 26, workspace_bytes=1 << 40), -2), (dict(N=1 << 24, P=1 << 22, workspace_bytes=1 << 60), -2),
 ])
 def test_attention_refuses(lib, over, code):
     assert lib.arrol_cache_attention(_ctx(), C.byref(_attend(**over)), None) == code
