@@ -64,8 +64,9 @@ const char* arrol_status_string(int status); /* static string, never NULL */
  * arrol_prune_rebatch_host, the policy loss, the training step of a bf16 MLP head) must be ordered on the device with respect to one
  * another, e.g. by issuing them on one stream.  Calls that work in the caller's buffers alone may be in flight on several
  * streams at once, each with a workspace and outputs of its own: arrol_token_logprob and its variants,
- * arrol_lm_head_backward, attention, scoring and training of a linear head, training of an fp32 head, arrol_select, the vote, the
- * trace confidence, and the calibrator's calls (those on one state in order).  They share the GPU then; results do not depend on it. */
+ * arrol_lm_head_backward, attention, rotary positions, the 8-bit cache (appends to different pages), scoring and training of a linear
+ * head, training of an fp32 head, arrol_select, the vote, the trace confidence, and the calibrator's calls (those on one state in order).
+ * They share the GPU then; results do not depend on it. */
 int arrol_create(arrol_ctx** out, int device);
 int arrol_destroy(arrol_ctx* ctx);
 
@@ -485,15 +486,16 @@ int arrol_rotary_backward(arrol_ctx* ctx, const arrol_rotary_args* args, void* s
  *     z_j = scale q[i, h] . k_j[g];   o[i, h] = sum_j exp(z_j - lse[i, h]) v_j[g];   lse[i, h] = log sum_j exp(z_j),   g = h / (Hq / Hkv).
  * A rollout without any key gets o = 0, lse = -inf; rows of rollouts that are not kept are not written.  A prompt's pages are read once for all of its live rollouts (up to
  * 64 query rows, rollouts x Hq / Hkv, per key head).  Without prompts: prompt_table, prompt_lengths NULL, P = 0.  q is scaled by a power of two for each row
- * and taken as fp16, which is exact for bf16 (entries below 2^-27 of their row's largest are rounded at 2^-39 of it); e4m3 numbers are exact in fp16; sums are fp32; probabilities
- * are rounded to fp16 before the product with values.  Every sum
- * has a fixed order, so equal calls give equal bits.
+ * and taken as fp16, which is exact for bf16 (entries below 2^-27 of their row's largest are rounded at 2^-39 of it); e4m3 numbers are exact in fp16; sums are fp32;
+ * probabilities are rounded to fp16 before the product with values, those below 2^-21 of the largest to steps of 2^-31 of it.  Every sum has a fixed order, so equal calls
+ * give equal bits.
  *
- * D a multiple of 16, 16 <= D <= 128; Hq a multiple of Hkv, Hq / Hkv <= 64; G <= 1024, N <= 2^24; pages, tokens of a table row < 2^31; for the attention N * Hkv * (tokens of
- * a table row) below 2^34 (2^31 with Hq / Hkv > 16), the same product of prompts (each counted once for every 64 query rows of its group) below 2^31; scale finite, above 0; bf16 tensors as in
- * the attention calls.  A length that is negative or more than its table row holds, fewer tokens than new ones, or a page number outside [0, pages) is not followed (in
- * attention a sequence or prompt with such a length counts as empty, and what rollouts over such pages get is not defined) and ARROL_DEV_BAD_INDEX is recorded.  The calls use nothing of the context's buffers and may be captured;
- * workspace: arrol_cache_attention_workspace(...) bytes, 256-byte aligned, contents need not be initialised or kept. */
+ * D a multiple of 16, 16 <= D <= 128; Hq a multiple of Hkv, Hq / Hkv <= 64; G <= 1024, N <= 2^24; pages, tokens of a table row < 2^31; for the attention
+ * N * Hkv * (tokens of a table row + 160) below 2^34 (2^31 with Hq / Hkv > 16), the same product of prompts (each counted once for every 64 query rows of its group)
+ * below 2^31; scale finite, above 0; bf16 tensors as in the attention calls.  A length that is negative or more than its table row holds, fewer tokens than new ones, or a
+ * page number outside [0, pages) is not followed (in attention a sequence or prompt with such a length counts as empty, and what rollouts over such pages get is not
+ * defined) and ARROL_DEV_BAD_INDEX is recorded.  The calls use nothing of the context's buffers and may be captured; workspace:
+ * arrol_cache_attention_workspace(...) bytes, 256-byte aligned, contents need not be initialised or kept; what N, P and G take serves calls with fewer, of the same heads. */
 typedef struct arrol_cache {
     void *k_cache, *v_cache;
     int64_t k_page_stride, v_page_stride;

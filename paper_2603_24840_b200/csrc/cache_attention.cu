@@ -355,8 +355,9 @@ struct Fetch {
     }
 };
 
-// A tile of up to 16 query rows against the pieces of its unit.  A lane (g, t) = (lane / 4, lane % 4) has the scores of query rows 2 t and 2 t + 1 (of each eight) with tokens g and, of the second eight of
-// sixteen, 8 + (g + 4) % 8: in that order eight rows of keys, and the sixteen of values that a lane's four scores belong to, are read without two in a bank.
+// A tile of up to 16 query rows against the pieces of its unit.  A lane (g, t) = (lane / 4, lane % 4) has the scores of query rows 2 t and 2 t + 1 (of each eight) with
+// tokens g and, of the second eight of sixteen, 8 + (g + 4) % 8: in that order eight rows of keys, and the sixteen of values that a lane's four scores belong to, are read
+// without two in a bank.
 template <int DP>
 struct RowTile {
     using C = CacheConf<DP>;
