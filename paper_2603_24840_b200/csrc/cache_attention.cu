@@ -1,9 +1,10 @@
 // arrol_cache_attention: one generated token per rollout over its group's prompt and its own tokens, both in the paged 8-bit cache.
 //
 // Bound by HBM in the large: every live rollout's pages and every group's prompt pages are read once, half of a bf16 cache's bytes.  Measured (calls one behind another):
-// 256 live rollouts of 2,200 tokens over 32 prompts, 16 heads of 128 on 8 (1.23 GB) 259 us, 4.8 TB/s; with nothing computed the same copies take 233, so the rest is for the
-// start (a scan, then three loads that depend on one another: 8 us), the merge (10) and the products behind the last copies.  8 rollouts of 6,600 tokens, 32 heads (118 MB) 46 to
-// 53 us.  384 rollouts of 160 tokens over 24 prompts of 4,850, 32 heads of 64 (188 MB) 136 us: there it is the work of 64 query rows behind every key.
+// 256 live rollouts of 2,200 tokens over 32 prompts, 16 heads of 128 on 8 (1.23 GB) 237 us, 5.2 TB/s.  By clocks in the kernel the first pieces are there after 11 us (a scan
+// of 4, then loads that depend on one another, and everybody's copies at once), warps end between 184 and 215, the merge takes 10.  8 rollouts of 6,600 tokens, 32 heads
+// (118 MB) 51 us: pieces from 10 to 38, the merge behind them.  384 rollouts of 160 tokens over 24 prompts of 4,850, 32 heads of 64 (188 MB) 133 us: there it is the work of
+// 64 query rows behind every key, each warp a chain of 2,000 cycles for 32 tokens of 16 rows, three of them an SM's quarter.
 //
 // The products are m16n8k16 mma.sync in fp16, transposed: tokens (of S^T = K Q^T) and dimensions (of O^T = V^T P^T) are the sixteen rows, query rows the eight columns, so that
 // eight query heads waste nothing.  e4m3 numbers widen to fp16 exactly, two an instruction, and q, scaled by a power of two for each row, is exact in fp16 too (bf16 has
@@ -27,14 +28,16 @@ constexpr int CA_WARPS = 4, CA_THREADS = 32 * (CA_WARPS + 1);      // consumers;
 constexpr int CA_ROWS = 64;                        // query rows of a shared unit
 constexpr int CA_ALONE = 16;                       // query rows up to which a unit is a warp's
 constexpr int CA_TOKENS = 32;                      // a single piece; a shared one is four of them, two for more than 32 rows, so that a warp has two to compute
-// The line that the work is cut along, in single pieces: what a shared piece costs, and what a unit costs before its first piece (queries, results) in pieces of its kind.
-// From clocks around the parts (cycles with heads up to 64 and above): a shared piece 4,000 and 6,300 to 8,400 of four warps, a single one 1,640 and 2,700 of one; a single unit's
-// queries, first wait and results 5,800 and 7,000 to 9,000.
+// The line that the work is cut along: what a shared piece costs, a unit before its first single piece (queries, results), a single piece of up to eight rows and one of more.
+// A shared unit's setup counts as one of its pieces.  By the ends of all blocks and whole calls over {36 .. 80, 12 .. 36, 4, 4 .. 6}; against {48, 12, 4, 4} heads of 128 take
+// 231 us instead of 256 (256 rollouts of 2,200 tokens; pieces of nine rows or more ended last), 252 instead of 265 (24 prompts of 5,100 with 14 rollouts of 160 tokens, 32 heads on 8).
 constexpr int CA_SHARED_SETUP = 1;
 struct LineCosts {
-    int shared, single_setup;
+    int shared, single_setup, few, many;
 };
-__host__ __device__ inline LineCosts line_costs(int D) { return D <= 64 ? LineCosts{10, 4} : LineCosts{12, 3}; }
+constexpr LineCosts CA_COSTS_64 = {44, 24, 4, 5}, CA_COSTS_128 = {54, 28, 4, 5};
+// The same in steps of a piece, where tables are so long that the line could pass 32 bits.
+constexpr LineCosts CA_COSTS_COARSE = {13, 7, 1, 1};
 constexpr int CA_SCANNED = 768;                    // entries that a block keeps in shared memory between the two passes of its scan
 constexpr float CA_RESCALE_AT = 8.0f;              // the running maximum follows once it is 2^8 behind
 constexpr float CA_P_SCALE = 128.0f;               // probabilities up to 2^8 times 2^7 stay below fp16's largest
@@ -92,16 +95,21 @@ struct CacheParams {
 
 // ---- the line of pieces.  The host sees to it that its length fits 31 bits.
 struct Line {
-    int shared, single;      // lengths: units' pieces and setups
+    int shared, single;      // lengths: units' pieces and setups, the single ones' by their cost
     int per;                 // cost that a block takes
-    int cost;                      // of a shared piece
+    int cost;                // of a shared piece
+    int begin;               // of the single line
 };
-// Shares are such that every block (warp) between the first and the last that has some of a unit has one of its pieces: a share holds a shared piece, and the single
-// line begins where four warps have as much of it each.
-__device__ __forceinline__ int single_begin(int shared, int cost) { return (shared * cost + CA_WARPS - 1) / CA_WARPS * CA_WARPS; }
-__device__ __forceinline__ Line make_line(int shared, int single, int grid, int cost) {
-    const int each = (single_begin(shared, cost) + single + grid - 1) / grid;
-    return {shared, single, (max(each, (shared > 0 ? cost : 1)) + CA_WARPS - 1) / CA_WARPS * CA_WARPS, cost};
+// Shares are such that every block (warp) between the first and the last that has some of a unit has one of its pieces: a share holds a shared piece, a warp's part of one any
+// single piece (`many`: some are of more than eight rows), and the single line begins where four warps have as much of it each, at the next block if that were less.
+__device__ __forceinline__ Line make_line(int shared, int single, bool many, int grid, const LineCosts& costs) {
+    const int least = CA_WARPS * (many ? costs.many : costs.few);
+    Line l = {shared, single, 0, costs.shared, (shared * costs.shared + CA_WARPS - 1) / CA_WARPS * CA_WARPS};
+    const int each = max((l.begin + single + least + grid - 1) / grid, max(shared > 0 ? costs.shared : 0, least));
+    l.per = (each + CA_WARPS - 1) / CA_WARPS * CA_WARPS;
+    const int used = l.begin % l.per;
+    if (used > 0 && l.per - used < least) l.begin += l.per - used;
+    return l;
 }
 // the shared line from there on is block b's or a later one's
 __device__ __forceinline__ int shared_begin(const Line& l, int b) {
@@ -110,8 +118,8 @@ __device__ __forceinline__ int shared_begin(const Line& l, int b) {
 }
 // a warp's part of the single line, from y0 to y1 (none where that is not more); warps are counted over all blocks
 __device__ __forceinline__ void warp_range(const Line& l, int warp, int& y0, int& y1) {
-    const int begin = single_begin(l.shared, l.cost), b = warp / CA_WARPS, k = warp % CA_WARPS;
-    const int lo = max(b * l.per - begin, 0), each = max((b + 1) * l.per - begin - lo, 0) / CA_WARPS;
+    const int b = warp / CA_WARPS, k = warp % CA_WARPS;
+    const int lo = max(b * l.per - l.begin, 0), each = max((b + 1) * l.per - l.begin - lo, 0) / CA_WARPS;
     y0 = lo + k * each;
     y1 = min(y0 + each, l.single);
 }
@@ -138,6 +146,8 @@ __device__ __forceinline__ int entry_pieces(int rows, int tokens) {
     return (int)(((int64_t)tokens + of - 1) / of);
 }
 __device__ __forceinline__ int unit_setup(const CacheParams& p, int rows) { return rows > CA_ALONE ? CA_SHARED_SETUP : p.costs.single_setup; }
+// of a piece, on its line
+__device__ __forceinline__ int piece_length(const CacheParams& p, int rows) { return rows > CA_ALONE ? 1 : rows > 8 ? p.costs.many : p.costs.few; }
 // {tokens, rows} of an entry; no rows where it is left out.
 __device__ __forceinline__ int2 entry_size(const CacheParams& p, int e, bool& bad) {
     const arrol_cache_attention_args& a = p.a;
@@ -231,51 +241,60 @@ struct CacheConf {
     static __device__ __forceinline__ uint32_t at(int row, int chunk) { return row * DP + ((chunk ^ (DP == 128 ? row & 7 : row >> 1 & 3)) << 4); }
 };
 
-// Walks over a part of a line, piece by piece.  What comes next is asked for before it is needed.
+// Walks over a part of a line, piece by piece: those that begin in it.  What comes next is asked for before it is needed.
 struct Cursor {
     CacheEntry e, next;
     const CacheEntry* list;
-    int left;                // of the part, from the piece that the cursor is at on
-    int number, last;              // of the list's entries
-    int head, piece, setup;
+    int left;                // of the part, from the beginning of the cursor's piece on
+    int number, last;        // of the list's entries
+    int head, piece, setup, length;
     __device__ __forceinline__ void fetch() {
         if (number + 1 <= last) next = list[number + 1];
     }
-    __device__ __forceinline__ void begin(const CacheParams& p, const CacheEntry* l, const Start& s, int entries, int length) {
+    __device__ __forceinline__ void begin(const CacheParams& p, const CacheEntry* l, const Start& s, int entries, int part, int heads) {
         list = l;
         e = s.e;
         number = s.number;
         last = entries - 1;
-        left = length;
+        left = part;
         setup = unit_setup(p, e.rows);
-        head = (int)(s.offset / (e.pieces + setup));
-        piece = (int)(s.offset - head * (e.pieces + setup)) - setup;
-        if (piece < 0) { left += piece; piece = 0; }
+        length = piece_length(p, e.rows);
+        const int unit = e.pieces * length + setup;
+        head = s.offset / unit;
+        const int at = s.offset - head * unit - setup;
+        piece = at > 0 ? (at + length - 1) / length : 0;
+        left += at - piece * length;                     // negative: before the unit's first piece
         fetch();
+        if (piece == e.pieces) {                         // its last one began before the part
+            --piece;
+            left += length;
+            advance(p, heads);
+        }
     }
-    __device__ __forceinline__ void advance(int heads) {
-        --left;
+    __device__ __forceinline__ void advance(const CacheParams& p, int heads) {
+        left -= length;
         if (++piece < e.pieces) return;
         piece = 0;
         left -= setup;
         if (++head < heads) return;
         head = 0;
         e = next;
+        length = piece_length(p, e.rows);
         ++number;
         fetch();
     }
     // so many pieces on, or past the part's end
-    __device__ __forceinline__ void skip(int n, int heads) {
+    __device__ __forceinline__ void skip(const CacheParams& p, int n, int heads) {
         if (left > 0 && piece + n < e.pieces) {
             piece += n;
-            left -= n;
+            left -= n * length;
             return;
         }
 #pragma unroll 1
-        for (; n > 0 && left > 0; --n) advance(heads);
+        for (; n > 0 && left > 0; --n) advance(p, heads);
     }
     // whether the piece is the part's last one
-    __device__ __forceinline__ bool is_last() const { return left == 1 || (piece == e.pieces - 1 && left <= 1 + setup); }
+    __device__ __forceinline__ bool is_last() const { return left <= length || (piece == e.pieces - 1 && left <= length + setup); }
 };
 
 // Pages of the first and the second 16 tokens from `tok` on, -1 where there are none.
@@ -641,11 +660,13 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
     const int each = (p.entries + CA_THREADS - 1) / CA_THREADS;
     const int e0 = min((int)threadIdx.x * each, p.entries), e1 = min(e0 + each, p.entries);
     auto size = [&](int e) { return e < CA_SCANNED ? sm.sizes[e] : entry_size(p, e, bad); };
-    auto length = [&](int2 x) { return (entry_pieces(x.y, x.x) + unit_setup(p, x.y)) * Hkv; };
+    auto length = [&](int2 x) { return (entry_pieces(x.y, x.x) * piece_length(p, x.y) + unit_setup(p, x.y)) * Hkv; };
     ScanSums mine = {0, 0, 0, 0};
+    bool many = false;
     for (int e = e0; e < e1; ++e) {
         const int2 x = size(e);
         if (x.x == 0) continue;
+        many |= x.y > 8 && x.y <= CA_ALONE;
         if (x.y > CA_ALONE) { mine.shared += length(x); ++mine.shared_entries; }
         else { mine.single += length(x); ++mine.single_entries; }
     }
@@ -657,14 +678,14 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
         if (lane >= d) sum = sum + x;
     }
     if (lane == 31) sm.warp_sums[warp] = sum;
-    __syncthreads();
+    many = __syncthreads_or(many);
     ScanSums total = {0, 0, 0, 0}, at = {sum.shared - mine.shared, sum.single - mine.single, sum.shared_entries - mine.shared_entries, sum.single_entries - mine.single_entries};
 #pragma unroll
     for (int w = 0; w < CA_WARPS + 1; ++w) {
         if (w < warp) at = at + sm.warp_sums[w];
         total = total + sm.warp_sums[w];
     }
-    const Line line = make_line(total.shared, total.single, p.grid, p.costs.shared);
+    const Line line = make_line(total.shared, total.single, many, p.grid, p.costs);
     const int x0 = shared_begin(line, b), x1 = shared_begin(line, b + 1);
     int y0[CA_WARPS], y1[CA_WARPS];
 #pragma unroll
@@ -713,10 +734,10 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
             if (phase == 0) { from = x0; to = x1; }
             Cursor c;
             c.left = 0;
-            if (from < to) c.begin(p, phase ? p.w.single : p.w.shared, phase ? sm.single[of] : sm.shared, phase ? total.single_entries : total.shared_entries, to - from);
+            if (from < to) c.begin(p, phase ? p.w.single : p.w.shared, phase ? sm.single[of] : sm.shared, phase ? total.single_entries : total.shared_entries, to - from, Hkv);
             // a part that its piece does not have begins where no tokens are
             auto token = [&] { const int parts = piece_parts(c.e.rows); return phase ? c.piece * CA_TOKENS : of < parts ? (c.piece * parts + of) * CA_TOKENS : c.e.tokens; };
-            for (int i = 0; i < k && c.left > 0; ++i) c.advance(Hkv);
+            for (int i = 0; i < k && c.left > 0; ++i) c.advance(p, Hkv);
             Fetch now, next;
             bool there = c.left > 0, more = false;
             bool copied = false;
@@ -744,7 +765,7 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
                     }
                     begun = true;
                     at = 0;
-                    c.skip(8, Hkv);
+                    c.skip(p, 8, Hkv);
                     more = there && c.left > 0;
                     if (more) next.find(p, c, token(), false);
                 }
@@ -850,7 +871,8 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
     if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, ARROL_DEV_WAIT_EXPIRED);
 }
 
-// A warp per (rollout, query head): the prompt's records, then its own, in order; four dimensions a lane.  Records are asked for eight at a time.
+// A warp, or with heads up to 64 half a warp, per (rollout, query head): the prompt's records, then its own, in order; four dimensions a lane.  Records are asked for eight
+// at a time.
 struct Merged {
     static constexpr int AT_ONCE = 8;
     float top, total;
@@ -872,13 +894,13 @@ struct Merged {
     }
 };
 
+template <int LANES>
 __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
     pdl_launch_dependents();
     pdl_wait();
     const arrol_cache_attention_args& a = p.a;
-    const int lane = threadIdx.x & 31, D = a.cache.D, Hkv = a.cache.Hkv, d = lane * 4;
-    const int64_t row = blockIdx.x * (int64_t)8 + (threadIdx.x >> 5);
-    if (row >= (int64_t)a.N * a.Hq) return;
+    const int lane = threadIdx.x % LANES, part = (threadIdx.x & 31) - lane, D = a.cache.D, Hkv = a.cache.Hkv, d = lane * 4;
+    const int64_t rows = (int64_t)a.N * a.Hq, asked = (blockIdx.x * (int64_t)256 + threadIdx.x) / LANES, row = asked < rows ? asked : rows - 1;      // both halves go on together
     const int i = (int)(row / a.Hq), hq = (int)(row - (int64_t)i * a.Hq), h = hq / p.ratio, r = hq - h * p.ratio;
     const int2* owners = pdl_acquire(p.w.owners);
     const float2* ml = pdl_acquire(p.w.ml);
@@ -892,19 +914,19 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
         const int q = i / a.G, G = a.G;
         prompt_tokens = cache_tokens(a.prompt_lengths, q, a.prompt_table_pages, a.cache.page, bad);
         int before = 0, live = 0;                             // live rollouts of the group: before this one, all
-        for (int j0 = 0; j0 < G; j0 += 32) {
+        for (int j0 = 0; j0 < G; j0 += LANES) {
             const int j = j0 + lane;
-            const uint32_t all = __ballot_sync(0xffffffffu, j < G && (!a.keep || a.keep[(int64_t)q * G + j]));
+            const uint32_t all = (__ballot_sync(0xffffffffu, j < G && (!a.keep || a.keep[(int64_t)q * G + j])) >> part) & (0xffffffffu >> (32 - LANES));
             const int left = i - q * G - j0;
             live += __popc(all);
-            before += __popc(left >= 32 ? all : left <= 0 ? 0u : all & ((1u << left) - 1u));
+            before += __popc(left >= LANES ? all : left <= 0 ? 0u : all & ((1u << left) - 1u));
         }
         entry = q * p.blocks + before / p.group;
         prompt_rows = min(live - before / p.group * p.group, p.group) * p.ratio;
         prompt_row = before % p.group * p.ratio + r;
         shared = owners[(int64_t)entry * Hkv + h];
     }
-    if (a.keep && !a.keep[i]) return;
+    if (asked >= rows || (a.keep && !a.keep[i])) return;
     Merged m = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
     // The records of a unit: `count` of the blocks (warps) that have some of it, `step` rows apart; of shared units of up to 32 rows two each, CA_ROWS / 2 apart.
     struct Records { int64_t first; int count, step, twice; };
@@ -977,7 +999,8 @@ int launch_cache_attention(arrol_ctx* ctx, const CacheParams& p, cudaStream_t s)
                                 make_map_pages(ctx, &v, p.a.cache, p.a.cache.v_cache, p.a.cache.v_page_stride, DP) != ARROL_OK))
         return ARROL_ERR_CUDA;
     ARROL_CUDA_OK(arrol_launch_pdl(cache_units_kernel<DP>, dim3((unsigned)p.grid), dim3(CA_THREADS), C::SMEM, s, k, v, p));
-    ARROL_CUDA_OK(arrol_launch_pdl(cache_merge_kernel, dim3((unsigned)(((int64_t)p.a.N * p.a.Hq + 7) / 8)), dim3(256), 0, s, p));
+    constexpr int LANES = DP / 4;
+    ARROL_CUDA_OK(arrol_launch_pdl(cache_merge_kernel<LANES>, dim3((unsigned)(((int64_t)p.a.N * p.a.Hq * LANES + 255) / 256)), dim3(256), 0, s, p));
     ctx->launches += 2;
     return ARROL_OK;
 }
@@ -1019,15 +1042,18 @@ extern "C" int arrol_cache_attention(arrol_ctx* ctx, const arrol_cache_attention
     p.entries = p.prompts + a->N;
     p.page_shift = __builtin_ctz((unsigned)a->cache.page);
     p.grid = ctx->sm_count * ca_per_sm(a->cache.D);
-    p.costs = line_costs(a->cache.D);
     // The line is counted in 32 bits: with every table full it stays below 2^30.
     const int64_t own_most = (int64_t)a->table_pages * a->cache.page, prompt_most = (int64_t)a->prompt_table_pages * a->cache.page;
-    auto longest = [&](int64_t units, int64_t tokens, bool shared) {
-        const double pieces = shared ? (double)(tokens / 64 + 2) * p.costs.shared : (double)(tokens / 32 + 1 + p.costs.single_setup);
-        return (double)units * a->cache.Hkv * pieces;
+    if (own_most > INT32_MAX || prompt_most > INT32_MAX) return ARROL_ERR_UNSUPPORTED;
+    auto fits = [&](const LineCosts& c) {
+        auto longest = [&](int64_t units, int64_t tokens, bool shared) {
+            return (double)units * a->cache.Hkv * (shared ? (double)(tokens / 64 + 2) * c.shared : (double)(tokens / 32 + 1) * c.many + c.single_setup);
+        };
+        return longest(a->N, own_most, p.ratio > CA_ALONE) + longest(p.prompts, prompt_most, true) < 1073741824.0;
     };
-    if (own_most > INT32_MAX || prompt_most > INT32_MAX || longest(a->N, own_most, p.ratio > CA_ALONE) + longest(p.prompts, prompt_most, true) >= 1073741824.0)
-        return ARROL_ERR_UNSUPPORTED;
+    p.costs = a->cache.D <= 64 ? CA_COSTS_64 : CA_COSTS_128;
+    if (!fits(p.costs)) p.costs = CA_COSTS_COARSE;
+    if (!fits(p.costs)) return ARROL_ERR_UNSUPPORTED;
     p.own_most = (int)own_most;
     p.scale_log2 = a->scale * LOG2E;
     p.status = ctx->d_status;

@@ -342,6 +342,18 @@ def test_pages_beyond_32_bit_offsets(ctx):
         p.check(p.run(ctx))
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,pages", [(8, 4, 64, 1 << 24), (24, 2, 128, 1 << 25), (64, 2, 128, 1 << 23)])
+def test_tables_for_very_long_sequences(ctx, Hq, Hkv, D, pages):
+    """Room for more tokens than the line counts in its finer steps, few of them there."""
+    p = Attend([70, 3000, 1, 555, 0, 64, 33, 1200], [40, 900], 4, Hq, Hkv, D, 16, [1, 1, 1, 0, 1, 1, 1, 1], seed=26)
+    want = p.run(ctx)
+    p.check(*want)
+    wide = torch.full((p.N, pages), -5, dtype=torch.int32, device="cuda")
+    wide[:, :p.table.shape[1]] = p.table
+    p.table = wide
+    p.check(*p.run(ctx))
+
+
 def test_a_workspace_for_more_serves_less(ctx):
     """Of the same heads: with fewer rollouts, prompts or rollouts a prompt; what an earlier call left there does not matter."""
     big = Attend([50, 300] * 20, [100, 9, 0, 400], 10, 8, 2, 64, 16, seed=22)
