@@ -31,6 +31,7 @@ struct arrol_ctx {
     bool attention_backward_smem_set[2];
     bool attention_decode_smem_set[2];
     bool cache_attention_smem_set[2];
+    bool cache_append_smem_set[2][3];     // 1,024 and 512 threads; chunks of 8, 4, 2 numbers
     bool prune_smem_set;       // likewise for the fused prune step
     int score_max_clusters[3][9]; // scoring kernel, tiles of 128 x 64, 64 x 64 and 128 x 128 rollouts x hidden units: clusters of so many
                                // blocks that are resident at once; 0 = not asked yet

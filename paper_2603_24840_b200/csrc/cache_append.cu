@@ -2,10 +2,10 @@
 //
 // Bound by HBM where there are many tokens (bf16 in, 8 bits out, queries in and out), by one launch and a chain of dependent loads (length, page number, scale) where
 // there are few.  A page's scale needs the largest entry of all of its new tokens before the first can be rounded, so a page and head belong to one block
-// (append_runs_kernel: runs of tokens) or one warp (append_one_kernel: a token per sequence), which keeps what it loaded in registers in between (but for pages that are
-// more than a block can hold, odd sizes only) and needs no atomics in global memory.
+// (append_runs_kernel: runs of tokens) or one warp (append_one_kernel: a token per sequence), which keeps what it loaded in shared memory or registers in between (but for
+// odd sizes) and needs no atomics in global memory.
 //
-// 38,000 prompt tokens of 16 heads of 128 on 8 (600 MB) 143 us, 4.2 TB/s: the meeting of a block for each head, and the turning twice, are not all hidden.  One token each of
+// 38,000 prompt tokens of 16 heads of 128 on 8 (600 MB) 137 us, 4.4 TB/s: no unit is full (instructions issued in half of the cycles, DRAM at 0.55); the values are turned twice.  One token each of
 // 512 live rollouts, 32 heads on 8 (12 MB), 18 us.
 #include <type_traits>
 
@@ -155,10 +155,22 @@ __device__ __forceinline__ void append_codes(uint8_t* to, const float (&x)[V], f
     }
 }
 
-template <int V, int THREADS>
+// Heads on their way.  38,000 prompt tokens: 2 140 us, 3 or 4 137, 6 149 (shared memory is then taken from what the spilled registers lie in); the next head in registers 143.
+// Two heads a meeting: 137, four 150.
+constexpr int APPEND_DEPTH = 4;
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+}
+
+// RING: a page's units fit the block.  A thread's own chunks come by asynchronous copies into places of its own, several heads ahead; otherwise they are read where they lie.
+template <int V, int THREADS, bool RING>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_runs_kernel(const AppendParams p) {
     typedef typename Bf16Chunk<V>::type Chunk;
     __shared__ uint32_t most[3];                             // largest of a head, as bits: in turn
+    extern __shared__ __align__(16) uint8_t ring[];          // [APPEND_DEPTH][2][threads] chunks
     pdl_launch_dependents();
     pdl_wait();
     const arrol_cache_append_args& a = p.a;
@@ -191,7 +203,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_runs_kernel(co
     int tok = threadIdx.x / p.units;
     RotaryUnit<V> unit(p.pairs, threadIdx.x - tok * p.units);
     bool mine = (int)threadIdx.x < items;
-    const int passes = THREADS == 512 ? 1 : p.passes;        // a small block's page always fits
+    const int passes = RING || THREADS == 512 ? 1 : p.passes;
     auto pass_to = [&](int pass) {                           // only where a page's units are more than the block's threads
         const int x = threadIdx.x + pass * blockDim.x;
         tok = x / p.units;
@@ -199,28 +211,59 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_runs_kernel(co
         mine = x < items;
         if (mine && blockIdx.z == 0) unit.at(p.pairs, first_position + tok);
     };
-    if (mine && blockIdx.z == 0) unit.at(p.pairs, first_position + tok);
     const bool values = blockIdx.z != 0;
     const __nv_bfloat16* const rows = static_cast<const __nv_bfloat16*>(values ? a.v : a.k) + first_row * (values ? a.v_stride : a.k_stride);
+    const __nv_bfloat16* const queries = static_cast<const __nv_bfloat16*>(a.q) + first_row * a.q_stride;
     const int64_t stride = values ? a.v_stride : a.k_stride;
     float* const scales = values ? a.cache.v_scale + page * a.cache.v_scale_stride : a.cache.k_scale + page * a.cache.k_scale_stride;
     uint8_t* const codes = static_cast<uint8_t*>(values ? a.cache.v_cache : a.cache.k_cache) + page * (values ? a.cache.v_page_stride : a.cache.k_page_stride);
-    // What was loaded stays as it came, and is turned twice, for the largest and for the codes: as floats it would need twice the registers, and half of the threads would
-    // not fit.  The next head's loads are under way while this one's largest is found.
-    struct Raw { Chunk a, b; };
-    auto load = [&](int h) {
-        Raw r = {};
-        if (mine) {
-            const __nv_bfloat16* row = rows + tok * stride + h * D;
-            r.a = *reinterpret_cast<const Chunk*>(row + unit.a);
-            r.b = *reinterpret_cast<const Chunk*>(row + unit.b);
-        }
-        return r;
+    // The block's heads one behind another: of keys or values, then of queries.
+    const int split = gridDim.y, heads = ((int)blockIdx.y < Hkv ? (Hkv - 1 - (int)blockIdx.y) / split + 1 : 0);
+    const int all = heads + (!values && a.q && (int)blockIdx.y < a.Hq ? (a.Hq - 1 - (int)blockIdx.y) / split + 1 : 0);
+    auto source = [&](int t) {
+        return t < heads ? rows + tok * stride + (int64_t)(blockIdx.y + t * split) * D : queries + tok * a.q_stride + (int64_t)(blockIdx.y + (t - heads) * split) * D;
     };
-    auto turned = [&](const Raw& r, float (&x)[V], float (&y)[V]) {
-        chunk_to_floats<V>(r.a, x);
-        chunk_to_floats<V>(r.b, y);
+    const uint32_t place = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * (uint32_t)sizeof(Chunk);
+    auto place_of = [&](int slot, int second) { return (uint32_t)(slot * 2 + second) * blockDim.x * (uint32_t)sizeof(Chunk); };
+    // head t into its place, which nobody but this thread reads, and which it has read
+    auto bring = [&](int t, int slot) {
+        if constexpr (RING) {
+            if (mine && t < all) {
+                const __nv_bfloat16* row = source(t);
+                copy_async<sizeof(Chunk)>(place + place_of(slot, 0), row + unit.a);
+                copy_async<sizeof(Chunk)>(place + place_of(slot, 1), row + unit.b);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    };
+    auto arrived = [&] {
+        if constexpr (RING) asm volatile("cp.async.wait_group %0;" ::"n"(APPEND_DEPTH - 1) : "memory");
+    };
+    int at = 0;                                              // place of the head that is worked on
+    if constexpr (RING)
+        for (int t = 0; t < APPEND_DEPTH; ++t) bring(t, t);
+    if (mine && blockIdx.z == 0) unit.at(p.pairs, first_position + tok);
+    // What was loaded is turned twice, for the largest and for the codes: kept as floats it would need twice the registers, and half of the threads would not fit.
+    auto turned = [&](int t, float (&x)[V], float (&y)[V]) {
+        Chunk c = {}, d = {};
+        if (mine) {
+            if constexpr (RING) {
+                const Chunk* from = reinterpret_cast<const Chunk*>(ring) + threadIdx.x;
+                c = from[(at * 2) * blockDim.x];
+                d = from[(at * 2 + 1) * blockDim.x];
+            } else {
+                const __nv_bfloat16* row = source(t);
+                c = *reinterpret_cast<const Chunk*>(row + unit.a);
+                d = *reinterpret_cast<const Chunk*>(row + unit.b);
+            }
+        }
+        chunk_to_floats<V>(c, x);
+        chunk_to_floats<V>(d, y);
         if (!values) unit.turn(p.pairs, x, y);
+    };
+    auto done = [&](int t) {
+        bring(t + APPEND_DEPTH, at);
+        at = at == APPEND_DEPTH - 1 ? 0 : at + 1;
     };
     // The largest of all threads' values; what is not finite is left out only where there is an infinity among them (a NaN the maximum passes over by itself).
     auto largest = [&](float m, int slot) {
@@ -230,28 +273,22 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_runs_kernel(co
         return __uint_as_float(most[slot]);
     };
     int slot = 0;
-    Raw raw = {};
-    if (passes == 1 && (int)blockIdx.y < Hkv) raw = load(blockIdx.y);
-    for (int h = blockIdx.y; h < Hkv; h += gridDim.y) {
+    for (int t = 0; t < heads; ++t) {
+        const int h = blockIdx.y + t * split;
         const float old = slot0 ? scales[h] : 0.f;
+        arrived();
         auto own_largest = [&](auto finite) {
             float m = 0.f;
             for (int pass = 0; pass < passes; ++pass) {
-                if (passes > 1) {
-                    pass_to(pass);
-                    raw = load(h);
-                }
+                if (passes > 1) pass_to(pass);
                 float x[V], y[V];
-                turned(raw, x, y);
+                turned(t, x, y);
 #pragma unroll
                 for (int j = 0; j < V; ++j) m = decltype(finite)::value ? finite_max(finite_max(m, x[j]), y[j]) : fmaxf(fmaxf(m, fabsf(x[j])), fabsf(y[j]));
             }
             return m;
         };
-        const float own = own_largest(std::false_type());
-        Raw after = {};
-        if (passes == 1 && h + (int)gridDim.y < Hkv) after = load(h + gridDim.y);
-        float m = largest(own, slot);
+        float m = largest(own_largest(std::false_type()), slot);
         // A word is cleared two meetings before it is used again: all have read it then, in front of the meeting between.
         auto next_slot = [&] {
             if (threadIdx.x == 0) most[slot == 0 ? 2 : slot - 1] = 0u;
@@ -269,59 +306,51 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_runs_kernel(co
         const float by = cache_power(-e);
         if (grows) append_rescale(to_head, slot0 * D, old * by, threadIdx.x, blockDim.x);
         for (int pass = 0; pass < passes; ++pass) {
-            if (passes > 1) {
-                pass_to(pass);
-                raw = load(h);
-            }
+            if (passes > 1) pass_to(pass);
             if (mine) {
-                const int at = (slot0 + tok) * D;
+                const int to = (slot0 + tok) * D;
                 float x[V], y[V];
-                turned(raw, x, y);
+                turned(t, x, y);
                 if (!values && a.k_out) {
                     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.k_out) + (first_row + tok) * a.k_out_stride + h * D;
                     *reinterpret_cast<Chunk*>(out + unit.a) = floats_to_chunk<V>(x);
                     *reinterpret_cast<Chunk*>(out + unit.b) = floats_to_chunk<V>(y);
                 }
                 if (__builtin_expect(infinite, 0)) not_finite_to_nan<V>(x, y);
-                append_codes<V>(to_head + at + unit.a, x, by);
-                append_codes<V>(to_head + at + unit.b, y, by);
+                append_codes<V>(to_head + to + unit.a, x, by);
+                append_codes<V>(to_head + to + unit.b, y, by);
             }
         }
         if (threadIdx.x == 0 && (slot0 == 0 || grows)) scales[h] = cache_power(e);
-        raw = after;
+        done(t);
     }
-    if (values) return;
-    if (!a.q) return;
-    for (int pass = 0; pass < passes; ++pass) {
-        if (passes > 1) pass_to(pass);
-        if (!mine) continue;
-        const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.q) + (first_row + tok) * a.q_stride;
-        __nv_bfloat16* const qo = static_cast<__nv_bfloat16*>(a.q_out) + (first_row + tok) * a.q_out_stride;
-        constexpr int AT_ONCE = 2;
-        for (int h = blockIdx.y; h < a.Hq; h += gridDim.y * AT_ONCE) {
-            Chunk ca[AT_ONCE], cb[AT_ONCE];
-#pragma unroll
-            for (int j = 0; j < AT_ONCE; ++j) {
-                const int hh = h + j * gridDim.y;
-                if (hh < a.Hq) {
-                    ca[j] = *reinterpret_cast<const Chunk*>(q + (int64_t)hh * D + unit.a);
-                    cb[j] = *reinterpret_cast<const Chunk*>(q + (int64_t)hh * D + unit.b);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < AT_ONCE; ++j) {
-                const int hh = h + j * gridDim.y;
-                if (hh < a.Hq) {
-                    float x[V], y[V];
-                    chunk_to_floats<V>(ca[j], x);
-                    chunk_to_floats<V>(cb[j], y);
-                    unit.turn(p.pairs, x, y);
-                    *reinterpret_cast<Chunk*>(qo + (int64_t)hh * D + unit.a) = floats_to_chunk<V>(x);
-                    *reinterpret_cast<Chunk*>(qo + (int64_t)hh * D + unit.b) = floats_to_chunk<V>(y);
-                }
+    for (int t = heads; t < all; ++t) {
+        const int h = blockIdx.y + (t - heads) * split;
+        arrived();
+        for (int pass = 0; pass < passes; ++pass) {
+            if (passes > 1) pass_to(pass);
+            if (mine) {
+                __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(a.q_out) + (first_row + tok) * a.q_out_stride + (int64_t)h * D;
+                float x[V], y[V];
+                turned(t, x, y);
+                *reinterpret_cast<Chunk*>(to + unit.a) = floats_to_chunk<V>(x);
+                *reinterpret_cast<Chunk*>(to + unit.b) = floats_to_chunk<V>(y);
             }
         }
+        done(t);
     }
+}
+
+template <int V, int THREADS, bool RING>
+int launch_append_runs(arrol_ctx* ctx, const AppendParams& p, dim3 grid, int threads, bool& set, cudaStream_t s) {
+    const size_t bytes = RING ? (size_t)APPEND_DEPTH * 2 * threads * 2 * V : 0;
+    if (RING && !set) {
+        ARROL_CUDA_OK(cudaFuncSetAttribute(append_runs_kernel<V, THREADS, RING>, cudaFuncAttributeMaxDynamicSharedMemorySize, APPEND_DEPTH * 2 * THREADS * 2 * V));
+        set = true;
+    }
+    ARROL_CUDA_OK(arrol_launch_pdl(append_runs_kernel<V, THREADS, RING>, grid, dim3(threads), bytes, s, p));
+    ctx->launches += 1;
+    return ARROL_OK;
 }
 
 }  // namespace
@@ -355,7 +384,7 @@ extern "C" int arrol_cache_append(arrol_ctx* ctx, const arrol_cache_append_args*
         if ((warps + ONE_WARPS - 1) / ONE_WARPS >= ((int64_t)1 << 31)) return ARROL_ERR_UNSUPPORTED;
         ARROL_CUDA_OK(arrol_launch_pdl(append_one_kernel, dim3((unsigned)((warps + ONE_WARPS - 1) / ONE_WARPS)), dim3(32 * ONE_WARPS), 0, (cudaStream_t)stream, p));
     } else {
-        // The widest chunks that the sizes allow: 4 numbers and twice the threads take 200 to 247 us instead of 143 for 38,000 prompt tokens.
+        // The widest chunks that the sizes allow: 4 numbers and twice the threads took 200 to 247 us where this took 143 for 38,000 prompt tokens.
         const int V = rotary_vector(D, a->R);
         p.units = D / (2 * V);
         const int items = a->cache.page * p.units, threads = items > 1024 ? 1024 : (items + 31) & ~31;
@@ -365,10 +394,17 @@ extern "C" int arrol_cache_append(arrol_ctx* ctx, const arrol_cache_append_args*
         const int most = a->q && a->Hq > Hkv ? a->Hq : Hkv;
         int64_t split = (int64_t)(4 * ctx->sm_count) * 512 / threads / (a->rows / a->cache.page + 1);
         split = split < 1 ? 1 : split > most ? most : split;
-        void (*kernel)(AppendParams);
-        if (threads <= 512) kernel = V == 8 ? append_runs_kernel<8, 512> : V == 4 ? append_runs_kernel<4, 512> : V == 2 ? append_runs_kernel<2, 512> : append_runs_kernel<1, 512>;
-        else kernel = V == 8 ? append_runs_kernel<8, 1024> : V == 4 ? append_runs_kernel<4, 1024> : V == 2 ? append_runs_kernel<2, 1024> : append_runs_kernel<1, 1024>;
-        ARROL_CUDA_OK(arrol_launch_pdl(kernel, dim3((unsigned)pages, (unsigned)split, 2), dim3(threads), 0, (cudaStream_t)stream, p));
+        const dim3 grid((unsigned)pages, (unsigned)split, 2);
+        const cudaStream_t s = (cudaStream_t)stream;
+        const bool small = threads <= 512;
+        bool* set = ctx->cache_append_smem_set[small];
+        if (p.passes > 1)                                    // chunks of 8 numbers always fit
+            return V == 4 ? launch_append_runs<4, 1024, false>(ctx, p, grid, threads, set[0], s) : V == 2 ? launch_append_runs<2, 1024, false>(ctx, p, grid, threads, set[0], s)
+                                                                                                 : launch_append_runs<1, 1024, false>(ctx, p, grid, threads, set[0], s);
+        if (V == 8) return small ? launch_append_runs<8, 512, true>(ctx, p, grid, threads, set[0], s) : launch_append_runs<8, 1024, true>(ctx, p, grid, threads, set[0], s);
+        if (V == 4) return small ? launch_append_runs<4, 512, true>(ctx, p, grid, threads, set[1], s) : launch_append_runs<4, 1024, true>(ctx, p, grid, threads, set[1], s);
+        if (V == 2) return small ? launch_append_runs<2, 512, true>(ctx, p, grid, threads, set[2], s) : launch_append_runs<2, 1024, true>(ctx, p, grid, threads, set[2], s);
+        return small ? launch_append_runs<1, 512, false>(ctx, p, grid, threads, set[0], s) : launch_append_runs<1, 1024, false>(ctx, p, grid, threads, set[0], s);
     }
     ctx->launches += 1;
     return ARROL_OK;
