@@ -5,8 +5,8 @@
 // (append_runs_kernel: runs of tokens) or one warp (append_one_kernel: a token per sequence), which keeps what it loaded in shared memory or registers in between (but for
 // odd sizes) and needs no atomics in global memory.
 //
-// 38,000 prompt tokens of 16 heads of 128 on 8 (600 MB) 137 us, 4.4 TB/s: no unit is full (instructions issued in half of the cycles, DRAM at 0.55); the values are turned twice.  One token each of
-// 512 live rollouts, 32 heads on 8 (12 MB), 18 us.
+// 38,000 prompt tokens of 16 heads of 128 on 8 (600 MB) 137 us, 4.4 TB/s: no unit is full (instructions issued in half of the cycles, DRAM at 0.55); the values are turned twice.  One
+// token each of 512 live rollouts, 32 heads on 8 (12 MB), 12 us from a graph.
 #include <type_traits>
 
 #include "cache_common.cuh"
@@ -63,72 +63,108 @@ __device__ __forceinline__ int append_exponent(float amax, int slot, float old, 
     return e;
 }
 
-// ---- one token per sequence: a warp per (sequence, head of q, k or v), four dimensions a lane
+// ---- one token per sequence: a warp per sequence and PER of its heads (keys', then values', then queries'), four dimensions a lane.  Where one a head
+// would be more warps than the SMs have places for, four heads share the angles and the chain of loads in front of them (heads of 128, 32 on 8, from a graph: 64 rollouts 4.5 us
+// with one and 5.1 with four, 256 9.1 and 6.5, 512 live of 1,024 17.7 and 11.6, 4,096 109 and 68; with two 13.0 and 76, with eight 15.9 and 88, for the last two).
+template <int PER>
 __global__ void __launch_bounds__(32 * ONE_WARPS) append_one_kernel(const AppendParams p) {
     pdl_launch_dependents();
     pdl_wait();
     const arrol_cache_append_args& a = p.a;
-    const int lane = threadIdx.x & 31, tasks = 2 * a.cache.Hkv + (a.q ? a.Hq : 0), D = a.cache.D;
+    const int lane = threadIdx.x & 31, Hkv = a.cache.Hkv, tasks = 2 * Hkv + (a.q ? a.Hq : 0), groups = (tasks + PER - 1) / PER, D = a.cache.D, R = p.pairs.R, half = R / 2;
     const int64_t item = (int64_t)blockIdx.x * ONE_WARPS + (threadIdx.x >> 5);
-    const int64_t seq = item / tasks;
+    const int64_t seq = item / groups;
     if (seq >= a.N) return;
-    const int i = (int)seq, task = (int)(item - seq * tasks);
+    const int i = (int)seq, task0 = (int)(item - seq * groups) * PER;
     if (a.keep && !a.keep[i]) return;
-    // keys, then values, then queries
-    const bool value = task >= a.cache.Hkv && task < 2 * a.cache.Hkv, query = task >= 2 * a.cache.Hkv;
-    const int h = query ? task - 2 * a.cache.Hkv : value ? task - a.cache.Hkv : task;
-    const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(query ? a.q : value ? a.v : a.k) + (query ? a.q_stride : value ? a.v_stride : a.k_stride) * i + (int64_t)h * D;
     const int d0 = lane * 4;
-    float y[4] = {0.f, 0.f, 0.f, 0.f};
-    if (d0 < D) chunk_to_floats<4>(*reinterpret_cast<const uint2*>(x + d0), y);
-    float partner[4];
-    bool turns[4];
-    const int R = value ? 0 : p.pairs.R;
+    const bool interleaved = p.pairs.interleaved;
+    uint2 raw[PER];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int d = d0 + j;
-        turns[j] = d < R;
-        partner[j] = turns[j] ? __bfloat162float(x[p.pairs.interleaved ? d ^ 1 : d < R / 2 ? d + R / 2 : d - R / 2]) : 0.f;
+    for (int k = 0; k < PER; ++k) {
+        const int task = task0 + k;
+        const bool value = task >= Hkv && task < 2 * Hkv, query = task >= 2 * Hkv;
+        const int h = query ? task - 2 * Hkv : value ? task - Hkv : task;
+        const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(query ? a.q : value ? a.v : a.k) + (query ? a.q_stride : value ? a.v_stride : a.k_stride) * i + (int64_t)h * D;
+        raw[k] = task < tasks && d0 < D ? *reinterpret_cast<const uint2*>(x + d0) : make_uint2(0u, 0u);
     }
     bool bad = false;
     int64_t start;
     int len, page = 0;
     bool ok = append_start(a, i, 1, start, len, bad);
     const int64_t position = start + append_offset(a, i);
-    if (ok && !query) ok = append_page(a, i, start / a.cache.page, page, bad);
+    if (ok && task0 < 2 * Hkv) ok = append_page(a, i, start / a.cache.page, page, bad);
     if (bad && lane == 0) atomicOr(p.status, ARROL_DEV_BAD_INDEX);
     if (!ok) return;
     const int slot = (int)(start % a.cache.page);
-    float* const scale = query ? nullptr : value ? a.cache.v_scale + page * a.cache.v_scale_stride + h : a.cache.k_scale + page * a.cache.k_scale_stride + h;
-    const float old = query || slot == 0 ? 0.f : *scale;
+    float* scale[PER];
+    float old[PER];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (turns[j]) {
-            const int d = d0 + j;
-            const bool first = p.pairs.interleaved ? (d & 1) == 0 : d < R / 2;
-            const float2 cs = rotary_cos_sin(p.pairs, p.pairs.interleaved ? d >> 1 : first ? d : d - R / 2, position);
-            y[j] = first ? rotary_first(y[j], partner[j], cs) : rotary_second(partner[j], y[j], cs);
-        }
-    __syncwarp();                                            // in place: every lane has read its partners
-    if (query || (!value && a.k_out)) {
-        __nv_bfloat16* to = query ? static_cast<__nv_bfloat16*>(a.q_out) + a.q_out_stride * i : static_cast<__nv_bfloat16*>(a.k_out) + a.k_out_stride * i;
-        if (d0 < D) *reinterpret_cast<uint2*>(to + (int64_t)h * D + d0) = floats_to_chunk<4>(y);
+    for (int k = 0; k < PER; ++k) {
+        const int task = task0 + k;
+        scale[k] = task < Hkv ? a.cache.k_scale + page * a.cache.k_scale_stride + task : a.cache.v_scale + page * a.cache.v_scale_stride + (task - Hkv);
+        old[k] = task < 2 * Hkv && slot ? *scale[k] : 0.f;
     }
-    if (query) return;
-    float amax = 0.f;
+    float2 cs[4];
+    const bool all_values = task0 >= Hkv && task0 + PER <= 2 * Hkv;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) amax = finite_max(amax, y[j]);
+    for (int j = 0; j < 4; ++j) {
+        const int d = d0 + j;
+        cs[j] = make_float2(1.f, 0.f);
+        if (d < R && !all_values) cs[j] = rotary_cos_sin(p.pairs, interleaved ? d >> 1 : d < half ? d : d - half, position);
+    }
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
-    bool grows;
-    const int e = append_exponent(amax, slot, old, grows);
-    uint8_t* const codes = static_cast<uint8_t*>(value ? a.cache.v_cache : a.cache.k_cache) + page * (value ? a.cache.v_page_stride : a.cache.k_page_stride) +
-                           (int64_t)h * a.cache.page * D;
-    if (grows) append_rescale(codes, slot * D, old * cache_power(-e), lane, 32);
-    const float by = cache_power(-e);
-    if (d0 < D)
-        *reinterpret_cast<uint32_t*>(codes + slot * D + d0) = e4m3_pair(y[0] * by, y[1] * by) | (uint32_t)e4m3_pair(y[2] * by, y[3] * by) << 16;
-    if (lane == 0 && (slot == 0 || grows)) *scale = cache_power(e);
+    for (int k = 0; k < PER; ++k) {
+        const int task = task0 + k;
+        if (task >= tasks) break;
+        const bool value = task >= Hkv && task < 2 * Hkv, query = task >= 2 * Hkv;
+        const int h = query ? task - 2 * Hkv : value ? task - Hkv : task;
+        float y[4];
+        chunk_to_floats<4>(raw[k], y);
+        if (!value && R > 0) {
+            // the partners lie in other lanes, but for pairs of neighbours
+            float partner[4];
+            if (interleaved) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) partner[j] = y[j ^ 1];
+            } else if (half % 4 == 0) {
+                const int from = d0 < half ? lane + half / 4 : lane - half / 4;
+                const uint2 other = make_uint2(__shfl_sync(0xffffffffu, raw[k].x, from & 31), __shfl_sync(0xffffffffu, raw[k].y, from & 31));
+                chunk_to_floats<4>(other, partner);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int d = d0 + j, of = d < half ? d + half : d - half;
+                    const uint32_t lo = __shfl_sync(0xffffffffu, raw[k].x, (of >> 2) & 31), hi = __shfl_sync(0xffffffffu, raw[k].y, (of >> 2) & 31), w = of & 2 ? hi : lo;
+                    partner[j] = __uint_as_float(of & 1 ? w & 0xFFFF0000u : w << 16);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (d0 + j < R) {
+                    const bool first = interleaved ? (j & 1) == 0 : d0 + j < half;
+                    y[j] = first ? rotary_first(y[j], partner[j], cs[j]) : rotary_second(partner[j], y[j], cs[j]);
+                }
+        }
+        if (query || (!value && a.k_out)) {
+            __nv_bfloat16* to = query ? static_cast<__nv_bfloat16*>(a.q_out) + a.q_out_stride * i : static_cast<__nv_bfloat16*>(a.k_out) + a.k_out_stride * i;
+            if (d0 < D) *reinterpret_cast<uint2*>(to + (int64_t)h * D + d0) = floats_to_chunk<4>(y);
+        }
+        if (query) continue;
+        float amax = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) amax = finite_max(amax, y[j]);
+        amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
+        bool grows;
+        const int e = append_exponent(amax, slot, old[k], grows);
+        uint8_t* const codes = static_cast<uint8_t*>(value ? a.cache.v_cache : a.cache.k_cache) + page * (value ? a.cache.v_page_stride : a.cache.k_page_stride) +
+                               (int64_t)h * a.cache.page * D;
+        if (grows) append_rescale(codes, slot * D, old[k] * cache_power(-e), lane, 32);
+        const float by = cache_power(-e);
+        if (d0 < D)
+            *reinterpret_cast<uint32_t*>(codes + slot * D + d0) = e4m3_pair(y[0] * by, y[1] * by) | (uint32_t)e4m3_pair(y[2] * by, y[3] * by) << 16;
+        if (lane == 0 && (slot == 0 || grows)) *scale[k] = cache_power(e);
+    }
 }
 
 // ---- runs of tokens: a block per page that gets some, for keys and queries or for values (and part of the heads); a thread has one unit of one token, its angles in
@@ -380,9 +416,11 @@ extern "C" int arrol_cache_append(arrol_ctx* ctx, const arrol_cache_append_args*
     ArrolDeviceGuard guard(ctx->device);
     if (!guard.ok) return ARROL_ERR_CUDA;
     if (!a->cu_new) {
-        const int64_t warps = (int64_t)a->N * (2 * Hkv + (a->q ? a->Hq : 0));
-        if ((warps + ONE_WARPS - 1) / ONE_WARPS >= ((int64_t)1 << 31)) return ARROL_ERR_UNSUPPORTED;
-        ARROL_CUDA_OK(arrol_launch_pdl(append_one_kernel, dim3((unsigned)((warps + ONE_WARPS - 1) / ONE_WARPS)), dim3(32 * ONE_WARPS), 0, (cudaStream_t)stream, p));
+        const int tasks = 2 * Hkv + (a->q ? a->Hq : 0);
+        const int per = (int64_t)a->N * tasks > (int64_t)ctx->sm_count * 64 ? 4 : 1;
+        const int64_t blocks = ((int64_t)a->N * ((tasks + per - 1) / per) + ONE_WARPS - 1) / ONE_WARPS;
+        if (blocks >= ((int64_t)1 << 31)) return ARROL_ERR_UNSUPPORTED;
+        ARROL_CUDA_OK(arrol_launch_pdl(per == 4 ? append_one_kernel<4> : append_one_kernel<1>, dim3((unsigned)blocks), dim3(32 * ONE_WARPS), 0, (cudaStream_t)stream, p));
     } else {
         // The widest chunks that the sizes allow: 4 numbers and twice the threads took 200 to 247 us where this took 143 for 38,000 prompt tokens.
         const int V = rotary_vector(D, a->R);
