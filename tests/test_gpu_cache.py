@@ -491,6 +491,17 @@ def test_append_matches_the_definition(ctx, lengths, new, prompts, G, Hq, Hkv, D
     p.check(p.run(ctx))
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,n,interleaved", [(9, 3, 32, 6, False), (10, 5, 48, 48, False), (16, 2, 16, 10, True), (12, 1, 128, 0, False), (14, 7, 80, 36, False)])
+def test_one_token_each_of_many_rollouts(ctx, Hq, Hkv, D, n, interleaved):
+    """More heads than there are places for warps: keys, values and queries of a rollout meet in one warp, and some of its places stay empty."""
+    N = -(-10000 // (Hq + 2 * Hkv) // 2) * 2
+    g = torch.Generator().manual_seed(N)
+    lengths = torch.randint(1, 12, (N,), generator=g).tolist()
+    keep = (torch.rand(N, generator=g) < 0.7).int().tolist()
+    p = Append(lengths, None, [3, 1000], N // 2, Hq, Hkv, D, n, 16, keep, seed=N, interleaved=interleaved, by=3.0)
+    p.check(p.run(ctx))
+
+
 @pytest.mark.parametrize("new", [None, [1, 1, 1], [9, 20, 3]])
 @pytest.mark.parametrize("by", [300.0, 1e-3, 1e30, 1e-32, 0.0])
 def test_scales_grow_and_do_not_shrink(ctx, by, new):
