@@ -9,7 +9,7 @@
 
 namespace {
 
-// Two heads loaded at once and eight blocks of 128 threads an SM: 15,400 tokens of 24 heads of 80 22 us, 138,000 of 24 heads of 128 259.  Four at once take 80 registers:
+// Two heads loaded at once and eight blocks of 128 threads an SM: 15,400 tokens of 24 heads of 80 22 to 26 us, 138,000 of 24 heads of 128 259.  Four at once take 80 registers:
 // six blocks, 27 and 255 (one of 256 threads at 88 registers 29 and 264).
 constexpr int ROT_THREADS = 128, ROT_PER_SM = 8;
 constexpr int ROT_AT_ONCE = 2;
