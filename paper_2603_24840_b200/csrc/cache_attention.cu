@@ -9,7 +9,8 @@
 // The products are m16n8k16 mma.sync in fp16, transposed: tokens (of S^T = K Q^T) and dimensions (of O^T = V^T P^T) are the sixteen rows, query rows the eight columns, so that
 // eight query heads waste nothing.  e4m3 numbers widen to fp16 exactly, two an instruction, and q, scaled by a power of two for each row, is exact in fp16 too (bf16 has
 // fewer bits; what is below 2^-27 of the row's largest is rounded at 2^-39 of it).  Probabilities are rounded to fp16, which holds a long tail of keys at 2^-20 of the
-// largest one's weight as well as that one; its smallest steps are 2^-31 of that weight.  Scales of pages and heads join the scores and the probabilities.  (Products of
+// largest one's weight as well as that one; its smallest steps are 2^-31 of that weight.  Scales of pages and heads join the scores and the probabilities, the latter in front of
+// their rounding, in units of the largest: where they lie more than 2^8 apart small values would be rounded away, and the merge computes such rows anew in fp32.  (Products of
 // e4m3 operands by mma.sync are widened by the compiler, at each use: 12 instructions for one.)
 //
 // Work is cut without a plan: the lengths make a line of pieces and units' setups by their cost, every block takes an equal part of it, and each finds its own by a scan over
@@ -41,6 +42,9 @@ constexpr LineCosts CA_COSTS_COARSE = {13, 7, 1, 1};
 constexpr int CA_SCANNED = 768;                    // entries that a block keeps in shared memory between the two passes of its scan
 constexpr float CA_RESCALE_AT = 8.0f;              // the running maximum follows once it is 2^8 behind
 constexpr float CA_P_SCALE = 128.0f;               // probabilities up to 2^8 times 2^7 stay below fp16's largest
+// Scales of values join the probabilities down to 2^-8 of the largest, so that fp16 holds probabilities to half a step from 2^-13 on whatever their pages' scales.  A record with
+// others is marked, by its sum's sign, and the merge computes its rows anew (row_apart).
+constexpr float CA_NEAR = 0.00390625f;
 
 // Tokens that one set of query rows has in common: a rollout's own (rows = Hq / Hkv), or a prompt with the rows of some of its live rollouts.
 struct alignas(16) CacheEntry {
@@ -51,7 +55,7 @@ struct CacheWorkspace {
     int2* owners;              // [entries][Hkv]: the first and the last block (warp) that has some of the unit
     CacheEntry* shared;        // entries with pieces, in order
     CacheEntry* single;
-    float2* ml;                // per record row: reference (of scores log2 e), sum
+    float2* ml;                // per record row: reference (of scores log2 e), sum, negative where the row is computed anew
     float* o;                  // [record rows][D]
     int64_t rows_own, rows_prompt, rows_shared;    // record rows of the three kinds, one behind the other
     size_t bytes;
@@ -354,6 +358,9 @@ struct Fetch {
             info.scales[1] = c.k_scale[pages.second * c.k_scale_stride + info.head];
             info.scales[3] = c.v_scale[pages.second * c.v_scale_stride + info.head];
         }
+        // values that are not there have the others' scale, not one of their own
+        if (pages.second < 0) info.scales[3] = info.scales[2];
+        if (pages.first < 0) info.scales[2] = info.scales[3];
     }
     // The copies; the arrival that lets the stage be read is the caller's.
     template <int DP>
@@ -383,7 +390,7 @@ struct RowTile {
     uint32_t q[C::CHUNKS][2][2];      // per 16 dimensions and eight rows: row g's dimensions 4 t .. 4 t + 3
     float by[2][2];                   // what a product's sum times the key's scale is multiplied by
     float o[C::CHUNKS][2][4], m[2][2], l[2][2];
-    float v_scale;                    // largest scale of the values so far: o is in units of it / CA_P_SCALE
+    float v_scale, v_least;           // largest scale of the values so far, o is in units of it / CA_P_SCALE; the smallest
 
     // `row`: this lane's row g, or null; r: of the first or the second eight
     __device__ __forceinline__ void load(const CacheParams& p, int lane, const __nv_bfloat16* row, int r) {
@@ -424,6 +431,7 @@ struct RowTile {
         m[r][0] = m[r][1] = -INFINITY;
         l[r][0] = l[r][1] = 0.f;
         v_scale = 0.f;
+        v_least = INFINITY;
     }
 
     // A piece with at least one token, ROWS x 8 query rows.
@@ -489,6 +497,7 @@ struct RowTile {
                 behind |= mx[r][b] > m[r][b] + CA_RESCALE_AT;
             }
         const float vs = fmaxf(scales.z, scales.w);
+        v_least = fminf(v_least, fminf(scales.z, scales.w));
         if (__builtin_expect(__any_sync(0xffffffffu, behind || vs > v_scale), 0)) {
             const float shrink = vs > v_scale ? v_scale / vs : 1.f;
             v_scale = fmaxf(vs, v_scale);
@@ -560,7 +569,7 @@ struct RowTile {
                             out[c * 16] = o[c][r][b] * unit;
                             out[c * 16 + 8] = o[c][r][2 + b] * unit;
                         }
-                    if (g == 0) p.w.ml[at + row] = make_float2(m[r][b], sum);
+                    if (g == 0) p.w.ml[at + row] = make_float2(m[r][b], v_least < v_scale * CA_NEAR ? -sum : sum);      // marked
                 }
             }
     }
@@ -877,6 +886,7 @@ struct Merged {
     static constexpr int AT_ONCE = 8;
     float top, total;
     float4 sum;
+    float least;               // of the records' sums: below 0 where one is marked
     __device__ __forceinline__ void add(const float2 (&x)[AT_ONCE], const float4 (&v)[AT_ONCE]) {
         float next = top;
 #pragma unroll
@@ -888,19 +898,149 @@ struct Merged {
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             const float by = x[k].x == -INFINITY ? (x[k].y == 0.f ? 0.f : 1.f) : ex2_approx(x[k].x - top);      // a NaN without a maximum stays one
+            least = fminf(least, x[k].y);
             total += by * x[k].y;
             sum.x += by * v[k].x; sum.y += by * v[k].y; sum.z += by * v[k].z; sum.w += by * v[k].w;
         }
     }
+    // `any`: there are keys
+    __device__ __forceinline__ void write(const arrol_cache_attention_args& a, int64_t row, int i, int hq, int lane, bool any) const {
+        const int D = a.cache.D, d = lane * 4;
+        const float inv = any ? 1.f / total : 0.f;
+        if (d < D) {
+            uint2 w = make_uint2(0u, 0u);
+            if (any) {
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.x) : "f"(sum.y * inv), "f"(sum.x * inv));
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.y) : "f"(sum.w * inv), "f"(sum.z * inv));
+            }
+            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + i * a.o_stride + (int64_t)hq * D + d) = w;
+        }
+        if (lane == 0 && a.lse) a.lse[row] = any ? (top + log2f(total)) * LN2 : -INFINITY;
+    }
 };
 
+constexpr int MERGE_THREADS = 256, MERGE_WARPS = MERGE_THREADS / 32;
+struct ApartShared {
+    int apart[MERGE_THREADS / 16];
+    float q[CACHE_MAX_D], m[MERGE_WARPS], l[MERGE_WARPS];
+    float4 o[MERGE_WARPS][32];
+};
+// A row from the pages themselves, all in fp32, by a whole block, for rows with a marked record: 32 tokens a warp, a lane a token for the scores, four dimensions a lane for the values.
+// Slow (about 10 us a row for every 500 tokens, eight rows a block one behind another), for caches whose values hardly occur.  Forms for such pieces among the products (sums of
+// their own, joined in fp32; a unit that follows the scales; records that are added to) took 5 to 60 % from all other calls, by instructions and registers alone; this takes 1 to 4.
+__device__ __noinline__ void row_apart(const CacheParams& p, int64_t row, ApartShared& sm) {
+    const arrol_cache_attention_args& a = p.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.cache.D, d = lane * 4;
+    const int i = (int)(row / a.Hq), hq = (int)(row - (int64_t)i * a.Hq), h = hq / p.ratio;
+    // the query as in RowTile::load
+    uint2 raw = make_uint2(0u, 0u);
+    if (d < D) raw = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.q) + i * a.q_stride + (int64_t)hq * D + d);
+    const float x[4] = {__uint_as_float(raw.x << 16), __uint_as_float(raw.x & 0xFFFF0000u), __uint_as_float(raw.y << 16), __uint_as_float(raw.y & 0xFFFF0000u)};
+    float most = 0.f, odd = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { most = finite_max(most, x[j]); odd += x[j] - x[j]; }
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) { most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s)); odd += __shfl_xor_sync(0xffffffffu, odd, s); }
+    const int exponent = cache_exponent(most) - 5;
+    const float by = cache_power(exponent) * p.scale_log2 + odd;
+    if (warp == 0 && d < D)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sm.q[d + j] = x[j] * cache_power(-exponent);
+    __syncthreads();
+    bool bad = false;
+    const int own = cache_tokens(a.lengths, i, a.table_pages, a.cache.page, bad);
+    const int prompt = p.prompts ? cache_tokens(a.prompt_lengths, i / a.G, a.prompt_table_pages, a.cache.page, bad) : 0;
+    const uint8_t* const k_cache = static_cast<const uint8_t*>(a.cache.k_cache);
+    const uint8_t* const v_cache = static_cast<const uint8_t*>(a.cache.v_cache);
+    const int64_t tokens = (int64_t)prompt + own;
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int64_t t0 = warp * 32; t0 < tokens; t0 += MERGE_THREADS) {
+        const int64_t token = t0 + lane;
+        int page = -1, slot = 0;
+        if (token < tokens) {
+            const bool shared = token < prompt;
+            const int at = (int)(shared ? token : token - prompt);
+            page = shared ? a.prompt_table[(int64_t)(i / a.G) * a.prompt_table_stride + (at >> p.page_shift)] : a.page_table[(int64_t)i * a.table_stride + (at >> p.page_shift)];
+            slot = at & (a.cache.page - 1);
+            if (page >= a.cache.pages) page = -1;
+        }
+        float z = -INFINITY, vs = 0.f;
+        const int64_t inside = ((int64_t)h * a.cache.page + slot) * D;
+        if (page >= 0) {
+            const uint8_t* const key = k_cache + page * a.cache.k_page_stride + inside;
+            float dot = 0.f;
+#pragma unroll 4
+            for (int c = 0; c < D; c += 16) {
+                const uint4 w = *reinterpret_cast<const uint4*>(key + c);
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 lo = e4m3_pair_to_float((uint16_t)u[j]), hi = e4m3_pair_to_float((uint16_t)(u[j] >> 16));
+                    const float4 q = *reinterpret_cast<const float4*>(&sm.q[c + 4 * j]);
+                    dot = fmaf(lo.x, q.x, fmaf(lo.y, q.y, fmaf(hi.x, q.z, fmaf(hi.y, q.w, dot))));
+                }
+            }
+            z = dot * (by * a.cache.k_scale[page * a.cache.k_scale_stride + h]);
+            vs = a.cache.v_scale[page * a.cache.v_scale_stride + h];
+        }
+        float top = fmaxf(m, z);                              // a NaN is passed over
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+        const float e = ex2_approx(z - (top == -INFINITY ? 0.f : top)), fall = top == m ? 1.f : ex2_approx(m - top), weight = e * vs;
+        m = top;
+        l = fmaf(l, fall, e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] *= fall;
+        const uint64_t value = reinterpret_cast<uint64_t>(v_cache) + (page >= 0 ? page * a.cache.v_page_stride + inside : 0);
+        const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
+#pragma unroll 1
+        for (int t = 0; t < 32 && there >> t; t += 8) {
+            uint32_t u[8];
+            float w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                w[j] = __shfl_sync(0xffffffffu, weight, t + j);
+                const uint64_t at = __shfl_sync(0xffffffffu, value, t + j);
+                u[j] = d < D && (there >> (t + j) & 1u) ? *reinterpret_cast<const uint32_t*>(at + d) : 0u;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float2 lo = e4m3_pair_to_float((uint16_t)u[j]), hi = e4m3_pair_to_float((uint16_t)(u[j] >> 16));
+                o[0] = fmaf(w[j], lo.x, o[0]); o[1] = fmaf(w[j], lo.y, o[1]); o[2] = fmaf(w[j], hi.x, o[2]); o[3] = fmaf(w[j], hi.y, o[3]);
+            }
+        }
+    }
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+    if (lane == 0) { sm.m[warp] = m; sm.l[warp] = l; }
+    sm.o[warp][lane] = make_float4(o[0], o[1], o[2], o[3]);
+    __syncthreads();
+    if (warp == 0) {
+        float top = -INFINITY, total = 0.f;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int w = 0; w < MERGE_WARPS; ++w) top = fmaxf(top, sm.m[w]);
+#pragma unroll 1
+        for (int w = 0; w < MERGE_WARPS; ++w) {
+            const float by = sm.m[w] == -INFINITY ? (sm.l[w] == 0.f ? 0.f : 1.f) : ex2_approx(sm.m[w] - top);
+            const float4 v = sm.o[w][lane];
+            total += by * sm.l[w];
+            sum.x += by * v.x; sum.y += by * v.y; sum.z += by * v.z; sum.w += by * v.w;
+        }
+        const Merged all = {top, total, sum, 0.f};
+        all.write(a, row, i, hq, lane, true);
+    }
+    __syncthreads();
+}
+
 template <int LANES>
-__global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
+__global__ void __launch_bounds__(MERGE_THREADS, 3) cache_merge_kernel(const __grid_constant__ CacheParams p) {
     pdl_launch_dependents();
     pdl_wait();
     const arrol_cache_attention_args& a = p.a;
     const int lane = threadIdx.x % LANES, part = (threadIdx.x & 31) - lane, D = a.cache.D, Hkv = a.cache.Hkv, d = lane * 4;
-    const int64_t rows = (int64_t)a.N * a.Hq, asked = (blockIdx.x * (int64_t)256 + threadIdx.x) / LANES, row = asked < rows ? asked : rows - 1;      // both halves go on together
+    const int64_t rows = (int64_t)a.N * a.Hq, asked = (blockIdx.x * (int64_t)MERGE_THREADS + threadIdx.x) / LANES, row = asked < rows ? asked : rows - 1;      // both halves go on together
     const int i = (int)(row / a.Hq), hq = (int)(row - (int64_t)i * a.Hq), h = hq / p.ratio, r = hq - h * p.ratio;
     const int2* owners = pdl_acquire(p.w.owners);
     const float2* ml = pdl_acquire(p.w.ml);
@@ -926,8 +1066,8 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
         prompt_row = before % p.group * p.ratio + r;
         shared = owners[(int64_t)entry * Hkv + h];
     }
-    if (asked >= rows || (a.keep && !a.keep[i])) return;
-    Merged m = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    const bool wanted = asked < rows && (!a.keep || a.keep[i]);
+    Merged m = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}, 0.f};
     // The records of a unit: `count` of the blocks (warps) that have some of it, `step` rows apart; of shared units of up to 32 rows two each, CA_ROWS / 2 apart.
     struct Records { int64_t first; int count, step, twice; };
     const int64_t own_number = (int64_t)i * Hkv + h, prompt_number = (int64_t)entry * Hkv + h, shared_rows = p.w.rows_own + p.w.rows_prompt;
@@ -940,9 +1080,9 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
         return Records{first + (int64_t)from * step, (to - from + 1) << twice, step, twice};
     };
     Records a_prompt = {0, 0, 0, 0}, an_own = {0, 0, 0, 0};
-    if (prompt_tokens > 0)
+    if (wanted && prompt_tokens > 0)
         a_prompt = records(prompt_rows, shared, shared_rows + prompt_number * CA_ROWS + prompt_row, p.w.rows_own + prompt_number * CA_ALONE + prompt_row, CA_ALONE);
-    if (own_tokens > 0) an_own = records(p.ratio, own, shared_rows + ((int64_t)p.prompts * Hkv + own_number) * CA_ROWS + r, own_number * p.ratio + r, p.ratio);
+    if (wanted && own_tokens > 0) an_own = records(p.ratio, own, shared_rows + ((int64_t)p.prompts * Hkv + own_number) * CA_ROWS + r, own_number * p.ratio + r, p.ratio);
     for (int w = 0; w < a_prompt.count + an_own.count; w += Merged::AT_ONCE) {
         float2 x[Merged::AT_ONCE];
         float4 v[Merged::AT_ONCE];
@@ -961,17 +1101,15 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(const CacheParams p) {
         }
         m.add(x, v);
     }
-    const bool any = prompt_tokens > 0 || own_tokens > 0;     // none: no key
-    const float inv = any ? 1.f / m.total : 0.f;
-    if (d < D) {
-        uint2 w = make_uint2(0u, 0u);
-        if (any) {
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.x) : "f"(m.sum.y * inv), "f"(m.sum.x * inv));
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.y) : "f"(m.sum.w * inv), "f"(m.sum.z * inv));
-        }
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + i * a.o_stride + (int64_t)hq * D + d) = w;
+    if (wanted && !(m.least < 0.f)) m.write(a, row, i, hq, lane, prompt_tokens > 0 || own_tokens > 0);
+    __shared__ ApartShared sm;
+    if (__builtin_expect(__syncthreads_or(wanted && m.least < 0.f), 0)) {
+        if (lane == 0) sm.apart[threadIdx.x / LANES] = wanted && m.least < 0.f;
+        __syncthreads();
+#pragma unroll 1
+        for (int x = 0; x < MERGE_THREADS / LANES; ++x)
+            if (sm.apart[x]) row_apart(p, (int64_t)blockIdx.x * (MERGE_THREADS / LANES) + x, sm);
     }
-    if (lane == 0 && a.lse) a.lse[row] = any ? (m.top + log2f(m.total)) * LN2 : -INFINITY;
 }
 
 // [pages, Hkv, page, D] numbers as boxes of up to 32 tokens x DP bytes of one page and head, rows of DP bytes in shared memory, swizzled over as many; dimensions past D are zeros.
@@ -1000,7 +1138,7 @@ int launch_cache_attention(arrol_ctx* ctx, const CacheParams& p, cudaStream_t s)
         return ARROL_ERR_CUDA;
     ARROL_CUDA_OK(arrol_launch_pdl(cache_units_kernel<DP>, dim3((unsigned)p.grid), dim3(CA_THREADS), C::SMEM, s, k, v, p));
     constexpr int LANES = DP / 4;
-    ARROL_CUDA_OK(arrol_launch_pdl(cache_merge_kernel<LANES>, dim3((unsigned)(((int64_t)p.a.N * p.a.Hq * LANES + 255) / 256)), dim3(256), 0, s, p));
+    ARROL_CUDA_OK(arrol_launch_pdl(cache_merge_kernel<LANES>, dim3((unsigned)(((int64_t)p.a.N * p.a.Hq * LANES + MERGE_THREADS - 1) / MERGE_THREADS)), dim3(MERGE_THREADS), 0, s, p));
     ctx->launches += 2;
     return ARROL_OK;
 }

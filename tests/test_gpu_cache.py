@@ -161,6 +161,67 @@ def test_scales_that_differ_from_page_to_page(ctx, D, Hq, Hkv):
     p.check(*p.run(ctx))
 
 
+WIDE = [
+    # lengths, prompts, G, Hq, Hkv, D, page: a few query rows a key head, 9 to 16, 17 to 32, 33 to 64; pages of half a piece, of one, of several
+    ([300, 33, 700], None, 1, 4, 2, 64, 16),
+    ([300, 33, 700], None, 1, 8, 1, 128, 32),
+    ([1500, 20], None, 1, 12, 1, 128, 16),
+    ([300, 150], None, 1, 20, 1, 64, 16),
+    ([40, 100, 1, 7], [600, 90], 2, 16, 1, 128, 64),
+    ([40, 100, 1, 7], [600], 4, 16, 1, 64, 16),
+    ([40, 100, 1], [600], 3, 16, 1, 128, 128),
+]
+
+
+def _weigh(p, page, nats):
+    """All tokens of this page score so much more than others do, whose keys have 0 in that dimension; queries have sqrt(D) there."""
+    codes = p.pool.k.view(torch.uint8)
+    codes[page] = 0
+    codes[page, :, :, 1] = torch.tensor(nats * 4.0, device="cuda").to(F8).view(torch.uint8)
+    p.pool.ks[page] = 0.25
+
+
+@pytest.mark.parametrize("place", [0.0, 0.5, 1.0])
+@pytest.mark.parametrize("lengths,prompts,G,Hq,Hkv,D,page", WIDE)
+def test_a_page_with_values_far_larger_than_the_others(ctx, lengths, prompts, G, Hq, Hkv, D, page, place):
+    """Large in one dimension and zero in the others, first, in the middle and last: it carries that dimension, or nothing of it, and the other pages the rest.  Its tokens weigh 2^12
+    to 2^-58 of the others'."""
+    p = Attend(lengths, prompts, G, Hq, Hkv, D, page, seed=30, q_scale=0.25, spread=0.5)
+    p.q[..., 1] = math.sqrt(D)
+    p.pool.k.view(torch.uint8)[..., 1] = 0
+    tables = [(p.table, lengths)] + ([(p.p_table, prompts)] if prompts else [])
+    far = [int(t[i, int(place * (-(-n // page) - 1))]) for t, counts in tables for i, n in enumerate(counts) if n > page]
+    far = far[:1] if prompts is None else far[-1:]
+    codes, scale = p.pool.v.view(torch.uint8), p.pool.vs[far].clone()
+    codes[far, :, :, :3] = 0
+    codes[far, :, :, 4:] = 0
+    for weight in (0, 8, 12, -58):
+        for x in far:
+            _weigh(p, x, weight * math.log(2))
+        for ratio in (4, 5, 8, 12, 16, 20, 26, 34, 60, 100, -4, -5, -9, -60, -90):
+            p.pool.vs[far] = scale * 2.0 ** ratio
+            p.check(*p.run(ctx))
+
+
+@pytest.mark.parametrize("most", [3, 8, 30, 90])
+@pytest.mark.parametrize("lengths,prompts,G,Hq,Hkv,D,page", WIDE)
+def test_pages_of_values_of_all_sizes(ctx, lengths, prompts, G, Hq, Hkv, D, page, most):
+    """Every page has a scale of its own, up to 2^most either way, an eighth of the dimensions, and scores 2^-6 to 2^6 of the others'."""
+    p = Attend(lengths, prompts, G, Hq, Hkv, D, page, seed=31 + most, q_scale=0.25, spread=0.5)
+    p.q[..., 1] = math.sqrt(D)
+    g = p.pool.g
+    used = torch.cat([t[t >= 0] for t in [p.table] + ([p.p_table] if prompts else [])]).long()
+    codes = p.pool.k.view(torch.uint8)
+    codes[..., 1] = (torch.randint(-6, 7, (p.pool.pages, 1, 1), generator=g, device="cuda") * (math.log(2) * 2.0 ** 6)).expand(-1, p.pool.Hkv, page).to(F8).view(torch.uint8)
+    p.pool.ks[used] = 2.0 ** -6
+    p.pool.vs[used] = torch.exp2(torch.randint(-most, most + 1, (len(used), p.pool.Hkv), generator=g, device="cuda").float())
+    p.pool.v.view(torch.uint8)[torch.rand(p.pool.pages, p.pool.Hkv, 1, D, generator=g, device="cuda").expand(p.pool.v.shape) > 0.125] = 0
+    p.check(*p.run(ctx))
+    p.pool.v.view(torch.uint8)[used[::3]] = 0          # zeros and nothing else: the least scale
+    p.pool.vs[used[::3]] = 2.0 ** -100
+    p.check(*p.run(ctx))
+
+
 def test_a_long_tail_behind_one_key_that_takes_most(ctx):
     """Eight thousand keys at 2^-18 of the first's weight carry a thirtieth of the sum: probabilities of four or five bits would lose them."""
     for D, Hq, Hkv in ((64, 4, 1), (128, 32, 1)):
