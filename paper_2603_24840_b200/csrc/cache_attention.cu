@@ -852,6 +852,7 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
                     const uint32_t st = n % C::STAGES, parity = (n / C::STAGES) & 1u;
                     ok = mbar_wait_warp(&sm.full[st][lane % CA_WARPS], parity, abort_flag);       // all four at once, a lane each
                     if (!ok) break;
+                    __syncwarp();                             // the vote orders nothing: each lane has learnt of one part only
                     for (int w = share; w < CA_WARPS; w += CA_WARPS / row_tiles)
                         if (sm.info[st][w].there > 0 && left > 0) tile.template piece<2>(stage(n, w), sm.info[st][w], lane);
                     const bool last = sm.info[st][warp].flags & PIECE_LAST;

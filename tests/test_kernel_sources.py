@@ -113,3 +113,14 @@ def test_stages_read_by_warps_are_handed_back_behind_a_proxy_fence():
             found += 1
             assert code[:m.start()].endswith("fence_proxy_async_smem(); __syncwarp(); "), os.path.basename(path)
     assert found == 1
+
+
+def test_lanes_that_wait_for_different_barriers_meet_before_they_read():
+    """A vote orders no memory: what one lane has learnt from its barrier another may read only behind a __syncwarp()."""
+    found = 0
+    for path in SOURCES:
+        code = re.sub(r"\s+", " ", _code(path))
+        for m in re.finditer(r"mbar_wait_warp\(&[^;]*?\blane\b[^;]*; if \(!ok\) [^;]*; (\S+)", code):
+            found += 1
+            assert m.group(1) == "__syncwarp();", os.path.basename(path)
+    assert found == 1
