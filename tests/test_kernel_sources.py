@@ -124,3 +124,11 @@ def test_lanes_that_wait_for_different_barriers_meet_before_they_read():
             found += 1
             assert m.group(1) == "__syncwarp();", os.path.basename(path)
     assert found == 1
+
+
+def test_query_rows_that_a_tile_computes_are_loaded():
+    """Shared pieces are computed for two eights of query rows: a tile without rows in the second has zeros there, not what was left from another unit."""
+    code = re.sub(r"\s+", " ", _code(os.path.join(CSRC, "cache_attention.cu")))
+    assert "if (left > 8) tile.load(p, lane, query_row(p, e, sm.live[warp], row0 + 8 + (lane >> 2)), 1);" in code
+    assert "if (shared) { if (left <= 8) tile.clear(); for (;;)" in code
+    assert len(re.findall(r"\.template piece<", code)) == 2 and "} else if (left > 8) { single_pieces(std::integral_constant<int, 2>()); } else {" in code
