@@ -319,21 +319,21 @@ struct alignas(16) PieceInfo {
     float scales[4];               // of the keys of the first and the second 16 tokens (below 0: none there), of the values
     int entry, head, there, flags; // there: tokens from its first one to the entry's end
 };
-// The first and the last of a unit in this block or warp; of the unit; no piece, but the end; query rows from bit 8 on.
-constexpr int PIECE_FIRST = 1, PIECE_LAST = 2, PIECE_BEGIN = 4, PIECE_END = 8, PIECE_NONE = 16, PIECE_ROWS = 8;
+// The last of a unit in this block or warp; the first and the last of the unit; no piece, but the end; query rows from bit 8 on.
+constexpr int PIECE_LAST = 1, PIECE_BEGIN = 2, PIECE_END = 4, PIECE_NONE = 8, PIECE_ROWS = 8;
 
 // A piece on its way: first its page numbers are asked for, then its scales, then its copies.
 struct Fetch {
     PagePair pages;
     int tok;
     PieceInfo info;
-    __device__ __forceinline__ void find(const CacheParams& p, const Cursor& c, int token, bool first) {
+    __device__ __forceinline__ void find(const CacheParams& p, const Cursor& c, int token) {
         tok = token;
         pages = find_pages(p, c, token);
         info.entry = c.e.entry;
         info.head = c.head;
         info.there = c.e.tokens - token;
-        info.flags = (first || c.piece == 0 ? PIECE_FIRST : 0) | (c.piece == 0 ? PIECE_BEGIN : 0) | (c.piece == c.e.pieces - 1 ? PIECE_LAST | PIECE_END : 0) |
+        info.flags = (c.piece == 0 ? PIECE_BEGIN : 0) | (c.piece == c.e.pieces - 1 ? PIECE_LAST | PIECE_END : 0) |
                      (c.is_last() ? PIECE_LAST : 0) | c.e.rows << PIECE_ROWS;
     }
     // pages that are none are reported and left out
@@ -759,7 +759,7 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
             bool there = c.left > 0, more = false;
             bool copied = false;
             if (there) {
-                now.find(p, c, token(), k == 0);
+                now.find(p, c, token());
                 // The very first pieces find their stages free: their copies need not wait for the scales.
                 if (n == 0 && k < C::STAGES) {
                     now.check(p);
@@ -784,7 +784,7 @@ __global__ void __launch_bounds__(CA_THREADS, CacheConf<DP>::PER_SM) cache_units
                     at = 0;
                     c.skip(p, 8, Hkv);
                     more = there && c.left > 0;
-                    if (more) next.find(p, c, token(), false);
+                    if (more) next.find(p, c, token());
                 }
                 if (!__any_sync(0xffffffffu, there)) break;
                 const uint32_t mine = n + k, st = mine % C::STAGES;

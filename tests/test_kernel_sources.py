@@ -132,3 +132,11 @@ def test_query_rows_that_a_tile_computes_are_loaded():
     assert "if (left > 8) tile.load(p, lane, query_row(p, e, sm.live[warp], row0 + 8 + (lane >> 2)), 1);" in code
     assert "if (shared) { if (left <= 8) tile.clear(); for (;;)" in code
     assert len(re.findall(r"\.template piece<", code)) == 2 and "} else if (left > 8) { single_pieces(std::integral_constant<int, 2>()); } else {" in code
+
+
+def test_flags_of_a_piece_are_set_and_read():
+    code = _code(os.path.join(CSRC, "cache_attention.cu"))
+    names = set(re.findall(r"\bPIECE_\w+", code)) - {"PIECE_ROWS"}
+    assert len(names) == 4
+    for name in names:
+        assert re.search(r"flags & %s\b" % name, code), name
