@@ -1178,11 +1178,8 @@ extern "C" int arrol_cache_attention(arrol_ctx* ctx, const arrol_cache_attention
     if (!cache_rows_ok(a->q, a->q_stride, a->Hq, a->cache.D) || !cache_rows_ok(a->o, a->o_stride, a->Hq, a->cache.D) || !a->lengths ||
         (a->table_pages > 0 && !a->page_table))
         return ARROL_ERR_INVALID_ARG;
-    if (!a->workspace || !arrol_aligned(a->workspace, 256)) return ARROL_ERR_WORKSPACE;
     CacheParams p = {};
     p.a = *a;
-    p.w = cache_workspace(a->workspace, ctx->sm_count, a->N, a->P, a->G, a->Hq, a->cache.Hkv, a->cache.D);
-    if (a->workspace_bytes < p.w.bytes) return ARROL_ERR_WORKSPACE;
     p.ratio = a->Hq / a->cache.Hkv;
     p.group = ca_group(p.ratio);
     p.blocks = ca_blocks(a->G, p.ratio);
@@ -1202,6 +1199,9 @@ extern "C" int arrol_cache_attention(arrol_ctx* ctx, const arrol_cache_attention
     p.costs = a->cache.D <= 64 ? CA_COSTS_64 : CA_COSTS_128;
     if (!fits(p.costs)) p.costs = CA_COSTS_COARSE;
     if (!fits(p.costs)) return ARROL_ERR_UNSUPPORTED;
+    if (!a->workspace || !arrol_aligned(a->workspace, 256)) return ARROL_ERR_WORKSPACE;
+    p.w = cache_workspace(a->workspace, ctx->sm_count, a->N, a->P, a->G, a->Hq, a->cache.Hkv, a->cache.D);
+    if (a->workspace_bytes < p.w.bytes) return ARROL_ERR_WORKSPACE;
     p.own_most = (int)own_most;
     p.scale_log2 = a->scale * LOG2E;
     p.status = ctx->d_status;

@@ -240,6 +240,28 @@ def test_attention_refuses(lib, over, code):
     assert lib.arrol_cache_attention(_ctx(), C.byref(_attend(**over)), None) == code
 
 
+@pytest.mark.parametrize("Hq,Hkv,G,N", [(33, 1, 64, 256), (22, 1, 5, 40), (20, 2, 3, 30), (64, 1, 4, 64), (8, 4, 16, 512), (64, 8, 100, 400)])
+def test_tables_up_to_the_limits_are_taken(lib, Hq, Hkv, G, N):
+    """A prompt counts once for every floor(64 / (Hq / Hkv)) rollouts of its group, for these read it together.  Tables of own tokens and of prompts right below what the interface
+    promises are taken, both at once; what is well above is refused.  Sizes are looked at before the workspace, which is missing here."""
+    ratio, P = Hq // Hkv, N // G
+    rollouts = 64 // ratio
+    own = ((1 << (31 if ratio > 16 else 34)) - 1) // (N * Hkv) - 256
+    prompts = ((1 << 31) - 1) // (P * -(-G // rollouts) * Hkv) - 256
+    pool = dict(Hkv=Hkv, page=16, k_page_stride=1 << 24, v_page_stride=1 << 24, k_scale_stride=64, v_scale_stride=64)
+    base = dict(N=N, P=P, G=G, Hq=Hq, q_stride=1 << 14, o_stride=1 << 14, workspace=None)
+
+    def call(own, prompts):
+        own, prompts = min(own, (1 << 31) - 16) // 16, min(prompts, (1 << 31) - 16) // 16
+        return lib.arrol_cache_attention(_ctx(), C.byref(_attend(pool=pool, table_pages=own, table_stride=own, prompt_table_pages=prompts, prompt_table_stride=prompts, **base)), None)
+
+    assert call(own, prompts) == call(own, 16) == call(16, prompts) == -3
+    if 3 * prompts < 1 << 31:
+        assert call(own, 3 * prompts) == call(16, 3 * prompts) == -2
+    if 3 * own < 1 << 31:
+        assert call(3 * own, 16) == -2
+
+
 def test_null_contexts_and_empty_calls(lib):
     null = C.c_void_p()
     for call in ("arrol_rotary", "arrol_rotary_backward", "arrol_cache_append", "arrol_cache_attention"):
