@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(32 * ONE_WARPS) append_one_kernel(const Append
     int len, page = 0;
     bool ok = append_start(a, i, 1, start, len, bad);
     const int64_t position = start + append_offset(a, i);
-    if (ok && task0 < 2 * Hkv) ok = append_page(a, i, start / a.cache.page, page, bad);
+    if (ok) ok = append_page(a, i, start / a.cache.page, page, bad);        // for queries too: a token that has no page has no rows
     if (bad && lane == 0) atomicOr(p.status, ARROL_DEV_BAD_INDEX);
     if (!ok) return;
     const int slot = (int)(start % a.cache.page);

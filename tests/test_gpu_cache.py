@@ -646,6 +646,27 @@ def test_bad_appends_are_reported_and_not_followed(ctx):
         p.run(ctx, status=16)
 
 
+@pytest.mark.parametrize("N,new", [(3, None), (1500, None), (3, [7, 1, 30])])
+def test_rows_of_refused_tokens_are_left_as_they_were(ctx, N, new):
+    """Queries too, however many sequences a call has; rows of the sequence's other pages are written."""
+    for name, at, value in (("d_len", 1, 1 << 30), ("table", (1, 2), -1), ("table", (1, 2), 1 << 29)):
+        good, bad = (Append([20, 33, 64] + [33] * (N - 3), new, page=16, seed=8) for _ in range(2))
+        getattr(bad, name)[at] = value
+        good.run(ctx)
+        bad.run(ctx, status=16)
+        left = torch.zeros(good.starts[-1], dtype=torch.bool, device="cuda")
+        left[bad.starts[1]:bad.starts[2]] = True              # of 33 tokens the new one is the third page's
+        for x, y in ((good.q_out, bad.q_out), (good.k_out, bad.k_out)):
+            assert (y[left] == -7).all() and torch.equal(x[~left], y[~left])
+    if new is not None:
+        p = Append([20, 40, 64], [7, 30, 30], page=16, seed=8)
+        p.table[1, 1] = -5                                    # tokens 16 .. 31 of 10 .. 39
+        p.run(ctx, status=16)
+        for x in (p.q_out, p.k_out):
+            rows = x[p.starts[1]:p.starts[2]]
+            assert (rows[6:22] == -7).all() and not (rows[:6] == -7).all(-1).any() and not (rows[22:] == -7).all(-1).any()
+
+
 def test_appends_captured_and_replayed(ctx):
     p = Append([20, 33, 64], None, [3], 3, page=16, seed=10)
     q = Append([20, 33, 64], None, [3], 3, page=16, seed=10)
