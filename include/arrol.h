@@ -493,7 +493,7 @@ int arrol_rotary_backward(arrol_ctx* ctx, const arrol_rotary_args* args, void* s
  * D a multiple of 16, 16 <= D <= 128; Hq a multiple of Hkv, Hq / Hkv <= 64; G <= 1024, N <= 2^24; pages, tokens of a table row < 2^31; for the attention
  * N * Hkv * (tokens of a table row + 256) below 2^34 (2^31 with Hq / Hkv > 16), the same product of prompts (each counted once for every
  * floor(64 / (Hq / Hkv)) rollouts of its group) below 2^31; scale finite, above 0; bf16 tensors as in the attention calls.  A length that is negative or more than its table
- * row holds, fewer tokens than new ones, or a page number outside [0, pages) is not followed (an append writes nothing of such tokens, output rows included; in attention a
+ * row holds, fewer tokens than new ones, entries of cu_new out of order or outside, or a page number outside [0, pages) is not followed (an append writes nothing of such tokens, output rows included; in attention a
  * sequence or prompt with such a length counts as empty, and what rollouts over such pages get is not defined) and ARROL_DEV_BAD_INDEX is recorded.  The calls use nothing of
  * the context's buffers and may be captured; workspace:
  * arrol_cache_attention_workspace(...) bytes, 256-byte aligned, contents need not be initialised or kept; what N, P and G take serves calls with fewer, of the same heads. */

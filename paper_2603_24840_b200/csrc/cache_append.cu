@@ -213,6 +213,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_runs_kernel(co
     const int page_size = a.cache.page, D = a.cache.D, Hkv = a.cache.Hkv, lane = threadIdx.x & 31;
     const int64_t* cu = pdl_acquire(a.cu_new);
     if (threadIdx.x < 3) most[threadIdx.x] = 0u;             // published by the search's barriers
+    // Rows out of order or behind the last may belong to sequences that no block comes to: the grid, more threads than sequences, looks at all of them.
+    const int64_t seen = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (blockIdx.y == 0 && blockIdx.z == 0 && seen < a.N) {
+        const int64_t first = cu[seen], end = cu[seen + 1];
+        if (first < 0 || end < first || end > a.rows || (seen == 0 && first != 0)) atomicOr(p.status, ARROL_DEV_BAD_INDEX);
+    }
     // Sequence i has the blocks from cu[i] / page + 2 i on: a run of n tokens touches n / page + 2 pages at most, whatever slot it begins in.
     const int64_t u = blockIdx.x;
     const int64_t i64 = block_search(a.N, [&](int64_t i) { return cu[i + 1] / page_size + 2 * (i + 1) <= u; });

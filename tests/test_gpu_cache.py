@@ -667,6 +667,27 @@ def test_rows_of_refused_tokens_are_left_as_they_were(ctx, N, new):
             assert (rows[6:22] == -7).all() and not (rows[:6] == -7).all(-1).any() and not (rows[22:] == -7).all(-1).any()
 
 
+def test_rows_out_of_order_are_reported_where_nothing_follows_them(ctx):
+    """Sequences of which no block is launched, or which are left out: those in front of them are written as ever."""
+    for cu, keep in (([0, 7, 10 ** 6, 10 ** 6 + 30], [1, 0, 1]), ([0, 7, 1 << 62, (1 << 62) + 30], [1, 0, 1]), ([0, 7, -(1 << 40), 37], [0, 0, 0]), ([0, 7, 3, 37], [0, 0, 0]),
+                     ([0, 7, 37, 39], [1, 0, 0]), ([3, 7, 8, 38], [0, 0, 0]), ([-1, 7, 8, 38], [0, 0, 0])):
+        good, bad = (Append([20, 33, 64], [7, 1, 30], page=16, keep=[1 if k and i == 0 else 0 for i, k in enumerate(keep)], seed=9) for _ in range(2))
+        bad.cu.copy_(torch.tensor(cu, dtype=torch.int64))
+        bad.d_keep.copy_(torch.tensor(keep, dtype=torch.uint8))
+        good.run(ctx)
+        bad.run(ctx, status=16)
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(good.snapshot() + [good.q_out, good.k_out], bad.snapshot() + [bad.q_out, bad.k_out]))
+    many = Append([20] * 600, [2] * 600, page=16, keep=[0] * 600, seed=9)             # more sequences than a block has threads
+    many.cu[577] = 1 << 40
+    many.run(ctx, status=16)
+    p = Append([20, 33, 64], [7, 1, 30], page=16, seed=9)                             # rows behind the last sequence are nobody's
+    p.cu = torch.tensor([0, 7, 8, 38], dtype=torch.int64, device="cuda")
+    p.k, p.v, p.q = (torch.cat([x, x[:5]]) for x in (p.k, p.v, p.q))
+    p.q_out, p.k_out = (torch.cat([x, x[:5]]) for x in (p.q_out, p.k_out))
+    p.check(p.run(ctx))
+    assert (p.q_out[38:] == -7).all() and (p.k_out[38:] == -7).all()
+
+
 def test_appends_captured_and_replayed(ctx):
     p = Append([20, 33, 64], None, [3], 3, page=16, seed=10)
     q = Append([20, 33, 64], None, [3], 3, page=16, seed=10)
