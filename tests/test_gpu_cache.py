@@ -222,6 +222,71 @@ def test_pages_of_values_of_all_sizes(ctx, lengths, prompts, G, Hq, Hkv, D, page
     p.check(*p.run(ctx))
 
 
+def _far_apart(p, most=40):
+    """Scales of values up to 2^most either way, each page with an eighth of the dimensions."""
+    g = p.pool.g
+    used = torch.isfinite(p.pool.vs)
+    p.pool.vs.copy_(torch.where(used, torch.exp2(torch.randint(-most, most + 1, p.pool.vs.shape, generator=g, device="cuda").float()), p.pool.vs))
+    values = p.pool.v.view(torch.uint8)
+    drop = torch.rand(p.pool.pages, p.pool.Hkv, 1, p.pool.D, generator=g, device="cuda").expand(values.shape) > 0.125
+    values[drop & used[:, :, None, None]] = 0
+    return p
+
+
+@pytest.mark.parametrize("lengths,prompts,G,Hq,Hkv,D,page,keep", ATTEND)
+def test_scales_far_apart_match_the_definition(ctx, lengths, prompts, G, Hq, Hkv, D, page, keep):
+    p = _far_apart(Attend(lengths, prompts, G, Hq, Hkv, D, page, keep, seed=len(lengths) + Hq, both=len(lengths) % 2 == 0, q_scale=0.5))
+    p.check(*p.run(ctx))
+
+
+def test_rows_with_scales_far_apart_beside_ordinary_ones(ctx):
+    """One rollout's, or one key head's: the others keep their bits; the same bits every time, with strided rows, without lse and from a graph; NaN and infinities reach their rows alone."""
+    p = Attend([400, 150, 900, 64], [165, 40], 2, 12, 3, 128, 16, seed=33)
+    plain = p.run(ctx)
+    at = int(p.table[2, 7])
+    p.pool.vs[at, 1] *= 2.0 ** 30
+    p.pool.v.view(torch.uint8)[at, 1, :, 1:] = 0
+    o, lse = p.run(ctx)
+    p.check(o, lse)
+    others = torch.ones(4, 12, dtype=torch.bool, device="cuda")
+    others[2, 4:8] = False
+    assert torch.equal(o[others], plain[0][others]) and torch.equal(lse[others], plain[1][others]) and not torch.equal(o[~others], plain[0][~others])
+    wide, ws = torch.full((4, 20, 128), -7.0, dtype=BF, device="cuda"), p.workspace(ctx)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        p.call(ctx, wide[:, 3:15], None, ws)
+    for _ in range(3):
+        wide.fill_(-7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, wide[:, 3:15]) and (wide[:, :3] == -7).all() and (wide[:, 15:] == -7).all()
+    first = int(p.table[2, 0])
+    for name, value in (("k", 0x7F), ("v", 0x7F)):
+        codes = getattr(p.pool, name).view(torch.uint8)
+        had = int(codes[first, 1, 3, 5])
+        codes[first, 1, 3, 5] = value
+        bad = p.run(ctx)
+        p.check(*bad)
+        assert torch.equal(o[others], bad[0][others]) and not torch.isfinite(bad[0][2, 4:8, 5]).any()
+        codes[first, 1, 3, 5] = had
+    p.q[2, 5, 9], p.q[2, 6, 0] = math.nan, math.inf
+    bad = p.run(ctx)
+    assert torch.equal(o[others], bad[0][others]) and not torch.isfinite(bad[0][2, 5:7]).any() and torch.equal(o[2, [4, 7]], bad[0][2, [4, 7]])
+
+
+def test_scales_far_apart_in_pages_beyond_32_bit_offsets_and_bad_pages(ctx):
+    p = _far_apart(Attend([70, 33, 1, 200], [40], 4, 4, 2, 64, 32, seed=20))
+    want = p.run(ctx)
+    p.check(*want)
+    p.table[3, 4], p.table[1, 0] = -3, 1 << 30
+    for x, y in zip(want, p.run(ctx, status=16)):
+        assert torch.equal(x[[0, 2]], y[[0, 2]])
+    p = _far_apart(Attend([70, 33, 1, 200], [40], 4, 4, 2, 64, 32, seed=20))
+    _spread(p.pool, -(-(1 << 33) // p.pool.pages) // 16 * 16)
+    assert all(torch.equal(x, y) for x, y in zip(want, p.run(ctx)))
+
+
 def test_a_long_tail_behind_one_key_that_takes_most(ctx):
     """Eight thousand keys at 2^-18 of the first's weight carry a thirtieth of the sum: probabilities of four or five bits would lose them."""
     for D, Hq, Hkv in ((64, 4, 1), (128, 32, 1)):
