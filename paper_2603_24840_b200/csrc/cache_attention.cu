@@ -91,6 +91,7 @@ struct CacheParams {
     CacheWorkspace w;
     int ratio, group, blocks, prompts, entries;    // rollouts a prompt entry, entries a prompt, prompt entries, all
     int page_shift, grid;
+    bool merge_apart;                              // a block of the merge has rows from all over, not one behind another
     int own_most;                                  // tokens that a row of page_table holds
     LineCosts costs;
     float scale_log2;
@@ -1050,7 +1051,8 @@ __global__ void __launch_bounds__(MERGE_THREADS, 3) cache_merge_kernel(const __g
     pdl_wait();
     const arrol_cache_attention_args& a = p.a;
     const int lane = threadIdx.x % LANES, part = (threadIdx.x & 31) - lane, D = a.cache.D, Hkv = a.cache.Hkv, d = lane * 4;
-    const int64_t rows = (int64_t)a.N * a.Hq, asked = (blockIdx.x * (int64_t)MERGE_THREADS + threadIdx.x) / LANES, row = asked < rows ? asked : rows - 1;      // both halves go on together
+    const int64_t step = p.merge_apart ? gridDim.x : 1, first = p.merge_apart ? blockIdx.x : (int64_t)blockIdx.x * (MERGE_THREADS / LANES);
+    const int64_t rows = (int64_t)a.N * a.Hq, asked = first + (int64_t)(threadIdx.x / LANES) * step, row = asked < rows ? asked : rows - 1;      // both halves go on together
     const int i = (int)(row / a.Hq), hq = (int)(row - (int64_t)i * a.Hq), h = hq / p.ratio, r = hq - h * p.ratio;
     const int2* owners = pdl_acquire(p.w.owners);
     const float2* ml = pdl_acquire(p.w.ml);
@@ -1118,7 +1120,7 @@ __global__ void __launch_bounds__(MERGE_THREADS, 3) cache_merge_kernel(const __g
         __syncthreads();
 #pragma unroll 1
         for (int x = 0; x < MERGE_THREADS / LANES; ++x)
-            if (sm.apart[x]) row_apart(p, (int64_t)blockIdx.x * (MERGE_THREADS / LANES) + x, sm);
+            if (sm.apart[x]) row_apart(p, first + x * step, sm);
     }
 }
 
@@ -1135,7 +1137,7 @@ int make_map_pages(arrol_ctx* ctx, CUtensorMap* map, const arrol_cache& c, const
 }
 
 template <int DP>
-int launch_cache_attention(arrol_ctx* ctx, const CacheParams& p, cudaStream_t s) {
+int launch_cache_attention(arrol_ctx* ctx, CacheParams& p, cudaStream_t s) {
     using C = CacheConf<DP>;
     bool& set = ctx->cache_attention_smem_set[DP == 128];
     if (!set) {
@@ -1146,9 +1148,13 @@ int launch_cache_attention(arrol_ctx* ctx, const CacheParams& p, cudaStream_t s)
     if (p.a.cache.pages > 0 && (make_map_pages(ctx, &k, p.a.cache, p.a.cache.k_cache, p.a.cache.k_page_stride, DP) != ARROL_OK ||
                                 make_map_pages(ctx, &v, p.a.cache, p.a.cache.v_cache, p.a.cache.v_page_stride, DP) != ARROL_OK))
         return ARROL_ERR_CUDA;
-    ARROL_CUDA_OK(arrol_launch_pdl(cache_units_kernel<DP>, dim3((unsigned)p.grid), dim3(CA_THREADS), C::SMEM, s, k, v, p));
     constexpr int LANES = DP / 4;
-    ARROL_CUDA_OK(arrol_launch_pdl(cache_merge_kernel<LANES>, dim3((unsigned)(((int64_t)p.a.N * p.a.Hq * LANES + MERGE_THREADS - 1) / MERGE_THREADS)), dim3(MERGE_THREADS), 0, s, p));
+    const int64_t blocks = ((int64_t)p.a.N * p.a.Hq * LANES + MERGE_THREADS - 1) / MERGE_THREADS;
+    // Few blocks: rows of one rollout over many of them, so that those that are not live, or computed anew, leave none idle (16 rollouts of 32 heads 56.3 -> 55.3 us; scales far apart in one of
+    // them 1,504 -> 267).  Many: side by side, for what their rollouts have in common (512 rollouts of 16 heads 235, all over 237.5).
+    p.merge_apart = blocks <= 2 * ctx->sm_count;
+    ARROL_CUDA_OK(arrol_launch_pdl(cache_units_kernel<DP>, dim3((unsigned)p.grid), dim3(CA_THREADS), C::SMEM, s, k, v, p));
+    ARROL_CUDA_OK(arrol_launch_pdl(cache_merge_kernel<LANES>, dim3((unsigned)blocks), dim3(MERGE_THREADS), 0, s, p));
     ctx->launches += 2;
     return ARROL_OK;
 }
