@@ -239,6 +239,14 @@ def test_scales_far_apart_match_the_definition(ctx, lengths, prompts, G, Hq, Hkv
     p.check(*p.run(ctx))
 
 
+@pytest.mark.parametrize("lengths,prompts,G,Hq,Hkv,D", [([33, 20] * 20, None, 1, 64, 8, 128), ([7, 40] * 40, [50] * 10, 8, 64, 4, 64)])
+def test_scales_far_apart_in_many_rows(ctx, lengths, prompts, G, Hq, Hkv, D):
+    """More rows than the merge spreads over its blocks; some of them ordinary."""
+    p = Attend(lengths, prompts, G, Hq, Hkv, D, 16, seed=34, q_scale=0.5)
+    _far_apart(p, 6)
+    p.check(*p.run(ctx))
+
+
 def test_rows_with_scales_far_apart_beside_ordinary_ones(ctx):
     """One rollout's, or one key head's: the others keep their bits; the same bits every time, with strided rows, without lse and from a graph; NaN and infinities reach their rows alone."""
     p = Attend([400, 150, 900, 64], [165, 40], 2, 12, 3, 128, 16, seed=33)
