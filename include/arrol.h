@@ -435,7 +435,7 @@ int arrol_attention_decode(arrol_ctx* ctx, const arrol_decode_args* args, void* 
  *                        ceil(i(low)) (both kept within 0 .. R - 1, at least 0.001 apart), the frequency is (1 - s) f + s f / stretch.
  * low, high, original are for the last two kinds.  A longer base (a change of base) needs no kind.  *factor (may be NULL) receives the factor on cosine and sine:
  * 0.1 log(stretch) + 1 for ARROL_ROTARY_RAMP with stretch > 1, else 1.  INVALID_ARG for R odd or < 2, base <= 1, stretch <= 0, original <= 0, low <= 0, high <= low or values
- * that are not finite. */
+ * that are not finite, of those that the kind uses (stretch: all but ARROL_ROTARY_PLAIN). */
 #define ARROL_ROTARY_PLAIN 0
 #define ARROL_ROTARY_LINEAR 1
 #define ARROL_ROTARY_BANDS 2
@@ -480,6 +480,8 @@ int arrol_rotary_backward(arrol_ctx* ctx, const arrol_rotary_args* args, void* s
  *   q_out [rows, Hq, D] receives q; k_out [rows, Hkv, D], if not NULL, k, both bf16; k is stored from its fp32 value.  In place as in arrol_rotary.
  *   keep [N] uint8 or NULL: sequences with 0 are left out, their pages and output rows untouched, their lengths and tables not followed.
  *   Pages that receive tokens belong to one sequence of the call; pages that are only read (forked prefixes) may be shared.
+ *   There is no attention of several tokens of a sequence over its pages: what the tokens of a piece attend to, arrol_attention takes in bf16, k_out and v of the piece itself and,
+ *   as its prompt, of the pieces before it.
  *
  * arrol_cache_attention is attention of one token per rollout, as arrol_attention_decode, over such a cache: rollout i < N with keep[i] != 0 attends with q[i] (bf16) to
  * the prompt_lengths[p] tokens of its group's prompt, p = i / G, pages prompt_table[p * prompt_table_stride + ...], and to its own lengths[i] tokens:

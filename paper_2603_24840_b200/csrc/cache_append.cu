@@ -3,10 +3,10 @@
 // Bound by HBM where there are many tokens (bf16 in, 8 bits out, queries in and out), by one launch and a chain of dependent loads (length, page number, scale) where
 // there are few.  A page's scale needs the largest entry of all of its new tokens before the first can be rounded, so a page and head belong to one block
 // (append_runs_kernel: runs of tokens) or one warp (append_one_kernel: a token per sequence), which keeps what it loaded in shared memory or registers in between (but for
-// odd sizes) and needs no atomics in global memory.
+// odd sizes, see append_runs_kernel) and needs no atomics in global memory.
 //
-// 38,000 prompt tokens of 16 heads of 128 on 8 (600 MB) 137 us, 4.4 TB/s: no unit is full (instructions issued in half of the cycles, DRAM at 0.55); the values are turned twice.  One
-// token each of 512 live rollouts, 32 heads on 8 (12 MB), 12 us from a graph.
+// 38,000 prompt tokens of 16 heads of 128 on 8 (600 MB) 137 us, 4.4 TB/s: no unit is full (instructions issued in half of the cycles, DRAM at 0.55); the keys are turned twice.  One
+// token each of 512 live rollouts, 32 heads on 8 (12 MB), 12 us from a graph, of 4,096 70: a warp of four heads has its own chain of loads and its own angles.
 #include <type_traits>
 
 #include "cache_common.cuh"
@@ -65,7 +65,7 @@ __device__ __forceinline__ int append_exponent(float amax, int slot, float old, 
 
 // ---- one token per sequence: a warp per sequence and PER of its heads (keys', then values', then queries'), four dimensions a lane.  Where one a head
 // would be more warps than the SMs have places for, four heads share the angles and the chain of loads in front of them (heads of 128, 32 on 8, from a graph: 64 rollouts 4.5 us
-// with one and 5.1 with four, 256 9.1 and 6.5, 512 live of 1,024 17.7 and 11.6, 4,096 109 and 68; with two 13.0 and 76, with eight 15.9 and 88, for the last two).
+// with one and 5.1 with four, 256 9.1 and 6.5, 512 live of 1,024 17.7 and 11.7, 4,096 109 and 70; with two 13.0 and 76, with eight 15.9 and 88, for the last two).
 template <int PER>
 __global__ void __launch_bounds__(32 * ONE_WARPS) append_one_kernel(const AppendParams p) {
     pdl_launch_dependents();
@@ -168,7 +168,8 @@ __global__ void __launch_bounds__(32 * ONE_WARPS) append_one_kernel(const Append
 }
 
 // ---- runs of tokens: a block per page that gets some, for keys and queries or for values (and part of the heads); a thread has one unit of one token, its angles in
-// registers, and goes through the heads
+// registers, and goes through the heads.  Where a page's units are more than 1,024 threads (pages of 128 tokens with narrow chunks) it has several units in turn, reads their rows twice
+// and forms their angles anew for every head: 38,000 tokens, 16 heads of 80 on 8, 40 of 80 turned, 322 us with pages of 128, 139 of 64.  Chunks of 8 numbers: 64 registers, 60 bytes spilled.
 template <int V>
 __device__ __forceinline__ void not_finite_to_nan(float (&x)[V], float (&y)[V]) {
 #pragma unroll

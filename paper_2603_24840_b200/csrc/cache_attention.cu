@@ -1,10 +1,11 @@
 // arrol_cache_attention: one generated token per rollout over its group's prompt and its own tokens, both in the paged 8-bit cache.
 //
 // Bound by HBM in the large: every live rollout's pages and every group's prompt pages are read once, half of a bf16 cache's bytes.  Measured (calls one behind another):
-// 256 live rollouts of 2,200 tokens over 32 prompts, 16 heads of 128 on 8 (1.23 GB) 236 us, 5.2 TB/s.  By clocks in the kernel the first pieces are there after 11 us (a scan
+// 256 live rollouts of 2,200 tokens over 32 prompts, 16 heads of 128 on 8 (1.23 GB) 235 us, 5.2 TB/s.  By clocks in the kernel the first pieces are there after 11 us (a scan
 // of 4, then loads that depend on one another, and everybody's copies at once), warps end between 184 and 215, the merge takes 10.  8 rollouts of 6,600 tokens, 32 heads
-// (118 MB) 51 us: pieces from 10 to 38, the merge behind them.  384 rollouts of 160 tokens over 24 prompts of 4,850, 32 heads of 64 (188 MB) 133 us: there it is the work of
-// 64 query rows behind every key, each warp a chain of 2,000 cycles for 32 tokens of 16 rows, three of them an SM's quarter.
+// (118 MB) 55 us: pieces from 10 to 38, the merge behind them.  384 rollouts of 160 tokens over 24 prompts of 4,850, 32 heads of 64 (188 MB) 140 us: there it is the work of
+// 64 query rows behind every key, each warp a chain of 2,000 cycles for 32 tokens of 16 rows, three of them an SM's quarter.  168 registers (heads up to 64: 128), at the edge: 28
+// bytes are spilled, and instructions in the pieces' loops, run or jumped over, show in all calls.
 //
 // The products are m16n8k16 mma.sync in fp16, transposed: tokens (of S^T = K Q^T) and dimensions (of O^T = V^T P^T) are the sixteen rows, query rows the eight columns, so that
 // eight query heads waste nothing.  e4m3 numbers widen to fp16 exactly, two an instruction, and q, scaled by a power of two for each row, is exact in fp16 too (bf16 has
