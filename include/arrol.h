@@ -490,7 +490,7 @@ int arrol_rotary_backward(arrol_ctx* ctx, const arrol_rotary_args* args, void* s
  * 64 query rows, rollouts x Hq / Hkv, per key head).  Without prompts: prompt_table, prompt_lengths NULL, P = 0.  q is scaled by a power of two for each row
  * and taken as fp16, which is exact for bf16 (entries below 2^-27 of their row's largest are rounded at 2^-39 of it); e4m3 numbers are exact in fp16; sums are fp32;
  * probabilities are rounded to fp16 before the product with values, those below 2^-13 of the largest to steps of 2^-23 of it (2^-21 and 2^-31 where the pages' values have one
- * scale); rows of rollouts with scales of values more than 2^8 apart are computed in fp32, which takes longer.  Every sum has a fixed order, so equal calls give equal bits.
+ * scale); rows of rollouts with scales of values more than 2^8 apart are computed in fp32, which takes longer.  (Sums over values beyond 2^90 may pass fp32's largest.)  Every sum has a fixed order, so equal calls give equal bits.
  *
  * D a multiple of 16, 16 <= D <= 128; Hq a multiple of Hkv, Hq / Hkv <= 64; G <= 1024, N <= 2^24; pages, tokens of a table row < 2^31; for the attention
  * N * Hkv * (tokens of a table row + 256) below 2^34 (2^31 with Hq / Hkv > 16), the same product of prompts (each counted once for every
